@@ -17,4 +17,7 @@ from .binding import (  # noqa: F401
     OB_CFG_TWO_PASS_COMPRESS, OB_CFG_NO_FUSED_APPLY, OB_CFG_TWO_PASS_WARMUP, OB_CFG_NO_BARRIERS, OB_SPIN_NONE,
     ob_lamb_server_reduce_static, ob_lamb_static_max_chunk_len, ob_lamb_diag_copy, ob_lamb_workspace_bytes, ob_lamb_error_dense, ob_lamb_server_error_dense,
     OB_VF_MAX_OLD, ObLambVfHistory, make_vf_history, ob_lamb_ratios_apply_hist, ob_lamb_ratios_apply_hist_lp, ob_lamb_variance_dense, ob_lamb_big_tile_params,
+    OB_EXPERTS_KN, OB_EXPERTS_NK, ObExpertsConfig, ObMuonConfig, ob_experts_create, ob_experts_destroy, ob_experts_forward,
+    ob_experts_input_grad, ob_experts_weight_grad, ob_experts_workspace_bytes, ob_muon_create, ob_muon_destroy,
+    ob_muon_orthogonalize, ob_muon_step, ob_muon_workspace_bytes,
 )

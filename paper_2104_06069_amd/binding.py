@@ -51,6 +51,22 @@ class ObLambVfHistory(C.Structure):
                 ("bits", C.c_void_p * OB_VF_MAX_OLD), ("scales", C.c_void_p * OB_VF_MAX_OLD)]
 
 
+# include/ob_matrix.h
+OB_EXPERTS_KN, OB_EXPERTS_NK = 0, 1
+
+
+class ObExpertsConfig(C.Structure):
+    _fields_ = [("num_groups", C.c_int32), ("dtype", C.c_int32), ("w_layout", C.c_int32), ("reserved", C.c_int32),
+                ("k", C.c_int64), ("n", C.c_int64), ("max_rows", C.c_int64), ("w_stride", C.c_int64)]
+
+
+class ObMuonConfig(C.Structure):
+    _fields_ = [("num_layers", C.c_int64), ("layer_offsets", C.POINTER(C.c_int64)), ("layer_rows", C.POINTER(C.c_int64)),
+                ("layer_scale", C.POINTER(C.c_float)), ("coefficients", C.POINTER(C.c_float)),
+                ("num_coefficients", C.c_int32), ("steps", C.c_int32), ("eps", C.c_float), ("beta", C.c_float),
+                ("weight_decay", C.c_float), ("nesterov", C.c_int32), ("precision", C.c_int32)]
+
+
 def lib_path():
     return os.path.join(_PKG, "lib", "libonebitlamb.so")
 
@@ -109,6 +125,19 @@ def lib():
             "ob_lamb_profile_enable": (C.c_int, [vp, C.c_int]),
             "ob_lamb_profile_read": (i32, [vp, i32, C.POINTER(C.c_char_p), C.POINTER(C.c_double),
                                            C.POINTER(i64)]),
+            "ob_experts_create": (C.c_int, [C.POINTER(ObExpertsConfig), C.POINTER(vp)]),
+            "ob_experts_destroy": (None, [vp]),
+            "ob_experts_workspace_bytes": (C.c_size_t, [vp]),
+            "ob_experts_last_hip_error": (C.c_char_p, [vp]),
+            "ob_experts_forward": (C.c_int, [vp, vp, i64, vp, vp, i64, vp, i64, C.c_int, vp]),
+            "ob_experts_input_grad": (C.c_int, [vp, vp, i64, vp, vp, i64, vp, i64, C.c_int, vp]),
+            "ob_experts_weight_grad": (C.c_int, [vp, vp, i64, vp, i64, vp, i64, vp, C.c_int, i32, vp]),
+            "ob_muon_create": (C.c_int, [C.POINTER(ObMuonConfig), C.POINTER(vp)]),
+            "ob_muon_destroy": (None, [vp]),
+            "ob_muon_workspace_bytes": (C.c_size_t, [vp]),
+            "ob_muon_last_hip_error": (C.c_char_p, [vp]),
+            "ob_muon_orthogonalize": (C.c_int, [vp, vp, C.c_int, vp, C.c_int, vp]),
+            "ob_muon_step": (C.c_int, [vp, vp, vp, vp, C.c_int, f, f, vp, C.c_int, vp]),
         }
         for name, (res, args) in sig.items():
             fn = getattr(L, name)
@@ -393,3 +422,83 @@ def ob_lamb_profile_read(ctx):
     cnt = (C.c_int64 * cap)()
     n = lib().ob_lamb_profile_read(ctx, cap, names, ms, cnt)
     return {names[i].decode(): (ms[i], int(cnt[i])) for i in range(min(n, cap))}
+
+
+# ---- matrix operators (include/ob_matrix.h) ----------------------------------------------------
+def _check_matrix(status, ctx, where, last_error):
+    if status:
+        raise ObLambError(status, where, last_error(ctx).decode() if ctx else "")
+
+
+def ob_experts_create(num_groups, k, n, dtype, w_layout=OB_EXPERTS_KN, max_rows=0, w_stride=0):
+    """-> opaque context handle (on the current HIP device)."""
+    cfg = ObExpertsConfig(int(num_groups), int(dtype), int(w_layout), 0, int(k), int(n), int(max_rows), int(w_stride))
+    out = C.c_void_p()
+    st = lib().ob_experts_create(C.byref(cfg), C.byref(out))
+    if st != OB_OK:
+        raise ObLambError(st, "ob_experts_create")
+    return out
+
+
+def ob_experts_destroy(ctx):
+    lib().ob_experts_destroy(ctx)
+
+
+def ob_experts_workspace_bytes(ctx):
+    return int(lib().ob_experts_workspace_bytes(ctx))
+
+
+def ob_experts_forward(ctx, x, ldx, w, offsets, rows, y, ldy, y_dtype, stream=None):
+    L = lib()
+    _check_matrix(L.ob_experts_forward(ctx, _addr(x), ldx, _addr(w), _addr(offsets), rows, _addr(y), ldy, y_dtype, _addr(stream)),
+                  ctx, "ob_experts_forward", L.ob_experts_last_hip_error)
+
+
+def ob_experts_input_grad(ctx, dy, lddy, w, offsets, rows, dx, lddx, dx_dtype, stream=None):
+    L = lib()
+    _check_matrix(L.ob_experts_input_grad(ctx, _addr(dy), lddy, _addr(w), _addr(offsets), rows, _addr(dx), lddx, dx_dtype, _addr(stream)),
+                  ctx, "ob_experts_input_grad", L.ob_experts_last_hip_error)
+
+
+def ob_experts_weight_grad(ctx, x, ldx, dy, lddy, offsets, rows, dw, dw_dtype, accumulate=False, stream=None):
+    L = lib()
+    _check_matrix(L.ob_experts_weight_grad(ctx, _addr(x), ldx, _addr(dy), lddy, _addr(offsets), rows, _addr(dw), dw_dtype,
+                                           int(bool(accumulate)), _addr(stream)),
+                  ctx, "ob_experts_weight_grad", L.ob_experts_last_hip_error)
+
+
+def ob_muon_create(layer_offsets, layer_rows, layer_scale=None, coefficients=(3.4445, -4.7750, 2.0315), steps=5, eps=1e-7,
+                   beta=0.95, weight_decay=0.0, nesterov=True, precision=OB_F32):
+    """coefficients: a, b, c of each step in a row (the last three serve the steps that follow).
+    -> opaque context handle (on the current HIP device)."""
+    offs, rows, coef = [int(o) for o in layer_offsets], [int(r) for r in layer_rows], [float(c) for c in coefficients]
+    if len(rows) != len(offs) - 1 or len(coef) % 3 or (layer_scale is not None and len(layer_scale) != len(rows)):
+        raise ObLambError(OB_ERR_ARG, "ob_muon_create", "one layer_rows and layer_scale a tensor, three coefficients a step")
+    cfg = ObMuonConfig(len(rows), (C.c_int64 * len(offs))(*offs), (C.c_int64 * len(rows))(*rows),
+                       None if layer_scale is None else (C.c_float * len(rows))(*[float(s) for s in layer_scale]),
+                       (C.c_float * len(coef))(*coef), len(coef) // 3, int(steps), eps, beta, weight_decay, int(bool(nesterov)), int(precision))
+    out = C.c_void_p()
+    st = lib().ob_muon_create(C.byref(cfg), C.byref(out))
+    if st != OB_OK:
+        raise ObLambError(st, "ob_muon_create")
+    return out
+
+
+def ob_muon_destroy(ctx):
+    lib().ob_muon_destroy(ctx)
+
+
+def ob_muon_workspace_bytes(ctx):
+    return int(lib().ob_muon_workspace_bytes(ctx))
+
+
+def ob_muon_orthogonalize(ctx, src, src_dtype, out, out_dtype, stream=None):
+    L = lib()
+    _check_matrix(L.ob_muon_orthogonalize(ctx, _addr(src), src_dtype, _addr(out), out_dtype, _addr(stream)), ctx,
+                  "ob_muon_orthogonalize", L.ob_muon_last_hip_error)
+
+
+def ob_muon_step(ctx, x, m, grad, grad_dtype, grad_scale, lr, x_lp=None, x_dtype=OB_F32, stream=None):
+    L = lib()
+    _check_matrix(L.ob_muon_step(ctx, _addr(x), _addr(m), _addr(grad), grad_dtype, grad_scale, lr, _addr(x_lp), x_dtype, _addr(stream)),
+                  ctx, "ob_muon_step", L.ob_muon_last_hip_error)

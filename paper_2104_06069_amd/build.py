@@ -5,7 +5,7 @@ import sys
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
-SRC = [os.path.join(PKG, "csrc", "onebitlamb.hip")]
+SRC = [os.path.join(PKG, "csrc", f) for f in ("onebitlamb.hip", "ob_matrix.hip")]
 LIB = os.path.join(PKG, "lib", "libonebitlamb.so")
 
 # -ffp-contract=off: one rounding per operation (the sign bits must match a plain IEEE evaluation).

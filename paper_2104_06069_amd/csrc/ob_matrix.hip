@@ -1,0 +1,441 @@
+// libonebitlamb: host side of the matrix operators (include/ob_matrix.h) -- contexts, tile lists, argument validation and
+// launches.  The kernels live in ob_matrix_kernels.h and ob_mm.h.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <limits>
+#include <new>
+#include <string>
+#include <vector>
+
+#include "ob_matrix.h"
+#include "ob_matrix_kernels.h"
+
+using namespace obm;
+
+namespace {
+
+using S64 = Shape<64, 64, 64, 2, 2>;
+using S64x2 = Shape<64, 64, 32, 2, 2>;
+
+inline int elem_size(int dtype) { return dtype == OB_F32 ? 4 : 2; }
+inline bool off_element(const void* p, int dtype) { return reinterpret_cast<uintptr_t>(p) % elem_size(dtype) != 0; }
+inline bool at16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+inline bool any_dtype(int d) { return d == OB_F32 || d == OB_F16 || d == OB_BF16; }
+
+template <class Ctx>
+bool hip_ok(Ctx* ctx, hipError_t e, const char* what) {
+  if (e == hipSuccess) return true;
+  try {
+    ctx->hip_err = std::string(what) + ": " + hipGetErrorString(e);
+  } catch (...) {
+  }
+  return false;
+}
+
+bool on_device(int device) {
+  int dev = -1;
+  return hipGetDevice(&dev) == hipSuccess && dev == device;
+}
+
+// A kernel may ask for more than 64 KB of LDS once it has been told.
+template <class K>
+hipError_t allow_lds(K kernel, int bytes) {
+  return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+}
+
+}  // namespace
+
+// ---- expert layers -------------------------------------------------------------------------------------------------
+struct ob_experts_ctx {
+  ob_experts_config cfg;
+  int device = -1;
+  std::string hip_err;
+};
+
+namespace {
+
+template <class S, bool BF, int FB>
+ob_status launch_rows(ob_experts_ctx* ctx, const RowsArgs& p, hipStream_t stream) {
+  using P = Product<S, BF, KC, FB, 1, 1, true>;
+  const int64_t tiles = ((int64_t)p.groups.rows / S::BM + std::min<int64_t>(p.groups.n, p.groups.rows)) * ((p.width + S::BN - 1) / S::BN);
+  const int64_t grid = (tiles + 7) / 8 * 8;
+  if (grid > 0x7fffffff) return OB_ERR_SIZE;
+  hipLaunchKernelGGL((k_experts_rows<S, BF, FB>), dim3((unsigned)grid), dim3(S::NT), P::LDS_BYTES, stream, p);
+  return hip_ok(ctx, hipGetLastError(), "k_experts_rows") ? OB_OK : OB_ERR_HIP;
+}
+
+template <class S, bool BF>
+ob_status launch_weights(ob_experts_ctx* ctx, const WeightsArgs& p, hipStream_t stream) {
+  using P = Product<S, BF, KS, KS, 1, 1, true>;
+  const int64_t tiles = (int64_t)p.groups.n * ((p.height + S::BM - 1) / S::BM) * ((p.width + S::BN - 1) / S::BN);
+  const int64_t grid = (tiles + 7) / 8 * 8;
+  if (grid > 0x7fffffff) return OB_ERR_SIZE;
+  hipLaunchKernelGGL((k_experts_weights<S, BF>), dim3((unsigned)grid), dim3(S::NT), P::LDS_BYTES, stream, p);
+  return hip_ok(ctx, hipGetLastError(), "k_experts_weights") ? OB_OK : OB_ERR_HIP;
+}
+
+constexpr int64_t MAX_LD = (int64_t)1 << 22;      // a tile's offsets are 32-bit
+
+ob_status rows_call(ob_experts_ctx* ctx, const void* a, int64_t lda, const void* w, const int32_t* offsets, int64_t rows,
+                    void* out, int64_t ldo, int out_dtype, bool transposed, void* hip_stream) {
+  if (!ctx || !offsets) return OB_ERR_NULL;
+  const ob_experts_config& c = ctx->cfg;
+  const int64_t depth = transposed ? c.n : c.k, width = transposed ? c.k : c.n;
+  if (rows < 0 || rows > c.max_rows || lda < depth || ldo < width || lda >= MAX_LD || ldo >= MAX_LD) return OB_ERR_ARG;
+  if (out_dtype != c.dtype && out_dtype != OB_F32) return OB_ERR_ARG;
+  if (!on_device(ctx->device)) return OB_ERR_ARG;
+  if (!w || (rows && (!a || !out))) return OB_ERR_NULL;
+  if (off_element(a, c.dtype) || off_element(w, c.dtype) || off_element(out, out_dtype) || off_element(offsets, OB_F32)) return OB_ERR_ALIGN;
+  if (rows == 0) return OB_OK;
+  RowsArgs p;
+  p.groups = Groups{offsets, c.num_groups, (int)rows};
+  p.a = static_cast<const uint16_t*>(a);
+  p.w = static_cast<const uint16_t*>(w);
+  p.out = out;
+  p.lda = lda;
+  p.ldo = ldo;
+  p.w_stride = c.w_stride;
+  p.depth = (int)depth;
+  p.width = (int)width;
+  p.out_dtype = out_dtype;
+  p.ldw = c.w_layout == OB_EXPERTS_KN ? c.n : c.k;
+  const bool strided = (c.w_layout == OB_EXPERTS_KN) != transposed;      // W's columns, as the product has them, are its rows in memory
+  p.a_direct = at16(a) && lda % 8 == 0;
+  p.w_direct = at16(w) && p.ldw % 8 == 0 && c.w_stride % 8 == 0 && (!strided || width % 8 == 0);
+  const hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  if (c.dtype == OB_BF16) return strided ? launch_rows<S64, true, KS>(ctx, p, s) : launch_rows<S64, true, KC>(ctx, p, s);
+  return strided ? launch_rows<S64, false, KS>(ctx, p, s) : launch_rows<S64, false, KC>(ctx, p, s);
+}
+
+}  // namespace
+
+extern "C" {
+
+ob_status ob_experts_create(const ob_experts_config* cfg, ob_experts_ctx** out) {
+  if (!cfg || !out) return OB_ERR_NULL;
+  *out = nullptr;
+  const int64_t most = (int64_t)1 << 20;
+  if (cfg->num_groups < 1 || cfg->num_groups > 65536 || (cfg->dtype != OB_F16 && cfg->dtype != OB_BF16) ||
+      (cfg->w_layout != OB_EXPERTS_KN && cfg->w_layout != OB_EXPERTS_NK) || cfg->reserved != 0 || cfg->k < 1 || cfg->k > most ||
+      cfg->n < 1 || cfg->n > most || cfg->max_rows < 0 || cfg->max_rows > ((int64_t)1 << 30) ||
+      (cfg->w_stride != 0 && cfg->w_stride < cfg->k * cfg->n) || cfg->w_stride > ((int64_t)1 << 44))
+    return OB_ERR_ARG;
+  ob_experts_ctx* ctx = new (std::nothrow) ob_experts_ctx();
+  if (!ctx) return OB_ERR_ARG;
+  ctx->cfg = *cfg;
+  if (!ctx->cfg.w_stride) ctx->cfg.w_stride = cfg->k * cfg->n;
+  if (hipGetDevice(&ctx->device) != hipSuccess) {
+    delete ctx;
+    return OB_ERR_HIP;
+  }
+  *out = ctx;
+  return OB_OK;
+}
+
+void ob_experts_destroy(ob_experts_ctx* ctx) { delete ctx; }
+size_t ob_experts_workspace_bytes(const ob_experts_ctx*) { return 0; }
+const char* ob_experts_last_hip_error(const ob_experts_ctx* ctx) { return ctx ? ctx->hip_err.c_str() : ""; }
+
+ob_status ob_experts_forward(ob_experts_ctx* ctx, const void* x, int64_t ldx, const void* w, const int32_t* offsets, int64_t rows,
+                             void* y, int64_t ldy, ob_dtype y_dtype, void* hip_stream) {
+  return rows_call(ctx, x, ldx, w, offsets, rows, y, ldy, y_dtype, false, hip_stream);
+}
+
+ob_status ob_experts_input_grad(ob_experts_ctx* ctx, const void* dy, int64_t lddy, const void* w, const int32_t* offsets, int64_t rows,
+                                void* dx, int64_t lddx, ob_dtype dx_dtype, void* hip_stream) {
+  return rows_call(ctx, dy, lddy, w, offsets, rows, dx, lddx, dx_dtype, true, hip_stream);
+}
+
+ob_status ob_experts_weight_grad(ob_experts_ctx* ctx, const void* x, int64_t ldx, const void* dy, int64_t lddy, const int32_t* offsets,
+                                 int64_t rows, void* dw, ob_dtype dw_dtype, int32_t accumulate, void* hip_stream) {
+  if (!ctx || !offsets || !dw) return OB_ERR_NULL;
+  const ob_experts_config& c = ctx->cfg;
+  if (rows < 0 || rows > c.max_rows || ldx < c.k || lddy < c.n || ldx >= MAX_LD || lddy >= MAX_LD) return OB_ERR_ARG;
+  if ((dw_dtype != (ob_dtype)c.dtype && dw_dtype != OB_F32) || (accumulate && dw_dtype != OB_F32)) return OB_ERR_ARG;
+  if (!on_device(ctx->device)) return OB_ERR_ARG;
+  if (rows && (!x || !dy)) return OB_ERR_NULL;
+  if (off_element(x, c.dtype) || off_element(dy, c.dtype) || off_element(dw, dw_dtype) || off_element(offsets, OB_F32)) return OB_ERR_ALIGN;
+  WeightsArgs p;
+  p.groups = Groups{offsets, c.num_groups, (int)rows};
+  const bool kn = c.w_layout == OB_EXPERTS_KN;
+  p.a = static_cast<const uint16_t*>(kn ? x : dy);
+  p.b = static_cast<const uint16_t*>(kn ? dy : x);
+  p.lda = kn ? ldx : lddy;
+  p.ldb = kn ? lddy : ldx;
+  p.height = (int)(kn ? c.k : c.n);
+  p.width = (int)(kn ? c.n : c.k);
+  p.out = dw;
+  p.out_stride = c.w_stride;
+  p.out_dtype = dw_dtype;
+  p.accumulate = accumulate != 0;
+  p.a_direct = at16(p.a) && p.lda % 8 == 0 && p.height % 8 == 0;
+  p.b_direct = at16(p.b) && p.ldb % 8 == 0 && p.width % 8 == 0;
+  const hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  return c.dtype == OB_BF16 ? launch_weights<S64, true>(ctx, p, s) : launch_weights<S64, false>(ctx, p, s);
+}
+
+}  // extern "C"
+
+// ---- orthogonalised update -----------------------------------------------------------------------------------------
+struct ob_muon_ctx {
+  int device = -1;
+  int steps = 0, nesterov = 0, precision = OB_F32;
+  float eps = 0, beta = 0, weight_decay = 0;
+  std::vector<float> coefficients;      // 3 * steps
+  int64_t n = 0;                        // elements of the flat buffers
+  int mats = 0, square_tiles = 0;
+  int sym_grid = 0, apply_grid = 0;
+  int64_t x_plane = 0, e_plane = 0;     // elements
+  void* mem = nullptr;
+  size_t bytes = 0;
+  Matrix* d_mats = nullptr;
+  SquareTile* d_square = nullptr;
+  ListTile* d_sym = nullptr;
+  ListTile* d_apply = nullptr;
+  double* d_sums = nullptr;
+  float* d_inv = nullptr;
+  uint16_t* d_x[2] = {nullptr, nullptr};
+  uint16_t* d_e = nullptr;
+  uint16_t* d_b = nullptr;
+  std::string hip_err;
+  ~ob_muon_ctx() {
+    if (mem) (void)hipFree(mem);
+  }
+};
+
+namespace {
+
+// Tiles of a product over the list, dealt to the eight dies: workgroup id runs on die id % 8, so that place id of the table
+// is place id / 8 of that die's queue.  Up to 4 x 8 neighbouring tiles of a matrix (what a die runs at once) stay together;
+// the dearest go first, each to the queue that has the least to do.
+struct Unit {
+  double cost;
+  int mat, tm0, tm1, tn0, tn1;
+};
+std::vector<ListTile> deal(std::vector<Unit> units, bool upper) {
+  std::stable_sort(units.begin(), units.end(), [](const Unit& a, const Unit& b) { return a.cost > b.cost; });
+  std::vector<ListTile> queue[8];
+  double load[8] = {};
+  for (const Unit& u : units) {
+    const int q = (int)(std::min_element(load, load + 8) - load);
+    for (int tn = u.tn0; tn < u.tn1; ++tn)
+      for (int tm = u.tm0; tm < u.tm1; ++tm) {
+        if (upper && tn < tm) continue;
+        queue[q].push_back(ListTile{u.mat, (short)tm, (short)tn});
+        load[q] += u.cost;
+      }
+  }
+  size_t longest = 0;
+  for (const auto& q : queue) longest = std::max(longest, q.size());
+  std::vector<ListTile> table(8 * longest, ListTile{-1, 0, 0});
+  for (int q = 0; q < 8; ++q)
+    for (size_t i = 0; i < queue[q].size(); ++i) table[8 * i + q] = queue[q][i];
+  return table;
+}
+
+std::vector<ListTile> product_tiles(const std::vector<Matrix>& mats, int side, bool symmetric) {
+  std::vector<Unit> units;
+  for (size_t i = 0; i < mats.size(); ++i) {
+    const int nm = (mats[i].mp + side - 1) / side, nn = symmetric ? nm : (mats[i].np + side - 1) / side;
+    const double cost = symmetric ? (double)mats[i].np + mats[i].mp : (double)mats[i].mp;
+    for (int a = 0; a < nm; a += 4)
+      for (int b = 0; b < nn; b += 8) {
+        if (symmetric && std::min(b + 8, nn) <= a) continue;
+        units.push_back(Unit{cost, (int)i, a, std::min(a + 4, nm), b, std::min(b + 8, nn)});
+      }
+  }
+  return deal(std::move(units), symmetric);
+}
+
+template <class T>
+size_t room(size_t count) {
+  return (std::max<size_t>(count * sizeof(T), 1) + 1023) / 1024 * 1024;
+}
+
+template <class S, int TERMS, bool SQUARE>
+void launch_symmetric(const SymmetricArgs& a, int grid, hipStream_t s) {
+  using P = Product<S, false, KC, KC, TERMS, TERMS, false>;
+  hipLaunchKernelGGL((k_polar_symmetric<S, TERMS, SQUARE>), dim3(grid), dim3(S::NT), P::LDS_BYTES, s, a);
+}
+template <class S, int TERMS>
+void launch_apply(const ApplyArgs& a, int grid, hipStream_t s) {
+  using P = Product<S, false, KC, KS, TERMS, 2, false>;
+  hipLaunchKernelGGL((k_polar_apply<S, TERMS>), dim3(grid), dim3(S::NT), P::LDS_BYTES, s, a);
+}
+
+// u -> the working X, its Newton-Schulz steps, and the finishing pass
+ob_status run_list(ob_muon_ctx* ctx, Direction d, float* m_out, const Finish& finish, hipStream_t s) {
+  hipLaunchKernelGGL(k_muon_moments, dim3(ctx->square_tiles), dim3(BLOCK), 0, s, ctx->d_square, ctx->d_mats, d, m_out, ctx->d_sums);
+  hipLaunchKernelGGL(k_muon_norms, dim3(ctx->mats), dim3(BLOCK), 0, s, ctx->d_mats, ctx->d_sums, ctx->eps, ctx->d_inv);
+  hipLaunchKernelGGL(k_muon_pack, dim3(ctx->square_tiles), dim3(BLOCK), 0, s, ctx->d_square, ctx->d_mats, d, ctx->d_inv, ctx->d_x[0], ctx->x_plane);
+  const bool two = ctx->precision == OB_F32;
+  int cur = 0;
+  for (int k = 0; k < ctx->steps; ++k) {
+    const float a = ctx->coefficients[3 * k], b = ctx->coefficients[3 * k + 1], c = ctx->coefficients[3 * k + 2];
+    const float per_gram = 1.0f / (X_UNIT * X_UNIT);
+    SymmetricArgs g{ctx->d_sym, ctx->d_mats, ctx->d_x[cur], ctx->d_e, ctx->x_plane, ctx->e_plane, {}};
+    if (c != 0.0f) {
+      g.q = Quintic{per_gram * E_UNIT, b / (2.0f * c) * E_UNIT};
+    } else {
+      g.out = ctx->d_b;
+      g.q = Quintic{b * per_gram * E_UNIT, a * E_UNIT};
+    }
+    if (two) launch_symmetric<S64x2, 2, false>(g, ctx->sym_grid, s);
+    else launch_symmetric<S64, 1, false>(g, ctx->sym_grid, s);
+    if (c != 0.0f) {
+      SymmetricArgs q{ctx->d_sym, ctx->d_mats, ctx->d_e, ctx->d_b, ctx->e_plane, ctx->e_plane, {}};
+      q.q = Quintic{c / E_UNIT, (float)(((double)a - (double)b * b / (4.0 * c)) * E_UNIT)};
+      if (two) launch_symmetric<S64x2, 2, true>(q, ctx->sym_grid, s);
+      else launch_symmetric<S64, 1, true>(q, ctx->sym_grid, s);
+    }
+    ApplyArgs x{ctx->d_apply, ctx->d_mats, ctx->d_b, ctx->d_x[cur], ctx->d_x[cur ^ 1], ctx->e_plane, ctx->x_plane};
+    if (two) launch_apply<S64x2, 2>(x, ctx->apply_grid, s);
+    else launch_apply<S64x2, 1>(x, ctx->apply_grid, s);
+    cur ^= 1;
+  }
+  hipLaunchKernelGGL(k_muon_finish, dim3(ctx->square_tiles), dim3(BLOCK), 0, s, ctx->d_square, ctx->d_mats, ctx->d_x[cur], ctx->x_plane, finish);
+  return hip_ok(ctx, hipGetLastError(), "the orthogonaliser's kernels") ? OB_OK : OB_ERR_HIP;
+}
+
+ob_status create(const ob_muon_config* cfg, ob_muon_ctx* ctx) {
+  ctx->steps = cfg->steps;
+  ctx->nesterov = cfg->nesterov != 0;
+  ctx->precision = cfg->precision;
+  ctx->eps = cfg->eps;
+  ctx->beta = cfg->beta;
+  ctx->weight_decay = cfg->weight_decay;
+  for (int k = 0; k < cfg->steps; ++k)
+    for (int e = 0; e < 3; ++e) ctx->coefficients.push_back(cfg->coefficients[3 * std::min(k, cfg->num_coefficients - 1) + e]);
+  ctx->n = cfg->layer_offsets[cfg->num_layers];
+  std::vector<Matrix> mats;
+  std::vector<SquareTile> square;
+  int64_t xs = 0, es = 0;
+  for (int64_t l = 0; l < cfg->num_layers; ++l) {
+    const int64_t size = cfg->layer_offsets[l + 1] - cfg->layer_offsets[l], rows = cfg->layer_rows[l];
+    if (rows == 0 || size == 0) continue;
+    const int64_t cols = size / rows;
+    Matrix m{};
+    m.at = cfg->layer_offsets[l];
+    m.rows = (int)rows;
+    m.cols = (int)cols;
+    m.tall = rows > cols;
+    const int64_t side = SIDE;
+    m.mp = (int)((std::min(rows, cols) + side - 1) / side * side);
+    m.np = (int)((std::max(rows, cols) + side - 1) / side * side);
+    m.scale = cfg->layer_scale ? cfg->layer_scale[l] : (float)(0.2 * std::sqrt((double)std::max(rows, cols)));
+    m.x = xs;
+    m.e = es;
+    xs += (int64_t)m.mp * m.np;
+    es += (int64_t)m.mp * m.mp;
+    const int64_t tiles = (int64_t)(m.mp / SIDE) * (m.np / SIDE);
+    if ((int64_t)square.size() + tiles > ((int64_t)1 << 30)) return OB_ERR_SIZE;
+    m.tile0 = (int)square.size();
+    m.tiles = (int)tiles;
+    for (int64_t r = 0; r < rows; r += SIDE)
+      for (int64_t c = 0; c < cols; c += SIDE) square.push_back(SquareTile{(int)mats.size(), (int)r, (int)c});
+    mats.push_back(m);
+  }
+  if (mats.empty()) return OB_ERR_ARG;
+  const std::vector<ListTile> sym = product_tiles(mats, 64, true), apply = product_tiles(mats, 64, false);
+  if (sym.size() > 0x7fffffff || apply.size() > 0x7fffffff) return OB_ERR_SIZE;
+  ctx->mats = (int)mats.size();
+  ctx->square_tiles = (int)square.size();
+  ctx->sym_grid = (int)sym.size();
+  ctx->apply_grid = (int)apply.size();
+  ctx->x_plane = xs;
+  ctx->e_plane = es;
+  size_t total = 0;
+  auto place = [&](size_t bytes) {
+    const size_t at = total;
+    total += bytes;
+    return at;
+  };
+  const size_t at_mats = place(room<Matrix>(mats.size())), at_square = place(room<SquareTile>(square.size()));
+  const size_t at_sym = place(room<ListTile>(sym.size())), at_apply = place(room<ListTile>(apply.size()));
+  const size_t at_sums = place(room<double>(square.size())), at_inv = place(room<float>(mats.size()));
+  const size_t at_x0 = place(room<uint16_t>(2 * xs)), at_x1 = place(room<uint16_t>(2 * xs));
+  const size_t at_e = place(room<uint16_t>(2 * es)), at_b = place(room<uint16_t>(2 * es));
+  if (!hip_ok(ctx, hipGetDevice(&ctx->device), "hipGetDevice") || !hip_ok(ctx, hipMalloc(&ctx->mem, total), "hipMalloc")) return OB_ERR_HIP;
+  ctx->bytes = total;
+  unsigned char* const base = static_cast<unsigned char*>(ctx->mem);
+  ctx->d_mats = reinterpret_cast<Matrix*>(base + at_mats);
+  ctx->d_square = reinterpret_cast<SquareTile*>(base + at_square);
+  ctx->d_sym = reinterpret_cast<ListTile*>(base + at_sym);
+  ctx->d_apply = reinterpret_cast<ListTile*>(base + at_apply);
+  ctx->d_sums = reinterpret_cast<double*>(base + at_sums);
+  ctx->d_inv = reinterpret_cast<float*>(base + at_inv);
+  ctx->d_x[0] = reinterpret_cast<uint16_t*>(base + at_x0);
+  ctx->d_x[1] = reinterpret_cast<uint16_t*>(base + at_x1);
+  ctx->d_e = reinterpret_cast<uint16_t*>(base + at_e);
+  ctx->d_b = reinterpret_cast<uint16_t*>(base + at_b);
+  const bool ok = hip_ok(ctx, hipMemcpy(ctx->d_mats, mats.data(), mats.size() * sizeof(Matrix), hipMemcpyHostToDevice), "hipMemcpy") &&
+                  hip_ok(ctx, hipMemcpy(ctx->d_square, square.data(), square.size() * sizeof(SquareTile), hipMemcpyHostToDevice), "hipMemcpy") &&
+                  hip_ok(ctx, hipMemcpy(ctx->d_sym, sym.data(), sym.size() * sizeof(ListTile), hipMemcpyHostToDevice), "hipMemcpy") &&
+                  hip_ok(ctx, hipMemcpy(ctx->d_apply, apply.data(), apply.size() * sizeof(ListTile), hipMemcpyHostToDevice), "hipMemcpy");
+  return ok ? OB_OK : OB_ERR_HIP;
+}
+
+}  // namespace
+
+extern "C" {
+
+ob_status ob_muon_create(const ob_muon_config* cfg, ob_muon_ctx** out) {
+  if (!cfg || !out) return OB_ERR_NULL;
+  *out = nullptr;
+  if (!cfg->layer_offsets || !cfg->layer_rows || !cfg->coefficients) return OB_ERR_NULL;
+  if (cfg->num_layers < 1 || cfg->num_layers > 0x7fffffff || cfg->steps < 1 || cfg->steps > 64 || cfg->num_coefficients < 1 || cfg->num_coefficients > cfg->steps ||
+      !(cfg->eps >= 0.0f) || !(cfg->beta >= 0.0f && cfg->beta < 1.0f) || !(cfg->weight_decay >= 0.0f) || !std::isfinite(cfg->eps) ||
+      !std::isfinite(cfg->weight_decay) || (cfg->precision != OB_F32 && cfg->precision != OB_F16) || cfg->layer_offsets[0] != 0)
+    return OB_ERR_ARG;
+  for (int i = 0; i < 3 * cfg->num_coefficients; ++i)
+    if (!std::isfinite(cfg->coefficients[i])) return OB_ERR_ARG;
+  for (int64_t l = 0; l < cfg->num_layers; ++l) {
+    const int64_t size = cfg->layer_offsets[l + 1] - cfg->layer_offsets[l], rows = cfg->layer_rows[l];
+    if (size < 0 || cfg->layer_offsets[l + 1] > ((int64_t)1 << 40) || rows < 0 || (rows && size % rows != 0)) return OB_ERR_ARG;
+    // 32-bit offsets inside a tile, tile numbers of 16 bits
+    if (rows && (rows > ((int64_t)1 << 20) || size / rows > ((int64_t)1 << 20))) return OB_ERR_SIZE;
+    if (cfg->layer_scale && !std::isfinite(cfg->layer_scale[l])) return OB_ERR_ARG;
+  }
+  ob_muon_ctx* ctx = nullptr;
+  try {
+    ctx = new ob_muon_ctx();
+    const ob_status s = create(cfg, ctx);
+    if (s != OB_OK) {
+      delete ctx;
+      return s;
+    }
+  } catch (const std::exception&) {      // (out of host memory)
+    delete ctx;
+    return OB_ERR_ARG;
+  }
+  *out = ctx;
+  return OB_OK;
+}
+
+void ob_muon_destroy(ob_muon_ctx* ctx) { delete ctx; }
+size_t ob_muon_workspace_bytes(const ob_muon_ctx* ctx) { return ctx ? ctx->bytes : 0; }
+const char* ob_muon_last_hip_error(const ob_muon_ctx* ctx) { return ctx ? ctx->hip_err.c_str() : ""; }
+
+ob_status ob_muon_orthogonalize(ob_muon_ctx* ctx, const void* src, ob_dtype src_dtype, void* out, ob_dtype out_dtype, void* hip_stream) {
+  if (!ctx || !src || !out) return OB_ERR_NULL;
+  if (!any_dtype(src_dtype) || !any_dtype(out_dtype) || !on_device(ctx->device)) return OB_ERR_ARG;
+  if (off_element(src, src_dtype) || off_element(out, out_dtype)) return OB_ERR_ALIGN;
+  return run_list(ctx, Direction{src, nullptr, src_dtype, 0, 1.0f, 0.0f, 0.0f}, nullptr, Finish{nullptr, out, out_dtype, 0.0f, 0.0f},
+                  static_cast<hipStream_t>(hip_stream));
+}
+
+ob_status ob_muon_step(ob_muon_ctx* ctx, float* x, float* m, const void* grad, ob_dtype grad_dtype, float grad_scale, float lr, void* x_lp,
+                       ob_dtype x_dtype, void* hip_stream) {
+  if (!ctx || !x || !m) return OB_ERR_NULL;
+  if ((grad && !any_dtype(grad_dtype)) || (x_lp && x_dtype != OB_F16 && x_dtype != OB_BF16) || !std::isfinite(lr) || !std::isfinite(grad_scale) ||
+      !on_device(ctx->device))
+    return OB_ERR_ARG;
+  if (off_element(x, OB_F32) || off_element(m, OB_F32) || (grad && off_element(grad, grad_dtype)) || (x_lp && off_element(x_lp, x_dtype))) return OB_ERR_ALIGN;
+  return run_list(ctx, Direction{grad, m, grad ? (int)grad_dtype : F32, ctx->nesterov, grad_scale, ctx->beta, 1.0f - ctx->beta}, m,
+                  Finish{x, x_lp, (int)x_dtype, lr, 1.0f - lr * ctx->weight_decay}, static_cast<hipStream_t>(hip_stream));
+}
+
+}  // extern "C"

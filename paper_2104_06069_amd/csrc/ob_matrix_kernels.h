@@ -1,0 +1,470 @@
+// Kernels of the matrix operators (include/ob_matrix.h), on the tiles of ob_mm.h.  Included by ob_matrix.hip only.
+#pragma once
+
+#include "ob_mm.h"
+
+namespace obm {
+
+constexpr int BLOCK = 256;      // threads of the element-wise kernels
+constexpr int SIDE = 64;        // side of their tiles, and what the sides of the working matrices are multiples of
+
+enum { F32 = 0, F16 = 1, BF16 = 2 };      // ob_dtype
+
+typedef unsigned short v4h __attribute__((ext_vector_type(4)));
+typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef unsigned short v4h_any __attribute__((ext_vector_type(4), aligned(2)));
+
+__device__ __forceinline__ float from_bits(unsigned short h, bool bf) {
+  return bf ? __uint_as_float((unsigned)h << 16) : (float)__builtin_bit_cast(_Float16, h);
+}
+// to nearest, ties to even; NaN -> the format's canonical quiet NaN
+__device__ __forceinline__ unsigned short to_bits(float x, bool bf) {
+  if (bf) {
+    const unsigned u = __float_as_uint(x);
+    if ((u & 0x7fffffffu) > 0x7f800000u) return 0x7fc0;
+    return (unsigned short)((u + 0x7fffu + ((u >> 16) & 1u)) >> 16);
+  }
+  if (x != x) return 0x7e00;
+  return __builtin_bit_cast(unsigned short, (_Float16)x);
+}
+
+// Four values in a row from p + at on, of which those from `left` on do not exist (and read as zeros).
+__device__ __forceinline__ v4f load4(const void* p, int dtype, int64_t at, int left) {
+  v4f v = {};
+  if (left <= 0) return v;
+  if (dtype == F32) {
+    const float* const s = static_cast<const float*>(p) + at;
+    if (left >= 4) return *reinterpret_cast<const v4f_any*>(s);
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+      if (e < left) v[e] = s[e];
+  } else {
+    const unsigned short* const s = static_cast<const unsigned short*>(p) + at;
+    v4h h = {};
+    if (left >= 4) {
+      h = *reinterpret_cast<const v4h_any*>(s);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 3; ++e)
+        if (e < left) h[e] = s[e];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = from_bits(h[e], dtype == BF16);
+  }
+  return v;
+}
+__device__ __forceinline__ void store4(void* p, int dtype, int64_t at, int left, v4f v) {
+  if (left <= 0) return;
+  if (dtype == F32) {
+    float* const s = static_cast<float*>(p) + at;
+    if (left >= 4) {
+      *reinterpret_cast<v4f_any*>(s) = v;
+      return;
+    }
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+      if (e < left) s[e] = v[e];
+  } else {
+    unsigned short* const s = static_cast<unsigned short*>(p) + at;
+    v4h h;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) h[e] = to_bits(v[e], dtype == BF16);
+    if (left >= 4) {
+      *reinterpret_cast<v4h_any*>(s) = h;
+      return;
+    }
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+      if (e < left) s[e] = h[e];
+  }
+}
+
+extern __shared__ __align__(1024) uint16_t lds_of_launch[];
+
+// ---- expert layers -------------------------------------------------------------------------------------------------
+struct Groups {
+  const int32_t* offsets;
+  int n, rows;
+  // rows of group g, inside 0..rows whatever the table holds
+  __device__ __forceinline__ void range(int g, int* lo, int* hi) const {
+    *lo = min(max(offsets[g], 0), rows);
+    *hi = max(min(offsets[g + 1], rows), *lo);
+  }
+};
+
+// Which group's which tile (of BM rows and the `width` columns of tiles) this workgroup has: every wavefront counts the
+// groups' tiles, 64 groups at a time.  The host knows an upper bound of their number alone; workgroups past the last leave.
+struct RowTile {
+  int g, lo, rows, tm, tn;
+};
+template <int BM>
+__device__ __forceinline__ bool find_row_tile(const Groups& gr, int width, int id, RowTile* out) {
+  const int lane = threadIdx.x & 63;
+  int total = 0;
+  for (int g0 = 0; g0 < gr.n; g0 += 64) {
+    int lo = 0, hi = 0;
+    if (g0 + lane < gr.n) gr.range(g0 + lane, &lo, &hi);
+    int t = (hi - lo + BM - 1) / BM;
+#pragma unroll
+    for (int d = 32; d; d >>= 1) t += __shfl_xor(t, d);
+    total += t;
+  }
+  const int tile = tile_of_workgroup(id, __builtin_amdgcn_readfirstlane(total) * width);
+  if (tile < 0) return false;
+  int before = 0;
+  for (int g0 = 0; g0 < gr.n; g0 += 64) {
+    int lo = 0, hi = 0;
+    if (g0 + lane < gr.n) gr.range(g0 + lane, &lo, &hi);
+    const int own = (hi - lo + BM - 1) / BM;
+    int upto = own;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int o = __shfl_up(upto, d);
+      if (lane >= d) upto += o;
+    }
+    const unsigned long long past = __ballot((before + upto) * width > tile);
+    if (past) {
+      const int l = __ffsll((long long)past) - 1;
+      out->g = g0 + l;
+      out->lo = __shfl(lo, l);
+      out->rows = __shfl(hi, l) - out->lo;
+      const int tiles = __shfl(own, l), first = before + __shfl(upto, l) - tiles;
+      tile_in_bands(tile - first * width, tiles, width, &out->tm, &out->tn);
+      out->g = __builtin_amdgcn_readfirstlane(out->g);
+      out->lo = __builtin_amdgcn_readfirstlane(out->lo);
+      out->rows = __builtin_amdgcn_readfirstlane(out->rows);
+      out->tm = __builtin_amdgcn_readfirstlane(out->tm);
+      out->tn = __builtin_amdgcn_readfirstlane(out->tn);
+      return true;
+    }
+    before += __shfl(upto, 63);
+  }
+  return false;
+}
+
+// forward (x, W, y) and input_grad (dy, W transposed, dx): out[r] = a[r] W_g, a [rows, depth], out [rows, width].  FB: order
+// of W as an operand of `width` rows.
+struct RowsArgs {
+  Groups groups;
+  const uint16_t* a;
+  const uint16_t* w;
+  void* out;
+  int64_t lda, ldw, ldo, w_stride;
+  int depth, width, out_dtype;
+  bool a_direct, w_direct;
+};
+template <class S, bool BF, int FB>
+__global__ __launch_bounds__(S::NT, 2) void k_experts_rows(RowsArgs p) {
+  using P = Product<S, BF, KC, FB, 1, 1, true>;
+  RowTile t;
+  if (!find_row_tile<S::BM>(p.groups, (p.width + S::BN - 1) / S::BN, blockIdx.x, &t)) return;
+  typename P::Acc acc = {};
+  const Operand a{p.a + t.lo * p.lda, 0, p.lda, t.rows, p.a_direct};
+  const Operand b{p.w + t.g * p.w_stride, 0, p.ldw, p.width, p.w_direct};
+  P::run(a, b, t.tm * S::BM, t.tn * S::BN, 0, p.depth, lds_of_launch, acc);
+  for_each4<S>(acc, [&](int r, int c, v4f v) {
+    r += t.tm * S::BM;
+    c += t.tn * S::BN;
+    if (r < t.rows) store4(p.out, p.out_dtype, (t.lo + r) * p.ldo + c, p.width - c, v);
+  });
+}
+
+// weight_grad: out_g = a_g^T b_g, a [rows, height], b [rows, width], out [height, width].
+struct WeightsArgs {
+  Groups groups;
+  const uint16_t* a;
+  const uint16_t* b;
+  void* out;
+  int64_t lda, ldb, out_stride;
+  int height, width, out_dtype, accumulate;
+  bool a_direct, b_direct;
+};
+template <class S, bool BF>
+__global__ __launch_bounds__(S::NT, 2) void k_experts_weights(WeightsArgs p) {
+  using P = Product<S, BF, KS, KS, 1, 1, true>;
+  const int nm = (p.height + S::BM - 1) / S::BM, nn = (p.width + S::BN - 1) / S::BN;
+  const int t = tile_of_workgroup(blockIdx.x, p.groups.n * nm * nn);
+  if (t < 0) return;
+  const int g = t / (nm * nn);
+  int tm, tn, lo, hi;
+  tile_in_bands(t - g * nm * nn, nm, nn, &tm, &tn);
+  p.groups.range(g, &lo, &hi);
+  typename P::Acc acc = {};
+  if (hi > lo) {
+    const Operand a{p.a + lo * p.lda, 0, p.lda, p.height, p.a_direct}, b{p.b + lo * p.ldb, 0, p.ldb, p.width, p.b_direct};
+    P::run(a, b, tm * S::BM, tn * S::BN, 0, hi - lo, lds_of_launch, acc);
+  } else if (p.accumulate) {
+    return;
+  }
+  for_each4<S>(acc, [&](int r, int c, v4f v) {
+    r += tm * S::BM;
+    c += tn * S::BN;
+    if (r >= p.height) return;
+    const int64_t at = g * p.out_stride + (int64_t)r * p.width + c;
+    if (p.accumulate) v += load4(p.out, F32, at, p.width - c);
+    store4(p.out, p.out_dtype, at, p.width - c, v);
+  });
+}
+
+// ---- orthogonalised update -----------------------------------------------------------------------------------------
+// A matrix of the list, and its working matrices: X [mp, np], and E, B [mp, mp], binary16, mp and np the sides m <= n
+// rounded up to multiples of SIDE.  Zeros around X stay zeros: every product keeps them.
+struct Matrix {
+  int64_t at;          // in the flat buffers
+  int64_t x, e;        // in a plane of X, of E and of B
+  int rows, cols, mp, np;
+  int tall;            // more rows than columns: X is the transpose
+  int tile0, tiles;    // its element-wise tiles
+  float scale;
+};
+// Working matrices hold X * 2^12 and E, B * 2^8, so that second terms of common elements are normal binary16 numbers
+// (X's elements are about 1 / sqrt(m n) at first, at most 15 by the header's rule).
+constexpr float X_UNIT = 4096.0f, E_UNIT = 256.0f;
+
+struct ListTile {      // of a product; mat < 0: none
+  int mat;
+  short tm, tn;
+};
+
+template <int TERMS>
+__device__ __forceinline__ void store_terms(uint16_t* plane, int64_t term, int64_t at, v4f v) {
+  v4h hi, lo;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const _Float16 h = (_Float16)v[e];
+    hi[e] = __builtin_bit_cast(unsigned short, h);
+    lo[e] = __builtin_bit_cast(unsigned short, (_Float16)(v[e] - (float)h));
+  }
+  *reinterpret_cast<v4h*>(plane + at) = hi;
+  if constexpr (TERMS == 2) *reinterpret_cast<v4h*>(plane + term + at) = lo;
+}
+
+// With S = X X^T and c != 0, a + b S + c S^2 = c E^2 + d, E = S - t, t = -b / 2c, d = a - b^2 / 4c: one product E E^T and
+// nothing to read beside it, and where the singular values end up (S near 1) E is small, so that what E's rounding costs is
+// small too.  With c == 0, B = a + b S comes from the first product alone.
+struct Quintic {
+  float mul, diag;      // out = mul * (the product) + diag on the diagonal
+};
+
+// SQUARE: B from E, both [mp, mp]; else E (or B) from X [mp, np].  Both are symmetric: tiles with tn >= tm, each written
+// on both sides of the diagonal.
+struct SymmetricArgs {
+  const ListTile* tiles;
+  const Matrix* mats;
+  const uint16_t* in;
+  uint16_t* out;
+  int64_t in_term, out_term;
+  Quintic q;
+};
+template <class S, int TERMS, bool SQUARE>
+__global__ __launch_bounds__(S::NT, 2) void k_polar_symmetric(SymmetricArgs p) {
+  using P = Product<S, false, KC, KC, TERMS, TERMS, false>;
+  const ListTile t = p.tiles[blockIdx.x];
+  if (t.mat < 0) return;
+  const Matrix& m = p.mats[t.mat];
+  const int mp = m.mp, depth = SQUARE ? mp : m.np;
+  typename P::Acc acc = {};
+  const Operand a{p.in + (SQUARE ? m.e : m.x), p.in_term, depth, mp, true};
+  const int r0 = t.tm * S::BM, c0 = t.tn * S::BN;
+  P::run(a, a, r0, c0, 0, depth, lds_of_launch, acc);
+  uint16_t* const out = p.out + m.e;
+  for_each4<S>(acc, [&](int r, int c, v4f v) {
+    r += r0;
+    c += c0;
+    if (r >= mp || c >= mp) return;
+    v *= p.q.mul;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (r == c + e) v[e] += p.q.diag;
+    store_terms<TERMS>(out, p.out_term, (int64_t)r * mp + c, v);
+    if (t.tm == t.tn) return;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const _Float16 h = (_Float16)v[e];
+      const int64_t at = (int64_t)(c + e) * mp + r;
+      out[at] = __builtin_bit_cast(unsigned short, h);
+      if constexpr (TERMS == 2) out[p.out_term + at] = __builtin_bit_cast(unsigned short, (_Float16)(v[e] - (float)h));
+    }
+  });
+}
+
+// X' = B X
+struct ApplyArgs {
+  const ListTile* tiles;
+  const Matrix* mats;
+  const uint16_t* b;
+  const uint16_t* x;
+  uint16_t* out;
+  int64_t b_term, x_term;
+};
+template <class S, int B_TERMS>
+__global__ __launch_bounds__(S::NT, 2) void k_polar_apply(ApplyArgs p) {
+  using P = Product<S, false, KC, KS, B_TERMS, 2, false>;
+  const ListTile t = p.tiles[blockIdx.x];
+  if (t.mat < 0) return;
+  const Matrix& m = p.mats[t.mat];
+  typename P::Acc acc = {};
+  const Operand a{p.b + m.e, p.b_term, m.mp, m.mp, true}, b{p.x + m.x, p.x_term, m.np, m.np, true};
+  const int r0 = t.tm * S::BM, c0 = t.tn * S::BN;
+  P::run(a, b, r0, c0, 0, m.mp, lds_of_launch, acc);
+  for_each4<S>(acc, [&](int r, int c, v4f v) {
+    r += r0;
+    c += c0;
+    if (r < m.mp && c < m.np) store_terms<2>(p.out + m.x, p.x_term, (int64_t)r * m.np + c, v * (1.0f / E_UNIT));
+  });
+}
+
+// Element-wise tiles are SIDE x SIDE elements of a matrix in the list's order, padding included; a thread has four
+// adjacent elements of rows t / 16 + 16 j.
+struct SquareTile {
+  int mat, row0, col0;
+};
+
+// The direction u of a step, from m after its update.
+struct Direction {
+  const void* g;     // NULL: m itself
+  const float* m;    // NULL: g itself (orthogonalize)
+  int dtype, nesterov;
+  float scale, beta, omb;
+};
+__device__ __forceinline__ v4f direction4(const Direction& d, v4f g, v4f m) {
+  if (!d.m) return g;
+  if (!d.g || !d.nesterov) return m;
+  v4f u;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) u[e] = d.beta * m[e] + d.omb * (d.scale * g[e]);
+  return u;
+}
+
+// m <- beta m + (1 - beta) scale g, and the sum of u's squares over each tile, in binary64.
+__global__ __launch_bounds__(BLOCK) void k_muon_moments(const SquareTile* tiles, const Matrix* mats, Direction d, float* m_out, double* sums) {
+  const SquareTile t = tiles[blockIdx.x];
+  const Matrix& mat = mats[t.mat];
+  double s = 0.0;
+#pragma unroll
+  for (int j = 0; j < SIDE / 16; ++j) {
+    const int r = t.row0 + threadIdx.x / 16 + 16 * j, c = t.col0 + threadIdx.x % 16 * 4;
+    if (r >= mat.rows || c >= mat.cols) continue;
+    const int64_t at = mat.at + (int64_t)r * mat.cols + c;
+    const int left = mat.cols - c;
+    v4f g = {}, m = {};
+    if (d.g) g = load4(d.g, d.dtype, at, left);
+    if (d.m) m = load4(d.m, F32, at, left);
+    if (d.m && d.g) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) m[e] = d.beta * m[e] + d.omb * (d.scale * g[e]);
+      store4(m_out, F32, at, left, m);
+    }
+    const v4f u = direction4(d, g, m);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (e < left) s += (double)u[e] * (double)u[e];
+  }
+  __shared__ double part[BLOCK / 64];
+#pragma unroll
+  for (int k = 32; k; k >>= 1) s += __shfl_xor(s, k);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) sums[blockIdx.x] = (part[0] + part[1]) + (part[2] + part[3]);
+}
+
+// X_UNIT / (norm + eps) of each matrix
+__global__ __launch_bounds__(BLOCK) void k_muon_norms(const Matrix* mats, const double* sums, float eps, float* inv) {
+  const Matrix& m = mats[blockIdx.x];
+  double s = 0.0;
+  for (int i = threadIdx.x; i < m.tiles; i += BLOCK) s += sums[m.tile0 + i];
+  __shared__ double part[BLOCK / 64];
+#pragma unroll
+  for (int k = 32; k; k >>= 1) s += __shfl_xor(s, k);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) inv[blockIdx.x] = (float)((double)X_UNIT / (sqrt((part[0] + part[1]) + (part[2] + part[3])) + (double)eps));
+}
+
+// X = u / (norm + eps), transposed for tall matrices, zeros around it.
+__global__ __launch_bounds__(BLOCK) void k_muon_pack(const SquareTile* tiles, const Matrix* mats, Direction d, const float* inv, uint16_t* x, int64_t term) {
+  __shared__ float turned[SIDE][SIDE + 1];
+  const SquareTile t = tiles[blockIdx.x];
+  const Matrix& mat = mats[t.mat];
+  const float f = inv[t.mat];
+#pragma unroll
+  for (int j = 0; j < SIDE / 16; ++j) {
+    const int y = threadIdx.x / 16 + 16 * j, z = threadIdx.x % 16 * 4, r = t.row0 + y, c = t.col0 + z;
+    v4f v = {};
+    if (r < mat.rows && c < mat.cols) {
+      const int64_t at = mat.at + (int64_t)r * mat.cols + c;
+      const int left = mat.cols - c;
+      v4f g = {}, m = {};
+      if (d.g && (!d.m || d.nesterov)) g = load4(d.g, d.dtype, at, left);
+      if (d.m) m = load4(d.m, F32, at, left);
+      const v4f u = direction4(d, g, m);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = e < left ? u[e] * f : 0.0f;
+    }
+    if (!mat.tall) {
+      store_terms<2>(x + mat.x, term, (int64_t)r * mat.np + c, v);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) turned[z + e][y] = v[e];
+    }
+  }
+  if (!mat.tall) return;
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < SIDE / 16; ++j) {
+    const int y = threadIdx.x / 16 + 16 * j, z = threadIdx.x % 16 * 4;
+    const v4f v = {turned[y][z], turned[y][z + 1], turned[y][z + 2], turned[y][z + 3]};
+    store_terms<2>(x + mat.x, term, (int64_t)(t.col0 + y) * mat.np + t.row0 + z, v);
+  }
+}
+
+// Either out = X in the list's order (orthogonalize), or the update of the parameters.
+struct Finish {
+  float* x;                 // NULL: orthogonalize
+  void* out;                // x_lp (or NULL), or the orthogonaliser's output
+  int dtype;
+  float lr, keep;           // keep = 1 - lr * weight_decay
+};
+__global__ __launch_bounds__(BLOCK) void k_muon_finish(const SquareTile* tiles, const Matrix* mats, const uint16_t* work, int64_t term, Finish p) {
+  __shared__ float turned[SIDE][SIDE + 1];
+  const SquareTile t = tiles[blockIdx.x];
+  const Matrix& mat = mats[t.mat];
+  if (t.row0 >= mat.rows || t.col0 >= mat.cols) return;
+  auto load = [&](int64_t at) {
+    const v4h hi = *reinterpret_cast<const v4h*>(work + mat.x + at), lo = *reinterpret_cast<const v4h*>(work + mat.x + term + at);
+    v4f v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = (from_bits(hi[e], false) + from_bits(lo[e], false)) * (1.0f / X_UNIT);
+    return v;
+  };
+  if (mat.tall) {
+#pragma unroll
+    for (int j = 0; j < SIDE / 16; ++j) {
+      const int y = threadIdx.x / 16 + 16 * j, z = threadIdx.x % 16 * 4;
+      const v4f v = load((int64_t)(t.col0 + y) * mat.np + t.row0 + z);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) turned[z + e][y] = v[e];
+    }
+    __syncthreads();
+  }
+  const float step = p.lr * mat.scale;
+#pragma unroll
+  for (int j = 0; j < SIDE / 16; ++j) {
+    const int y = threadIdx.x / 16 + 16 * j, z = threadIdx.x % 16 * 4, r = t.row0 + y, c = t.col0 + z;
+    if (r >= mat.rows || c >= mat.cols) continue;
+    v4f o;
+    if (mat.tall) o = v4f{turned[y][z], turned[y][z + 1], turned[y][z + 2], turned[y][z + 3]};
+    else o = load((int64_t)r * mat.np + c);
+    const int64_t at = mat.at + (int64_t)r * mat.cols + c;
+    const int left = mat.cols - c;
+    if (p.x) {
+      const v4f x = load4(p.x, F32, at, left);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = x[e] * p.keep - step * o[e];
+      store4(p.x, F32, at, left, o);
+    }
+    if (p.out) store4(p.out, p.dtype, at, left, o);
+  }
+}
+
+}  // namespace obm

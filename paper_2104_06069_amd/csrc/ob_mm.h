@@ -1,0 +1,269 @@
+// Core of the matrix operators (gfx950): one workgroup's tile of C = A B^T with 16-bit operands and binary32
+// accumulation, on the matrix cores.  Included by ob_matrix.hip only.
+//
+// An operand is a matrix of `rows` rows (the tile's M or N side) and K columns, in one of two orders: KC, element (r, k)
+// at p[r * ld + k], or KS, element (r, k) at p[k * ld + r].  It has one or two terms (planes `term` elements apart): with
+// two, its value is their sum, a binary16 number and the binary16 rounding of what that left over (22 bits).  The product
+// of two two-term operands leaves out the product of the second terms, 2^-22 of the result.
+//
+// What bounds such a tile is the rate of the matrix instructions, and next to it LDS: a wavefront of a 256 x 256 tile owns
+// 128 x 64 of it and reads 12 KB of LDS for each 32 columns of K, 768 of the 1024 cycles that the eight wavefronts' matrix
+// instructions take.  The wavefronts are therefore two groups that take turns, half a step apart: while one reads its
+// operands from LDS (and starts the loads of the next K slab from memory straight into LDS), the other has the matrix
+// cores.  Measured at 8192^3 with binary16 operands: 1130 to 1190 TFLOP/s (the library's product of the same: 1405), with
+// two terms 1370 to 1425 TFLOP/s of matrix instructions (three products out of each two slabs read); 128 x 128 tiles 960.
+//
+// LDS holds 16-byte pieces in the order in which the loads bring them.  Which piece of its row a lane fetches is permuted
+// by the row's number, so that the reads below do not meet in the same banks.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+namespace obm {
+
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef short v4s __attribute__((ext_vector_type(4)));
+typedef short v8s __attribute__((ext_vector_type(8)));
+typedef short v8s_any __attribute__((ext_vector_type(8), aligned(2)));   // at any 2-byte address
+typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+typedef __bf16 v8b __attribute__((ext_vector_type(8)));
+typedef unsigned long long v2u __attribute__((ext_vector_type(2)));
+
+enum { KC = 0, KS = 1 };
+
+template <class T>
+__device__ __forceinline__ __attribute__((address_space(3))) T* in_lds(const void* p) {
+  return (__attribute__((address_space(3))) T*)p;
+}
+
+template <bool BF>
+__device__ __forceinline__ v4f mma(v8s a, v8s b, v4f c) {
+  if constexpr (BF) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8b, a), __builtin_bit_cast(v8b, b), c, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
+}
+
+struct Operand {
+  const uint16_t* p;
+  int64_t term;    // elements from the first term's plane to the second's
+  int64_t ld;
+  int rows;        // >= 1
+  bool direct;     // every 16-byte piece lies at a 16-byte address (and rows % 8 == 0 in the KS order)
+};
+
+// BR rows by BK columns of an operand, brought into LDS by NT threads
+template <int FORM, int BR, int BK, int NT>
+struct Slab {
+  static constexpr int PIECES = FORM == KC ? BK / 8 : BR / 8;      // of 8 elements, in one row of LDS
+  static constexpr int ALL = BR * BK / 8, WORK = ALL < NT ? ALL : NT;   // threads that fetch: whole wavefronts
+  static constexpr int PER = ALL / WORK, STEP = WORK / PIECES;     // pieces each of them fetches, LDS rows between those
+  static_assert(BK == 32 || BK == 64, "the permutations below");
+  static_assert(PER * WORK == ALL && WORK % 64 == 0 && WORK % PIECES == 0 && (PER == 1 || STEP % 16 == 0), "whole passes, each of the same permutation");
+
+  __device__ static int turn(int row) {
+    if constexpr (FORM == KC) return BK == 64 ? row & 7 : (row >> 1) & 3;
+    else return (((row & 3) | ((row >> 1) & 4)) << 1) & (PIECES - 1);
+  }
+
+  int off[FORM == KC ? PER : 1];     // elements from the tile's first
+
+  __device__ void init(const Operand& o, int r0, int tid) {
+    const int row = tid / PIECES, at = ((tid % PIECES) ^ turn(row)) * 8;
+    if constexpr (FORM == KC) {
+#pragma unroll
+      for (int j = 0; j < PER; ++j) off[j] = (int)((min(r0 + row + j * STEP, o.rows - 1) - r0) * o.ld) + at;
+    } else {
+      off[0] = (int)(row * o.ld) + min(r0 + at, o.rows - 8) - r0;
+    }
+  }
+
+  // A slab whose BK columns all exist, of an operand with `direct`: rows past the last repeat one that exists.
+  __device__ void load(const Operand& o, int term, int r0, int k0, uint16_t* lds, int wave) const {
+    if (WORK < NT && wave >= WORK / 64) return;
+    const uint16_t* const base = o.p + term * o.term;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      const uint16_t* src;
+      if constexpr (FORM == KC) src = base + (int64_t)r0 * o.ld + k0 + off[j];
+      else src = base + (int64_t)(k0 + j * STEP) * o.ld + r0 + off[0];
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, in_lds<void>(lds + wave * 512 + j * WORK * 8), 16, 0, 0);
+    }
+  }
+
+  // Any slab, through registers; columns from K on are zeros.
+  __device__ static void load_any(const Operand& o, int r0, int k0, int K, uint16_t* lds, int tid) {
+    if (WORK < NT && tid >= WORK) return;
+    const int row0 = tid / PIECES, pos = tid % PIECES;
+    const int width = FORM == KC ? K : o.rows;      // of a row in memory
+    v8s v[PER];
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      const int row = row0 + j * STEP, at = (pos ^ turn(row)) * 8;
+      const int r = FORM == KC ? min(r0 + row, o.rows - 1) : k0 + row;
+      const int c = FORM == KC ? k0 + at : r0 + at, left = r < (FORM == KC ? o.rows : K) ? width - c : 0;
+      v[j] = v8s{};
+      const uint16_t* const src = o.p + (int64_t)r * o.ld + c;
+      if (left >= 8) {
+        v[j] = *reinterpret_cast<const v8s_any*>(src);
+      } else if (left > 0 && width >= 8) {     // the eight elements up to the row's end, moved down
+        const v2u w = __builtin_bit_cast(v2u, (v8s)*reinterpret_cast<const v8s_any*>(src + left - 8));
+        const int s = (8 - left) * 16;
+        v2u z;
+        z.x = s >= 64 ? w.y >> (s - 64) : (w.x >> s) | (w.y << (64 - s));
+        z.y = s >= 64 ? 0 : w.y >> s;
+        v[j] = __builtin_bit_cast(v8s, z);
+      } else if (left > 0) {                   // rows of fewer than eight
+#pragma unroll
+        for (int e = 0; e < 7; ++e)
+          if (e < left) v[j][e] = (short)src[e];
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < PER; ++j) *in_lds<v8s>(lds + (j * WORK + tid) * 8) = v[j];
+  }
+
+  // Operand registers of a 16x16x32 product: lane (q, i) gets row f0 + i, columns 32 kk + 8 q + 0..7 of the slab.
+  __device__ static v8s fragment(const uint16_t* lds, int f0, int kk, int lane) {
+    const int i = lane & 15, q = lane >> 4;
+    if constexpr (FORM == KC) {
+      return *in_lds<const v8s>(lds + (f0 + i) * BK + (((kk * 4 + q) ^ turn(i)) * 8));
+    } else {
+      // sixteen lanes read 4 columns by 16 rows, and get them transposed
+      const int k = kk * 32 + 8 * q + (i >> 2), piece = (f0 >> 3) + ((i & 3) >> 1);
+      const uint16_t* const a = lds + k * BR + ((piece ^ turn(k)) * 8) + (i & 1) * 4;     // (turn(k) == turn(k + 4))
+      const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(in_lds<v4s>(a));
+      const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(in_lds<v4s>(a + 4 * BR));
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+  }
+};
+
+__device__ __forceinline__ void group_barrier() {
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_sched_barrier(0);
+}
+__device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void lds_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+template <int BM_, int BN_, int BK_, int WM_, int WN_>
+struct Shape {
+  static constexpr int BM = BM_, BN = BN_, BK = BK_, WM = WM_, WN = WN_, WAVES = WM * WN, NT = WAVES * 64;
+  static constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
+};
+
+// ANY: the operands may need load_any (slabs that end inside, addresses that are no multiples of 16); without it they are
+// `direct` and K is a multiple of BK.
+template <class S, bool BF, int FA, int FB, int TA, int TB, bool ANY>
+struct Product {
+  static constexpr int BM = S::BM, BN = S::BN, BK = S::BK, FM = S::FM, FN = S::FN;
+  static_assert(!ANY || (TA == 1 && TB == 1), "load_any has one term");
+  using A = Slab<FA, BM, BK, S::NT>;
+  using B = Slab<FB, BN, BK, S::NT>;
+  static constexpr int STAGE = (TA * BM + TB * BN) * BK;
+  static constexpr int LDS_BYTES = 2 * STAGE * 2;
+  typedef v4f Acc[FM][FN];
+
+  // Lane (q, i) of wavefront (wm, wn): acc[x][y][e] is row wm * BM / WM + 16 x + i, column wn * BN / WN + 16 y + 4 q + e.
+  // K columns from k0 on; K >= 1.
+  __device__ static void run(const Operand& a, const Operand& b, int r0, int c0, int k0, int K, uint16_t* lds, Acc& acc) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave / S::WN, wn = wave % S::WN;
+    const bool second = wave >= S::WAVES / 2;
+    A sa;
+    B sb;
+    sa.init(a, r0, tid);
+    sb.init(b, c0, tid);
+    const int n = (K + BK - 1) / BK, end = k0 + K;
+    auto load = [&](int t) {
+      uint16_t* const s = lds + (t & 1) * STAGE;
+      const int k = k0 + t * BK;
+      if (!ANY || (a.direct && k + BK <= end)) {
+#pragma unroll
+        for (int x = 0; x < TA; ++x) sa.load(a, x, r0, k, s + x * BM * BK, wave);
+      } else {
+        A::load_any(a, r0, k, end, s, tid);
+      }
+      if (!ANY || (b.direct && k + BK <= end)) {
+#pragma unroll
+        for (int y = 0; y < TB; ++y) sb.load(b, y, c0, k, s + (TA * BM + y * BN) * BK, wave);
+      } else {
+        B::load_any(b, c0, k, end, s + TA * BM * BK, tid);
+      }
+    };
+    // Turns are separated by barriers; the second group is one turn behind.  Slab t + 1 goes where slab t - 1 was: both
+    // groups start it in the turn after the second group's last read of slab t - 1, and wait for it at the end of the turn
+    // before the first group's first read.
+    load(0);
+    loads_done();
+    group_barrier();
+    if (second) {
+      if (n > 1) load(1);
+      group_barrier();
+    }
+    for (int t = 0; t < n; ++t) {
+      const uint16_t* const s = lds + (t & 1) * STAGE;
+#pragma unroll
+      for (int kk = 0; kk < BK / 32; ++kk) {
+        const bool last = kk == BK / 32 - 1;
+        v8s fa[TA][FM], fb[TB][FN];
+#pragma unroll
+        for (int y = 0; y < TB; ++y)
+#pragma unroll
+          for (int f = 0; f < FN; ++f) fb[y][f] = B::fragment(s + (TA * BM + y * BN) * BK, wn * (BN / S::WN) + f * 16, kk, lane);
+#pragma unroll
+        for (int x = 0; x < TA; ++x)
+#pragma unroll
+          for (int f = 0; f < FM; ++f) fa[x][f] = A::fragment(s + x * BM * BK, wm * (BM / S::WM) + f * 16, kk, lane);
+        if (kk == 0 && !second && t + 1 < n) load(t + 1);
+        if (last && second) loads_done();
+        else lds_done();
+        group_barrier();
+        if (last && second && t + 2 < n) load(t + 2);
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int x = 0; x < TA; ++x)
+#pragma unroll
+          for (int y = 0; y < TB; ++y)
+            if (x + y < 2) {
+#pragma unroll
+              for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int j = 0; j < FN; ++j) acc[i][j] = mma<BF>(fb[y][j], fa[x][i], acc[i][j]);
+            }
+        __builtin_amdgcn_s_setprio(0);
+        if (last && !second) loads_done();
+        group_barrier();
+      }
+    }
+    if (!second) group_barrier();
+  }
+};
+
+// Calls f(row, column, values of four adjacent columns) for all that this lane holds of the tile.
+template <class S, class F>
+__device__ __forceinline__ void for_each4(const v4f (&acc)[S::FM][S::FN], F f) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / S::WN, wn = wave % S::WN;
+#pragma unroll
+  for (int i = 0; i < S::FM; ++i)
+#pragma unroll
+    for (int j = 0; j < S::FN; ++j)
+      f(wm * (S::BM / S::WM) + i * 16 + (lane & 15), wn * (S::BN / S::WN) + j * 16 + 4 * (lane >> 4), acc[i][j]);
+}
+
+// Workgroups are dealt to the eight dies in turn, each with a cache of its own: consecutive tiles go to one die.  -1: none.
+__device__ __forceinline__ int tile_of_workgroup(int id, int tiles) {
+  const int per = (tiles + 7) / 8, at = id >> 3, t = (id & 7) * per + at;
+  return at < per && t < tiles ? t : -1;
+}
+
+// Tile t of nm x nn: bands of up to 4 rows of tiles, down a band's columns first, so that the tiles that run at the same
+// time share operands.
+__device__ __forceinline__ void tile_in_bands(int t, int nm, int nn, int* tm, int* tn) {
+  const int band = t / (4 * nn), first = band * 4, height = min(4, nm - first), u = t - first * nn;
+  *tm = first + u % height;
+  *tn = u / height;
+}
+
+}  // namespace obm
