@@ -8,6 +8,7 @@
 #include <limits>
 #include <new>
 #include <string>
+#include <type_traits>
 #include <vector>
 
 #include "ob_matrix.h"
@@ -17,8 +18,28 @@ using namespace obm;
 
 namespace {
 
-using S64 = Shape<64, 64, 64, 2, 2>;
-using S64x2 = Shape<64, 64, 32, 2, 2>;
+// Tiles of the products, by side: 256 (eight wavefronts, one workgroup on a CU), 128 and 64 (four).  Slabs of 64 columns, or
+// with two terms of 32: the same LDS.
+template <int SIDE_, int BK>
+using Tile = Shape<SIDE_, SIDE_, BK, 2, SIDE_ == 256 ? 4 : 2>;
+
+template <class F>
+auto with_side(int side, F f) {
+  if (side == 256) return f(std::integral_constant<int, 256>{});
+  if (side == 128) return f(std::integral_constant<int, 128>{});
+  return f(std::integral_constant<int, 64>{});
+}
+
+// A workgroup's share of the matrix cores' rate, and how many run at once: 8192^3 at 1150, 960 and (64 x 64) 420 TFLOP/s.
+struct Side {
+  int side, at_once;
+  double rate;      // multiply-adds a microsecond and CU
+};
+constexpr Side SIDES[] = {{256, 256, 2.2e6}, {128, 512, 1.9e6}, {64, 1024, 0.8e6}};
+// Time of `tiles` tiles of the given mean depth, in microseconds, if they are dealt evenly
+double tiles_time(const Side& s, double tiles, double depth) {
+  return std::ceil(tiles / s.at_once) * (s.at_once / 256) * s.side * s.side * depth / s.rate;
+}
 
 inline int elem_size(int dtype) { return dtype == OB_F32 ? 4 : 2; }
 inline bool off_element(const void* p, int dtype) { return reinterpret_cast<uintptr_t>(p) % elem_size(dtype) != 0; }
@@ -42,7 +63,7 @@ bool on_device(int device) {
 
 // A kernel may ask for more than 64 KB of LDS once it has been told.
 template <class K>
-hipError_t allow_lds(K kernel, int bytes) {
+hipError_t allow_lds(K* kernel, int bytes) {
   return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
 }
 
@@ -57,24 +78,64 @@ struct ob_experts_ctx {
 
 namespace {
 
-template <class S, bool BF, int FB>
+// The side whose tiles take the shortest, for `tiles(side)` tiles
+template <class F>
+int best_side(F tiles, double depth) {
+  int best = 64;
+  double least = 1e300;
+  for (const Side& s : SIDES) {
+    const double t = tiles_time(s, tiles(s.side), depth);
+    if (t < least) {
+      least = t;
+      best = s.side;
+    }
+  }
+  return best;
+}
+
+template <class S, bool BF, int FB, int MODE>
 ob_status launch_rows(ob_experts_ctx* ctx, const RowsArgs& p, hipStream_t stream) {
-  using P = Product<S, BF, KC, FB, 1, 1, true>;
   const int64_t tiles = ((int64_t)p.groups.rows / S::BM + std::min<int64_t>(p.groups.n, p.groups.rows)) * ((p.width + S::BN - 1) / S::BN);
   const int64_t grid = (tiles + 7) / 8 * 8;
   if (grid > 0x7fffffff) return OB_ERR_SIZE;
-  hipLaunchKernelGGL((k_experts_rows<S, BF, FB>), dim3((unsigned)grid), dim3(S::NT), P::LDS_BYTES, stream, p);
+  hipLaunchKernelGGL((k_experts_rows<S, BF, FB, MODE>), dim3((unsigned)grid), dim3(S::NT), (Product<S, BF, KC, FB, 1, 1, MODE>::LDS_BYTES), stream, p);
   return hip_ok(ctx, hipGetLastError(), "k_experts_rows") ? OB_OK : OB_ERR_HIP;
 }
 
-template <class S, bool BF>
+template <class S, bool BF, int MODE>
 ob_status launch_weights(ob_experts_ctx* ctx, const WeightsArgs& p, hipStream_t stream) {
-  using P = Product<S, BF, KS, KS, 1, 1, true>;
   const int64_t tiles = (int64_t)p.groups.n * ((p.height + S::BM - 1) / S::BM) * ((p.width + S::BN - 1) / S::BN);
   const int64_t grid = (tiles + 7) / 8 * 8;
   if (grid > 0x7fffffff) return OB_ERR_SIZE;
-  hipLaunchKernelGGL((k_experts_weights<S, BF>), dim3((unsigned)grid), dim3(S::NT), P::LDS_BYTES, stream, p);
+  hipLaunchKernelGGL((k_experts_weights<S, BF, MODE>), dim3((unsigned)grid), dim3(S::NT), (Product<S, BF, KS, KS, 1, 1, MODE>::LDS_BYTES), stream, p);
   return hip_ok(ctx, hipGetLastError(), "k_experts_weights") ? OB_OK : OB_ERR_HIP;
+}
+
+// f(side, mode): operands that are not `direct` have tiles of up to 128 (ob_mm.h)
+template <class F>
+auto with_side_and_mode(int side, bool direct, F f) {
+  if (!direct) {
+    if (side >= 128) return f(std::integral_constant<int, 128>{}, std::integral_constant<int, ANY>{});
+    return f(std::integral_constant<int, 64>{}, std::integral_constant<int, ANY>{});
+  }
+  return with_side(side, [&](auto n) { return f(n, std::integral_constant<int, TAIL>{}); });
+}
+
+template <bool BF>
+hipError_t allow_experts() {
+  hipError_t e = hipSuccess;
+  for (const Side& side : SIDES)
+    for (const bool direct : {false, true}) {
+      if (e != hipSuccess) return e;
+      e = with_side_and_mode(side.side, direct, [&](auto n, auto mode) {
+        using S = Tile<n, 64>;
+        hipError_t e = allow_lds(k_experts_rows<S, BF, KC, mode>, Product<S, BF, KC, KC, 1, 1, mode>::LDS_BYTES);
+        if (e == hipSuccess) e = allow_lds(k_experts_rows<S, BF, KS, mode>, Product<S, BF, KC, KS, 1, 1, mode>::LDS_BYTES);
+        if (e == hipSuccess) e = allow_lds(k_experts_weights<S, BF, mode>, Product<S, BF, KS, KS, 1, 1, mode>::LDS_BYTES);
+        return e;
+      });
+    }
+  return e;
 }
 
 constexpr int64_t MAX_LD = (int64_t)1 << 22;      // a tile's offsets are 32-bit
@@ -106,8 +167,14 @@ ob_status rows_call(ob_experts_ctx* ctx, const void* a, int64_t lda, const void*
   p.a_direct = at16(a) && lda % 8 == 0;
   p.w_direct = at16(w) && p.ldw % 8 == 0 && c.w_stride % 8 == 0 && (!strided || width % 8 == 0);
   const hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  if (c.dtype == OB_BF16) return strided ? launch_rows<S64, true, KS>(ctx, p, s) : launch_rows<S64, true, KC>(ctx, p, s);
-  return strided ? launch_rows<S64, false, KS>(ctx, p, s) : launch_rows<S64, false, KC>(ctx, p, s);
+  // (a group's last tile is half full in the mean)
+  const double groups = (double)std::min<int64_t>(c.num_groups, rows);
+  const int side = best_side([&](int n) { return std::max(groups, rows / (double)n + 0.5 * groups) * (double)((width + n - 1) / n); }, (double)depth);
+  return with_side_and_mode(side, p.a_direct && p.w_direct, [&](auto n, auto mode) {
+    using S = Tile<n, 64>;
+    if (c.dtype == OB_BF16) return strided ? launch_rows<S, true, KS, mode>(ctx, p, s) : launch_rows<S, true, KC, mode>(ctx, p, s);
+    return strided ? launch_rows<S, false, KS, mode>(ctx, p, s) : launch_rows<S, false, KC, mode>(ctx, p, s);
+  });
 }
 
 }  // namespace
@@ -127,7 +194,9 @@ ob_status ob_experts_create(const ob_experts_config* cfg, ob_experts_ctx** out) 
   if (!ctx) return OB_ERR_ARG;
   ctx->cfg = *cfg;
   if (!ctx->cfg.w_stride) ctx->cfg.w_stride = cfg->k * cfg->n;
-  if (hipGetDevice(&ctx->device) != hipSuccess) {
+  hipError_t e = hipGetDevice(&ctx->device);
+  if (e == hipSuccess) e = cfg->dtype == OB_BF16 ? allow_experts<true>() : allow_experts<false>();
+  if (e != hipSuccess) {
     delete ctx;
     return OB_ERR_HIP;
   }
@@ -174,7 +243,12 @@ ob_status ob_experts_weight_grad(ob_experts_ctx* ctx, const void* x, int64_t ldx
   p.a_direct = at16(p.a) && p.lda % 8 == 0 && p.height % 8 == 0;
   p.b_direct = at16(p.b) && p.ldb % 8 == 0 && p.width % 8 == 0;
   const hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  return c.dtype == OB_BF16 ? launch_weights<S64, true>(ctx, p, s) : launch_weights<S64, false>(ctx, p, s);
+  const int side = best_side([&](int n) { return (double)c.num_groups * ((p.height + n - 1) / n) * ((p.width + n - 1) / n); },
+                             (double)rows / c.num_groups);
+  return with_side_and_mode(side, p.a_direct && p.b_direct, [&](auto n, auto mode) {
+    using S = Tile<n, 64>;
+    return c.dtype == OB_BF16 ? launch_weights<S, true, mode>(ctx, p, s) : launch_weights<S, false, mode>(ctx, p, s);
+  });
 }
 
 }  // extern "C"
@@ -187,7 +261,7 @@ struct ob_muon_ctx {
   std::vector<float> coefficients;      // 3 * steps
   int64_t n = 0;                        // elements of the flat buffers
   int mats = 0, square_tiles = 0;
-  int sym_grid = 0, apply_grid = 0;
+  int sym_side = 64, apply_side = 64, sym_grid = 0, apply_grid = 0;
   int64_t x_plane = 0, e_plane = 0;     // elements
   void* mem = nullptr;
   size_t bytes = 0;
@@ -257,13 +331,22 @@ size_t room(size_t count) {
 
 template <class S, int TERMS, bool SQUARE>
 void launch_symmetric(const SymmetricArgs& a, int grid, hipStream_t s) {
-  using P = Product<S, false, KC, KC, TERMS, TERMS, false>;
+  using P = Product<S, false, KC, KC, TERMS, TERMS, WHOLE>;
   hipLaunchKernelGGL((k_polar_symmetric<S, TERMS, SQUARE>), dim3(grid), dim3(S::NT), P::LDS_BYTES, s, a);
 }
 template <class S, int TERMS>
 void launch_apply(const ApplyArgs& a, int grid, hipStream_t s) {
-  using P = Product<S, false, KC, KS, TERMS, 2, false>;
+  using P = Product<S, false, KC, KS, TERMS, 2, WHOLE>;
   hipLaunchKernelGGL((k_polar_apply<S, TERMS>), dim3(grid), dim3(S::NT), P::LDS_BYTES, s, a);
+}
+
+template <int N, int TERMS>
+hipError_t allow_muon() {
+  using S = Tile<N, TERMS == 2 ? 32 : 64>;
+  hipError_t e = allow_lds(k_polar_symmetric<S, TERMS, false>, Product<S, false, KC, KC, TERMS, TERMS, WHOLE>::LDS_BYTES);
+  if (e == hipSuccess) e = allow_lds(k_polar_symmetric<S, TERMS, true>, Product<S, false, KC, KC, TERMS, TERMS, WHOLE>::LDS_BYTES);
+  if (e == hipSuccess) e = allow_lds(k_polar_apply<Tile<N, 32>, TERMS>, Product<Tile<N, 32>, false, KC, KS, TERMS, 2, WHOLE>::LDS_BYTES);
+  return e;
 }
 
 // u -> the working X, its Newton-Schulz steps, and the finishing pass
@@ -283,17 +366,23 @@ ob_status run_list(ob_muon_ctx* ctx, Direction d, float* m_out, const Finish& fi
       g.out = ctx->d_b;
       g.q = Quintic{b * per_gram * E_UNIT, a * E_UNIT};
     }
-    if (two) launch_symmetric<S64x2, 2, false>(g, ctx->sym_grid, s);
-    else launch_symmetric<S64, 1, false>(g, ctx->sym_grid, s);
+    with_side(ctx->sym_side, [&](auto n) {
+      if (two) launch_symmetric<Tile<n, 32>, 2, false>(g, ctx->sym_grid, s);
+      else launch_symmetric<Tile<n, 64>, 1, false>(g, ctx->sym_grid, s);
+    });
     if (c != 0.0f) {
       SymmetricArgs q{ctx->d_sym, ctx->d_mats, ctx->d_e, ctx->d_b, ctx->e_plane, ctx->e_plane, {}};
       q.q = Quintic{c / E_UNIT, (float)(((double)a - (double)b * b / (4.0 * c)) * E_UNIT)};
-      if (two) launch_symmetric<S64x2, 2, true>(q, ctx->sym_grid, s);
-      else launch_symmetric<S64, 1, true>(q, ctx->sym_grid, s);
+      with_side(ctx->sym_side, [&](auto n) {
+        if (two) launch_symmetric<Tile<n, 32>, 2, true>(q, ctx->sym_grid, s);
+        else launch_symmetric<Tile<n, 64>, 1, true>(q, ctx->sym_grid, s);
+      });
     }
     ApplyArgs x{ctx->d_apply, ctx->d_mats, ctx->d_b, ctx->d_x[cur], ctx->d_x[cur ^ 1], ctx->e_plane, ctx->x_plane};
-    if (two) launch_apply<S64x2, 2>(x, ctx->apply_grid, s);
-    else launch_apply<S64x2, 1>(x, ctx->apply_grid, s);
+    with_side(ctx->apply_side, [&](auto n) {
+      if (two) launch_apply<Tile<n, 32>, 2>(x, ctx->apply_grid, s);
+      else launch_apply<Tile<n, 32>, 1>(x, ctx->apply_grid, s);
+    });
     cur ^= 1;
   }
   hipLaunchKernelGGL(k_muon_finish, dim3(ctx->square_tiles), dim3(BLOCK), 0, s, ctx->d_square, ctx->d_mats, ctx->d_x[cur], ctx->x_plane, finish);
@@ -339,7 +428,27 @@ ob_status create(const ob_muon_config* cfg, ob_muon_ctx* ctx) {
     mats.push_back(m);
   }
   if (mats.empty()) return OB_ERR_ARG;
-  const std::vector<ListTile> sym = product_tiles(mats, 64, true), apply = product_tiles(mats, 64, false);
+  for (const bool symmetric : {true, false}) {
+    double depth = 0, elements = 0;      // of X's columns or rows, weighted by what is computed of them
+    for (const Matrix& m : mats) {
+      const double out = symmetric ? 0.5 * m.mp * m.mp : (double)m.mp * m.np;
+      depth += out * (symmetric ? 0.5 * (m.mp + m.np) : m.mp);
+      elements += out;
+    }
+    (symmetric ? ctx->sym_side : ctx->apply_side) = best_side([&](int n) {
+      double tiles = 0;
+      for (const Matrix& m : mats) {
+        const double nm = (m.mp + n - 1) / n, nn = (m.np + n - 1) / n;
+        tiles += symmetric ? 0.5 * nm * (nm + 1) : nm * nn;
+      }
+      return tiles;
+    }, depth / elements);
+  }
+  for (const Side& side : SIDES) {
+    const hipError_t e = with_side(side.side, [&](auto n) { return ctx->precision == OB_F32 ? allow_muon<n, 2>() : allow_muon<n, 1>(); });
+    if (!hip_ok(ctx, e, "hipFuncSetAttribute")) return OB_ERR_HIP;
+  }
+  const std::vector<ListTile> sym = product_tiles(mats, ctx->sym_side, true), apply = product_tiles(mats, ctx->apply_side, false);
   if (sym.size() > 0x7fffffff || apply.size() > 0x7fffffff) return OB_ERR_SIZE;
   ctx->mats = (int)mats.size();
   ctx->square_tiles = (int)square.size();

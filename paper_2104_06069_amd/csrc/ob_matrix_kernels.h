@@ -153,16 +153,16 @@ struct RowsArgs {
   int depth, width, out_dtype;
   bool a_direct, w_direct;
 };
-template <class S, bool BF, int FB>
+template <class S, bool BF, int FB, int MODE>
 __global__ __launch_bounds__(S::NT, 2) void k_experts_rows(RowsArgs p) {
-  using P = Product<S, BF, KC, FB, 1, 1, true>;
+  using P = Product<S, BF, KC, FB, 1, 1, MODE>;
   RowTile t;
   if (!find_row_tile<S::BM>(p.groups, (p.width + S::BN - 1) / S::BN, blockIdx.x, &t)) return;
   typename P::Acc acc = {};
   const Operand a{p.a + t.lo * p.lda, 0, p.lda, t.rows, p.a_direct};
   const Operand b{p.w + t.g * p.w_stride, 0, p.ldw, p.width, p.w_direct};
   P::run(a, b, t.tm * S::BM, t.tn * S::BN, 0, p.depth, lds_of_launch, acc);
-  for_each4<S>(acc, [&](int r, int c, v4f v) {
+  Results<S>::visit(acc, lds_of_launch, [&](int r, int c, v4f v) {
     r += t.tm * S::BM;
     c += t.tn * S::BN;
     if (r < t.rows) store4(p.out, p.out_dtype, (t.lo + r) * p.ldo + c, p.width - c, v);
@@ -179,9 +179,9 @@ struct WeightsArgs {
   int height, width, out_dtype, accumulate;
   bool a_direct, b_direct;
 };
-template <class S, bool BF>
+template <class S, bool BF, int MODE>
 __global__ __launch_bounds__(S::NT, 2) void k_experts_weights(WeightsArgs p) {
-  using P = Product<S, BF, KS, KS, 1, 1, true>;
+  using P = Product<S, BF, KS, KS, 1, 1, MODE>;
   const int nm = (p.height + S::BM - 1) / S::BM, nn = (p.width + S::BN - 1) / S::BN;
   const int t = tile_of_workgroup(blockIdx.x, p.groups.n * nm * nn);
   if (t < 0) return;
@@ -196,7 +196,7 @@ __global__ __launch_bounds__(S::NT, 2) void k_experts_weights(WeightsArgs p) {
   } else if (p.accumulate) {
     return;
   }
-  for_each4<S>(acc, [&](int r, int c, v4f v) {
+  Results<S>::visit(acc, lds_of_launch, [&](int r, int c, v4f v) {
     r += tm * S::BM;
     c += tn * S::BN;
     if (r >= p.height) return;
@@ -258,7 +258,7 @@ struct SymmetricArgs {
 };
 template <class S, int TERMS, bool SQUARE>
 __global__ __launch_bounds__(S::NT, 2) void k_polar_symmetric(SymmetricArgs p) {
-  using P = Product<S, false, KC, KC, TERMS, TERMS, false>;
+  using P = Product<S, false, KC, KC, TERMS, TERMS, WHOLE>;
   const ListTile t = p.tiles[blockIdx.x];
   if (t.mat < 0) return;
   const Matrix& m = p.mats[t.mat];
@@ -268,24 +268,27 @@ __global__ __launch_bounds__(S::NT, 2) void k_polar_symmetric(SymmetricArgs p) {
   const int r0 = t.tm * S::BM, c0 = t.tn * S::BN;
   P::run(a, a, r0, c0, 0, depth, lds_of_launch, acc);
   uint16_t* const out = p.out + m.e;
-  for_each4<S>(acc, [&](int r, int c, v4f v) {
-    r += r0;
-    c += c0;
-    if (r >= mp || c >= mp) return;
+  const auto finish = [&](int r, int c, v4f v, int dr, int dc) {      // v[e] is element (r + e dr, c + e dc)
     v *= p.q.mul;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      if (r == c + e) v[e] += p.q.diag;
-    store_terms<TERMS>(out, p.out_term, (int64_t)r * mp + c, v);
-    if (t.tm == t.tn) return;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const _Float16 h = (_Float16)v[e];
-      const int64_t at = (int64_t)(c + e) * mp + r;
-      out[at] = __builtin_bit_cast(unsigned short, h);
-      if constexpr (TERMS == 2) out[p.out_term + at] = __builtin_bit_cast(unsigned short, (_Float16)(v[e] - (float)h));
-    }
-  });
+      if (r + e * dr == c + e * dc) v[e] += p.q.diag;
+    store_terms<TERMS>(out, p.out_term, dc ? (int64_t)r * mp + c : (int64_t)c * mp + r, v);
+  };
+  const auto by_row = [&](int r, int c, v4f v) {
+    r += r0;
+    c += c0;
+    if (r < mp && c < mp) finish(r, c, v, 0, 1);
+  };
+  if (t.tm == t.tn) {
+    Results<S>::visit(acc, lds_of_launch, by_row);
+  } else {
+    Results<S>::template visit<true>(acc, lds_of_launch, by_row, [&](int r, int c, v4f v) {
+      r += r0;
+      c += c0;
+      if (r < mp && c < mp) finish(r, c, v, 1, 0);
+    });
+  }
 }
 
 // X' = B X
@@ -299,7 +302,7 @@ struct ApplyArgs {
 };
 template <class S, int B_TERMS>
 __global__ __launch_bounds__(S::NT, 2) void k_polar_apply(ApplyArgs p) {
-  using P = Product<S, false, KC, KS, B_TERMS, 2, false>;
+  using P = Product<S, false, KC, KS, B_TERMS, 2, WHOLE>;
   const ListTile t = p.tiles[blockIdx.x];
   if (t.mat < 0) return;
   const Matrix& m = p.mats[t.mat];
@@ -307,7 +310,7 @@ __global__ __launch_bounds__(S::NT, 2) void k_polar_apply(ApplyArgs p) {
   const Operand a{p.b + m.e, p.b_term, m.mp, m.mp, true}, b{p.x + m.x, p.x_term, m.np, m.np, true};
   const int r0 = t.tm * S::BM, c0 = t.tn * S::BN;
   P::run(a, b, r0, c0, 0, m.mp, lds_of_launch, acc);
-  for_each4<S>(acc, [&](int r, int c, v4f v) {
+  Results<S>::visit(acc, lds_of_launch, [&](int r, int c, v4f v) {
     r += r0;
     c += c0;
     if (r < m.mp && c < m.np) store_terms<2>(p.out + m.x, p.x_term, (int64_t)r * m.np + c, v * (1.0f / E_UNIT));

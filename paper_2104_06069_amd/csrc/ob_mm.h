@@ -153,16 +153,65 @@ struct Shape {
   static constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
 };
 
-// ANY: the operands may need load_any (slabs that end inside, addresses that are no multiples of 16); without it they are
-// `direct` and K is a multiple of BK.
-template <class S, bool BF, int FA, int FB, int TA, int TB, bool ANY>
+// The tile's results, turned in LDS from the matrix cores' layout to rows.  Each wavefront has a part of LDS of its own and
+// turns up to four times sixteen of its rows at a time.
+template <class S>
+struct Results {
+  static constexpr int WIDTH = S::BN / S::WN, GROUP = S::FM < 4 ? S::FM : 4, ROWS = GROUP * 16;
+  static constexpr int STRIDE = WIDTH + 4;        // floats: rows four banks apart
+  static constexpr int LDS_BYTES = S::WAVES * ROWS * STRIDE * 4;
+
+  // Calls by_row(row, column, values of four adjacent columns), and with MIRROR by_column(row, column, values of four adjacent
+  // rows), for all of the tile.  To be called after Product::run, whose last barrier ends the reads of LDS.
+  template <bool MIRROR, class F, class G>
+  __device__ static __forceinline__ void visit(const v4f (&acc)[S::FM][S::FN], uint16_t* lds, F by_row, G by_column) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r0 = wave / S::WN * (S::BM / S::WM), c0 = wave % S::WN * WIDTH;
+    float* const own = reinterpret_cast<float*>(lds) + wave * ROWS * STRIDE;
+#pragma unroll
+    for (int g = 0; g < S::FM / GROUP; ++g) {
+#pragma unroll
+      for (int i = 0; i < GROUP; ++i)
+#pragma unroll
+        for (int j = 0; j < S::FN; ++j)
+          *in_lds<v4f>(own + (i * 16 + (lane & 15)) * STRIDE + j * 16 + 4 * (lane >> 4)) = acc[g * GROUP + i][j];
+      lds_done();
+#pragma unroll 1
+      for (int k = lane; k < ROWS * WIDTH / 4; k += 64) {
+        const int r = k / (WIDTH / 4), c = k % (WIDTH / 4) * 4;
+        by_row(r0 + g * ROWS + r, c0 + c, *in_lds<const v4f>(own + r * STRIDE + c));
+      }
+      if constexpr (MIRROR) {
+#pragma unroll 1
+        for (int k = lane; k < ROWS * WIDTH / 4; k += 64) {
+          const int c = k / (ROWS / 4), r = k % (ROWS / 4) * 4;
+          const float* const at = own + r * STRIDE + c;
+          by_column(r0 + g * ROWS + r, c0 + c, v4f{*in_lds<const float>(at), *in_lds<const float>(at + STRIDE), *in_lds<const float>(at + 2 * STRIDE),
+                                                   *in_lds<const float>(at + 3 * STRIDE)});
+        }
+      }
+      lds_done();
+    }
+  }
+  template <class F>
+  __device__ static __forceinline__ void visit(const v4f (&acc)[S::FM][S::FN], uint16_t* lds, F by_row) {
+    visit<false>(acc, lds, by_row, [](int, int, v4f) {});
+  }
+};
+
+// What the operands may be.  WHOLE: `direct`, K a multiple of BK; TAIL: `direct`, any K, the last slab through registers once
+// the others are done; ANY: each slab as it has to be (the registers that takes at every slab do not fit beside a 256 x 256
+// tile's).
+enum { WHOLE = 0, TAIL = 1, ANY = 2 };
+
+template <class S, bool BF, int FA, int FB, int TA, int TB, int MODE>
 struct Product {
   static constexpr int BM = S::BM, BN = S::BN, BK = S::BK, FM = S::FM, FN = S::FN;
-  static_assert(!ANY || (TA == 1 && TB == 1), "load_any has one term");
+  static_assert(MODE == WHOLE || (TA == 1 && TB == 1), "load_any has one term");
   using A = Slab<FA, BM, BK, S::NT>;
   using B = Slab<FB, BN, BK, S::NT>;
   static constexpr int STAGE = (TA * BM + TB * BN) * BK;
-  static constexpr int LDS_BYTES = 2 * STAGE * 2;
+  static constexpr int LDS_BYTES = 2 * STAGE * 2 > Results<S>::LDS_BYTES ? 2 * STAGE * 2 : Results<S>::LDS_BYTES;
   typedef v4f Acc[FM][FN];
 
   // Lane (q, i) of wavefront (wm, wn): acc[x][y][e] is row wm * BM / WM + 16 x + i, column wn * BN / WN + 16 y + 4 q + e.
@@ -175,82 +224,93 @@ struct Product {
     B sb;
     sa.init(a, r0, tid);
     sb.init(b, c0, tid);
-    const int n = (K + BK - 1) / BK, end = k0 + K;
+    const int n = MODE == ANY ? (K + BK - 1) / BK : K / BK, end = k0 + K;
     auto load = [&](int t) {
       uint16_t* const s = lds + (t & 1) * STAGE;
       const int k = k0 + t * BK;
-      if (!ANY || (a.direct && k + BK <= end)) {
+      if (MODE != ANY || (a.direct && k + BK <= end)) {
 #pragma unroll
         for (int x = 0; x < TA; ++x) sa.load(a, x, r0, k, s + x * BM * BK, wave);
       } else {
         A::load_any(a, r0, k, end, s, tid);
       }
-      if (!ANY || (b.direct && k + BK <= end)) {
+      if (MODE != ANY || (b.direct && k + BK <= end)) {
 #pragma unroll
         for (int y = 0; y < TB; ++y) sb.load(b, y, c0, k, s + (TA * BM + y * BN) * BK, wave);
       } else {
         B::load_any(b, c0, k, end, s + TA * BM * BK, tid);
       }
     };
+    auto read = [&](const uint16_t* s, int kk, v8s (&fa)[TA][FM], v8s (&fb)[TB][FN]) {
+#pragma unroll
+      for (int y = 0; y < TB; ++y)
+#pragma unroll
+        for (int f = 0; f < FN; ++f) fb[y][f] = B::fragment(s + (TA * BM + y * BN) * BK, wn * (BN / S::WN) + f * 16, kk, lane);
+#pragma unroll
+      for (int x = 0; x < TA; ++x)
+#pragma unroll
+        for (int f = 0; f < FM; ++f) fa[x][f] = A::fragment(s + x * BM * BK, wm * (BM / S::WM) + f * 16, kk, lane);
+    };
+    auto multiply = [&](const v8s (&fa)[TA][FM], const v8s (&fb)[TB][FN]) {
+#pragma unroll
+      for (int x = 0; x < TA; ++x)
+#pragma unroll
+        for (int y = 0; y < TB; ++y)
+          if (x + y < 2) {
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+              for (int j = 0; j < FN; ++j) acc[i][j] = mma<BF>(fb[y][j], fa[x][i], acc[i][j]);
+          }
+    };
     // Turns are separated by barriers; the second group is one turn behind.  Slab t + 1 goes where slab t - 1 was: both
     // groups start it in the turn after the second group's last read of slab t - 1, and wait for it at the end of the turn
     // before the first group's first read.
-    load(0);
-    loads_done();
-    group_barrier();
-    if (second) {
-      if (n > 1) load(1);
+    if (n > 0) {
+      load(0);
+      loads_done();
       group_barrier();
-    }
-    for (int t = 0; t < n; ++t) {
-      const uint16_t* const s = lds + (t & 1) * STAGE;
-#pragma unroll
-      for (int kk = 0; kk < BK / 32; ++kk) {
-        const bool last = kk == BK / 32 - 1;
-        v8s fa[TA][FM], fb[TB][FN];
-#pragma unroll
-        for (int y = 0; y < TB; ++y)
-#pragma unroll
-          for (int f = 0; f < FN; ++f) fb[y][f] = B::fragment(s + (TA * BM + y * BN) * BK, wn * (BN / S::WN) + f * 16, kk, lane);
-#pragma unroll
-        for (int x = 0; x < TA; ++x)
-#pragma unroll
-          for (int f = 0; f < FM; ++f) fa[x][f] = A::fragment(s + x * BM * BK, wm * (BM / S::WM) + f * 16, kk, lane);
-        if (kk == 0 && !second && t + 1 < n) load(t + 1);
-        if (last && second) loads_done();
-        else lds_done();
-        group_barrier();
-        if (last && second && t + 2 < n) load(t + 2);
-        __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-        for (int x = 0; x < TA; ++x)
-#pragma unroll
-          for (int y = 0; y < TB; ++y)
-            if (x + y < 2) {
-#pragma unroll
-              for (int i = 0; i < FM; ++i)
-#pragma unroll
-                for (int j = 0; j < FN; ++j) acc[i][j] = mma<BF>(fb[y][j], fa[x][i], acc[i][j]);
-            }
-        __builtin_amdgcn_s_setprio(0);
-        if (last && !second) loads_done();
+      if (second) {
+        if (n > 1) load(1);
         group_barrier();
       }
+      for (int t = 0; t < n; ++t) {
+        const uint16_t* const s = lds + (t & 1) * STAGE;
+#pragma unroll
+        for (int kk = 0; kk < BK / 32; ++kk) {
+          const bool last = kk == BK / 32 - 1;
+          v8s fa[TA][FM], fb[TB][FN];
+          read(s, kk, fa, fb);
+          if (kk == 0 && !second && t + 1 < n) load(t + 1);
+          if (last && second) loads_done();
+          else lds_done();
+          group_barrier();
+          if (last && second && t + 2 < n) load(t + 2);
+          __builtin_amdgcn_s_setprio(1);
+          multiply(fa, fb);
+          __builtin_amdgcn_s_setprio(0);
+          if (last && !second) loads_done();
+          group_barrier();
+        }
+      }
+      if (!second) group_barrier();
     }
-    if (!second) group_barrier();
+    if (MODE == TAIL && n * BK < K) {
+      A::load_any(a, r0, k0 + n * BK, end, lds, tid);
+      B::load_any(b, c0, k0 + n * BK, end, lds + TA * BM * BK, tid);
+      lds_done();
+      group_barrier();
+#pragma unroll
+      for (int kk = 0; kk < BK / 32; ++kk) {
+        v8s fa[TA][FM], fb[TB][FN];
+        read(lds, kk, fa, fb);
+        lds_done();
+        multiply(fa, fb);
+      }
+      group_barrier();
+    }
   }
 };
-
-// Calls f(row, column, values of four adjacent columns) for all that this lane holds of the tile.
-template <class S, class F>
-__device__ __forceinline__ void for_each4(const v4f (&acc)[S::FM][S::FN], F f) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / S::WN, wn = wave % S::WN;
-#pragma unroll
-  for (int i = 0; i < S::FM; ++i)
-#pragma unroll
-    for (int j = 0; j < S::FN; ++j)
-      f(wm * (S::BM / S::WM) + i * 16 + (lane & 15), wn * (S::BN / S::WN) + j * 16 + 4 * (lane >> 4), acc[i][j]);
-}
 
 // Workgroups are dealt to the eight dies in turn, each with a cache of its own: consecutive tiles go to one die.  -1: none.
 __device__ __forceinline__ int tile_of_workgroup(int id, int tiles) {
