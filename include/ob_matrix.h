@@ -90,8 +90,8 @@ ob_status ob_experts_weight_grad(ob_experts_ctx* ctx, const void* x, int64_t ldx
  *   OB_F16  X is a sum of two, S and the polynomial's matrix are one (11 bits): half the time, 1e-3 to 2e-3 relative
  *           in the 2-norm over the matrix, for matrices of low numerical rank as well; meant for 16-bit outputs
  * Norms and the binary32 state are the same in both.
- * A matrix with an infinity or a NaN, or with singular values that the polynomial takes beyond 15, gives NaNs; other
- * matrices of the list are not touched by that.  A matrix of zeros gives zeros (eps > 0).
+ * A matrix with an infinity or a NaN, or with singular values that the polynomial takes beyond 3.9, gives NaNs
+ * (from a number beyond the working matrices' range); other matrices of the list are not touched by that.  A matrix of zeros gives zeros (eps > 0).
  */
 typedef struct ob_muon_ctx ob_muon_ctx; /* opaque */
 
@@ -100,7 +100,8 @@ typedef struct ob_muon_config {
   const int64_t* layer_offsets;  /* HOST, copied */
   const int64_t* layer_rows;     /* HOST [num_layers], copied; at least one is not 0 */
   const float* layer_scale;      /* HOST [num_layers], copied; NULL: 0.2 sqrt(max(rows, columns)) */
-  const float* coefficients;     /* HOST [3 * num_coefficients], copied: a, b, c of each step, the last ones for all that follow */
+  const float* coefficients;     /* HOST [3 * num_coefficients], copied: a, b, c of each step, the last ones for all that
+                                    follow; |a| + |b| + |c| <= 100 */
   int32_t num_coefficients;      /* 1 .. steps */
   int32_t steps;                 /* 1 .. 64 */
   float eps;                     /* >= 0 */

@@ -21,7 +21,7 @@ namespace {
 // Tiles of the products, by side: 256 (eight wavefronts, one workgroup on a CU), 128 and 64 (four).  Slabs of 64 columns, or
 // with two terms of 32: the same LDS.
 template <int SIDE_, int BK>
-using Tile = Shape<SIDE_, SIDE_, BK, 2, SIDE_ == 256 ? 4 : 2>;
+using Tile = Shape<SIDE_, SIDE_, BK, 2, SIDE_ == 256 ? 4 : 2, SIDE_ == 64 ? 3 : 2>;
 
 template <class F>
 auto with_side(int side, F f) {
@@ -30,15 +30,17 @@ auto with_side(int side, F f) {
   return f(std::integral_constant<int, 64>{});
 }
 
-// A workgroup's share of the matrix cores' rate, and how many run at once: 8192^3 at 1150, 960 and (64 x 64) 420 TFLOP/s.
+// How many of a side's tiles run at once on a CU, and the CU's rate with all of them and with one: 8192^3 at 1150, 960 and
+// (64 x 64) 420 TFLOP/s.
 struct Side {
-  int side, at_once;
-  double rate;      // multiply-adds a microsecond and CU
+  int side, per_cu;
+  double rate, alone;      // multiply-adds a microsecond and CU
 };
-constexpr Side SIDES[] = {{256, 256, 2.2e6}, {128, 512, 1.9e6}, {64, 1024, 0.8e6}};
+constexpr Side SIDES[] = {{256, 1, 2.2e6, 2.2e6}, {128, 2, 1.9e6, 1.1e6}, {64, 3, 0.8e6, 0.4e6}};
 // Time of `tiles` tiles of the given mean depth, in microseconds, if they are dealt evenly
 double tiles_time(const Side& s, double tiles, double depth) {
-  return std::ceil(tiles / s.at_once) * (s.at_once / 256) * s.side * s.side * depth / s.rate;
+  const double one = (double)s.side * s.side * depth, a_cu = std::ceil(tiles / 256);      // tiles that the busiest CU gets
+  return a_cu < s.per_cu ? one * a_cu / (s.alone + (s.rate - s.alone) * (a_cu - 1) / std::max(1, s.per_cu - 1)) : one * a_cu / s.rate;
 }
 
 inline int elem_size(int dtype) { return dtype == OB_F32 ? 4 : 2; }
@@ -254,6 +256,18 @@ ob_status ob_experts_weight_grad(ob_experts_ctx* ctx, const void* x, int64_t ldx
 }  // extern "C"
 
 // ---- orthogonalised update -----------------------------------------------------------------------------------------
+namespace {
+
+// Matrices that go through the steps together, and the tiles of their products
+struct Part {
+  bool follow_s = false;      // the 22-bit way (ob_matrix_kernels.h)
+  int sym_side = 64, apply_side = 64, sym_grid = 0, apply_grid = 0;
+  ListTile* d_sym = nullptr;
+  ListTile* d_apply = nullptr;
+};
+
+}  // namespace
+
 struct ob_muon_ctx {
   int device = -1;
   int steps = 0, nesterov = 0, precision = OB_F32;
@@ -261,19 +275,16 @@ struct ob_muon_ctx {
   std::vector<float> coefficients;      // 3 * steps
   int64_t n = 0;                        // elements of the flat buffers
   int mats = 0, square_tiles = 0;
-  int sym_side = 64, apply_side = 64, sym_grid = 0, apply_grid = 0;
+  std::vector<Part> parts;
   int64_t x_plane = 0, e_plane = 0;     // elements
   void* mem = nullptr;
   size_t bytes = 0;
   Matrix* d_mats = nullptr;
   SquareTile* d_square = nullptr;
-  ListTile* d_sym = nullptr;
-  ListTile* d_apply = nullptr;
   double* d_sums = nullptr;
   float* d_inv = nullptr;
   uint16_t* d_x[2] = {nullptr, nullptr};
-  uint16_t* d_e = nullptr;
-  uint16_t* d_b = nullptr;
+  uint16_t* d_e[5] = {};                // S or E, B, Y, and two of Q
   std::string hip_err;
   ~ob_muon_ctx() {
     if (mem) (void)hipFree(mem);
@@ -310,34 +321,40 @@ std::vector<ListTile> deal(std::vector<Unit> units, bool upper) {
   return table;
 }
 
-std::vector<ListTile> product_tiles(const std::vector<Matrix>& mats, int side, bool symmetric) {
+std::vector<ListTile> product_tiles(const std::vector<Matrix>& mats, const std::vector<int>& part, int side, bool symmetric) {
   std::vector<Unit> units;
-  for (size_t i = 0; i < mats.size(); ++i) {
+  for (const int i : part) {
     const int nm = (mats[i].mp + side - 1) / side, nn = symmetric ? nm : (mats[i].np + side - 1) / side;
-    const double cost = symmetric ? (double)mats[i].np + mats[i].mp : (double)mats[i].mp;
+    const double cost = (double)mats[i].mp;
     for (int a = 0; a < nm; a += 4)
       for (int b = 0; b < nn; b += 8) {
         if (symmetric && std::min(b + 8, nn) <= a) continue;
-        units.push_back(Unit{cost, (int)i, a, std::min(a + 4, nm), b, std::min(b + 8, nn)});
+        units.push_back(Unit{cost, i, a, std::min(a + 4, nm), b, std::min(b + 8, nn)});
       }
   }
   return deal(std::move(units), symmetric);
 }
 
+int product_side(const std::vector<Matrix>& mats, const std::vector<int>& part, bool symmetric) {
+  double depth = 0, elements = 0;      // of the products' K, weighted by what is computed of them
+  for (const int i : part) {
+    const double out = symmetric ? 0.5 * mats[i].mp * mats[i].mp : (double)mats[i].mp * mats[i].np;
+    depth += out * mats[i].mp;
+    elements += out;
+  }
+  return best_side([&](int n) {
+    double tiles = 0;
+    for (const int i : part) {
+      const double nm = (mats[i].mp + n - 1) / n, nn = (mats[i].np + n - 1) / n;
+      tiles += symmetric ? 0.5 * nm * (nm + 1) : nm * nn;
+    }
+    return tiles;
+  }, depth / elements);
+}
+
 template <class T>
 size_t room(size_t count) {
   return (std::max<size_t>(count * sizeof(T), 1) + 1023) / 1024 * 1024;
-}
-
-template <class S, int TERMS, bool SQUARE>
-void launch_symmetric(const SymmetricArgs& a, int grid, hipStream_t s) {
-  using P = Product<S, false, KC, KC, TERMS, TERMS, WHOLE>;
-  hipLaunchKernelGGL((k_polar_symmetric<S, TERMS, SQUARE>), dim3(grid), dim3(S::NT), P::LDS_BYTES, s, a);
-}
-template <class S, int TERMS>
-void launch_apply(const ApplyArgs& a, int grid, hipStream_t s) {
-  using P = Product<S, false, KC, KS, TERMS, 2, WHOLE>;
-  hipLaunchKernelGGL((k_polar_apply<S, TERMS>), dim3(grid), dim3(S::NT), P::LDS_BYTES, s, a);
 }
 
 template <int N, int TERMS>
@@ -349,43 +366,120 @@ hipError_t allow_muon() {
   return e;
 }
 
+template <int TERMS, bool GRAM>
+void symmetric(const Part& part, const SymmetricArgs& a, int products, hipStream_t s) {
+  with_side(part.sym_side, [&](auto n) {
+    using S = Tile<n, TERMS == 2 ? 32 : 64>;
+    using P = Product<S, false, KC, KC, TERMS, TERMS, WHOLE>;
+    hipLaunchKernelGGL((k_polar_symmetric<S, TERMS, GRAM>), dim3(part.sym_grid, products), dim3(S::NT), P::LDS_BYTES, s, a);
+  });
+}
+template <int TERMS>
+void apply(const Part& part, const ApplyArgs& a, hipStream_t s) {
+  with_side(part.apply_side, [&](auto n) {
+    using S = Tile<n, 32>;
+    using P = Product<S, false, KC, KS, TERMS, 2, WHOLE>;
+    hipLaunchKernelGGL((k_polar_apply<S, TERMS>), dim3(part.apply_grid), dim3(S::NT), P::LDS_BYTES, s, a);
+  });
+}
+
+// Steps that follow one S: the growth of a singular value's square up to the last of them (ob_matrix_kernels.h) is at most
+// 2^8, or 2^15 where an error of 2e-3 will do
+int steps_from(const ob_muon_ctx* ctx, int k) {
+  const int first = k;
+  double growth = 1.0;
+  for (; k < ctx->steps; ++k) {
+    if (k > first && growth > (ctx->precision == OB_F32 ? 256.0 : 32768.0)) break;
+    const double a = ctx->coefficients[3 * k];
+    growth *= std::max(1.0, a * a);
+  }
+  return k - first;
+}
+
+// The buffer of X that holds the result, given that X[0] holds the start
+int last_buffer(const ob_muon_ctx* ctx, const Part& part) {
+  if (!part.follow_s) return ctx->steps & 1;
+  int cur = 0;
+  for (int k = 0; k < ctx->steps; k += steps_from(ctx, k)) cur ^= 1;
+  return cur;
+}
+
+void follow_s(ob_muon_ctx* ctx, const Part& part, hipStream_t stream) {
+  uint16_t* const S = ctx->d_e[0];
+  uint16_t* const Y = ctx->d_e[2];
+  int cur = 0;
+  for (int first = 0, n; first < ctx->steps; first += n) {
+    n = steps_from(ctx, first);
+    SymmetricArgs g{part.d_sym, ctx->d_mats, ctx->d_x[cur], {}, nullptr, {S}, ctx->x_plane, ctx->e_plane, {S_UNIT / (X_UNIT * X_UNIT)}, 0.0f, 0.0f};
+    symmetric<2, true>(part, g, 1, stream);
+    double most = 1.0;      // what Q's elements can come to
+    for (int k = first; k < first + n; ++k)
+      most *= std::max(1.0, (double)std::fabs(ctx->coefficients[3 * k]));
+    const float q_unit = (float)std::exp2(std::min(8.0, std::floor(std::log2(32768.0 / most))));
+    uint16_t* q = ctx->d_e[3];
+    for (int k = first; k < first + n; ++k) {
+      const float a = ctx->coefficients[3 * k], b = ctx->coefficients[3 * k + 1], c = ctx->coefficients[3 * k + 2];
+      const bool start = k == first, end = k == first + n - 1;
+      // the first B is Q; it is kept in Q's unit
+      uint16_t* const B = start ? q : ctx->d_e[1];
+      const float unit = start ? q_unit : E_UNIT;
+      symmetric<2, false>(part, SymmetricArgs{part.d_sym, ctx->d_mats, S, {S}, S, {B}, 0, ctx->e_plane, {c * unit / (S_UNIT * S_UNIT)}, b * unit / S_UNIT, a * unit},
+                          1, stream);
+      SymmetricArgs p{part.d_sym, ctx->d_mats, B, {}, nullptr, {}, 0, ctx->e_plane, {}, 0.0f, 0.0f};
+      int products = 0;
+      if (!end) {
+        p.b[products] = S;
+        p.out[products] = Y;
+        p.mul[products++] = 1.0f / unit;
+      }
+      if (!start) {
+        uint16_t* const next = q == ctx->d_e[3] ? ctx->d_e[4] : ctx->d_e[3];
+        p.b[products] = q;
+        p.out[products] = next;
+        p.mul[products++] = 1.0f / unit;
+        q = next;
+      }
+      if (products) symmetric<2, false>(part, p, products, stream);
+      if (!end) symmetric<2, false>(part, SymmetricArgs{part.d_sym, ctx->d_mats, Y, {B}, nullptr, {S}, 0, ctx->e_plane, {1.0f / unit}, 0.0f, 0.0f}, 1, stream);
+    }
+    apply<2>(part, ApplyArgs{part.d_apply, ctx->d_mats, q, ctx->d_x[cur], ctx->d_x[cur ^ 1], ctx->e_plane, ctx->x_plane, 1.0f / q_unit}, stream);
+    cur ^= 1;
+  }
+}
+
+void step_by_step(ob_muon_ctx* ctx, const Part& part, hipStream_t stream) {
+  uint16_t* const E = ctx->d_e[0];
+  uint16_t* const B = ctx->d_e[1];
+  for (int k = 0; k < ctx->steps; ++k) {
+    const float a = ctx->coefficients[3 * k], b = ctx->coefficients[3 * k + 1], c = ctx->coefficients[3 * k + 2];
+    const float per_gram = E_UNIT / (X_UNIT * X_UNIT);
+    SymmetricArgs g{part.d_sym, ctx->d_mats, ctx->d_x[k & 1], {}, nullptr, {E}, ctx->x_plane, ctx->e_plane, {per_gram}, 0.0f, 0.0f};
+    if (c != 0.0f) {
+      g.diag = b / (2.0f * c) * E_UNIT;
+    } else {      // B = a + b S from the first product alone
+      g.out[0] = B;
+      g.mul[0] = b * per_gram;
+      g.diag = a * E_UNIT;
+    }
+    symmetric<1, true>(part, g, 1, stream);
+    if (c != 0.0f) {
+      const float d = (float)(((double)a - (double)b * b / (4.0 * c)) * E_UNIT);
+      symmetric<1, false>(part, SymmetricArgs{part.d_sym, ctx->d_mats, E, {E}, nullptr, {B}, 0, ctx->e_plane, {c / E_UNIT}, 0.0f, d}, 1, stream);
+    }
+    apply<1>(part, ApplyArgs{part.d_apply, ctx->d_mats, B, ctx->d_x[k & 1], ctx->d_x[(k & 1) ^ 1], ctx->e_plane, ctx->x_plane, 1.0f / E_UNIT}, stream);
+  }
+}
+
 // u -> the working X, its Newton-Schulz steps, and the finishing pass
 ob_status run_list(ob_muon_ctx* ctx, Direction d, float* m_out, const Finish& finish, hipStream_t s) {
   hipLaunchKernelGGL(k_muon_moments, dim3(ctx->square_tiles), dim3(BLOCK), 0, s, ctx->d_square, ctx->d_mats, d, m_out, ctx->d_sums);
   hipLaunchKernelGGL(k_muon_norms, dim3(ctx->mats), dim3(BLOCK), 0, s, ctx->d_mats, ctx->d_sums, ctx->eps, ctx->d_inv);
   hipLaunchKernelGGL(k_muon_pack, dim3(ctx->square_tiles), dim3(BLOCK), 0, s, ctx->d_square, ctx->d_mats, d, ctx->d_inv, ctx->d_x[0], ctx->x_plane);
-  const bool two = ctx->precision == OB_F32;
-  int cur = 0;
-  for (int k = 0; k < ctx->steps; ++k) {
-    const float a = ctx->coefficients[3 * k], b = ctx->coefficients[3 * k + 1], c = ctx->coefficients[3 * k + 2];
-    const float per_gram = 1.0f / (X_UNIT * X_UNIT);
-    SymmetricArgs g{ctx->d_sym, ctx->d_mats, ctx->d_x[cur], ctx->d_e, ctx->x_plane, ctx->e_plane, {}};
-    if (c != 0.0f) {
-      g.q = Quintic{per_gram * E_UNIT, b / (2.0f * c) * E_UNIT};
-    } else {
-      g.out = ctx->d_b;
-      g.q = Quintic{b * per_gram * E_UNIT, a * E_UNIT};
-    }
-    with_side(ctx->sym_side, [&](auto n) {
-      if (two) launch_symmetric<Tile<n, 32>, 2, false>(g, ctx->sym_grid, s);
-      else launch_symmetric<Tile<n, 64>, 1, false>(g, ctx->sym_grid, s);
-    });
-    if (c != 0.0f) {
-      SymmetricArgs q{ctx->d_sym, ctx->d_mats, ctx->d_e, ctx->d_b, ctx->e_plane, ctx->e_plane, {}};
-      q.q = Quintic{c / E_UNIT, (float)(((double)a - (double)b * b / (4.0 * c)) * E_UNIT)};
-      with_side(ctx->sym_side, [&](auto n) {
-        if (two) launch_symmetric<Tile<n, 32>, 2, true>(q, ctx->sym_grid, s);
-        else launch_symmetric<Tile<n, 64>, 1, true>(q, ctx->sym_grid, s);
-      });
-    }
-    ApplyArgs x{ctx->d_apply, ctx->d_mats, ctx->d_b, ctx->d_x[cur], ctx->d_x[cur ^ 1], ctx->e_plane, ctx->x_plane};
-    with_side(ctx->apply_side, [&](auto n) {
-      if (two) launch_apply<Tile<n, 32>, 2>(x, ctx->apply_grid, s);
-      else launch_apply<Tile<n, 32>, 1>(x, ctx->apply_grid, s);
-    });
-    cur ^= 1;
+  for (const Part& part : ctx->parts) {
+    if (part.follow_s) follow_s(ctx, part, s);
+    else step_by_step(ctx, part, s);
   }
-  hipLaunchKernelGGL(k_muon_finish, dim3(ctx->square_tiles), dim3(BLOCK), 0, s, ctx->d_square, ctx->d_mats, ctx->d_x[cur], ctx->x_plane, finish);
+  hipLaunchKernelGGL(k_muon_finish, dim3(ctx->square_tiles), dim3(BLOCK), 0, s, ctx->d_square, ctx->d_mats, ctx->d_x[0], ctx->d_x[1], ctx->x_plane, finish);
   return hip_ok(ctx, hipGetLastError(), "the orthogonaliser's kernels") ? OB_OK : OB_ERR_HIP;
 }
 
@@ -428,32 +522,43 @@ ob_status create(const ob_muon_config* cfg, ob_muon_ctx* ctx) {
     mats.push_back(m);
   }
   if (mats.empty()) return OB_ERR_ARG;
-  for (const bool symmetric : {true, false}) {
-    double depth = 0, elements = 0;      // of X's columns or rows, weighted by what is computed of them
-    for (const Matrix& m : mats) {
-      const double out = symmetric ? 0.5 * m.mp * m.mp : (double)m.mp * m.np;
-      depth += out * (symmetric ? 0.5 * (m.mp + m.np) : m.mp);
-      elements += out;
-    }
-    (symmetric ? ctx->sym_side : ctx->apply_side) = best_side([&](int n) {
-      double tiles = 0;
-      for (const Matrix& m : mats) {
-        const double nm = (m.mp + n - 1) / n, nn = (m.np + n - 1) / n;
-        tiles += symmetric ? 0.5 * nm * (nm + 1) : nm * nn;
-      }
-      return tiles;
-    }, depth / elements);
+  // The 11-bit way costs 12.5 n / m + 2.5 (in m^3, 5 steps), the 22-bit one three times 1.5 n / m + 8.5 (with one S, which
+  // will do here): less from n = 3 m on.
+  // That is worth launches of its own where there is much of it.
+  std::vector<int> each[2];
+  double narrow = 0;
+  for (size_t i = 0; i < mats.size(); ++i) {
+    const bool f = cfg->precision == OB_F32 || mats[i].np >= 3 * mats[i].mp;
+    each[f].push_back((int)i);
+    if (f) narrow += (double)mats[i].mp * mats[i].mp * mats[i].np;
+  }
+  if (cfg->precision == OB_F16 && narrow < 1e10) {
+    each[0].insert(each[0].end(), each[1].begin(), each[1].end());
+    each[1].clear();
+  }
+  std::vector<ListTile> tables[2][2];
+  for (const int f : {1, 0}) {
+    if (each[f].empty()) continue;
+    Part part;
+    part.follow_s = f == 1;
+    part.sym_side = product_side(mats, each[f], true);
+    part.apply_side = product_side(mats, each[f], false);
+    tables[f][0] = product_tiles(mats, each[f], part.sym_side, true);
+    tables[f][1] = product_tiles(mats, each[f], part.apply_side, false);
+    if (tables[f][0].size() > 0x7fffffff || tables[f][1].size() > 0x7fffffff) return OB_ERR_SIZE;
+    part.sym_grid = (int)tables[f][0].size();
+    part.apply_grid = (int)tables[f][1].size();
+    const int last = last_buffer(ctx, part);
+    for (const int i : each[f]) mats[i].last = last;
+    ctx->parts.push_back(part);
   }
   for (const Side& side : SIDES) {
-    const hipError_t e = with_side(side.side, [&](auto n) { return ctx->precision == OB_F32 ? allow_muon<n, 2>() : allow_muon<n, 1>(); });
+    hipError_t e = with_side(side.side, [&](auto n) { return allow_muon<n, 2>(); });
+    if (e == hipSuccess) e = with_side(side.side, [&](auto n) { return allow_muon<n, 1>(); });
     if (!hip_ok(ctx, e, "hipFuncSetAttribute")) return OB_ERR_HIP;
   }
-  const std::vector<ListTile> sym = product_tiles(mats, ctx->sym_side, true), apply = product_tiles(mats, ctx->apply_side, false);
-  if (sym.size() > 0x7fffffff || apply.size() > 0x7fffffff) return OB_ERR_SIZE;
   ctx->mats = (int)mats.size();
   ctx->square_tiles = (int)square.size();
-  ctx->sym_grid = (int)sym.size();
-  ctx->apply_grid = (int)apply.size();
   ctx->x_plane = xs;
   ctx->e_plane = es;
   size_t total = 0;
@@ -463,27 +568,32 @@ ob_status create(const ob_muon_config* cfg, ob_muon_ctx* ctx) {
     return at;
   };
   const size_t at_mats = place(room<Matrix>(mats.size())), at_square = place(room<SquareTile>(square.size()));
-  const size_t at_sym = place(room<ListTile>(sym.size())), at_apply = place(room<ListTile>(apply.size()));
+  size_t at_table[2][2];
+  for (const int f : {0, 1})
+    for (const int k : {0, 1}) at_table[f][k] = place(room<ListTile>(tables[f][k].size()));
   const size_t at_sums = place(room<double>(square.size())), at_inv = place(room<float>(mats.size()));
   const size_t at_x0 = place(room<uint16_t>(2 * xs)), at_x1 = place(room<uint16_t>(2 * xs));
-  const size_t at_e = place(room<uint16_t>(2 * es)), at_b = place(room<uint16_t>(2 * es));
+  size_t at_e[5];
+  for (size_t& at : at_e) at = place(room<uint16_t>(2 * es));
   if (!hip_ok(ctx, hipGetDevice(&ctx->device), "hipGetDevice") || !hip_ok(ctx, hipMalloc(&ctx->mem, total), "hipMalloc")) return OB_ERR_HIP;
   ctx->bytes = total;
   unsigned char* const base = static_cast<unsigned char*>(ctx->mem);
   ctx->d_mats = reinterpret_cast<Matrix*>(base + at_mats);
   ctx->d_square = reinterpret_cast<SquareTile*>(base + at_square);
-  ctx->d_sym = reinterpret_cast<ListTile*>(base + at_sym);
-  ctx->d_apply = reinterpret_cast<ListTile*>(base + at_apply);
   ctx->d_sums = reinterpret_cast<double*>(base + at_sums);
   ctx->d_inv = reinterpret_cast<float*>(base + at_inv);
   ctx->d_x[0] = reinterpret_cast<uint16_t*>(base + at_x0);
   ctx->d_x[1] = reinterpret_cast<uint16_t*>(base + at_x1);
-  ctx->d_e = reinterpret_cast<uint16_t*>(base + at_e);
-  ctx->d_b = reinterpret_cast<uint16_t*>(base + at_b);
-  const bool ok = hip_ok(ctx, hipMemcpy(ctx->d_mats, mats.data(), mats.size() * sizeof(Matrix), hipMemcpyHostToDevice), "hipMemcpy") &&
-                  hip_ok(ctx, hipMemcpy(ctx->d_square, square.data(), square.size() * sizeof(SquareTile), hipMemcpyHostToDevice), "hipMemcpy") &&
-                  hip_ok(ctx, hipMemcpy(ctx->d_sym, sym.data(), sym.size() * sizeof(ListTile), hipMemcpyHostToDevice), "hipMemcpy") &&
-                  hip_ok(ctx, hipMemcpy(ctx->d_apply, apply.data(), apply.size() * sizeof(ListTile), hipMemcpyHostToDevice), "hipMemcpy");
+  for (int i = 0; i < 5; ++i) ctx->d_e[i] = reinterpret_cast<uint16_t*>(base + at_e[i]);
+  bool ok = hip_ok(ctx, hipMemcpy(ctx->d_mats, mats.data(), mats.size() * sizeof(Matrix), hipMemcpyHostToDevice), "hipMemcpy") &&
+                  hip_ok(ctx, hipMemcpy(ctx->d_square, square.data(), square.size() * sizeof(SquareTile), hipMemcpyHostToDevice), "hipMemcpy");
+  for (Part& part : ctx->parts)
+    for (const int k : {0, 1}) {
+      const std::vector<ListTile>& table = tables[part.follow_s][k];
+      ListTile* const at = reinterpret_cast<ListTile*>(base + at_table[part.follow_s][k]);
+      (k ? part.d_apply : part.d_sym) = at;
+      ok = ok && hip_ok(ctx, hipMemcpy(at, table.data(), table.size() * sizeof(ListTile), hipMemcpyHostToDevice), "hipMemcpy");
+    }
   return ok ? OB_OK : OB_ERR_HIP;
 }
 
@@ -499,8 +609,10 @@ ob_status ob_muon_create(const ob_muon_config* cfg, ob_muon_ctx** out) {
       !(cfg->eps >= 0.0f) || !(cfg->beta >= 0.0f && cfg->beta < 1.0f) || !(cfg->weight_decay >= 0.0f) || !std::isfinite(cfg->eps) ||
       !std::isfinite(cfg->weight_decay) || (cfg->precision != OB_F32 && cfg->precision != OB_F16) || cfg->layer_offsets[0] != 0)
     return OB_ERR_ARG;
-  for (int i = 0; i < 3 * cfg->num_coefficients; ++i)
-    if (!std::isfinite(cfg->coefficients[i])) return OB_ERR_ARG;
+  for (int i = 0; i < cfg->num_coefficients; ++i) {      // (B's elements have a binary16 unit)
+    const float* const k = cfg->coefficients + 3 * i;
+    if (!(std::fabs(k[0]) + std::fabs(k[1]) + std::fabs(k[2]) <= 100.0f)) return OB_ERR_ARG;
+  }
   for (int64_t l = 0; l < cfg->num_layers; ++l) {
     const int64_t size = cfg->layer_offsets[l + 1] - cfg->layer_offsets[l], rows = cfg->layer_rows[l];
     if (size < 0 || cfg->layer_offsets[l + 1] > ((int64_t)1 << 40) || rows < 0 || (rows && size % rows != 0)) return OB_ERR_ARG;

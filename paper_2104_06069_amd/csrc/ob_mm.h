@@ -147,9 +147,20 @@ __device__ __forceinline__ void group_barrier() {
 __device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ void lds_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
-template <int BM_, int BN_, int BK_, int WM_, int WN_>
+// Until at most n of this wavefront's loads are under way
+template <int n>
+__device__ __forceinline__ void loads_left() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(n) : "memory");
+}
+
+// STAGES: slabs in LDS at once.  Eight wavefronts (two on each SIMD) take turns as described above, with two slabs; fewer
+// do not wait for each other in between: the loads of STAGES - 1 slabs are under way, and what one workgroup leaves idle
+// another one on the CU uses.
+template <int BM_, int BN_, int BK_, int WM_, int WN_, int STAGES_ = 2>
 struct Shape {
-  static constexpr int BM = BM_, BN = BN_, BK = BK_, WM = WM_, WN = WN_, WAVES = WM * WN, NT = WAVES * 64;
+  static constexpr int BM = BM_, BN = BN_, BK = BK_, WM = WM_, WN = WN_, WAVES = WM * WN, NT = WAVES * 64, STAGES = STAGES_;
+  static constexpr bool TURNS = WAVES == 8;
+  static_assert(!TURNS || STAGES == 2, "two slabs");
   static constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
 };
 
@@ -211,7 +222,7 @@ struct Product {
   using A = Slab<FA, BM, BK, S::NT>;
   using B = Slab<FB, BN, BK, S::NT>;
   static constexpr int STAGE = (TA * BM + TB * BN) * BK;
-  static constexpr int LDS_BYTES = 2 * STAGE * 2 > Results<S>::LDS_BYTES ? 2 * STAGE * 2 : Results<S>::LDS_BYTES;
+  static constexpr int LDS_BYTES = S::STAGES * STAGE * 2 > Results<S>::LDS_BYTES ? S::STAGES * STAGE * 2 : Results<S>::LDS_BYTES;
   typedef v4f Acc[FM][FN];
 
   // Lane (q, i) of wavefront (wm, wn): acc[x][y][e] is row wm * BM / WM + 16 x + i, column wn * BN / WN + 16 y + 4 q + e.
@@ -219,14 +230,13 @@ struct Product {
   __device__ static void run(const Operand& a, const Operand& b, int r0, int c0, int k0, int K, uint16_t* lds, Acc& acc) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / S::WN, wn = wave % S::WN;
-    const bool second = wave >= S::WAVES / 2;
     A sa;
     B sb;
     sa.init(a, r0, tid);
     sb.init(b, c0, tid);
     const int n = MODE == ANY ? (K + BK - 1) / BK : K / BK, end = k0 + K;
     auto load = [&](int t) {
-      uint16_t* const s = lds + (t & 1) * STAGE;
+      uint16_t* const s = lds + t % S::STAGES * STAGE;
       const int k = k0 + t * BK;
       if (MODE != ANY || (a.direct && k + BK <= end)) {
 #pragma unroll
@@ -263,6 +273,56 @@ struct Product {
               for (int j = 0; j < FN; ++j) acc[i][j] = mma<BF>(fb[y][j], fa[x][i], acc[i][j]);
           }
     };
+    if constexpr (S::TURNS) turns(n, lds, acc, load, read, multiply);
+    else straight(n, wave, lds, acc, load, read, multiply);
+    if (MODE == TAIL && n * BK < K) {
+      A::load_any(a, r0, k0 + n * BK, end, lds, tid);
+      B::load_any(b, c0, k0 + n * BK, end, lds + TA * BM * BK, tid);
+      lds_done();
+      group_barrier();
+#pragma unroll
+      for (int kk = 0; kk < BK / 32; ++kk) {
+        v8s fa[TA][FM], fb[TB][FN];
+        read(lds, kk, fa, fb);
+        lds_done();
+        multiply(fa, fb);
+      }
+      group_barrier();
+    }
+  }
+
+ private:
+  template <class L, class R, class M>
+  __device__ static __forceinline__ void straight(int n, int wave, uint16_t* lds, Acc& acc, L load, R read, M multiply) {
+    constexpr int AHEAD = S::STAGES - 1;
+    constexpr int NA = TA * A::PER, NB = TB * B::PER;      // loads of a slab, of the wavefronts that have such
+    const bool la = wave < A::WORK / 64, lb = wave < B::WORK / 64;
+#pragma unroll
+    for (int t = 0; t < AHEAD; ++t)
+      if (t < n) load(t);
+    for (int t = 0; t < n; ++t) {
+      if (MODE == ANY || AHEAD == 1 || t + AHEAD > n) loads_done();
+      else if (la && lb) loads_left<(NA + NB) * (AHEAD - 1)>();
+      else if (lb) loads_left<NB * (AHEAD - 1)>();
+      else if (la) loads_left<NA * (AHEAD - 1)>();
+      else lds_done();
+      group_barrier();      // slab t is there, and nobody reads slab t - 1 any more
+      if (t + AHEAD < n) load(t + AHEAD);
+      const uint16_t* const s = lds + t % S::STAGES * STAGE;
+#pragma unroll
+      for (int kk = 0; kk < BK / 32; ++kk) {
+        v8s fa[TA][FM], fb[TB][FN];
+        read(s, kk, fa, fb);
+        multiply(fa, fb);
+      }
+    }
+    lds_done();
+    group_barrier();
+  }
+
+  template <class L, class R, class M>
+  __device__ static __forceinline__ void turns(int n, uint16_t* lds, Acc& acc, L load, R read, M multiply) {
+    const bool second = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) >= S::WAVES / 2;
     // Turns are separated by barriers; the second group is one turn behind.  Slab t + 1 goes where slab t - 1 was: both
     // groups start it in the turn after the second group's last read of slab t - 1, and wait for it at the end of the turn
     // before the first group's first read.
@@ -294,20 +354,6 @@ struct Product {
         }
       }
       if (!second) group_barrier();
-    }
-    if (MODE == TAIL && n * BK < K) {
-      A::load_any(a, r0, k0 + n * BK, end, lds, tid);
-      B::load_any(b, c0, k0 + n * BK, end, lds + TA * BM * BK, tid);
-      lds_done();
-      group_barrier();
-#pragma unroll
-      for (int kk = 0; kk < BK / 32; ++kk) {
-        v8s fa[TA][FM], fb[TB][FN];
-        read(lds, kk, fa, fb);
-        lds_done();
-        multiply(fa, fb);
-      }
-      group_barrier();
     }
   }
 };
