@@ -18,29 +18,50 @@ using namespace obm;
 
 namespace {
 
-// Tiles of the products, by side: 256 (eight wavefronts, one workgroup on a CU), 128 and 64 (four).  Slabs of 64 columns, or
-// with two terms of 32: the same LDS.
-template <int SIDE_, int BK>
-using Tile = Shape<SIDE_, SIDE_, BK, 2, SIDE_ == 256 ? 4 : 2, SIDE_ == 64 ? 3 : 2>;
+// Tiles of the products: 256 x 256 (eight wavefronts, one workgroup on a CU), 128 x 128 and 64 x 64 (four).  Slabs of 64
+// columns, or with two terms of 32: the same LDS.  DEEP: 64 x 64 with seven slabs under way, for launches of which a CU has one
+// workgroup at most: its time is then that of its loads, one after the other.
+enum TileKind { T256, T128, T64, DEEP, KINDS };
+constexpr int side_of(int kind) { return kind == T256 ? 256 : kind == T128 ? 128 : 64; }
+template <int KIND, int BK>
+using Tile = Shape<side_of(KIND), side_of(KIND), BK, 2, KIND == T256 ? 4 : 2, KIND == DEEP ? 8 : KIND == T64 ? 3 : 2>;
 
 template <class F>
-auto with_side(int side, F f) {
-  if (side == 256) return f(std::integral_constant<int, 256>{});
-  if (side == 128) return f(std::integral_constant<int, 128>{});
-  return f(std::integral_constant<int, 64>{});
+auto with_tile(int kind, F f) {
+  switch (kind) {
+    case T256: return f(std::integral_constant<int, T256>{});
+    case T128: return f(std::integral_constant<int, T128>{});
+    case T64: return f(std::integral_constant<int, T64>{});
+    default: return f(std::integral_constant<int, DEEP>{});
+  }
 }
 
-// How many of a side's tiles run at once on a CU, and the CU's rate with all of them and with one: 8192^3 at 1150, 960 and
-// (64 x 64) 420 TFLOP/s.
-struct Side {
-  int side, per_cu;
-  double rate, alone;      // multiply-adds a microsecond and CU
+// How many of a kind run at once on a CU, and the CU's rate with all of them and with one, in multiply-adds a microsecond:
+// 8192^3 at 1250, 1100 and (64 x 64) 750 TFLOP/s.
+struct Rate {
+  int per_cu;
+  double all, one;
 };
-constexpr Side SIDES[] = {{256, 1, 2.2e6, 2.2e6}, {128, 2, 1.9e6, 1.1e6}, {64, 3, 0.8e6, 0.4e6}};
+constexpr Rate RATES[KINDS] = {{1, 2.4e6, 2.4e6}, {2, 2.1e6, 1.1e6}, {3, 1.4e6, 0.45e6}, {1, 0.8e6, 0.8e6}};
 // Time of `tiles` tiles of the given mean depth, in microseconds, if they are dealt evenly
-double tiles_time(const Side& s, double tiles, double depth) {
-  const double one = (double)s.side * s.side * depth, a_cu = std::ceil(tiles / 256);      // tiles that the busiest CU gets
-  return a_cu < s.per_cu ? one * a_cu / (s.alone + (s.rate - s.alone) * (a_cu - 1) / std::max(1, s.per_cu - 1)) : one * a_cu / s.rate;
+double tiles_time(int kind, double tiles, double depth) {
+  const Rate& r = RATES[kind];
+  const double one = (double)side_of(kind) * side_of(kind) * depth, a_cu = std::ceil(tiles / 256);      // tiles that the busiest CU gets
+  return one * a_cu / (a_cu < r.per_cu ? r.one + (r.all - r.one) * (a_cu - 1) / (r.per_cu - 1) : r.all);
+}
+// The kind whose tiles take the shortest, for `tiles(side)` tiles
+template <class F>
+int best_tile(F tiles, double depth) {
+  int best = T64;
+  double least = 1e300;
+  for (int kind = 0; kind < KINDS; ++kind) {
+    const double t = tiles_time(kind, tiles(side_of(kind)), depth);
+    if (t < least) {
+      least = t;
+      best = kind;
+    }
+  }
+  return best;
 }
 
 inline int elem_size(int dtype) { return dtype == OB_F32 ? 4 : 2; }
@@ -80,21 +101,6 @@ struct ob_experts_ctx {
 
 namespace {
 
-// The side whose tiles take the shortest, for `tiles(side)` tiles
-template <class F>
-int best_side(F tiles, double depth) {
-  int best = 64;
-  double least = 1e300;
-  for (const Side& s : SIDES) {
-    const double t = tiles_time(s, tiles(s.side), depth);
-    if (t < least) {
-      least = t;
-      best = s.side;
-    }
-  }
-  return best;
-}
-
 template <class S, bool BF, int FB, int MODE>
 ob_status launch_rows(ob_experts_ctx* ctx, const RowsArgs& p, hipStream_t stream) {
   const int64_t tiles = ((int64_t)p.groups.rows / S::BM + std::min<int64_t>(p.groups.n, p.groups.rows)) * ((p.width + S::BN - 1) / S::BN);
@@ -113,23 +119,23 @@ ob_status launch_weights(ob_experts_ctx* ctx, const WeightsArgs& p, hipStream_t 
   return hip_ok(ctx, hipGetLastError(), "k_experts_weights") ? OB_OK : OB_ERR_HIP;
 }
 
-// f(side, mode): operands that are not `direct` have tiles of up to 128 (ob_mm.h)
+// f(kind, mode): operands that are not `direct` have tiles of 128 or 64, whose loads are waited for at each slab (ob_mm.h)
 template <class F>
-auto with_side_and_mode(int side, bool direct, F f) {
+auto with_tile_and_mode(int kind, bool direct, F f) {
   if (!direct) {
-    if (side >= 128) return f(std::integral_constant<int, 128>{}, std::integral_constant<int, ANY>{});
-    return f(std::integral_constant<int, 64>{}, std::integral_constant<int, ANY>{});
+    if (kind == T256 || kind == T128) return f(std::integral_constant<int, T128>{}, std::integral_constant<int, ANY>{});
+    return f(std::integral_constant<int, T64>{}, std::integral_constant<int, ANY>{});
   }
-  return with_side(side, [&](auto n) { return f(n, std::integral_constant<int, TAIL>{}); });
+  return with_tile(kind, [&](auto n) { return f(n, std::integral_constant<int, TAIL>{}); });
 }
 
 template <bool BF>
 hipError_t allow_experts() {
   hipError_t e = hipSuccess;
-  for (const Side& side : SIDES)
+  for (int kind = 0; kind < KINDS; ++kind)
     for (const bool direct : {false, true}) {
       if (e != hipSuccess) return e;
-      e = with_side_and_mode(side.side, direct, [&](auto n, auto mode) {
+      e = with_tile_and_mode(kind, direct, [&](auto n, auto mode) {
         using S = Tile<n, 64>;
         hipError_t e = allow_lds(k_experts_rows<S, BF, KC, mode>, Product<S, BF, KC, KC, 1, 1, mode>::LDS_BYTES);
         if (e == hipSuccess) e = allow_lds(k_experts_rows<S, BF, KS, mode>, Product<S, BF, KC, KS, 1, 1, mode>::LDS_BYTES);
@@ -171,8 +177,8 @@ ob_status rows_call(ob_experts_ctx* ctx, const void* a, int64_t lda, const void*
   const hipStream_t s = static_cast<hipStream_t>(hip_stream);
   // (a group's last tile is half full in the mean)
   const double groups = (double)std::min<int64_t>(c.num_groups, rows);
-  const int side = best_side([&](int n) { return std::max(groups, rows / (double)n + 0.5 * groups) * (double)((width + n - 1) / n); }, (double)depth);
-  return with_side_and_mode(side, p.a_direct && p.w_direct, [&](auto n, auto mode) {
+  const int kind = best_tile([&](int n) { return std::max(groups, rows / (double)n + 0.5 * groups) * (double)((width + n - 1) / n); }, (double)depth);
+  return with_tile_and_mode(kind, p.a_direct && p.w_direct, [&](auto n, auto mode) {
     using S = Tile<n, 64>;
     if (c.dtype == OB_BF16) return strided ? launch_rows<S, true, KS, mode>(ctx, p, s) : launch_rows<S, true, KC, mode>(ctx, p, s);
     return strided ? launch_rows<S, false, KS, mode>(ctx, p, s) : launch_rows<S, false, KC, mode>(ctx, p, s);
@@ -245,9 +251,9 @@ ob_status ob_experts_weight_grad(ob_experts_ctx* ctx, const void* x, int64_t ldx
   p.a_direct = at16(p.a) && p.lda % 8 == 0 && p.height % 8 == 0;
   p.b_direct = at16(p.b) && p.ldb % 8 == 0 && p.width % 8 == 0;
   const hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  const int side = best_side([&](int n) { return (double)c.num_groups * ((p.height + n - 1) / n) * ((p.width + n - 1) / n); },
+  const int kind = best_tile([&](int n) { return (double)c.num_groups * ((p.height + n - 1) / n) * ((p.width + n - 1) / n); },
                              (double)rows / c.num_groups);
-  return with_side_and_mode(side, p.a_direct && p.b_direct, [&](auto n, auto mode) {
+  return with_tile_and_mode(kind, p.a_direct && p.b_direct, [&](auto n, auto mode) {
     using S = Tile<n, 64>;
     return c.dtype == OB_BF16 ? launch_weights<S, true, mode>(ctx, p, s) : launch_weights<S, false, mode>(ctx, p, s);
   });
@@ -261,9 +267,11 @@ namespace {
 // Matrices that go through the steps together, and the tiles of their products
 struct Part {
   bool follow_s = false;      // the 22-bit way (ob_matrix_kernels.h)
-  int sym_side = 64, apply_side = 64, sym_grid = 0, apply_grid = 0;
-  ListTile* d_sym = nullptr;
-  ListTile* d_apply = nullptr;
+  int sym_tile = T64, apply_tile = T64;
+  // tiles of X X^T, of the other symmetric products (the same ones, but not in the same order: only there depths differ by n)
+  // and of B X
+  int grid[3] = {0, 0, 0};
+  ListTile* d_tiles[3] = {nullptr, nullptr, nullptr};
 };
 
 }  // namespace
@@ -321,11 +329,13 @@ std::vector<ListTile> deal(std::vector<Unit> units, bool upper) {
   return table;
 }
 
-std::vector<ListTile> product_tiles(const std::vector<Matrix>& mats, const std::vector<int>& part, int side, bool symmetric) {
+enum ProductKind { GRAM, SYMMETRIC, APPLY };
+std::vector<ListTile> product_tiles(const std::vector<Matrix>& mats, const std::vector<int>& part, int side, ProductKind product) {
+  const bool symmetric = product != APPLY;
   std::vector<Unit> units;
   for (const int i : part) {
     const int nm = (mats[i].mp + side - 1) / side, nn = symmetric ? nm : (mats[i].np + side - 1) / side;
-    const double cost = (double)mats[i].mp;
+    const double cost = (double)(product == GRAM ? mats[i].np : mats[i].mp);
     for (int a = 0; a < nm; a += 4)
       for (int b = 0; b < nn; b += 8) {
         if (symmetric && std::min(b + 8, nn) <= a) continue;
@@ -335,14 +345,14 @@ std::vector<ListTile> product_tiles(const std::vector<Matrix>& mats, const std::
   return deal(std::move(units), symmetric);
 }
 
-int product_side(const std::vector<Matrix>& mats, const std::vector<int>& part, bool symmetric) {
+int product_tile(const std::vector<Matrix>& mats, const std::vector<int>& part, bool symmetric) {
   double depth = 0, elements = 0;      // of the products' K, weighted by what is computed of them
   for (const int i : part) {
     const double out = symmetric ? 0.5 * mats[i].mp * mats[i].mp : (double)mats[i].mp * mats[i].np;
     depth += out * mats[i].mp;
     elements += out;
   }
-  return best_side([&](int n) {
+  return best_tile([&](int n) {
     double tiles = 0;
     for (const int i : part) {
       const double nm = (mats[i].mp + n - 1) / n, nn = (mats[i].np + n - 1) / n;
@@ -366,20 +376,20 @@ hipError_t allow_muon() {
   return e;
 }
 
-template <int TERMS, bool GRAM>
+template <int TERMS, bool FROM_X>
 void symmetric(const Part& part, const SymmetricArgs& a, int products, hipStream_t s) {
-  with_side(part.sym_side, [&](auto n) {
+  with_tile(part.sym_tile, [&](auto n) {
     using S = Tile<n, TERMS == 2 ? 32 : 64>;
     using P = Product<S, false, KC, KC, TERMS, TERMS, WHOLE>;
-    hipLaunchKernelGGL((k_polar_symmetric<S, TERMS, GRAM>), dim3(part.sym_grid, products), dim3(S::NT), P::LDS_BYTES, s, a);
+    hipLaunchKernelGGL((k_polar_symmetric<S, TERMS, FROM_X>), dim3(part.grid[FROM_X ? GRAM : SYMMETRIC], products), dim3(S::NT), P::LDS_BYTES, s, a);
   });
 }
 template <int TERMS>
 void apply(const Part& part, const ApplyArgs& a, hipStream_t s) {
-  with_side(part.apply_side, [&](auto n) {
+  with_tile(part.apply_tile, [&](auto n) {
     using S = Tile<n, 32>;
     using P = Product<S, false, KC, KS, TERMS, 2, WHOLE>;
-    hipLaunchKernelGGL((k_polar_apply<S, TERMS>), dim3(part.apply_grid), dim3(S::NT), P::LDS_BYTES, s, a);
+    hipLaunchKernelGGL((k_polar_apply<S, TERMS>), dim3(part.grid[APPLY]), dim3(S::NT), P::LDS_BYTES, s, a);
   });
 }
 
@@ -410,7 +420,7 @@ void follow_s(ob_muon_ctx* ctx, const Part& part, hipStream_t stream) {
   int cur = 0;
   for (int first = 0, n; first < ctx->steps; first += n) {
     n = steps_from(ctx, first);
-    SymmetricArgs g{part.d_sym, ctx->d_mats, ctx->d_x[cur], {}, nullptr, {S}, ctx->x_plane, ctx->e_plane, {S_UNIT / (X_UNIT * X_UNIT)}, 0.0f, 0.0f};
+    SymmetricArgs g{part.d_tiles[GRAM], ctx->d_mats, ctx->d_x[cur], {}, nullptr, {S}, ctx->x_plane, ctx->e_plane, {S_UNIT / (X_UNIT * X_UNIT)}, 0.0f, 0.0f};
     symmetric<2, true>(part, g, 1, stream);
     double most = 1.0;      // what Q's elements can come to
     for (int k = first; k < first + n; ++k)
@@ -423,9 +433,9 @@ void follow_s(ob_muon_ctx* ctx, const Part& part, hipStream_t stream) {
       // the first B is Q; it is kept in Q's unit
       uint16_t* const B = start ? q : ctx->d_e[1];
       const float unit = start ? q_unit : E_UNIT;
-      symmetric<2, false>(part, SymmetricArgs{part.d_sym, ctx->d_mats, S, {S}, S, {B}, 0, ctx->e_plane, {c * unit / (S_UNIT * S_UNIT)}, b * unit / S_UNIT, a * unit},
+      symmetric<2, false>(part, SymmetricArgs{part.d_tiles[SYMMETRIC], ctx->d_mats, S, {S}, S, {B}, 0, ctx->e_plane, {c * unit / (S_UNIT * S_UNIT)}, b * unit / S_UNIT, a * unit},
                           1, stream);
-      SymmetricArgs p{part.d_sym, ctx->d_mats, B, {}, nullptr, {}, 0, ctx->e_plane, {}, 0.0f, 0.0f};
+      SymmetricArgs p{part.d_tiles[SYMMETRIC], ctx->d_mats, B, {}, nullptr, {}, 0, ctx->e_plane, {}, 0.0f, 0.0f};
       int products = 0;
       if (!end) {
         p.b[products] = S;
@@ -440,9 +450,9 @@ void follow_s(ob_muon_ctx* ctx, const Part& part, hipStream_t stream) {
         q = next;
       }
       if (products) symmetric<2, false>(part, p, products, stream);
-      if (!end) symmetric<2, false>(part, SymmetricArgs{part.d_sym, ctx->d_mats, Y, {B}, nullptr, {S}, 0, ctx->e_plane, {1.0f / unit}, 0.0f, 0.0f}, 1, stream);
+      if (!end) symmetric<2, false>(part, SymmetricArgs{part.d_tiles[SYMMETRIC], ctx->d_mats, Y, {B}, nullptr, {S}, 0, ctx->e_plane, {1.0f / unit}, 0.0f, 0.0f}, 1, stream);
     }
-    apply<2>(part, ApplyArgs{part.d_apply, ctx->d_mats, q, ctx->d_x[cur], ctx->d_x[cur ^ 1], ctx->e_plane, ctx->x_plane, 1.0f / q_unit}, stream);
+    apply<2>(part, ApplyArgs{part.d_tiles[APPLY], ctx->d_mats, q, ctx->d_x[cur], ctx->d_x[cur ^ 1], ctx->e_plane, ctx->x_plane, 1.0f / q_unit}, stream);
     cur ^= 1;
   }
 }
@@ -453,7 +463,7 @@ void step_by_step(ob_muon_ctx* ctx, const Part& part, hipStream_t stream) {
   for (int k = 0; k < ctx->steps; ++k) {
     const float a = ctx->coefficients[3 * k], b = ctx->coefficients[3 * k + 1], c = ctx->coefficients[3 * k + 2];
     const float per_gram = E_UNIT / (X_UNIT * X_UNIT);
-    SymmetricArgs g{part.d_sym, ctx->d_mats, ctx->d_x[k & 1], {}, nullptr, {E}, ctx->x_plane, ctx->e_plane, {per_gram}, 0.0f, 0.0f};
+    SymmetricArgs g{part.d_tiles[GRAM], ctx->d_mats, ctx->d_x[k & 1], {}, nullptr, {E}, ctx->x_plane, ctx->e_plane, {per_gram}, 0.0f, 0.0f};
     if (c != 0.0f) {
       g.diag = b / (2.0f * c) * E_UNIT;
     } else {      // B = a + b S from the first product alone
@@ -464,9 +474,9 @@ void step_by_step(ob_muon_ctx* ctx, const Part& part, hipStream_t stream) {
     symmetric<1, true>(part, g, 1, stream);
     if (c != 0.0f) {
       const float d = (float)(((double)a - (double)b * b / (4.0 * c)) * E_UNIT);
-      symmetric<1, false>(part, SymmetricArgs{part.d_sym, ctx->d_mats, E, {E}, nullptr, {B}, 0, ctx->e_plane, {c / E_UNIT}, 0.0f, d}, 1, stream);
+      symmetric<1, false>(part, SymmetricArgs{part.d_tiles[SYMMETRIC], ctx->d_mats, E, {E}, nullptr, {B}, 0, ctx->e_plane, {c / E_UNIT}, 0.0f, d}, 1, stream);
     }
-    apply<1>(part, ApplyArgs{part.d_apply, ctx->d_mats, B, ctx->d_x[k & 1], ctx->d_x[(k & 1) ^ 1], ctx->e_plane, ctx->x_plane, 1.0f / E_UNIT}, stream);
+    apply<1>(part, ApplyArgs{part.d_tiles[APPLY], ctx->d_mats, B, ctx->d_x[k & 1], ctx->d_x[(k & 1) ^ 1], ctx->e_plane, ctx->x_plane, 1.0f / E_UNIT}, stream);
   }
 }
 
@@ -536,25 +546,25 @@ ob_status create(const ob_muon_config* cfg, ob_muon_ctx* ctx) {
     each[0].insert(each[0].end(), each[1].begin(), each[1].end());
     each[1].clear();
   }
-  std::vector<ListTile> tables[2][2];
+  std::vector<ListTile> tables[2][3];
   for (const int f : {1, 0}) {
     if (each[f].empty()) continue;
     Part part;
     part.follow_s = f == 1;
-    part.sym_side = product_side(mats, each[f], true);
-    part.apply_side = product_side(mats, each[f], false);
-    tables[f][0] = product_tiles(mats, each[f], part.sym_side, true);
-    tables[f][1] = product_tiles(mats, each[f], part.apply_side, false);
-    if (tables[f][0].size() > 0x7fffffff || tables[f][1].size() > 0x7fffffff) return OB_ERR_SIZE;
-    part.sym_grid = (int)tables[f][0].size();
-    part.apply_grid = (int)tables[f][1].size();
+    part.sym_tile = product_tile(mats, each[f], true);
+    part.apply_tile = product_tile(mats, each[f], false);
+    for (const ProductKind k : {GRAM, SYMMETRIC, APPLY}) {
+      tables[f][k] = product_tiles(mats, each[f], side_of(k == APPLY ? part.apply_tile : part.sym_tile), k);
+      if (tables[f][k].size() > 0x7fffffff) return OB_ERR_SIZE;
+      part.grid[k] = (int)tables[f][k].size();
+    }
     const int last = last_buffer(ctx, part);
     for (const int i : each[f]) mats[i].last = last;
     ctx->parts.push_back(part);
   }
-  for (const Side& side : SIDES) {
-    hipError_t e = with_side(side.side, [&](auto n) { return allow_muon<n, 2>(); });
-    if (e == hipSuccess) e = with_side(side.side, [&](auto n) { return allow_muon<n, 1>(); });
+  for (int kind = 0; kind < KINDS; ++kind) {
+    hipError_t e = with_tile(kind, [&](auto n) { return allow_muon<n, 2>(); });
+    if (e == hipSuccess) e = with_tile(kind, [&](auto n) { return allow_muon<n, 1>(); });
     if (!hip_ok(ctx, e, "hipFuncSetAttribute")) return OB_ERR_HIP;
   }
   ctx->mats = (int)mats.size();
@@ -568,9 +578,9 @@ ob_status create(const ob_muon_config* cfg, ob_muon_ctx* ctx) {
     return at;
   };
   const size_t at_mats = place(room<Matrix>(mats.size())), at_square = place(room<SquareTile>(square.size()));
-  size_t at_table[2][2];
+  size_t at_table[2][3];
   for (const int f : {0, 1})
-    for (const int k : {0, 1}) at_table[f][k] = place(room<ListTile>(tables[f][k].size()));
+    for (const int k : {0, 1, 2}) at_table[f][k] = place(room<ListTile>(tables[f][k].size()));
   const size_t at_sums = place(room<double>(square.size())), at_inv = place(room<float>(mats.size()));
   const size_t at_x0 = place(room<uint16_t>(2 * xs)), at_x1 = place(room<uint16_t>(2 * xs));
   size_t at_e[5];
@@ -588,11 +598,10 @@ ob_status create(const ob_muon_config* cfg, ob_muon_ctx* ctx) {
   bool ok = hip_ok(ctx, hipMemcpy(ctx->d_mats, mats.data(), mats.size() * sizeof(Matrix), hipMemcpyHostToDevice), "hipMemcpy") &&
                   hip_ok(ctx, hipMemcpy(ctx->d_square, square.data(), square.size() * sizeof(SquareTile), hipMemcpyHostToDevice), "hipMemcpy");
   for (Part& part : ctx->parts)
-    for (const int k : {0, 1}) {
+    for (const int k : {0, 1, 2}) {
       const std::vector<ListTile>& table = tables[part.follow_s][k];
-      ListTile* const at = reinterpret_cast<ListTile*>(base + at_table[part.follow_s][k]);
-      (k ? part.d_apply : part.d_sym) = at;
-      ok = ok && hip_ok(ctx, hipMemcpy(at, table.data(), table.size() * sizeof(ListTile), hipMemcpyHostToDevice), "hipMemcpy");
+      part.d_tiles[k] = reinterpret_cast<ListTile*>(base + at_table[part.follow_s][k]);
+      ok = ok && hip_ok(ctx, hipMemcpy(part.d_tiles[k], table.data(), table.size() * sizeof(ListTile), hipMemcpyHostToDevice), "hipMemcpy");
     }
   return ok ? OB_OK : OB_ERR_HIP;
 }

@@ -271,7 +271,7 @@ struct SymmetricArgs {
   int64_t x_term, term;
   float mul[2], add_mul, diag;
 };
-template <class S, int TERMS, bool GRAM>
+template <class S, int TERMS, bool FROM_X>
 __global__ __launch_bounds__(S::NT, 2) void k_polar_symmetric(SymmetricArgs p) {
   using P = Product<S, false, KC, KC, TERMS, TERMS, WHOLE>;
   const ListTile t = p.tiles[blockIdx.x];
@@ -280,7 +280,7 @@ __global__ __launch_bounds__(S::NT, 2) void k_polar_symmetric(SymmetricArgs p) {
   const int mp = m.mp, which = blockIdx.y;
   typename P::Acc acc = {};
   const int r0 = t.tm * S::BM, c0 = t.tn * S::BN;
-  if constexpr (GRAM) {
+  if constexpr (FROM_X) {
     const Operand x{p.a + m.x, p.x_term, m.np, mp, true};
     P::run(x, x, r0, c0, 0, m.np, lds_of_launch, acc);
   } else {

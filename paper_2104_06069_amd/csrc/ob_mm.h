@@ -59,14 +59,15 @@ struct Slab {
   static constexpr int ALL = BR * BK / 8, WORK = ALL < NT ? ALL : NT;   // threads that fetch: whole wavefronts
   static constexpr int PER = ALL / WORK, STEP = WORK / PIECES;     // pieces each of them fetches, LDS rows between those
   static_assert(BK == 32 || BK == 64, "the permutations below");
-  static_assert(PER * WORK == ALL && WORK % 64 == 0 && WORK % PIECES == 0 && (PER == 1 || STEP % 16 == 0), "whole passes, each of the same permutation");
+  static_assert(PER * WORK == ALL && WORK % 64 == 0 && WORK % PIECES == 0 && (PER == 1 || STEP % 8 == 0), "whole passes; every one, or every second one, of the same permutation");
 
   __device__ static int turn(int row) {
     if constexpr (FORM == KC) return BK == 64 ? row & 7 : (row >> 1) & 3;
     else return (((row & 3) | ((row >> 1) & 4)) << 1) & (PIECES - 1);
   }
 
-  int off[FORM == KC ? PER : 1];     // elements from the tile's first
+  static constexpr int OFFS = FORM == KC ? PER : PER > 1 && STEP % 16 ? 2 : 1;
+  int off[OFFS];     // elements from the tile's first
 
   __device__ void init(const Operand& o, int r0, int tid) {
     const int row = tid / PIECES, at = ((tid % PIECES) ^ turn(row)) * 8;
@@ -74,7 +75,8 @@ struct Slab {
 #pragma unroll
       for (int j = 0; j < PER; ++j) off[j] = (int)((min(r0 + row + j * STEP, o.rows - 1) - r0) * o.ld) + at;
     } else {
-      off[0] = (int)(row * o.ld) + min(r0 + at, o.rows - 8) - r0;
+#pragma unroll
+      for (int j = 0; j < OFFS; ++j) off[j] = (int)(row * o.ld) + min(r0 + (tid % PIECES ^ turn(row + j * STEP)) * 8, o.rows - 8) - r0;
     }
   }
 
@@ -86,7 +88,7 @@ struct Slab {
     for (int j = 0; j < PER; ++j) {
       const uint16_t* src;
       if constexpr (FORM == KC) src = base + (int64_t)r0 * o.ld + k0 + off[j];
-      else src = base + (int64_t)(k0 + j * STEP) * o.ld + r0 + off[0];
+      else src = base + (int64_t)(k0 + j * STEP) * o.ld + r0 + off[j % OFFS];
       __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, in_lds<void>(lds + wave * 512 + j * WORK * 8), 16, 0, 0);
     }
   }
@@ -187,18 +189,36 @@ struct Results {
         for (int j = 0; j < S::FN; ++j)
           *in_lds<v4f>(own + (i * 16 + (lane & 15)) * STRIDE + j * 16 + 4 * (lane >> 4)) = acc[g * GROUP + i][j];
       lds_done();
+      constexpr int EACH = ROWS * WIDTH / 256, BATCH = EACH < 4 ? EACH : 4;      // pieces a lane; reads under way at once
 #pragma unroll 1
-      for (int k = lane; k < ROWS * WIDTH / 4; k += 64) {
-        const int r = k / (WIDTH / 4), c = k % (WIDTH / 4) * 4;
-        by_row(r0 + g * ROWS + r, c0 + c, *in_lds<const v4f>(own + r * STRIDE + c));
+      for (int k0 = lane; k0 < EACH * 64; k0 += BATCH * 64) {
+        v4f v[BATCH];
+#pragma unroll
+        for (int u = 0; u < BATCH; ++u) {
+          const int k = k0 + u * 64, r = k / (WIDTH / 4), c = k % (WIDTH / 4) * 4;
+          v[u] = *in_lds<const v4f>(own + r * STRIDE + c);
+        }
+#pragma unroll
+        for (int u = 0; u < BATCH; ++u) {
+          const int k = k0 + u * 64;
+          by_row(r0 + g * ROWS + k / (WIDTH / 4), c0 + k % (WIDTH / 4) * 4, v[u]);
+        }
       }
       if constexpr (MIRROR) {
 #pragma unroll 1
-        for (int k = lane; k < ROWS * WIDTH / 4; k += 64) {
-          const int c = k / (ROWS / 4), r = k % (ROWS / 4) * 4;
-          const float* const at = own + r * STRIDE + c;
-          by_column(r0 + g * ROWS + r, c0 + c, v4f{*in_lds<const float>(at), *in_lds<const float>(at + STRIDE), *in_lds<const float>(at + 2 * STRIDE),
-                                                   *in_lds<const float>(at + 3 * STRIDE)});
+        for (int k0 = lane; k0 < EACH * 64; k0 += BATCH * 64) {
+          v4f v[BATCH];
+#pragma unroll
+          for (int u = 0; u < BATCH; ++u) {
+            const int k = k0 + u * 64, c = k / (ROWS / 4), r = k % (ROWS / 4) * 4;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[u][e] = *in_lds<const float>(own + (r + e) * STRIDE + c);
+          }
+#pragma unroll
+          for (int u = 0; u < BATCH; ++u) {
+            const int k = k0 + u * 64;
+            by_column(r0 + g * ROWS + k % (ROWS / 4) * 4, c0 + k / (ROWS / 4), v[u]);
+          }
         }
       }
       lds_done();
