@@ -36,18 +36,19 @@ auto with_tile(int kind, F f) {
   }
 }
 
-// How many of a kind run at once on a CU, and the CU's rate with all of them and with one, in multiply-adds a microsecond:
-// 8192^3 at 1250, 1100 and (64 x 64) 750 TFLOP/s.
+// What a CU takes for as many tiles of a kind as it runs at once, in microseconds: `fixed` for loading the first slabs and for
+// the results, and for each column of K with all of them, or with one alone.  Measured at 8192 x 8192 by 512 to 8192, bfloat16.
 struct Rate {
   int per_cu;
-  double all, one;
+  double fixed, all, one;
 };
-constexpr Rate RATES[KINDS] = {{1, 2.4e6, 2.4e6}, {2, 2.1e6, 1.1e6}, {3, 1.4e6, 0.45e6}, {1, 0.8e6, 0.8e6}};
-// Time of `tiles` tiles of the given mean depth, in microseconds, if they are dealt evenly
+constexpr Rate RATES[KINDS] = {{1, 7.0, 0.0251, 0.0251}, {2, 3.6, 0.0149, 0.0095}, {3, 1.8, 0.0080, 0.0055}, {1, 1.8, 0.0050, 0.0050}};
+// Time of `tiles` tiles of the given mean depth, if they are dealt evenly
 double tiles_time(int kind, double tiles, double depth) {
   const Rate& r = RATES[kind];
-  const double one = (double)side_of(kind) * side_of(kind) * depth, a_cu = std::ceil(tiles / 256);      // tiles that the busiest CU gets
-  return one * a_cu / (a_cu < r.per_cu ? r.one + (r.all - r.one) * (a_cu - 1) / (r.per_cu - 1) : r.all);
+  const double a_cu = std::ceil(tiles / CUS), rounds = std::floor(a_cu / r.per_cu), rest = a_cu - rounds * r.per_cu;
+  const double last = rest > 0 ? r.fixed + depth * (r.one + (r.all - r.one) * (rest - 1) / (r.per_cu - 1)) : 0.0;
+  return rounds * (r.fixed + depth * r.all) + last;
 }
 // The kind whose tiles take the shortest, for `tiles(side)` tiles
 template <class F>
@@ -104,7 +105,7 @@ namespace {
 template <class S, bool BF, int FB, int MODE>
 ob_status launch_rows(ob_experts_ctx* ctx, const RowsArgs& p, hipStream_t stream) {
   const int64_t tiles = ((int64_t)p.groups.rows / S::BM + std::min<int64_t>(p.groups.n, p.groups.rows)) * ((p.width + S::BN - 1) / S::BN);
-  const int64_t grid = (tiles + 7) / 8 * 8;
+  const int64_t grid = (tiles + 7) / 8 * 8 + (S::BM == 256 ? CUS : 0);      // (with the split tiles of the last round)
   if (grid > 0x7fffffff) return OB_ERR_SIZE;
   hipLaunchKernelGGL((k_experts_rows<S, BF, FB, MODE>), dim3((unsigned)grid), dim3(S::NT), (Product<S, BF, KC, FB, 1, 1, MODE>::LDS_BYTES), stream, p);
   return hip_ok(ctx, hipGetLastError(), "k_experts_rows") ? OB_OK : OB_ERR_HIP;
@@ -112,8 +113,8 @@ ob_status launch_rows(ob_experts_ctx* ctx, const RowsArgs& p, hipStream_t stream
 
 template <class S, bool BF, int MODE>
 ob_status launch_weights(ob_experts_ctx* ctx, const WeightsArgs& p, hipStream_t stream) {
-  const int64_t tiles = (int64_t)p.groups.n * ((p.height + S::BM - 1) / S::BM) * ((p.width + S::BN - 1) / S::BN);
-  const int64_t grid = (tiles + 7) / 8 * 8;
+  const int64_t tiles = (int64_t)((p.height + S::BM - 1) / S::BM) * ((p.width + S::BN - 1) / S::BN);      // of a group
+  const int64_t grid = (tiles + 7) / 8 * 8 * p.groups.n;
   if (grid > 0x7fffffff) return OB_ERR_SIZE;
   hipLaunchKernelGGL((k_experts_weights<S, BF, MODE>), dim3((unsigned)grid), dim3(S::NT), (Product<S, BF, KS, KS, 1, 1, MODE>::LDS_BYTES), stream, p);
   return hip_ok(ctx, hipGetLastError(), "k_experts_weights") ? OB_OK : OB_ERR_HIP;
@@ -345,7 +346,7 @@ std::vector<ListTile> product_tiles(const std::vector<Matrix>& mats, const std::
   return deal(std::move(units), symmetric);
 }
 
-int product_tile(const std::vector<Matrix>& mats, const std::vector<int>& part, bool symmetric) {
+int product_tile(const std::vector<Matrix>& mats, const std::vector<int>& part, bool symmetric, bool two_terms) {
   double depth = 0, elements = 0;      // of the products' K, weighted by what is computed of them
   for (const int i : part) {
     const double out = symmetric ? 0.5 * mats[i].mp * mats[i].mp : (double)mats[i].mp * mats[i].np;
@@ -359,7 +360,7 @@ int product_tile(const std::vector<Matrix>& mats, const std::vector<int>& part, 
       tiles += symmetric ? 0.5 * nm * (nm + 1) : nm * nn;
     }
     return tiles;
-  }, depth / elements);
+  }, (two_terms ? 3.0 : symmetric ? 1.0 : 2.0) * depth / elements);      // products of terms
 }
 
 template <class T>
@@ -551,8 +552,8 @@ ob_status create(const ob_muon_config* cfg, ob_muon_ctx* ctx) {
     if (each[f].empty()) continue;
     Part part;
     part.follow_s = f == 1;
-    part.sym_tile = product_tile(mats, each[f], true);
-    part.apply_tile = product_tile(mats, each[f], false);
+    part.sym_tile = product_tile(mats, each[f], true, f == 1);
+    part.apply_tile = product_tile(mats, each[f], false, f == 1);
     for (const ProductKind k : {GRAM, SYMMETRIC, APPLY}) {
       tables[f][k] = product_tiles(mats, each[f], side_of(k == APPLY ? part.apply_tile : part.sym_tile), k);
       if (tables[f][k].size() > 0x7fffffff) return OB_ERR_SIZE;

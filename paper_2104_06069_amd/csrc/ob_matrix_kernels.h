@@ -5,6 +5,7 @@
 
 namespace obm {
 
+constexpr int CUS = 256;        // of an MI355X
 constexpr int BLOCK = 256;      // threads of the element-wise kernels
 constexpr int SIDE = 64;        // side of their tiles, and what the sides of the working matrices are multiples of
 
@@ -92,13 +93,10 @@ struct Groups {
   }
 };
 
-// Which group's which tile (of BM rows and the `width` columns of tiles) this workgroup has: every wavefront counts the
-// groups' tiles, 64 groups at a time.  The host knows an upper bound of their number alone; workgroups past the last leave.
-struct RowTile {
-  int g, lo, rows, tm, tn;
-};
+// The groups' tiles of BM rows, one after the other: every wavefront counts them, 64 groups at a time.  The host knows an
+// upper bound of their number alone.
 template <int BM>
-__device__ __forceinline__ bool find_row_tile(const Groups& gr, int width, int id, RowTile* out) {
+__device__ __forceinline__ int count_row_tiles(const Groups& gr) {
   const int lane = threadIdx.x & 63;
   int total = 0;
   for (int g0 = 0; g0 < gr.n; g0 += 64) {
@@ -109,8 +107,16 @@ __device__ __forceinline__ bool find_row_tile(const Groups& gr, int width, int i
     for (int d = 32; d; d >>= 1) t += __shfl_xor(t, d);
     total += t;
   }
-  const int tile = tile_of_workgroup(id, __builtin_amdgcn_readfirstlane(total) * width);
-  if (tile < 0) return false;
+  return __builtin_amdgcn_readfirstlane(total);
+}
+// Tile `tile` of them and of the `width` columns of tiles: its group's number, first row and number of rows, and its place
+struct RowTile {
+  int g, lo, rows, tm, tn;
+};
+template <int BM>
+__device__ __forceinline__ RowTile find_row_tile(const Groups& gr, int width, int tile) {
+  const int lane = threadIdx.x & 63;
+  RowTile out = {};
   int before = 0;
   for (int g0 = 0; g0 < gr.n; g0 += 64) {
     int lo = 0, hi = 0;
@@ -125,21 +131,19 @@ __device__ __forceinline__ bool find_row_tile(const Groups& gr, int width, int i
     const unsigned long long past = __ballot((before + upto) * width > tile);
     if (past) {
       const int l = __ffsll((long long)past) - 1;
-      out->g = g0 + l;
-      out->lo = __shfl(lo, l);
-      out->rows = __shfl(hi, l) - out->lo;
       const int tiles = __shfl(own, l), first = before + __shfl(upto, l) - tiles;
-      tile_in_bands(tile - first * width, tiles, width, &out->tm, &out->tn);
-      out->g = __builtin_amdgcn_readfirstlane(out->g);
-      out->lo = __builtin_amdgcn_readfirstlane(out->lo);
-      out->rows = __builtin_amdgcn_readfirstlane(out->rows);
-      out->tm = __builtin_amdgcn_readfirstlane(out->tm);
-      out->tn = __builtin_amdgcn_readfirstlane(out->tn);
-      return true;
+      int tm, tn;
+      tile_in_bands(tile - first * width, tiles, width, &tm, &tn);
+      out.g = __builtin_amdgcn_readfirstlane(g0 + l);
+      out.lo = __builtin_amdgcn_readfirstlane(__shfl(lo, l));
+      out.rows = __builtin_amdgcn_readfirstlane(__shfl(hi, l)) - out.lo;
+      out.tm = __builtin_amdgcn_readfirstlane(tm);
+      out.tn = __builtin_amdgcn_readfirstlane(tn);
+      return out;
     }
     before += __shfl(upto, 63);
   }
-  return false;
+  return out;
 }
 
 // forward (x, W, y) and input_grad (dy, W transposed, dx): out[r] = a[r] W_g, a [rows, depth], out [rows, width].  FB: order
@@ -154,19 +158,42 @@ struct RowsArgs {
   bool a_direct, w_direct;
 };
 template <class S, bool BF, int FB, int MODE>
-__global__ __launch_bounds__(S::NT, 2) void k_experts_rows(RowsArgs p) {
+__device__ __forceinline__ void rows_tile(const RowsArgs& p, const RowTile& t, int r0, int c0) {
   using P = Product<S, BF, KC, FB, 1, 1, MODE>;
-  RowTile t;
-  if (!find_row_tile<S::BM>(p.groups, (p.width + S::BN - 1) / S::BN, blockIdx.x, &t)) return;
+  if (r0 >= t.rows || c0 >= p.width) return;
   typename P::Acc acc = {};
   const Operand a{p.a + t.lo * p.lda, 0, p.lda, t.rows, p.a_direct};
   const Operand b{p.w + t.g * p.w_stride, 0, p.ldw, p.width, p.w_direct};
-  P::run(a, b, t.tm * S::BM, t.tn * S::BN, 0, p.depth, lds_of_launch, acc);
+  P::run(a, b, r0, c0, 0, p.depth, lds_of_launch, acc);
   Results<S>::visit(acc, lds_of_launch, [&](int r, int c, v4f v) {
-    r += t.tm * S::BM;
-    c += t.tn * S::BN;
+    r += r0;
+    c += c0;
     if (r < t.rows) store4(p.out, p.out_dtype, (t.lo + r) * p.ldo + c, p.width - c, v);
   });
+}
+template <class S, bool BF, int FB, int MODE>
+__global__ __launch_bounds__(S::NT, 2) void k_experts_rows(RowsArgs p) {
+  const int width = (p.width + S::BN - 1) / S::BN, tiles = count_row_tiles<S::BM>(p.groups) * width;
+  // A CU has one workgroup of 256 x 256 at a time.  Of the last round, if it would leave half the card or more idle, each tile is
+  // split between two workgroups, or four.  (Measured with 1088 tiles, 4.25 rounds: TODO-ROUNDS.)
+  const int rest = S::BM == 256 ? tiles % CUS : 0, parts = rest == 0 ? 1 : rest * 4 <= CUS ? 4 : rest * 2 <= CUS ? 2 : 1;
+  const int whole = parts > 1 ? tiles - rest : tiles;
+  const int id = blockIdx.x, before_rest = (whole + 7) / 8 * 8;
+  if (id < before_rest) {
+    const int tile = tile_of_workgroup(id, whole);
+    if (tile < 0) return;
+    const RowTile t = find_row_tile<S::BM>(p.groups, width, tile);
+    rows_tile<S, BF, FB, MODE>(p, t, t.tm * S::BM, t.tn * S::BN);
+    return;
+  }
+  if constexpr (S::BM == 256) {
+    const int part = id - before_rest;
+    if (parts == 1 || part >= rest * parts) return;
+    const RowTile t = find_row_tile<256>(p.groups, width, whole + part / parts);
+    const int k = part % parts;
+    if (parts == 4) rows_tile<Shape<128, 128, 64, 2, 4>, BF, FB, MODE>(p, t, t.tm * 256 + k / 2 * 128, t.tn * 256 + k % 2 * 128);
+    else rows_tile<Shape<128, 256, 64, 2, 4>, BF, FB, MODE>(p, t, t.tm * 256 + k * 128, t.tn * 256);
+  }
 }
 
 // weight_grad: out_g = a_g^T b_g, a [rows, height], b [rows, width], out [height, width].
@@ -183,11 +210,11 @@ template <class S, bool BF, int MODE>
 __global__ __launch_bounds__(S::NT, 2) void k_experts_weights(WeightsArgs p) {
   using P = Product<S, BF, KS, KS, 1, 1, MODE>;
   const int nm = (p.height + S::BM - 1) / S::BM, nn = (p.width + S::BN - 1) / S::BN;
-  const int t = tile_of_workgroup(blockIdx.x, p.groups.n * nm * nn);
-  if (t < 0) return;
-  const int g = t / (nm * nn);
+  // Each die (tile_of_workgroup) gets an eighth of every group's tiles, whose cost goes with the group's rows.
+  const int share = (nm * nn + 7) / 8, place = blockIdx.x >> 3, g = place / share, t = (blockIdx.x & 7) * share + place % share;
+  if (g >= p.groups.n || t >= nm * nn) return;
   int tm, tn, lo, hi;
-  tile_in_bands(t - g * nm * nn, nm, nn, &tm, &tn);
+  tile_in_bands(t, nm, nn, &tm, &tn);
   p.groups.range(g, &lo, &hi);
   typename P::Acc acc = {};
   if (hi > lo) {
