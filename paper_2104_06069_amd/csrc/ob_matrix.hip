@@ -111,6 +111,16 @@ ob_status launch_rows(ob_experts_ctx* ctx, const RowsArgs& p, hipStream_t stream
   return hip_ok(ctx, hipGetLastError(), "k_experts_rows") ? OB_OK : OB_ERR_HIP;
 }
 
+template <bool BF, int FB, int MODE>
+ob_status launch_few_rows(ob_experts_ctx* ctx, const RowsArgs& p, hipStream_t stream) {
+  using F = FewRows<BF, FB, MODE>;
+  const int64_t tiles = ((int64_t)p.groups.rows / F::BM + std::min<int64_t>(p.groups.n, p.groups.rows)) * ((p.width + F::BN - 1) / F::BN);
+  const int64_t grid = (tiles + 7) / 8 * 8;
+  if (grid > 0x7fffffff) return OB_ERR_SIZE;
+  hipLaunchKernelGGL((k_experts_few_rows<BF, FB, MODE>), dim3((unsigned)grid), dim3(256), (F::LDS_BYTES), stream, p);
+  return hip_ok(ctx, hipGetLastError(), "k_experts_few_rows") ? OB_OK : OB_ERR_HIP;
+}
+
 template <class S, bool BF, int MODE>
 ob_status launch_weights(ob_experts_ctx* ctx, const WeightsArgs& p, hipStream_t stream) {
   const int64_t tiles = (int64_t)((p.height + S::BM - 1) / S::BM) * ((p.width + S::BN - 1) / S::BN);      // of a group
@@ -130,9 +140,15 @@ auto with_tile_and_mode(int kind, bool direct, F f) {
   return with_tile(kind, [&](auto n) { return f(n, std::integral_constant<int, TAIL>{}); });
 }
 
+template <bool BF, int MODE>
+hipError_t allow_few_rows() {
+  const hipError_t e = allow_lds(k_experts_few_rows<BF, KC, MODE>, FewRows<BF, KC, MODE>::LDS_BYTES);
+  return e == hipSuccess ? allow_lds(k_experts_few_rows<BF, KS, MODE>, FewRows<BF, KS, MODE>::LDS_BYTES) : e;
+}
 template <bool BF>
 hipError_t allow_experts() {
-  hipError_t e = hipSuccess;
+  hipError_t e = allow_few_rows<BF, TAIL>();
+  if (e == hipSuccess) e = allow_few_rows<BF, ANY>();
   for (int kind = 0; kind < KINDS; ++kind)
     for (const bool direct : {false, true}) {
       if (e != hipSuccess) return e;
@@ -147,6 +163,7 @@ hipError_t allow_experts() {
   return e;
 }
 
+constexpr double FEW_ROWS = 16;      // rows a group (of those that can have one) up to which k_experts_few_rows is taken
 constexpr int64_t MAX_LD = (int64_t)1 << 22;      // a tile's offsets are 32-bit
 
 ob_status rows_call(ob_experts_ctx* ctx, const void* a, int64_t lda, const void* w, const int32_t* offsets, int64_t rows,
@@ -179,6 +196,13 @@ ob_status rows_call(ob_experts_ctx* ctx, const void* a, int64_t lda, const void*
   // (a group's last tile is half full in the mean)
   const double groups = (double)std::min<int64_t>(c.num_groups, rows);
   const int kind = best_tile([&](int n) { return std::max(groups, rows / (double)n + 0.5 * groups) * (double)((width + n - 1) / n); }, (double)depth);
+  if (rows <= FEW_ROWS * groups) {
+    const auto few = [&](auto mode) {
+      if (c.dtype == OB_BF16) return strided ? launch_few_rows<true, KS, mode>(ctx, p, s) : launch_few_rows<true, KC, mode>(ctx, p, s);
+      return strided ? launch_few_rows<false, KS, mode>(ctx, p, s) : launch_few_rows<false, KC, mode>(ctx, p, s);
+    };
+    return p.a_direct && p.w_direct ? few(std::integral_constant<int, TAIL>{}) : few(std::integral_constant<int, ANY>{});
+  }
   return with_tile_and_mode(kind, p.a_direct && p.w_direct, [&](auto n, auto mode) {
     using S = Tile<n, 64>;
     if (c.dtype == OB_BF16) return strided ? launch_rows<S, true, KS, mode>(ctx, p, s) : launch_rows<S, true, KC, mode>(ctx, p, s);

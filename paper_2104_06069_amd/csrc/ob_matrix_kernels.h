@@ -196,6 +196,104 @@ __global__ __launch_bounds__(S::NT, 2) void k_experts_rows(RowsArgs p) {
   }
 }
 
+// The same for few rows a group, where what counts is how fast the weights of the groups that have any are read.  A workgroup has
+// 16 rows by 32 columns; its wavefronts share out the slabs of K, each with slabs of its own in LDS and no barriers, so that
+// up to 4 x 3 slabs are under way at once, and their sums are added in a fixed order at the end.
+template <bool BF, int FB, int MODE>
+struct FewRows {
+  static constexpr int BM = 16, BN = 32, BK = 64, WAVES = 4, STAGES = 3;
+  using A = Slab<KC, BM, BK, 64>;
+  using B = Slab<FB, BN, BK, 64>;
+  static constexpr int STAGE = (BM + BN) * BK, STRIDE = BN + 4;
+  static constexpr int LDS_BYTES = WAVES * STAGES * STAGE * 2;
+  static_assert(BM * STRIDE * 4 <= STAGES * STAGE * 2, "a wavefront's sums lie where its slabs were");
+};
+template <bool BF, int FB, int MODE>
+__global__ __launch_bounds__(256, 2) void k_experts_few_rows(RowsArgs p) {
+  using F = FewRows<BF, FB, MODE>;
+  using A = typename F::A;
+  using B = typename F::B;
+  const int width = (p.width + F::BN - 1) / F::BN;
+  const int tile = tile_of_workgroup(blockIdx.x, count_row_tiles<F::BM>(p.groups) * width);
+  if (tile < 0) return;
+  const RowTile t = find_row_tile<F::BM>(p.groups, width, tile);
+  const Operand a{p.a + t.lo * p.lda, 0, p.lda, t.rows, p.a_direct};
+  const Operand b{p.w + t.g * p.w_stride, 0, p.ldw, p.width, p.w_direct};
+  const int r0 = t.tm * F::BM, c0 = t.tn * F::BN, lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  uint16_t* const own = lds_of_launch + wave * F::STAGES * F::STAGE;
+  A sa;
+  B sb;
+  sa.init(a, r0, lane);
+  sb.init(b, c0, lane);
+  v4f acc[2] = {};
+  const auto multiply = [&](const uint16_t* s) {
+#pragma unroll
+    for (int kk = 0; kk < F::BK / 32; ++kk) {
+      const v8s fa = A::fragment(s, 0, kk, lane);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) acc[j] = mma<BF>(B::fragment(s + F::BM * F::BK, j * 16, kk, lane), fa, acc[j]);
+    }
+  };
+  // slabs wave, wave + 4, ..
+  const int slabs = MODE == ANY ? (p.depth + F::BK - 1) / F::BK : p.depth / F::BK;
+  const int n = (slabs - wave + F::WAVES - 1) / F::WAVES;
+  const auto column = [&](int i) { return (wave + i * F::WAVES) * F::BK; };
+  if constexpr (MODE == ANY) {
+    typename A::Fetched va;
+    typename B::Fetched vb;
+    if (n > 0) {
+      A::fetch(a, r0, column(0), p.depth, lane, va);
+      B::fetch(b, c0, column(0), p.depth, lane, vb);
+    }
+    for (int i = 0; i < n; ++i) {
+      A::put(a, r0, column(i), p.depth, lane, va, own);
+      B::put(b, c0, column(i), p.depth, lane, vb, own + F::BM * F::BK);
+      if (i + 1 < n) {
+        A::fetch(a, r0, column(i + 1), p.depth, lane, va);
+        B::fetch(b, c0, column(i + 1), p.depth, lane, vb);
+      }
+      lds_done();
+      multiply(own);
+      lds_done();
+    }
+  } else {
+    const auto load = [&](int i) {
+      uint16_t* const s = own + i % F::STAGES * F::STAGE;
+      sa.load(a, 0, r0, column(i), s, 0);
+      sb.load(b, 0, c0, column(i), s + F::BM * F::BK, 0);
+    };
+#pragma unroll
+    for (int i = 0; i < F::STAGES; ++i)
+      if (i < n) load(i);
+    for (int i = 0; i < n; ++i) {
+      if (i + F::STAGES <= n) loads_left<(A::PER + B::PER) * (F::STAGES - 1)>();
+      else loads_done();
+      multiply(own + i % F::STAGES * F::STAGE);
+      lds_done();
+      if (i + F::STAGES < n) load(i + F::STAGES);
+    }
+    if (slabs * F::BK < p.depth && wave == slabs % F::WAVES) {      // the last slab, which ends inside
+      A::load_any(a, r0, slabs * F::BK, p.depth, own, lane);
+      B::load_any(b, c0, slabs * F::BK, p.depth, own + F::BM * F::BK, lane);
+      lds_done();
+      multiply(own);
+      lds_done();
+    }
+  }
+  float* const sums = reinterpret_cast<float*>(own);
+#pragma unroll
+  for (int j = 0; j < 2; ++j) *in_lds<v4f>(sums + (lane & 15) * F::STRIDE + j * 16 + 4 * (lane >> 4)) = acc[j];
+  __syncthreads();
+  if (threadIdx.x >= F::BM * F::BN / 4) return;
+  const int r = threadIdx.x / (F::BN / 4), c = threadIdx.x % (F::BN / 4) * 4;
+  v4f v = {};
+#pragma unroll
+  for (int w = 0; w < F::WAVES; ++w)
+    v += *in_lds<const v4f>(reinterpret_cast<const float*>(lds_of_launch + w * F::STAGES * F::STAGE) + r * F::STRIDE + c);
+  if (r0 + r < t.rows) store4(p.out, p.out_dtype, (t.lo + r0 + r) * p.ldo + c0 + c, p.width - c0 - c, v);
+}
+
 // weight_grad: out_g = a_g^T b_g, a [rows, height], b [rows, width], out [height, width].
 struct WeightsArgs {
   Groups groups;

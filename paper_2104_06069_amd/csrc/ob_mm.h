@@ -93,36 +93,56 @@ struct Slab {
     }
   }
 
-  // Any slab, through registers; columns from K on are zeros.
-  __device__ static void load_any(const Operand& o, int r0, int k0, int K, uint16_t* lds, int tid) {
+  // Any slab, through registers: fetch() starts its loads, put() takes them to LDS.  Columns from K on are zeros.
+  typedef v8s Fetched[PER];
+  // How many of the eight elements of piece j exist (8: all; 0 or less: none), and the width of a row in memory
+  __device__ static int piece_left(const Operand& o, int r0, int k0, int K, int tid, int j, int* r, int* c) {
+    const int row = tid / PIECES + j * STEP, at = (tid % PIECES ^ turn(row)) * 8;
+    *r = FORM == KC ? min(r0 + row, o.rows - 1) : k0 + row;
+    *c = FORM == KC ? k0 + at : r0 + at;
+    return *r < (FORM == KC ? o.rows : K) ? (FORM == KC ? K : o.rows) - *c : 0;
+  }
+  __device__ static void fetch(const Operand& o, int r0, int k0, int K, int tid, Fetched& v) {
     if (WORK < NT && tid >= WORK) return;
-    const int row0 = tid / PIECES, pos = tid % PIECES;
-    const int width = FORM == KC ? K : o.rows;      // of a row in memory
-    v8s v[PER];
+    const int width = FORM == KC ? K : o.rows;
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
-      const int row = row0 + j * STEP, at = (pos ^ turn(row)) * 8;
-      const int r = FORM == KC ? min(r0 + row, o.rows - 1) : k0 + row;
-      const int c = FORM == KC ? k0 + at : r0 + at, left = r < (FORM == KC ? o.rows : K) ? width - c : 0;
-      v[j] = v8s{};
+      int r, c;
+      const int left = piece_left(o, r0, k0, K, tid, j, &r, &c);
       const uint16_t* const src = o.p + (int64_t)r * o.ld + c;
-      if (left >= 8) {
-        v[j] = *reinterpret_cast<const v8s_any*>(src);
-      } else if (left > 0 && width >= 8) {     // the eight elements up to the row's end, moved down
-        const v2u w = __builtin_bit_cast(v2u, (v8s)*reinterpret_cast<const v8s_any*>(src + left - 8));
-        const int s = (8 - left) * 16;
-        v2u z;
-        z.x = s >= 64 ? w.y >> (s - 64) : (w.x >> s) | (w.y << (64 - s));
-        z.y = s >= 64 ? 0 : w.y >> s;
-        v[j] = __builtin_bit_cast(v8s, z);
-      } else if (left > 0) {                   // rows of fewer than eight
+      v[j] = v8s{};
+      if (left > 0 && width >= 8) {
+        v[j] = *reinterpret_cast<const v8s_any*>(src + min(left - 8, 0));      // at the end of a row: its last eight
+      } else if (left > 0) {
 #pragma unroll
         for (int e = 0; e < 7; ++e)
           if (e < left) v[j][e] = (short)src[e];
       }
     }
+  }
+  __device__ static void put(const Operand& o, int r0, int k0, int K, int tid, const Fetched& v, uint16_t* lds) {
+    if (WORK < NT && tid >= WORK) return;
+    const int width = FORM == KC ? K : o.rows;
 #pragma unroll
-    for (int j = 0; j < PER; ++j) *in_lds<v8s>(lds + (j * WORK + tid) * 8) = v[j];
+    for (int j = 0; j < PER; ++j) {
+      int r, c;
+      const int left = piece_left(o, r0, k0, K, tid, j, &r, &c);
+      v8s piece = v[j];
+      if (left > 0 && left < 8 && width >= 8) {      // moved down to where they belong, zeros behind them
+        const v2u w = __builtin_bit_cast(v2u, piece);
+        const int s = (8 - left) * 16;
+        v2u z;
+        z.x = s >= 64 ? w.y >> (s - 64) : (w.x >> s) | (w.y << (64 - s));
+        z.y = s >= 64 ? 0 : w.y >> s;
+        piece = __builtin_bit_cast(v8s, z);
+      }
+      *in_lds<v8s>(lds + (j * WORK + tid) * 8) = piece;
+    }
+  }
+  __device__ static void load_any(const Operand& o, int r0, int k0, int K, uint16_t* lds, int tid) {
+    Fetched v;
+    fetch(o, r0, k0, K, tid, v);
+    put(o, r0, k0, K, tid, v, lds);
   }
 
   // Operand registers of a 16x16x32 product: lane (q, i) gets row f0 + i, columns 32 kk + 8 q + 0..7 of the slab.
@@ -231,8 +251,8 @@ struct Results {
 };
 
 // What the operands may be.  WHOLE: `direct`, K a multiple of BK; TAIL: `direct`, any K, the last slab through registers once
-// the others are done; ANY: each slab as it has to be (the registers that takes at every slab do not fit beside a 256 x 256
-// tile's).
+// the others are done; ANY: every slab through registers, the next one's loads under way while one is multiplied (there are
+// not enough registers for that beside a 256 x 256 tile's).
 enum { WHOLE = 0, TAIL = 1, ANY = 2 };
 
 template <class S, bool BF, int FA, int FB, int TA, int TB, int MODE>
@@ -257,19 +277,10 @@ struct Product {
     const int n = MODE == ANY ? (K + BK - 1) / BK : K / BK, end = k0 + K;
     auto load = [&](int t) {
       uint16_t* const s = lds + t % S::STAGES * STAGE;
-      const int k = k0 + t * BK;
-      if (MODE != ANY || (a.direct && k + BK <= end)) {
 #pragma unroll
-        for (int x = 0; x < TA; ++x) sa.load(a, x, r0, k, s + x * BM * BK, wave);
-      } else {
-        A::load_any(a, r0, k, end, s, tid);
-      }
-      if (MODE != ANY || (b.direct && k + BK <= end)) {
+      for (int x = 0; x < TA; ++x) sa.load(a, x, r0, k0 + t * BK, s + x * BM * BK, wave);
 #pragma unroll
-        for (int y = 0; y < TB; ++y) sb.load(b, y, c0, k, s + (TA * BM + y * BN) * BK, wave);
-      } else {
-        B::load_any(b, c0, k, end, s + TA * BM * BK, tid);
-      }
+      for (int y = 0; y < TB; ++y) sb.load(b, y, c0, k0 + t * BK, s + (TA * BM + y * BN) * BK, wave);
     };
     auto read = [&](const uint16_t* s, int kk, v8s (&fa)[TA][FM], v8s (&fb)[TB][FN]) {
 #pragma unroll
@@ -293,7 +304,8 @@ struct Product {
               for (int j = 0; j < FN; ++j) acc[i][j] = mma<BF>(fb[y][j], fa[x][i], acc[i][j]);
           }
     };
-    if constexpr (S::TURNS) turns(n, lds, acc, load, read, multiply);
+    if constexpr (MODE == ANY) through_registers(a, b, r0, c0, k0, end, n, lds, read, multiply);
+    else if constexpr (S::TURNS) turns(n, lds, acc, load, read, multiply);
     else straight(n, wave, lds, acc, load, read, multiply);
     if (MODE == TAIL && n * BK < K) {
       A::load_any(a, r0, k0 + n * BK, end, lds, tid);
@@ -321,7 +333,7 @@ struct Product {
     for (int t = 0; t < AHEAD; ++t)
       if (t < n) load(t);
     for (int t = 0; t < n; ++t) {
-      if (MODE == ANY || AHEAD == 1 || t + AHEAD > n) loads_done();
+      if (AHEAD == 1 || t + AHEAD > n) loads_done();
       else if (la && lb) loads_left<(NA + NB) * (AHEAD - 1)>();
       else if (lb) loads_left<NB * (AHEAD - 1)>();
       else if (la) loads_left<NA * (AHEAD - 1)>();
@@ -329,6 +341,36 @@ struct Product {
       group_barrier();      // slab t is there, and nobody reads slab t - 1 any more
       if (t + AHEAD < n) load(t + AHEAD);
       const uint16_t* const s = lds + t % S::STAGES * STAGE;
+#pragma unroll
+      for (int kk = 0; kk < BK / 32; ++kk) {
+        v8s fa[TA][FM], fb[TB][FN];
+        read(s, kk, fa, fb);
+        multiply(fa, fb);
+      }
+    }
+    lds_done();
+    group_barrier();
+  }
+
+  template <class R, class M>
+  __device__ static __forceinline__ void through_registers(const Operand& a, const Operand& b, int r0, int c0, int k0, int end, int n, uint16_t* lds,
+                                                           R read, M multiply) {
+    const int tid = threadIdx.x;
+    typename A::Fetched va;
+    typename B::Fetched vb;
+    A::fetch(a, r0, k0, end, tid, va);
+    B::fetch(b, c0, k0, end, tid, vb);
+    for (int t = 0; t < n; ++t) {
+      uint16_t* const s = lds + t % 2 * STAGE;      // nobody reads slab t - 2 after the barrier of t - 1
+      const int k = k0 + t * BK;
+      A::put(a, r0, k, end, tid, va, s);
+      B::put(b, c0, k, end, tid, vb, s + TA * BM * BK);
+      lds_done();
+      group_barrier();
+      if (t + 1 < n) {
+        A::fetch(a, r0, k + BK, end, tid, va);
+        B::fetch(b, c0, k + BK, end, tid, vb);
+      }
 #pragma unroll
       for (int kk = 0; kk < BK / 32; ++kk) {
         v8s fa[TA][FM], fb[TB][FN];
