@@ -19,12 +19,13 @@ using namespace obm;
 namespace {
 
 // Tiles of the products: 256 x 256 (eight wavefronts, one workgroup on a CU), 128 x 128 and 64 x 64 (four).  Slabs of 64
-// columns, or with two terms of 32: the same LDS.  DEEP: 64 x 64 with seven slabs under way, for launches of which a CU has one
-// workgroup at most: its time is then that of its loads, one after the other.
+// columns, or with two terms of 32: the same LDS.  DEEP: 64 x 64 with two teams of wavefronts, slabs of 64 columns and 128 KB of
+// them, for launches of which a CU has one workgroup at most.
 enum TileKind { T256, T128, T64, DEEP, KINDS };
 constexpr int side_of(int kind) { return kind == T256 ? 256 : kind == T128 ? 128 : 64; }
 template <int KIND, int BK>
-using Tile = Shape<side_of(KIND), side_of(KIND), BK, 2, KIND == T256 ? 4 : 2, KIND == DEEP ? 8 : KIND == T64 ? 3 : 2>;
+using Tile = Shape<side_of(KIND), side_of(KIND), KIND == DEEP ? 64 : BK, 2, KIND == T256 ? 4 : 2,
+                   KIND == DEEP ? (BK == 32 ? 4 : 8) : KIND == T64 ? 3 : 2, KIND == DEEP ? 2 : 1>;
 
 template <class F>
 auto with_tile(int kind, F f) {
@@ -291,7 +292,8 @@ namespace {
 
 // Matrices that go through the steps together, and the tiles of their products
 struct Part {
-  bool follow_s = false;      // the 22-bit way (ob_matrix_kernels.h)
+  bool follow_s = false;      // the way that follows S (ob_matrix_kernels.h); else step by step
+  int terms = 2;
   int sym_tile = T64, apply_tile = T64;
   // tiles of X X^T, of the other symmetric products (the same ones, but not in the same order: only there depths differ by n)
   // and of B X
@@ -308,6 +310,7 @@ struct ob_muon_ctx {
   std::vector<float> coefficients;      // 3 * steps
   int64_t n = 0;                        // elements of the flat buffers
   int mats = 0, square_tiles = 0;
+  bool norms = false;                   // a launch of k_muon_norms
   std::vector<Part> parts;
   int64_t x_plane = 0, e_plane = 0;     // elements
   void* mem = nullptr;
@@ -333,7 +336,7 @@ struct Unit {
   double cost;
   int mat, tm0, tm1, tn0, tn1;
 };
-std::vector<ListTile> deal(std::vector<Unit> units, bool upper) {
+std::vector<ListTile> deal(const std::vector<Matrix>& mats, std::vector<Unit> units, bool upper) {
   std::stable_sort(units.begin(), units.end(), [](const Unit& a, const Unit& b) { return a.cost > b.cost; });
   std::vector<ListTile> queue[8];
   double load[8] = {};
@@ -342,13 +345,13 @@ std::vector<ListTile> deal(std::vector<Unit> units, bool upper) {
     for (int tn = u.tn0; tn < u.tn1; ++tn)
       for (int tm = u.tm0; tm < u.tm1; ++tm) {
         if (upper && tn < tm) continue;
-        queue[q].push_back(ListTile{u.mat, (short)tm, (short)tn});
+        queue[q].push_back(ListTile{mats[u.mat].x, mats[u.mat].e, mats[u.mat].mp, mats[u.mat].np, u.mat, (short)tm, (short)tn});
         load[q] += u.cost;
       }
   }
   size_t longest = 0;
   for (const auto& q : queue) longest = std::max(longest, q.size());
-  std::vector<ListTile> table(8 * longest, ListTile{-1, 0, 0});
+  std::vector<ListTile> table(8 * longest, ListTile{});
   for (int q = 0; q < 8; ++q)
     for (size_t i = 0; i < queue[q].size(); ++i) table[8 * i + q] = queue[q][i];
   return table;
@@ -367,7 +370,7 @@ std::vector<ListTile> product_tiles(const std::vector<Matrix>& mats, const std::
         units.push_back(Unit{cost, i, a, std::min(a + 4, nm), b, std::min(b + 8, nn)});
       }
   }
-  return deal(std::move(units), symmetric);
+  return deal(mats, std::move(units), symmetric);
 }
 
 int product_tile(const std::vector<Matrix>& mats, const std::vector<int>& part, bool symmetric, bool two_terms) {
@@ -397,7 +400,9 @@ hipError_t allow_muon() {
   using S = Tile<N, TERMS == 2 ? 32 : 64>;
   hipError_t e = allow_lds(k_polar_symmetric<S, TERMS, false>, Product<S, false, KC, KC, TERMS, TERMS, WHOLE>::LDS_BYTES);
   if (e == hipSuccess) e = allow_lds(k_polar_symmetric<S, TERMS, true>, Product<S, false, KC, KC, TERMS, TERMS, WHOLE>::LDS_BYTES);
-  if (e == hipSuccess) e = allow_lds(k_polar_apply<Tile<N, 32>, TERMS>, Product<Tile<N, 32>, false, KC, KS, TERMS, 2, WHOLE>::LDS_BYTES);
+  const int bytes = Product<Tile<N, 32>, false, KC, KS, TERMS, 2, WHOLE>::LDS_BYTES;
+  if (e == hipSuccess) e = allow_lds(k_polar_apply<Tile<N, 32>, TERMS, false>, bytes);
+  if (e == hipSuccess) e = allow_lds(k_polar_apply<Tile<N, 32>, TERMS, true>, bytes);
   return e;
 }
 
@@ -410,11 +415,12 @@ void symmetric(const Part& part, const SymmetricArgs& a, int products, hipStream
   });
 }
 template <int TERMS>
-void apply(const Part& part, const ApplyArgs& a, hipStream_t s) {
+void apply(const Part& part, const ApplyArgs& a, bool last, hipStream_t s) {
   with_tile(part.apply_tile, [&](auto n) {
     using S = Tile<n, 32>;
     using P = Product<S, false, KC, KS, TERMS, 2, WHOLE>;
-    hipLaunchKernelGGL((k_polar_apply<S, TERMS>), dim3(part.grid[APPLY]), dim3(S::NT), P::LDS_BYTES, s, a);
+    if (last) hipLaunchKernelGGL((k_polar_apply<S, TERMS, true>), dim3(part.grid[APPLY]), dim3(S::NT), P::LDS_BYTES, s, a);
+    else hipLaunchKernelGGL((k_polar_apply<S, TERMS, false>), dim3(part.grid[APPLY]), dim3(S::NT), P::LDS_BYTES, s, a);
   });
 }
 
@@ -431,21 +437,13 @@ int steps_from(const ob_muon_ctx* ctx, int k) {
   return k - first;
 }
 
-// The buffer of X that holds the result, given that X[0] holds the start
-int last_buffer(const ob_muon_ctx* ctx, const Part& part) {
-  if (!part.follow_s) return ctx->steps & 1;
-  int cur = 0;
-  for (int k = 0; k < ctx->steps; k += steps_from(ctx, k)) cur ^= 1;
-  return cur;
-}
-
-void follow_s(ob_muon_ctx* ctx, const Part& part, hipStream_t stream) {
+void follow_s(ob_muon_ctx* ctx, const Part& part, const Finish& finish, hipStream_t stream) {
   uint16_t* const S = ctx->d_e[0];
   uint16_t* const Y = ctx->d_e[2];
   int cur = 0;
   for (int first = 0, n; first < ctx->steps; first += n) {
     n = steps_from(ctx, first);
-    SymmetricArgs g{part.d_tiles[GRAM], ctx->d_mats, ctx->d_x[cur], {}, nullptr, {S}, ctx->x_plane, ctx->e_plane, {S_UNIT / (X_UNIT * X_UNIT)}, 0.0f, 0.0f};
+    SymmetricArgs g{part.d_tiles[GRAM], ctx->d_x[cur], {}, nullptr, {S}, ctx->x_plane, ctx->e_plane, {S_UNIT / (X_UNIT * X_UNIT)}, 0.0f, 0.0f};
     symmetric<2, true>(part, g, 1, stream);
     double most = 1.0;      // what Q's elements can come to
     for (int k = first; k < first + n; ++k)
@@ -458,9 +456,9 @@ void follow_s(ob_muon_ctx* ctx, const Part& part, hipStream_t stream) {
       // the first B is Q; it is kept in Q's unit
       uint16_t* const B = start ? q : ctx->d_e[1];
       const float unit = start ? q_unit : E_UNIT;
-      symmetric<2, false>(part, SymmetricArgs{part.d_tiles[SYMMETRIC], ctx->d_mats, S, {S}, S, {B}, 0, ctx->e_plane, {c * unit / (S_UNIT * S_UNIT)}, b * unit / S_UNIT, a * unit},
+      symmetric<2, false>(part, SymmetricArgs{part.d_tiles[SYMMETRIC], S, {S}, S, {B}, 0, ctx->e_plane, {c * unit / (S_UNIT * S_UNIT)}, b * unit / S_UNIT, a * unit},
                           1, stream);
-      SymmetricArgs p{part.d_tiles[SYMMETRIC], ctx->d_mats, B, {}, nullptr, {}, 0, ctx->e_plane, {}, 0.0f, 0.0f};
+      SymmetricArgs p{part.d_tiles[SYMMETRIC], B, {}, nullptr, {}, 0, ctx->e_plane, {}, 0.0f, 0.0f};
       int products = 0;
       if (!end) {
         p.b[products] = S;
@@ -475,20 +473,22 @@ void follow_s(ob_muon_ctx* ctx, const Part& part, hipStream_t stream) {
         q = next;
       }
       if (products) symmetric<2, false>(part, p, products, stream);
-      if (!end) symmetric<2, false>(part, SymmetricArgs{part.d_tiles[SYMMETRIC], ctx->d_mats, Y, {B}, nullptr, {S}, 0, ctx->e_plane, {1.0f / unit}, 0.0f, 0.0f}, 1, stream);
+      if (!end) symmetric<2, false>(part, SymmetricArgs{part.d_tiles[SYMMETRIC], Y, {B}, nullptr, {S}, 0, ctx->e_plane, {1.0f / unit}, 0.0f, 0.0f}, 1, stream);
     }
-    apply<2>(part, ApplyArgs{part.d_tiles[APPLY], ctx->d_mats, q, ctx->d_x[cur], ctx->d_x[cur ^ 1], ctx->e_plane, ctx->x_plane, 1.0f / q_unit}, stream);
+    apply<2>(part, ApplyArgs{part.d_tiles[APPLY], ctx->d_mats, q, ctx->d_x[cur], ctx->d_x[cur ^ 1], ctx->e_plane, ctx->x_plane, 1.0f / q_unit, finish},
+             first + n == ctx->steps, stream);
     cur ^= 1;
   }
 }
 
-void step_by_step(ob_muon_ctx* ctx, const Part& part, hipStream_t stream) {
+template <int TERMS>
+void step_by_step(ob_muon_ctx* ctx, const Part& part, const Finish& finish, hipStream_t stream) {
   uint16_t* const E = ctx->d_e[0];
   uint16_t* const B = ctx->d_e[1];
   for (int k = 0; k < ctx->steps; ++k) {
     const float a = ctx->coefficients[3 * k], b = ctx->coefficients[3 * k + 1], c = ctx->coefficients[3 * k + 2];
     const float per_gram = E_UNIT / (X_UNIT * X_UNIT);
-    SymmetricArgs g{part.d_tiles[GRAM], ctx->d_mats, ctx->d_x[k & 1], {}, nullptr, {E}, ctx->x_plane, ctx->e_plane, {per_gram}, 0.0f, 0.0f};
+    SymmetricArgs g{part.d_tiles[GRAM], ctx->d_x[k & 1], {}, nullptr, {E}, ctx->x_plane, ctx->e_plane, {per_gram}, 0.0f, 0.0f};
     if (c != 0.0f) {
       g.diag = b / (2.0f * c) * E_UNIT;
     } else {      // B = a + b S from the first product alone
@@ -496,26 +496,49 @@ void step_by_step(ob_muon_ctx* ctx, const Part& part, hipStream_t stream) {
       g.mul[0] = b * per_gram;
       g.diag = a * E_UNIT;
     }
-    symmetric<1, true>(part, g, 1, stream);
+    symmetric<TERMS, true>(part, g, 1, stream);
     if (c != 0.0f) {
       const float d = (float)(((double)a - (double)b * b / (4.0 * c)) * E_UNIT);
-      symmetric<1, false>(part, SymmetricArgs{part.d_tiles[SYMMETRIC], ctx->d_mats, E, {E}, nullptr, {B}, 0, ctx->e_plane, {c / E_UNIT}, 0.0f, d}, 1, stream);
+      symmetric<TERMS, false>(part, SymmetricArgs{part.d_tiles[SYMMETRIC], E, {E}, nullptr, {B}, 0, ctx->e_plane, {c / E_UNIT}, 0.0f, d}, 1, stream);
     }
-    apply<1>(part, ApplyArgs{part.d_tiles[APPLY], ctx->d_mats, B, ctx->d_x[k & 1], ctx->d_x[(k & 1) ^ 1], ctx->e_plane, ctx->x_plane, 1.0f / E_UNIT}, stream);
+    apply<TERMS>(part, ApplyArgs{part.d_tiles[APPLY], ctx->d_mats, B, ctx->d_x[k & 1], ctx->d_x[(k & 1) ^ 1], ctx->e_plane, ctx->x_plane, 1.0f / E_UNIT, finish},
+                 k + 1 == ctx->steps, stream);
   }
 }
 
-// u -> the working X, its Newton-Schulz steps, and the finishing pass
+// u -> the working X, and its Newton-Schulz steps, the last of which ends in `finish`
 ob_status run_list(ob_muon_ctx* ctx, Direction d, float* m_out, const Finish& finish, hipStream_t s) {
   hipLaunchKernelGGL(k_muon_moments, dim3(ctx->square_tiles), dim3(BLOCK), 0, s, ctx->d_square, ctx->d_mats, d, m_out, ctx->d_sums);
-  hipLaunchKernelGGL(k_muon_norms, dim3(ctx->mats), dim3(BLOCK), 0, s, ctx->d_mats, ctx->d_sums, ctx->eps, ctx->d_inv);
-  hipLaunchKernelGGL(k_muon_pack, dim3(ctx->square_tiles), dim3(BLOCK), 0, s, ctx->d_square, ctx->d_mats, d, ctx->d_inv, ctx->d_x[0], ctx->x_plane);
+  if (ctx->norms) hipLaunchKernelGGL(k_muon_norms, dim3(ctx->mats), dim3(BLOCK), 0, s, ctx->d_mats, ctx->d_sums, ctx->eps, ctx->d_inv);
+  hipLaunchKernelGGL(k_muon_pack, dim3(ctx->square_tiles), dim3(BLOCK), 0, s, ctx->d_square, ctx->d_mats, d, ctx->norms ? ctx->d_inv : nullptr,
+                     ctx->d_sums, ctx->eps, ctx->d_x[0], ctx->x_plane);
   for (const Part& part : ctx->parts) {
-    if (part.follow_s) follow_s(ctx, part, s);
-    else step_by_step(ctx, part, s);
+    if (part.follow_s) follow_s(ctx, part, finish, s);
+    else if (part.terms == 2) step_by_step<2>(ctx, part, finish, s);
+    else step_by_step<1>(ctx, part, finish, s);
   }
-  hipLaunchKernelGGL(k_muon_finish, dim3(ctx->square_tiles), dim3(BLOCK), 0, s, ctx->d_square, ctx->d_mats, ctx->d_x[0], ctx->d_x[1], ctx->x_plane, finish);
   return hip_ok(ctx, hipGetLastError(), "the orthogonaliser's kernels") ? OB_OK : OB_ERR_HIP;
+}
+
+// Whether following S takes less than going step by step, both with 22 bits, by the tiles' times and LAUNCH a launch
+bool following_pays(const ob_muon_ctx* ctx, const std::vector<Matrix>& mats, const std::vector<int>& list, const Part& part) {
+  constexpr double LAUNCH = 3.0;      // us, from the end of one kernel to the start of the next one's loads
+  double depth[3] = {}, out[3] = {};
+  for (const int i : list)
+    for (const ProductKind k : {GRAM, SYMMETRIC, APPLY}) {
+      const double n = k == APPLY ? (double)mats[i].mp * mats[i].np : 0.5 * mats[i].mp * mats[i].mp;
+      out[k] += n;
+      depth[k] += n * (k == GRAM ? mats[i].np : mats[i].mp);
+    }
+  double t[3];
+  for (const ProductKind k : {GRAM, SYMMETRIC, APPLY})
+    t[k] = LAUNCH + tiles_time(k == APPLY ? part.apply_tile : part.sym_tile, part.grid[k], 3.0 * depth[k] / out[k]);
+  double followed = 0;
+  for (int k = 0, n; k < ctx->steps; k += n) {
+    n = steps_from(ctx, k);
+    followed += t[GRAM] + t[APPLY] + t[SYMMETRIC] * (n + (n - 1)) + (t[SYMMETRIC] - LAUNCH) * 2 * (n - 1) + LAUNCH * n;
+  }
+  return followed < ctx->steps * (t[GRAM] + t[SYMMETRIC] + t[APPLY]);
 }
 
 ob_status create(const ob_muon_config* cfg, ob_muon_ctx* ctx) {
@@ -557,9 +580,8 @@ ob_status create(const ob_muon_config* cfg, ob_muon_ctx* ctx) {
     mats.push_back(m);
   }
   if (mats.empty()) return OB_ERR_ARG;
-  // The 11-bit way costs 12.5 n / m + 2.5 (in m^3, 5 steps), the 22-bit one three times 1.5 n / m + 8.5 (with one S, which
-  // will do here): less from n = 3 m on.
-  // That is worth launches of its own where there is much of it.
+  // 11 bits, step by step: 12.5 n / m + 2.5 (in m^3, 5 steps); 22 bits, following S with one S, which will do there: three
+  // times 1.5 n / m + 8.5, less from n = 3 m on, which is worth launches of its own where there is much of it.
   std::vector<int> each[2];
   double narrow = 0;
   for (size_t i = 0; i < mats.size(); ++i) {
@@ -575,7 +597,7 @@ ob_status create(const ob_muon_config* cfg, ob_muon_ctx* ctx) {
   for (const int f : {1, 0}) {
     if (each[f].empty()) continue;
     Part part;
-    part.follow_s = f == 1;
+    part.terms = f ? 2 : 1;
     part.sym_tile = product_tile(mats, each[f], true, f == 1);
     part.apply_tile = product_tile(mats, each[f], false, f == 1);
     for (const ProductKind k : {GRAM, SYMMETRIC, APPLY}) {
@@ -583,8 +605,8 @@ ob_status create(const ob_muon_config* cfg, ob_muon_ctx* ctx) {
       if (tables[f][k].size() > 0x7fffffff) return OB_ERR_SIZE;
       part.grid[k] = (int)tables[f][k].size();
     }
-    const int last = last_buffer(ctx, part);
-    for (const int i : each[f]) mats[i].last = last;
+    // With 22 bits following S takes fewer multiply-adds for n > m, but a launch more for every step but the first of each S
+    part.follow_s = f == 1 && (cfg->precision == OB_F16 || following_pays(ctx, mats, each[1], part));
     ctx->parts.push_back(part);
   }
   for (int kind = 0; kind < KINDS; ++kind) {
@@ -593,6 +615,7 @@ ob_status create(const ob_muon_config* cfg, ob_muon_ctx* ctx) {
     if (!hip_ok(ctx, e, "hipFuncSetAttribute")) return OB_ERR_HIP;
   }
   ctx->mats = (int)mats.size();
+  for (const Matrix& m : mats) ctx->norms = ctx->norms || m.tiles > 64;
   ctx->square_tiles = (int)square.size();
   ctx->x_plane = xs;
   ctx->e_plane = es;
@@ -624,8 +647,8 @@ ob_status create(const ob_muon_config* cfg, ob_muon_ctx* ctx) {
                   hip_ok(ctx, hipMemcpy(ctx->d_square, square.data(), square.size() * sizeof(SquareTile), hipMemcpyHostToDevice), "hipMemcpy");
   for (Part& part : ctx->parts)
     for (const int k : {0, 1, 2}) {
-      const std::vector<ListTile>& table = tables[part.follow_s][k];
-      part.d_tiles[k] = reinterpret_cast<ListTile*>(base + at_table[part.follow_s][k]);
+      const std::vector<ListTile>& table = tables[part.terms == 2][k];
+      part.d_tiles[k] = reinterpret_cast<ListTile*>(base + at_table[part.terms == 2][k]);
       ok = ok && hip_ok(ctx, hipMemcpy(part.d_tiles[k], table.data(), table.size() * sizeof(ListTile), hipMemcpyHostToDevice), "hipMemcpy");
     }
   return ok ? OB_OK : OB_ERR_HIP;

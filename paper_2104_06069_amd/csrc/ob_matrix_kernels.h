@@ -1,6 +1,8 @@
 // Kernels of the matrix operators (include/ob_matrix.h), on the tiles of ob_mm.h.  Included by ob_matrix.hip only.
 #pragma once
 
+#include <type_traits>
+
 #include "ob_mm.h"
 
 namespace obm {
@@ -165,7 +167,7 @@ __device__ __forceinline__ void rows_tile(const RowsArgs& p, const RowTile& t, i
   const Operand a{p.a + t.lo * p.lda, 0, p.lda, t.rows, p.a_direct};
   const Operand b{p.w + t.g * p.w_stride, 0, p.ldw, p.width, p.w_direct};
   P::run(a, b, r0, c0, 0, p.depth, lds_of_launch, acc);
-  Results<S>::visit(acc, lds_of_launch, [&](int r, int c, v4f v) {
+  Results<S>::by_rows(acc, lds_of_launch, [&](int r, int c, v4f v) {
     r += r0;
     c += c0;
     if (r < t.rows) store4(p.out, p.out_dtype, (t.lo + r) * p.ldo + c, p.width - c, v);
@@ -321,7 +323,7 @@ __global__ __launch_bounds__(S::NT, 2) void k_experts_weights(WeightsArgs p) {
   } else if (p.accumulate) {
     return;
   }
-  Results<S>::visit(acc, lds_of_launch, [&](int r, int c, v4f v) {
+  Results<S>::by_rows(acc, lds_of_launch, [&](int r, int c, v4f v) {
     r += tm * S::BM;
     c += tn * S::BN;
     if (r >= p.height) return;
@@ -339,7 +341,6 @@ struct Matrix {
   int64_t x, e;        // in a plane of X, and of a [mp, mp] matrix
   int rows, cols, mp, np;
   int tall;            // more rows than columns: X is the transpose
-  int last;            // which of the two X buffers holds the result
   int tile0, tiles;    // its element-wise tiles
   float scale;
 };
@@ -348,8 +349,9 @@ struct Matrix {
 // S's 1 / m at first.
 constexpr float X_UNIT = 4096.0f, S_UNIT = 4096.0f, E_UNIT = 256.0f;
 
-struct ListTile {      // of a product; mat < 0: none
-  int mat;
+struct ListTile {      // of a product, with what it needs of its matrix; mp == 0: none
+  int64_t x, e;
+  int mp, np, mat;
   short tm, tn;
 };
 
@@ -388,7 +390,6 @@ __device__ __forceinline__ void store_terms(uint16_t* plane, int64_t term, int64
 // diag on the diagonal.
 struct SymmetricArgs {
   const ListTile* tiles;
-  const Matrix* mats;
   const uint16_t* a;           // X, or [mp, mp]
   const uint16_t* b[2];
   const uint16_t* add;         // NULL: none; else added to the first
@@ -399,56 +400,65 @@ struct SymmetricArgs {
 template <class S, int TERMS, bool FROM_X>
 __global__ __launch_bounds__(S::NT, 2) void k_polar_symmetric(SymmetricArgs p) {
   using P = Product<S, false, KC, KC, TERMS, TERMS, WHOLE>;
+  using R = Results<S>;
   const ListTile t = p.tiles[blockIdx.x];
-  if (t.mat < 0) return;
-  const Matrix& m = p.mats[t.mat];
-  const int mp = m.mp, which = blockIdx.y;
+  if (t.mp == 0) return;
+  const int mp = t.mp, which = blockIdx.y;
   typename P::Acc acc = {};
-  const int r0 = t.tm * S::BM, c0 = t.tn * S::BN;
+  const int tr = t.tm * S::BM, tc = t.tn * S::BN;
   if constexpr (FROM_X) {
-    const Operand x{p.a + m.x, p.x_term, m.np, mp, true};
-    P::run(x, x, r0, c0, 0, m.np, lds_of_launch, acc);
+    const Operand x{p.a + t.x, p.x_term, t.np, mp, true};
+    P::run(x, x, tr, tc, 0, t.np, lds_of_launch, acc);
   } else {
-    const Operand a{p.a + m.e, p.term, mp, mp, true}, b{p.b[which] + m.e, p.term, mp, mp, true};
-    P::run(a, b, r0, c0, 0, mp, lds_of_launch, acc);
+    const Operand a{p.a + t.e, p.term, mp, mp, true}, b{p.b[which] + t.e, p.term, mp, mp, true};
+    P::run(a, b, tr, tc, 0, mp, lds_of_launch, acc);
   }
-  uint16_t* const out = p.out[which] + m.e;
-  const uint16_t* const add = which == 0 && p.add ? p.add + m.e : nullptr;
-  const float mul = p.mul[which];
-  const auto finish = [&](int r, int c, v4f v, int dr, int dc) {      // v[e] is element (r + e dr, c + e dc)
-    const int64_t at = dc ? (int64_t)r * mp + c : (int64_t)c * mp + r;      // (ADD is symmetric)
-    v *= mul;
-    if (add) {
-      const v4h hi = *reinterpret_cast<const v4h*>(add + at);
-      v4h lo = {};
-      if constexpr (TERMS == 2) lo = *reinterpret_cast<const v4h*>(add + p.term + at);
+  uint16_t* const out = p.out[which] + t.e;
+  const uint16_t* const add = which == 0 && p.add ? p.add + t.e : nullptr;
+  const float mul = p.mul[which], diag = which == 0 ? p.diag : 0.0f;
+  // Element (r + e dr, c + e dc) is element e of the four from (r, c) on; all of them lie in a row of `out` (and of ADD), turned over
+  // the diagonal where dr is 1.
+  const auto half = [&](const float* own, int r0, int c0, auto rowwise) {
+    constexpr int dr = rowwise ? 0 : 1, dc = rowwise ? 1 : 0;
+    const auto at = [&](int r, int c) { return rowwise ? (int64_t)(tr + r) * mp + tc + c : (int64_t)(tc + c) * mp + tr + r; };
+    const auto inside = [&](int r, int c) { return tr + r < mp && tc + c < mp; };
+    R::template pass<rowwise>(
+        own, r0, c0,
+        [&](int r, int c) {
+          v4f v = {};
+          if (add && inside(r, c)) {
+            const v4h hi = *reinterpret_cast<const v4h*>(add + at(r, c));
+            v4h lo = {};
+            if constexpr (TERMS == 2) lo = *reinterpret_cast<const v4h*>(add + p.term + at(r, c));
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] += p.add_mul * (from_bits(hi[e], false) + from_bits(lo[e], false));
-    }
-    if (which == 0) {
+            for (int e = 0; e < 4; ++e) v[e] = p.add_mul * (from_bits(hi[e], false) + from_bits(lo[e], false));
+          }
+          return v;
+        },
+        [&](int r, int c, v4f v, v4f w) {
+          if (!inside(r, c)) return;
+          v = v * mul + w;
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (r + e * dr == c + e * dc) v[e] += p.diag;
-    }
-    store_terms<TERMS>(out, p.term, at, v);
+          for (int e = 0; e < 4; ++e)
+            if (tr + r + e * dr == tc + c + e * dc) v[e] += diag;
+          store_terms<TERMS>(out, p.term, at(r, c), v);
+        });
   };
-  const auto by_row = [&](int r, int c, v4f v) {
-    r += r0;
-    c += c0;
-    if (r < mp && c < mp) finish(r, c, v, 0, 1);
-  };
-  if (t.tm == t.tn) {
-    Results<S>::visit(acc, lds_of_launch, by_row);
-  } else {
-    Results<S>::template visit<true>(acc, lds_of_launch, by_row, [&](int r, int c, v4f v) {
-      r += r0;
-      c += c0;
-      if (r < mp && c < mp) finish(r, c, v, 1, 0);
-    });
-  }
+  R::visit(acc, lds_of_launch, [&](const float* own, int r0, int c0) {
+    half(own, r0, c0, std::true_type{});
+    if (t.tm != t.tn) half(own, r0, c0, std::false_type{});
+  });
 }
 
-// X' = mul B X
+// What becomes of the last X: out = X in the list's order (orthogonalize), or the update of the parameters.
+struct Finish {
+  float* x;                 // NULL: orthogonalize
+  void* out;                // x_lp (or NULL), or the orthogonaliser's output
+  int dtype;
+  float lr, keep;           // keep = 1 - lr * weight_decay
+};
+
+// X' = mul B X, or with LAST what becomes of it
 struct ApplyArgs {
   const ListTile* tiles;
   const Matrix* mats;
@@ -457,22 +467,57 @@ struct ApplyArgs {
   uint16_t* out;
   int64_t b_term, x_term;
   float mul;
+  Finish finish;
 };
-template <class S, int B_TERMS>
+template <class S, int B_TERMS, bool LAST>
 __global__ __launch_bounds__(S::NT, 2) void k_polar_apply(ApplyArgs p) {
   using P = Product<S, false, KC, KS, B_TERMS, 2, WHOLE>;
+  using R = Results<S>;
   const ListTile t = p.tiles[blockIdx.x];
-  if (t.mat < 0) return;
-  const Matrix& m = p.mats[t.mat];
+  if (t.mp == 0) return;
   typename P::Acc acc = {};
-  const Operand a{p.b + m.e, p.b_term, m.mp, m.mp, true}, b{p.x + m.x, p.x_term, m.np, m.np, true};
-  const int r0 = t.tm * S::BM, c0 = t.tn * S::BN;
-  P::run(a, b, r0, c0, 0, m.mp, lds_of_launch, acc);
-  Results<S>::visit(acc, lds_of_launch, [&](int r, int c, v4f v) {
-    r += r0;
-    c += c0;
-    if (r < m.mp && c < m.np) store_terms<2>(p.out + m.x, p.x_term, (int64_t)r * m.np + c, v * p.mul);
-  });
+  const Operand a{p.b + t.e, p.b_term, t.mp, t.mp, true}, b{p.x + t.x, p.x_term, t.np, t.np, true};
+  const int tr = t.tm * S::BM, tc = t.tn * S::BN;
+  P::run(a, b, tr, tc, 0, t.mp, lds_of_launch, acc);
+  if constexpr (!LAST) {
+    R::by_rows(acc, lds_of_launch, [&](int r, int c, v4f v) {
+      r += tr;
+      c += tc;
+      if (r < t.mp && c < t.np) store_terms<2>(p.out + t.x, p.x_term, (int64_t)r * t.np + c, v * p.mul);
+    });
+  } else {
+    const Matrix& m = p.mats[t.mat];
+    const int rows = m.rows, cols = m.cols;
+    const int64_t base = m.at;
+    const float step = p.finish.lr * m.scale, mul = p.mul * (1.0f / X_UNIT);
+    // A tall matrix's X is its transpose: what is a column there is part of a row of the list's matrix.
+    const auto rows_of = [&](const float* own, int r0, int c0, auto rowwise) {
+      const auto row = [&](int r, int c) { return rowwise ? tr + r : tc + c; };
+      const auto col = [&](int r, int c) { return rowwise ? tc + c : tr + r; };
+      R::template pass<rowwise>(
+          own, r0, c0,
+          [&](int r, int c) {
+            if (!p.finish.x || row(r, c) >= rows) return v4f{};
+            return load4(p.finish.x, F32, base + (int64_t)row(r, c) * cols + col(r, c), cols - col(r, c));
+          },
+          [&](int r, int c, v4f v, v4f x) {
+            if (row(r, c) >= rows) return;
+            const int64_t at = base + (int64_t)row(r, c) * cols + col(r, c);
+            const int left = cols - col(r, c);
+            v4f o = v * mul;
+            if (p.finish.x) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[e] = x[e] * p.finish.keep - step * o[e];
+              store4(p.finish.x, F32, at, left, o);
+            }
+            if (p.finish.out) store4(p.finish.out, p.finish.dtype, at, left, o);
+          });
+    };
+    R::visit(acc, lds_of_launch, [&](const float* own, int r0, int c0) {
+      if (m.tall) rows_of(own, r0, c0, std::false_type{});
+      else rows_of(own, r0, c0, std::true_type{});
+    });
+  }
 }
 
 // Element-wise tiles are SIDE x SIDE elements of a matrix in the list's order, padding included; a thread has four
@@ -529,9 +574,8 @@ __global__ __launch_bounds__(BLOCK) void k_muon_moments(const SquareTile* tiles,
   if (threadIdx.x == 0) sums[blockIdx.x] = (part[0] + part[1]) + (part[2] + part[3]);
 }
 
-// X_UNIT / (norm + eps) of each matrix
-__global__ __launch_bounds__(BLOCK) void k_muon_norms(const Matrix* mats, const double* sums, float eps, float* inv) {
-  const Matrix& m = mats[blockIdx.x];
+// X_UNIT / (norm + eps) of a matrix, in every thread of a workgroup
+__device__ __forceinline__ float inverse_norm(const Matrix& m, const double* sums, float eps) {
   double s = 0.0;
   for (int i = threadIdx.x; i < m.tiles; i += BLOCK) s += sums[m.tile0 + i];
   __shared__ double part[BLOCK / 64];
@@ -539,15 +583,21 @@ __global__ __launch_bounds__(BLOCK) void k_muon_norms(const Matrix* mats, const 
   for (int k = 32; k; k >>= 1) s += __shfl_xor(s, k);
   if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
   __syncthreads();
-  if (threadIdx.x == 0) inv[blockIdx.x] = (float)((double)X_UNIT / (sqrt((part[0] + part[1]) + (part[2] + part[3])) + (double)eps));
+  return (float)((double)X_UNIT / (sqrt((part[0] + part[1]) + (part[2] + part[3])) + (double)eps));
+}
+__global__ __launch_bounds__(BLOCK) void k_muon_norms(const Matrix* mats, const double* sums, float eps, float* inv) {
+  const float f = inverse_norm(mats[blockIdx.x], sums, eps);
+  if (threadIdx.x == 0) inv[blockIdx.x] = f;
 }
 
-// X = u / (norm + eps), transposed for tall matrices, zeros around it.
-__global__ __launch_bounds__(BLOCK) void k_muon_pack(const SquareTile* tiles, const Matrix* mats, Direction d, const float* inv, uint16_t* x, int64_t term) {
+// X = u / (norm + eps), transposed for tall matrices, zeros around it.  inv == NULL: every workgroup adds up its matrix's sums
+// itself, which for matrices of few tiles takes less than a launch.
+__global__ __launch_bounds__(BLOCK) void k_muon_pack(const SquareTile* tiles, const Matrix* mats, Direction d, const float* inv, const double* sums,
+                                                     float eps, uint16_t* x, int64_t term) {
   __shared__ float turned[SIDE][SIDE + 1];
   const SquareTile t = tiles[blockIdx.x];
   const Matrix& mat = mats[t.mat];
-  const float f = inv[t.mat];
+  const float f = inv ? inv[t.mat] : inverse_norm(mat, sums, eps);
 #pragma unroll
   for (int j = 0; j < SIDE / 16; ++j) {
     const int y = threadIdx.x / 16 + 16 * j, z = threadIdx.x % 16 * 4, r = t.row0 + y, c = t.col0 + z;
@@ -576,55 +626,6 @@ __global__ __launch_bounds__(BLOCK) void k_muon_pack(const SquareTile* tiles, co
     const int y = threadIdx.x / 16 + 16 * j, z = threadIdx.x % 16 * 4;
     const v4f v = {turned[y][z], turned[y][z + 1], turned[y][z + 2], turned[y][z + 3]};
     store_terms<2>(x + mat.x, term, (int64_t)(t.col0 + y) * mat.np + t.row0 + z, v);
-  }
-}
-
-// Either out = X in the list's order (orthogonalize), or the update of the parameters.
-struct Finish {
-  float* x;                 // NULL: orthogonalize
-  void* out;                // x_lp (or NULL), or the orthogonaliser's output
-  int dtype;
-  float lr, keep;           // keep = 1 - lr * weight_decay
-};
-__global__ __launch_bounds__(BLOCK) void k_muon_finish(const SquareTile* tiles, const Matrix* mats, const uint16_t* x0, const uint16_t* x1, int64_t term, Finish p) {
-  __shared__ float turned[SIDE][SIDE + 1];
-  const SquareTile t = tiles[blockIdx.x];
-  const Matrix& mat = mats[t.mat];
-  const uint16_t* const work = mat.last ? x1 : x0;
-  auto load = [&](int64_t at) {
-    const v4h hi = *reinterpret_cast<const v4h*>(work + mat.x + at), lo = *reinterpret_cast<const v4h*>(work + mat.x + term + at);
-    v4f v;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = (from_bits(hi[e], false) + from_bits(lo[e], false)) * (1.0f / X_UNIT);
-    return v;
-  };
-  if (mat.tall) {
-#pragma unroll
-    for (int j = 0; j < SIDE / 16; ++j) {
-      const int y = threadIdx.x / 16 + 16 * j, z = threadIdx.x % 16 * 4;
-      const v4f v = load((int64_t)(t.col0 + y) * mat.np + t.row0 + z);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) turned[z + e][y] = v[e];
-    }
-    __syncthreads();
-  }
-  const float step = p.lr * mat.scale;
-#pragma unroll
-  for (int j = 0; j < SIDE / 16; ++j) {
-    const int y = threadIdx.x / 16 + 16 * j, z = threadIdx.x % 16 * 4, r = t.row0 + y, c = t.col0 + z;
-    if (r >= mat.rows || c >= mat.cols) continue;
-    v4f o;
-    if (mat.tall) o = v4f{turned[y][z], turned[y][z + 1], turned[y][z + 2], turned[y][z + 3]};
-    else o = load((int64_t)r * mat.np + c);
-    const int64_t at = mat.at + (int64_t)r * mat.cols + c;
-    const int left = mat.cols - c;
-    if (p.x) {
-      const v4f x = load4(p.x, F32, at, left);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] = x[e] * p.keep - step * o[e];
-      store4(p.x, F32, at, left, o);
-    }
-    if (p.out) store4(p.out, p.dtype, at, left, o);
   }
 }
 

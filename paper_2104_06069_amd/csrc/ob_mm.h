@@ -175,13 +175,16 @@ __device__ __forceinline__ void loads_left() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(n) : "memory");
 }
 
-// STAGES: slabs in LDS at once.  Eight wavefronts (two on each SIMD) take turns as described above, with two slabs; fewer
-// do not wait for each other in between: the loads of STAGES - 1 slabs are under way, and what one workgroup leaves idle
-// another one on the CU uses.
-template <int BM_, int BN_, int BK_, int WM_, int WN_, int STAGES_ = 2>
+// WM x WN wavefronts share out a tile.  STAGES: slabs in LDS at once.  Eight (two on each SIMD) take turns as described above,
+// with two slabs; fewer do not wait for each other in between: the loads of STAGES - 1 slabs are under way, and what one workgroup
+// leaves idle another one on the CU uses.  With two TEAMS the tile has twice as many wavefronts, and each team half the columns of
+// each slab: for tiles that have a CU to themselves, where every read of LDS is waited for.
+template <int BM_, int BN_, int BK_, int WM_, int WN_, int STAGES_ = 2, int TEAMS_ = 1>
 struct Shape {
-  static constexpr int BM = BM_, BN = BN_, BK = BK_, WM = WM_, WN = WN_, WAVES = WM * WN, NT = WAVES * 64, STAGES = STAGES_;
+  static constexpr int BM = BM_, BN = BN_, BK = BK_, WM = WM_, WN = WN_, STAGES = STAGES_, TEAMS = TEAMS_;
+  static constexpr int WAVES = WM * WN, NT = WAVES * TEAMS * 64;
   static constexpr bool TURNS = WAVES == 8;
+  static_assert(TEAMS == 1 || (!TURNS && BK / 32 % TEAMS == 0), "whole steps of 32 columns for each team");
   static_assert(!TURNS || STAGES == 2, "two slabs");
   static constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
 };
@@ -194,11 +197,44 @@ struct Results {
   static constexpr int STRIDE = WIDTH + 4;        // floats: rows four banks apart
   static constexpr int LDS_BYTES = S::WAVES * ROWS * STRIDE * 4;
 
-  // Calls by_row(row, column, values of four adjacent columns), and with MIRROR by_column(row, column, values of four adjacent
-  // rows), for all of the tile.  To be called after Product::run, whose last barrier ends the reads of LDS.
-  template <bool MIRROR, class F, class G>
-  __device__ static __forceinline__ void visit(const v4f (&acc)[S::FM][S::FN], uint16_t* lds, F by_row, G by_column) {
+  // For four adjacent columns of a row at a time (ROWWISE), or four adjacent rows of a column: calls before(row, column), for
+  // what has to be read beside them, and then after(row, column, values, what before() gave).
+  template <bool ROWWISE, class F, class G>
+  __device__ static __forceinline__ void pass(const float* own, int r0, int c0, F before, G after) {
+    constexpr int EACH = ROWS * WIDTH / 256, BATCH = EACH < 4 ? EACH : 4;      // pieces a lane; how many are under way at once
+    const int lane = threadIdx.x & 63;
+#pragma unroll 1
+    for (int k0 = lane; k0 < EACH * 64; k0 += BATCH * 64) {
+      v4f v[BATCH], w[BATCH];
+#pragma unroll
+      for (int u = 0; u < BATCH; ++u) {
+        const int k = k0 + u * 64;
+        if constexpr (ROWWISE) {
+          const int r = k / (WIDTH / 4), c = k % (WIDTH / 4) * 4;
+          v[u] = *in_lds<const v4f>(own + r * STRIDE + c);
+          w[u] = before(r0 + r, c0 + c);
+        } else {
+          const int c = k / (ROWS / 4), r = k % (ROWS / 4) * 4;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[u][e] = *in_lds<const float>(own + (r + e) * STRIDE + c);
+          w[u] = before(r0 + r, c0 + c);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < BATCH; ++u) {
+        const int k = k0 + u * 64;
+        if constexpr (ROWWISE) after(r0 + k / (WIDTH / 4), c0 + k % (WIDTH / 4) * 4, v[u], w[u]);
+        else after(r0 + k % (ROWS / 4) * 4, c0 + k / (ROWS / 4), v[u], w[u]);
+      }
+    }
+  }
+
+  // by(own, r0, c0): what to do with `own`, the rows r0 .. and columns c0 .. of the tile that this wavefront has turned (see
+  // pass()).  To be called after Product::run, whose last barrier ends the reads of LDS.
+  template <class F>
+  __device__ static __forceinline__ void visit(const v4f (&acc)[S::FM][S::FN], uint16_t* lds, F by) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (S::TEAMS > 1 && wave >= S::WAVES) return;      // (the first team has the sums)
     const int r0 = wave / S::WN * (S::BM / S::WM), c0 = wave % S::WN * WIDTH;
     float* const own = reinterpret_cast<float*>(lds) + wave * ROWS * STRIDE;
 #pragma unroll
@@ -209,44 +245,16 @@ struct Results {
         for (int j = 0; j < S::FN; ++j)
           *in_lds<v4f>(own + (i * 16 + (lane & 15)) * STRIDE + j * 16 + 4 * (lane >> 4)) = acc[g * GROUP + i][j];
       lds_done();
-      constexpr int EACH = ROWS * WIDTH / 256, BATCH = EACH < 4 ? EACH : 4;      // pieces a lane; reads under way at once
-#pragma unroll 1
-      for (int k0 = lane; k0 < EACH * 64; k0 += BATCH * 64) {
-        v4f v[BATCH];
-#pragma unroll
-        for (int u = 0; u < BATCH; ++u) {
-          const int k = k0 + u * 64, r = k / (WIDTH / 4), c = k % (WIDTH / 4) * 4;
-          v[u] = *in_lds<const v4f>(own + r * STRIDE + c);
-        }
-#pragma unroll
-        for (int u = 0; u < BATCH; ++u) {
-          const int k = k0 + u * 64;
-          by_row(r0 + g * ROWS + k / (WIDTH / 4), c0 + k % (WIDTH / 4) * 4, v[u]);
-        }
-      }
-      if constexpr (MIRROR) {
-#pragma unroll 1
-        for (int k0 = lane; k0 < EACH * 64; k0 += BATCH * 64) {
-          v4f v[BATCH];
-#pragma unroll
-          for (int u = 0; u < BATCH; ++u) {
-            const int k = k0 + u * 64, c = k / (ROWS / 4), r = k % (ROWS / 4) * 4;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[u][e] = *in_lds<const float>(own + (r + e) * STRIDE + c);
-          }
-#pragma unroll
-          for (int u = 0; u < BATCH; ++u) {
-            const int k = k0 + u * 64;
-            by_column(r0 + g * ROWS + k % (ROWS / 4) * 4, c0 + k / (ROWS / 4), v[u]);
-          }
-        }
-      }
+      by(own, r0 + g * ROWS, c0);
       lds_done();
     }
   }
-  template <class F>
-  __device__ static __forceinline__ void visit(const v4f (&acc)[S::FM][S::FN], uint16_t* lds, F by_row) {
-    visit<false>(acc, lds, by_row, [](int, int, v4f) {});
+  // after(row, column, values of four adjacent columns) for all of the tile
+  template <class G>
+  __device__ static __forceinline__ void by_rows(const v4f (&acc)[S::FM][S::FN], uint16_t* lds, G after) {
+    visit(acc, lds, [&](const float* own, int r0, int c0) {
+      pass<true>(own, r0, c0, [](int, int) { return v4f{}; }, [&](int r, int c, v4f v, v4f) { after(r, c, v); });
+    });
   }
 };
 
@@ -269,7 +277,7 @@ struct Product {
   // K columns from k0 on; K >= 1.
   __device__ static void run(const Operand& a, const Operand& b, int r0, int c0, int k0, int K, uint16_t* lds, Acc& acc) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wm = wave / S::WN, wn = wave % S::WN;
+    const int team = wave / S::WAVES, wm = wave % S::WAVES / S::WN, wn = wave % S::WN;
     A sa;
     B sb;
     sa.init(a, r0, tid);
@@ -304,28 +312,52 @@ struct Product {
               for (int j = 0; j < FN; ++j) acc[i][j] = mma<BF>(fb[y][j], fa[x][i], acc[i][j]);
           }
     };
-    if constexpr (MODE == ANY) through_registers(a, b, r0, c0, k0, end, n, lds, read, multiply);
+    if constexpr (MODE == ANY) through_registers(a, b, r0, c0, k0, end, n, team, lds, read, multiply);
     else if constexpr (S::TURNS) turns(n, lds, acc, load, read, multiply);
-    else straight(n, wave, lds, acc, load, read, multiply);
+    else straight(n, wave, team, lds, load, read, multiply);
     if (MODE == TAIL && n * BK < K) {
       A::load_any(a, r0, k0 + n * BK, end, lds, tid);
       B::load_any(b, c0, k0 + n * BK, end, lds + TA * BM * BK, tid);
       lds_done();
       group_barrier();
+      steps(lds, team, read, multiply);
+      lds_done();
+      group_barrier();
+    }
+    if constexpr (S::TEAMS > 1) {      // the second team's sums to the first
+      static_assert(S::TEAMS == 2 && S::WAVES * FM * FN * 1024 <= LDS_BYTES, "room for them");
+      float* const at = reinterpret_cast<float*>(lds) + (wave % S::WAVES) * FM * FN * 256 + lane * 4;
 #pragma unroll
-      for (int kk = 0; kk < BK / 32; ++kk) {
-        v8s fa[TA][FM], fb[TB][FN];
-        read(lds, kk, fa, fb);
-        lds_done();
-        multiply(fa, fb);
-      }
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+          if (team) *in_lds<v4f>(at + (i * FN + j) * 256) = acc[i][j];
+      lds_done();
+      group_barrier();
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+          if (!team) acc[i][j] += *in_lds<const v4f>(at + (i * FN + j) * 256);
+      lds_done();
       group_barrier();
     }
   }
 
  private:
+  // A team's share of a slab
+  template <class R, class M>
+  __device__ static __forceinline__ void steps(const uint16_t* s, int team, R read, M multiply) {
+#pragma unroll
+    for (int k = 0; k < BK / 32 / S::TEAMS; ++k) {
+      v8s fa[TA][FM], fb[TB][FN];
+      read(s, k * S::TEAMS + team, fa, fb);
+      multiply(fa, fb);
+    }
+  }
+
   template <class L, class R, class M>
-  __device__ static __forceinline__ void straight(int n, int wave, uint16_t* lds, Acc& acc, L load, R read, M multiply) {
+  __device__ static __forceinline__ void straight(int n, int wave, int team, uint16_t* lds, L load, R read, M multiply) {
     constexpr int AHEAD = S::STAGES - 1;
     constexpr int NA = TA * A::PER, NB = TB * B::PER;      // loads of a slab, of the wavefronts that have such
     const bool la = wave < A::WORK / 64, lb = wave < B::WORK / 64;
@@ -340,20 +372,14 @@ struct Product {
       else lds_done();
       group_barrier();      // slab t is there, and nobody reads slab t - 1 any more
       if (t + AHEAD < n) load(t + AHEAD);
-      const uint16_t* const s = lds + t % S::STAGES * STAGE;
-#pragma unroll
-      for (int kk = 0; kk < BK / 32; ++kk) {
-        v8s fa[TA][FM], fb[TB][FN];
-        read(s, kk, fa, fb);
-        multiply(fa, fb);
-      }
+      steps(lds + t % S::STAGES * STAGE, team, read, multiply);
     }
     lds_done();
     group_barrier();
   }
 
   template <class R, class M>
-  __device__ static __forceinline__ void through_registers(const Operand& a, const Operand& b, int r0, int c0, int k0, int end, int n, uint16_t* lds,
+  __device__ static __forceinline__ void through_registers(const Operand& a, const Operand& b, int r0, int c0, int k0, int end, int n, int team, uint16_t* lds,
                                                            R read, M multiply) {
     const int tid = threadIdx.x;
     typename A::Fetched va;
@@ -371,12 +397,7 @@ struct Product {
         A::fetch(a, r0, k + BK, end, tid, va);
         B::fetch(b, c0, k + BK, end, tid, vb);
       }
-#pragma unroll
-      for (int kk = 0; kk < BK / 32; ++kk) {
-        v8s fa[TA][FM], fb[TB][FN];
-        read(s, kk, fa, fb);
-        multiply(fa, fb);
-      }
+      steps(s, team, read, multiply);
     }
     lds_done();
     group_barrier();
