@@ -311,6 +311,7 @@ struct ob_muon_ctx {
   int64_t n = 0;                        // elements of the flat buffers
   int mats = 0, square_tiles = 0;
   bool norms = false;                   // a launch of k_muon_norms
+  int small_lds = 0;                    // not 0: the whole list in k_polar_small, with this much LDS
   std::vector<Part> parts;
   int64_t x_plane = 0, e_plane = 0;     // elements
   void* mem = nullptr;
@@ -508,6 +509,12 @@ void step_by_step(ob_muon_ctx* ctx, const Part& part, const Finish& finish, hipS
 
 // u -> the working X, and its Newton-Schulz steps, the last of which ends in `finish`
 ob_status run_list(ob_muon_ctx* ctx, Direction d, float* m_out, const Finish& finish, hipStream_t s) {
+  if (ctx->small_lds) {
+    SmallArgs a{ctx->d_mats, d, m_out, finish, ctx->eps, ctx->steps, {}};
+    std::copy(ctx->coefficients.begin(), ctx->coefficients.end(), a.coefficients);
+    hipLaunchKernelGGL(k_polar_small, dim3(ctx->mats), dim3(SMALL_NT), ctx->small_lds, s, a);
+    return hip_ok(ctx, hipGetLastError(), "k_polar_small") ? OB_OK : OB_ERR_HIP;
+  }
   hipLaunchKernelGGL(k_muon_moments, dim3(ctx->square_tiles), dim3(BLOCK), 0, s, ctx->d_square, ctx->d_mats, d, m_out, ctx->d_sums);
   if (ctx->norms) hipLaunchKernelGGL(k_muon_norms, dim3(ctx->mats), dim3(BLOCK), 0, s, ctx->d_mats, ctx->d_sums, ctx->eps, ctx->d_inv);
   hipLaunchKernelGGL(k_muon_pack, dim3(ctx->square_tiles), dim3(BLOCK), 0, s, ctx->d_square, ctx->d_mats, d, ctx->norms ? ctx->d_inv : nullptr,
@@ -580,6 +587,17 @@ ob_status create(const ob_muon_config* cfg, ob_muon_ctx* ctx) {
     mats.push_back(m);
   }
   if (mats.empty()) return OB_ERR_ARG;
+  int largest_m = 0, largest_n = 0;
+  for (const Matrix& m : mats) {
+    largest_m = std::max(largest_m, m.mp);
+    largest_n = std::max(largest_n, m.np);
+  }
+  if (largest_m <= SMALL_M && largest_n <= SMALL_N) {
+    ctx->small_lds = (2 * SMALL_M * largest_n + 2 * SMALL_M * SMALL_M) * 2;
+    if (!hip_ok(ctx, allow_lds(k_polar_small, ctx->small_lds), "hipFuncSetAttribute")) return OB_ERR_HIP;
+    xs = es = 0;      // no working matrices outside of LDS
+    square.clear();
+  }
   // 11 bits, step by step: 12.5 n / m + 2.5 (in m^3, 5 steps); 22 bits, following S with one S, which will do there: three
   // times 1.5 n / m + 8.5, less from n = 3 m on, which is worth launches of its own where there is much of it.
   std::vector<int> each[2];
@@ -595,7 +613,7 @@ ob_status create(const ob_muon_config* cfg, ob_muon_ctx* ctx) {
   }
   std::vector<ListTile> tables[2][3];
   for (const int f : {1, 0}) {
-    if (each[f].empty()) continue;
+    if (each[f].empty() || ctx->small_lds) continue;
     Part part;
     part.terms = f ? 2 : 1;
     part.sym_tile = product_tile(mats, each[f], true, f == 1);

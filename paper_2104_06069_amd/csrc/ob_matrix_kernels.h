@@ -629,4 +629,228 @@ __global__ __launch_bounds__(BLOCK) void k_muon_pack(const SquareTile* tiles, co
   }
 }
 
+// A whole list of small matrices (m <= 64, n <= 512) in one launch, a workgroup each: X stays in LDS as two terms from the
+// gradient to the updated parameters, step by step with 22 bits (in both precisions: it is not the multiply-adds that
+// count here, but the fifteen products' latency).  TODO-SMALL
+constexpr int SMALL_M = 64, SMALL_N = 512, SMALL_NT = 512, MAX_STEPS = 64;
+struct SmallArgs {
+  const Matrix* mats;
+  Direction d;
+  float* m_out;
+  Finish finish;
+  float eps;
+  int steps;
+  float coefficients[3 * MAX_STEPS];
+};
+// X's and E's rows of LDS: 16-byte pieces, permuted by the row's number
+__device__ __forceinline__ int small_at(int r, int c, int ld) { return r * ld + ((((c >> 3) ^ (r & 7)) << 3) | (c & 7)); }
+
+__global__ __launch_bounds__(SMALL_NT, 2) void k_polar_small(SmallArgs p) {
+  __shared__ double part[SMALL_NT / 64];
+  const Matrix& mat = p.mats[blockIdx.x];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, q = lane >> 4;
+  const int rows = mat.rows, cols = mat.cols, np = mat.np;
+  const bool tall = mat.tall;
+  uint16_t* const X = lds_of_launch;                       // [2][SMALL_M][np]
+  uint16_t* const E = lds_of_launch + 2 * SMALL_M * np;    // [2][SMALL_M][SMALL_M]: E, then B
+  const int x_term = SMALL_M * np, e_term = SMALL_M * SMALL_M;
+
+  // u, its norm, and X
+  constexpr int PER = SMALL_M * SMALL_N / 4 / SMALL_NT;
+  const int row_pieces = (cols + 3) / 4, pieces = rows * row_pieces;
+  v4f u[PER];
+  double s = 0.0;
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    const int k = tid + j * SMALL_NT;
+    u[j] = v4f{};
+    if (k >= pieces) continue;
+    const int r = k / row_pieces, c = (k - r * row_pieces) * 4, left = cols - c;
+    const int64_t at = mat.at + (int64_t)r * cols + c;
+    v4f g = {}, m = {};
+    if (p.d.g) g = load4(p.d.g, p.d.dtype, at, left);
+    if (p.d.m) m = load4(p.d.m, F32, at, left);
+    if (p.d.m && p.d.g) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) m[e] = p.d.beta * m[e] + p.d.omb * (p.d.scale * g[e]);
+      store4(p.m_out, F32, at, left, m);
+    }
+    u[j] = direction4(p.d, g, m);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (e >= left) u[j][e] = 0.0f;
+      s += (double)u[j][e] * (double)u[j][e];
+    }
+  }
+  for (int k = tid; k < SMALL_M * np / 4; k += SMALL_NT) *in_lds<v8s>(X + 8 * k) = v8s{};      // both planes, padding included
+#pragma unroll
+  for (int k = 32; k; k >>= 1) s += __shfl_xor(s, k);
+  if (lane == 0) part[wave] = s;
+  __syncthreads();
+  s = 0.0;
+#pragma unroll
+  for (int k = 0; k < SMALL_NT / 64; ++k) s += part[k];
+  const float f = (float)((double)X_UNIT / (sqrt(s) + (double)p.eps));
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    const int k = tid + j * SMALL_NT;
+    if (k >= pieces) continue;
+    const int r = k / row_pieces, c = (k - r * row_pieces) * 4;
+    v4h hi, lo;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float v = u[j][e] * f;
+      const _Float16 h = (_Float16)v;
+      hi[e] = __builtin_bit_cast(unsigned short, h);
+      lo[e] = __builtin_bit_cast(unsigned short, (_Float16)(v - (float)h));
+    }
+    if (!tall) {      // (what lies behind the row's end is zero, and inside the padding)
+      *in_lds<v4h>(X + small_at(r, c, np)) = hi;
+      *in_lds<v4h>(X + x_term + small_at(r, c, np)) = lo;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (c + e < cols) {
+          *in_lds<unsigned short>(X + small_at(c + e, r, np)) = hi[e];
+          *in_lds<unsigned short>(X + x_term + small_at(c + e, r, np)) = lo[e];
+        }
+    }
+  }
+  __syncthreads();
+
+  // rows f .. f + 15, columns 32 kk + 8 q + 0..7
+  const auto by_row = [&](const uint16_t* a, int f0, int kk, int ld) { return *in_lds<const v8s>(a + small_at(f0 + i, kk * 32 + 8 * q, ld)); };
+  // X's columns f .. f + 15, rows 32 kk + 8 q + 0..7
+  const auto by_column = [&](const uint16_t* a, int f0, int kk) {
+    const int r = kk * 32 + 8 * q + (i >> 2), c = f0 + (i & 3) * 4;
+    const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(in_lds<v4s>(a + small_at(r, c, np)));
+    const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(in_lds<v4s>(a + small_at(r + 4, c, np)));
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  const auto multiply = [](v4f acc, const v8s (&a)[2], const v8s (&b)[2]) {
+    acc = mma<false>(b[0], a[0], acc);
+    acc = mma<false>(b[1], a[0], acc);
+    return mma<false>(b[0], a[1], acc);
+  };
+  // Of [64, 64] a wavefront has 16 rows by 32 columns; lane (q, i) row i, four columns from 4 q on.
+  const int er = wave / 2 * 16, ec = wave % 2 * 32;
+  const auto put_e = [&](const v4f (&acc)[2], float mul, float diag) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int r = er + i, c = ec + j * 16 + 4 * q;
+      v4h hi, lo;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float v = acc[j][e] * mul + (r == c + e ? diag : 0.0f);
+        const _Float16 h = (_Float16)v;
+        hi[e] = __builtin_bit_cast(unsigned short, h);
+        lo[e] = __builtin_bit_cast(unsigned short, (_Float16)(v - (float)h));
+      }
+      *in_lds<v4h>(E + small_at(r, c, SMALL_M)) = hi;
+      *in_lds<v4h>(E + e_term + small_at(r, c, SMALL_M)) = lo;
+    }
+  };
+  const auto symmetric = [&](const uint16_t* a, int term, int ld, v4f (&acc)[2]) {
+    acc[0] = acc[1] = v4f{};
+    for (int kk = 0; kk < ld / 32; ++kk) {
+      const v8s left[2] = {by_row(a, er, kk, ld), by_row(a + term, er, kk, ld)};
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const v8s right[2] = {by_row(a, ec + 16 * j, kk, ld), by_row(a + term, ec + 16 * j, kk, ld)};
+        acc[j] = multiply(acc[j], left, right);
+      }
+    }
+  };
+
+  for (int k = 0; k < p.steps; ++k) {
+    const float a = p.coefficients[3 * k], b = p.coefficients[3 * k + 1], c = p.coefficients[3 * k + 2];
+    const bool last = k + 1 == p.steps;
+    constexpr float PER_GRAM = E_UNIT / (X_UNIT * X_UNIT);
+    v4f acc[2];
+    symmetric(X, x_term, np, acc);
+    if (c != 0.0f) {      // E, then B = c E^2 + d (k_polar_symmetric)
+      put_e(acc, PER_GRAM, b / (2.0f * c) * E_UNIT);
+      __syncthreads();
+      symmetric(E, e_term, SMALL_M, acc);
+      __syncthreads();
+      put_e(acc, c / E_UNIT, (float)(((double)a - (double)b * b / (4.0 * c)) * E_UNIT));
+    } else {
+      put_e(acc, b * PER_GRAM, a * E_UNIT);
+    }
+    __syncthreads();
+    // X <- B X, sixteen columns at a time: nobody else reads those
+    v8s B[4][2][2];
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+        B[t][kk][0] = by_row(E, t * 16, kk, SMALL_M);
+        B[t][kk][1] = by_row(E + e_term, t * 16, kk, SMALL_M);
+      }
+    for (int f0 = wave * 16; f0 < np; f0 += SMALL_NT / 64 * 16) {
+      v8s x[2][2];
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+        x[kk][0] = by_column(X, f0, kk);
+        x[kk][1] = by_column(X + x_term, f0, kk);
+      }
+      lds_done();
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        v4f o = {};
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) o = multiply(o, B[t][kk], x[kk]);
+        const int r = t * 16 + i, col = f0 + 4 * q;
+        if (!last) {
+          v4h hi, lo;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float v = o[e] * (1.0f / E_UNIT);
+            const _Float16 h = (_Float16)v;
+            hi[e] = __builtin_bit_cast(unsigned short, h);
+            lo[e] = __builtin_bit_cast(unsigned short, (_Float16)(v - (float)h));
+          }
+          *in_lds<v4h>(X + small_at(r, col, np)) = hi;
+          *in_lds<v4h>(X + x_term + small_at(r, col, np)) = lo;
+          continue;
+        }
+        o *= 1.0f / (E_UNIT * X_UNIT);
+        const float step = p.finish.lr * mat.scale;
+        // four elements of one of the list's rows, or one of each of four
+        const int64_t at = mat.at + (tall ? (int64_t)col * cols + r : (int64_t)r * cols + col);
+        const int left = r < (tall ? cols : rows) ? (tall ? rows : cols) - col : 0;
+        if (!tall) {
+          if (p.finish.x) {
+            const v4f x0 = load4(p.finish.x, F32, at, left);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = x0[e] * p.finish.keep - step * o[e];
+            store4(p.finish.x, F32, at, left, o);
+          }
+          if (p.finish.out) store4(p.finish.out, p.finish.dtype, at, left, o);
+        } else {
+          v4f x0 = {};
+          if (p.finish.x) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (e < left) x0[e] = p.finish.x[at + (int64_t)e * cols];
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if (e >= left) continue;
+            if (p.finish.x) {
+              o[e] = x0[e] * p.finish.keep - step * o[e];
+              p.finish.x[at + (int64_t)e * cols] = o[e];
+            }
+            if (p.finish.out) {
+              if (p.finish.dtype == F32) static_cast<float*>(p.finish.out)[at + (int64_t)e * cols] = o[e];
+              else static_cast<unsigned short*>(p.finish.out)[at + (int64_t)e * cols] = to_bits(o[e], p.finish.dtype == BF16);
+            }
+          }
+        }
+      }
+    }
+    __syncthreads();
+  }
+}
+
 }  // namespace obm

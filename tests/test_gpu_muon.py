@@ -262,3 +262,97 @@ def test_refusals_of_the_python_class():
                 lambda: muon([0, 12], [3, 4]), lambda: muon([0, 12], [3], precision=torch.bfloat16)):
         with pytest.raises(ObLambError):
             bad()
+
+
+SMALL = [(64, 64), (0, 3), (63, 200), (512, 33), (1, 1), (1, 511), (9, 7), (0, 1), (64, 512), (20, 64), (130, 17)]
+
+
+@pytest.mark.parametrize("precision", (torch.float32, torch.float16))
+@pytest.mark.parametrize("kind", ("normal", "student_t3", "low_rank"))
+def test_lists_of_small_matrices(kind, precision):
+    """Lists whose matrices all have a side of at most 64 and one of at most 512 take a kernel of their own."""
+    offsets, rows = layout(SMALL)
+    src = flat_of(SMALL, kind, seed=4, scale=1e-3)
+    for coefficients, steps in ((QUINTIC, 5), ((1.5, -0.5, 0.0) + QUINTIC, 3)):
+        out = muon(offsets, rows, precision=precision, coefficients=coefficients, steps=steps,
+                   own_state=False).orthogonalize(src.cuda(), torch.full((len(src),), 7.0, device="cuda"))
+        for (r, c), a, b in zip(SMALL, offsets[:-1], offsets[1:]):
+            if r:
+                assert off(out[a:b].view(r, c), definition(src[a:b].view(r, c), steps, coefficients)) <= BOUND[torch.float32], (r, c)
+            else:
+                assert (out[a:b] == 7.0).all()
+
+
+@pytest.mark.parametrize("nesterov", (True, False))
+@pytest.mark.parametrize("grad_dtype,x_lp", [(torch.float32, None), (torch.float16, torch.float16), (torch.bfloat16, torch.bfloat16)])
+def test_step_of_small_matrices(grad_dtype, x_lp, nesterov):
+    offsets, rows = layout(SMALL)
+    f = np.float32
+    x, m = flat_of(SMALL, seed=1, scale=0.02), flat_of(SMALL, seed=2, scale=1e-3)
+    scale, lr, wd, beta = (1.0 if grad_dtype == torch.float32 else 1 / 64), 3e-3, 0.1, 0.9
+    opt = muon(offsets, rows, momentum=beta, weight_decay=wd, nesterov=nesterov, grad_scale=scale, x_lp_dtype=x_lp)
+    opt.load_state(dict(x=x, m=m))
+    for t in range(2):
+        g = (flat_of(SMALL, seed=10 + t, scale=1e-3) / scale).to(grad_dtype)
+        before = opt.t["x"].clone()
+        opt.step(g.cuda(), lr)
+        gs, b, omb = g.float() * f(scale), float(f(beta)), float(f(1) - f(beta))
+        for (r, c), i, j in zip(SMALL, offsets[:-1], offsets[1:]):
+            if not r:
+                assert torch.equal(opt.t["m"][i:j].cpu(), m[i:j]) and torch.equal(opt.t["x"][i:j].cpu(), x[i:j])
+                continue
+            m[i:j] = b * m[i:j] + omb * gs[i:j]
+            u = b * m[i:j] + omb * gs[i:j] if nesterov else m[i:j]
+            assert torch.equal(opt.t["m"][i:j].cpu(), m[i:j])
+            moved = opt.t["x"][i:j].double().cpu() - before[i:j].double().cpu() * (1 - lr * wd)
+            want = -lr * 0.2 * max(r, c) ** 0.5 * definition(u.view(r, c)).reshape(-1)
+            slack = 4 * 2.0 ** -24 * before[i:j].double().cpu().norm().item()
+            assert (moved - want).norm() <= BOUND[torch.float32] * want.norm() + slack
+            if x_lp is not None:
+                assert torch.equal(opt.x_lp[i:j], opt.t["x"][i:j].to(x_lp))
+
+
+def test_small_matrices_with_zeros_infinities_and_nans():
+    offsets, rows = layout(SMALL)
+    src = flat_of(SMALL)
+    opt = muon(offsets, rows, own_state=False)
+    clean = opt.orthogonalize(src.cuda())
+    src[offsets[0]:offsets[1]] = 0
+    src[offsets[2] + 5] = float("inf")
+    src[offsets[6] + 7] = float("nan")
+    out = opt.orthogonalize(src.cuda())
+    assert (out[:offsets[1]] == 0).all()
+    assert torch.isnan(out[offsets[2]:offsets[3]]).any() and torch.isnan(out[offsets[6]:offsets[7]]).any()
+    for l in (3, 4, 5, 8, 9, 10):
+        assert torch.equal(out[offsets[l]:offsets[l + 1]], clean[offsets[l]:offsets[l + 1]])
+
+
+def test_groups_of_steps_that_follow_one_gram_matrix():
+    """More steps than one Gram matrix serves, on matrices large enough that following it pays: 12 steps are groups of three."""
+    shapes = [(512, 2048), (2048, 512)]
+    offsets, rows = layout(shapes)
+    src = flat_of(shapes * 1, "low_rank", seed=6)
+    coefficients = QUINTIC * 4 + (1.875, -1.25, 0.375)
+    opt = muon(offsets, rows, steps=12, coefficients=coefficients, own_state=False)
+    out = opt.orthogonalize(src.cuda())
+    for (r, c), a, b in zip(shapes, offsets[:-1], offsets[1:]):
+        assert off(out[a:b].view(r, c), definition(src[a:b].view(r, c).cuda().cpu(), 12, coefficients)) <= 12 / 5 * BOUND[torch.float32]
+
+
+@pytest.mark.parametrize("precision", (torch.float32, torch.float16))
+def test_wide_and_square_matrices_in_one_list(precision):
+    """Enough of the wide ones that they take a way of their own in precision float16."""
+    shapes = [(1024, 1024), (0, 9), (1024, 4096), (4096, 1024), (1000, 1024)]
+    offsets, rows = layout(shapes)
+    src = flat_of(shapes, seed=9).cuda()
+    out = muon(offsets, rows, precision=precision, own_state=False).orthogonalize(src)
+    for (r, c), a, b in zip(shapes, offsets[:-1], offsets[1:]):
+        if r:
+            G = src[a:b].view(r, c).double()
+            X = G.T if r > c else G
+            X = X / (X.norm() + 1e-7)
+            for _ in range(5):
+                S = X @ X.T.contiguous()
+                X = QUINTIC[0] * X + (QUINTIC[1] * S + QUINTIC[2] * S @ S) @ X
+            want = (X.T if r > c else X).cpu()
+            assert off(out[a:b].view(r, c), want) <= BOUND[precision]
