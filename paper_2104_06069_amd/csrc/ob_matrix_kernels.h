@@ -355,15 +355,23 @@ struct ListTile {      // of a product, with what it needs of its matrix; mp == 
   short tm, tn;
 };
 
+// v as a sum of two binary16 numbers.  Both have to come from the same binary32 number: left to itself the compiler may form the
+// first from a product before that is rounded to binary32 (v_fma_mixlo_f16), and the second from the rounded one, which puts
+// the sum off by 2^-11 for a value close to the middle between two binary16 numbers.
+__device__ __forceinline__ void split4(v4f v, v4h* hi, v4h* lo) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    float x = v[e];
+    asm("" : "+v"(x));
+    const _Float16 h = (_Float16)x;
+    (*hi)[e] = __builtin_bit_cast(unsigned short, h);
+    (*lo)[e] = __builtin_bit_cast(unsigned short, (_Float16)(x - (float)h));
+  }
+}
 template <int TERMS>
 __device__ __forceinline__ void store_terms(uint16_t* plane, int64_t term, int64_t at, v4f v) {
   v4h hi, lo;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const _Float16 h = (_Float16)v[e];
-    hi[e] = __builtin_bit_cast(unsigned short, h);
-    lo[e] = __builtin_bit_cast(unsigned short, (_Float16)(v[e] - (float)h));
-  }
+  split4(v, &hi, &lo);
   *reinterpret_cast<v4h*>(plane + at) = hi;
   if constexpr (TERMS == 2) *reinterpret_cast<v4h*>(plane + term + at) = lo;
 }
@@ -642,47 +650,64 @@ struct SmallArgs {
   int steps;
   float coefficients[3 * MAX_STEPS];
 };
-// X's and E's rows of LDS: 16-byte pieces, permuted by the row's number
-__device__ __forceinline__ int small_at(int r, int c, int ld) { return r * ld + ((((c >> 3) ^ (r & 7)) << 3) | (c & 7)); }
+// X and E in LDS: a row's eights of columns, permuted by the row's number, each 32 bytes: eight first terms and eight second
+// ones, or the same eight as binary32 (u at the start, the result at the end).
+__device__ __forceinline__ int small_at(int r, int c, int ld) { return r * 2 * ld + ((((c >> 3) ^ (r & 7)) << 4) | (c & 7)); }
+__device__ __forceinline__ float* small_f32(uint16_t* a, int r, int c, int ld) {
+  return reinterpret_cast<float*>(a + small_at(r, c & ~7, ld)) + (c & 7);
+}
+__device__ __forceinline__ void small_put4(uint16_t* at, v4f v) {
+  v4h hi, lo;
+  split4(v, &hi, &lo);
+  *in_lds<v4h>(at) = hi;
+  *in_lds<v4h>(at + 8) = lo;
+}
 
+// The loops are kept short: the code runs a few times only, and what is unrolled has to be fetched first (with everything
+// unrolled, 48 KB, it took twice as long).
 __global__ __launch_bounds__(SMALL_NT, 2) void k_polar_small(SmallArgs p) {
   __shared__ double part[SMALL_NT / 64];
   const Matrix& mat = p.mats[blockIdx.x];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, q = lane >> 4;
   const int rows = mat.rows, cols = mat.cols, np = mat.np;
   const bool tall = mat.tall;
-  uint16_t* const X = lds_of_launch;                       // [2][SMALL_M][np]
-  uint16_t* const E = lds_of_launch + 2 * SMALL_M * np;    // [2][SMALL_M][SMALL_M]: E, then B
-  const int x_term = SMALL_M * np, e_term = SMALL_M * SMALL_M;
-
-  // u, its norm, and X
-  constexpr int PER = SMALL_M * SMALL_N / 4 / SMALL_NT;
+  uint16_t* const X = lds_of_launch;                       // [SMALL_M][np]
+  uint16_t* const E = lds_of_launch + 2 * SMALL_M * np;    // [SMALL_M][SMALL_M]: E, then B
+  // The list's matrix, four elements of a row at a time: piece k is (r, c..c + 3); k advances by SMALL_NT
   const int row_pieces = (cols + 3) / 4, pieces = rows * row_pieces;
-  v4f u[PER];
+  const int step_r = SMALL_NT / row_pieces, step_c = SMALL_NT % row_pieces;
+
+  for (int k = tid; k < SMALL_M * np / 4; k += SMALL_NT) *in_lds<v8s>(X + 8 * k) = v8s{};      // (the padding)
+  __syncthreads();
+  // u, in binary32, and its norm
   double s = 0.0;
+  {
+    int r = tid / row_pieces, c4 = tid % row_pieces;
+#pragma unroll 2
+    for (int k = tid; k < pieces; k += SMALL_NT) {
+      const int c = c4 * 4, left = cols - c;
+      const int64_t at = mat.at + (int64_t)r * cols + c;
+      v4f g = {}, m = {};
+      if (p.d.g) g = load4(p.d.g, p.d.dtype, at, left);
+      if (p.d.m) m = load4(p.d.m, F32, at, left);
+      if (p.d.m && p.d.g) {
 #pragma unroll
-  for (int j = 0; j < PER; ++j) {
-    const int k = tid + j * SMALL_NT;
-    u[j] = v4f{};
-    if (k >= pieces) continue;
-    const int r = k / row_pieces, c = (k - r * row_pieces) * 4, left = cols - c;
-    const int64_t at = mat.at + (int64_t)r * cols + c;
-    v4f g = {}, m = {};
-    if (p.d.g) g = load4(p.d.g, p.d.dtype, at, left);
-    if (p.d.m) m = load4(p.d.m, F32, at, left);
-    if (p.d.m && p.d.g) {
+        for (int e = 0; e < 4; ++e) m[e] = p.d.beta * m[e] + p.d.omb * (p.d.scale * g[e]);
+        store4(p.m_out, F32, at, left, m);
+      }
+      v4f u = direction4(p.d, g, m);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) m[e] = p.d.beta * m[e] + p.d.omb * (p.d.scale * g[e]);
-      store4(p.m_out, F32, at, left, m);
-    }
-    u[j] = direction4(p.d, g, m);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      if (e >= left) u[j][e] = 0.0f;
-      s += (double)u[j][e] * (double)u[j][e];
+      for (int e = 0; e < 4; ++e) {
+        if (e >= left) u[e] = 0.0f;
+        s += (double)u[e] * (double)u[e];
+        if (tall && e < left) *in_lds<float>(small_f32(X, c + e, r, np)) = u[e];
+      }
+      if (!tall) *in_lds<v4f>(small_f32(X, r, c, np)) = u;
+      c4 += step_c;
+      r += step_r + (c4 >= row_pieces);
+      c4 -= c4 >= row_pieces ? row_pieces : 0;
     }
   }
-  for (int k = tid; k < SMALL_M * np / 4; k += SMALL_NT) *in_lds<v8s>(X + 8 * k) = v8s{};      // both planes, padding included
 #pragma unroll
   for (int k = 32; k; k >>= 1) s += __shfl_xor(s, k);
   if (lane == 0) part[wave] = s;
@@ -691,165 +716,124 @@ __global__ __launch_bounds__(SMALL_NT, 2) void k_polar_small(SmallArgs p) {
 #pragma unroll
   for (int k = 0; k < SMALL_NT / 64; ++k) s += part[k];
   const float f = (float)((double)X_UNIT / (sqrt(s) + (double)p.eps));
-#pragma unroll
-  for (int j = 0; j < PER; ++j) {
-    const int k = tid + j * SMALL_NT;
-    if (k >= pieces) continue;
-    const int r = k / row_pieces, c = (k - r * row_pieces) * 4;
-    v4h hi, lo;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float v = u[j][e] * f;
-      const _Float16 h = (_Float16)v;
-      hi[e] = __builtin_bit_cast(unsigned short, h);
-      lo[e] = __builtin_bit_cast(unsigned short, (_Float16)(v - (float)h));
-    }
-    if (!tall) {      // (what lies behind the row's end is zero, and inside the padding)
-      *in_lds<v4h>(X + small_at(r, c, np)) = hi;
-      *in_lds<v4h>(X + x_term + small_at(r, c, np)) = lo;
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (c + e < cols) {
-          *in_lds<unsigned short>(X + small_at(c + e, r, np)) = hi[e];
-          *in_lds<unsigned short>(X + x_term + small_at(c + e, r, np)) = lo[e];
-        }
-    }
+  for (int k = tid; k < SMALL_M * np / 8; k += SMALL_NT) {      // eights of X, wherever they are
+    uint16_t* const at = X + 16 * k;
+    const v4f u0 = *in_lds<const v4f>(at), u1 = *in_lds<const v4f>(at + 8);
+    small_put4(at, u0 * f);
+    small_put4(at + 4, u1 * f);
   }
   __syncthreads();
 
-  // rows f .. f + 15, columns 32 kk + 8 q + 0..7
-  const auto by_row = [&](const uint16_t* a, int f0, int kk, int ld) { return *in_lds<const v8s>(a + small_at(f0 + i, kk * 32 + 8 * q, ld)); };
+  // rows f .. f + 15, columns 32 kk + 8 q + 0..7; `term` 0 or 8
+  const auto by_row = [&](const uint16_t* a, int f0, int kk, int ld, int term) {
+    return *in_lds<const v8s>(a + small_at(f0 + i, kk * 32 + 8 * q, ld) + term);
+  };
   // X's columns f .. f + 15, rows 32 kk + 8 q + 0..7
-  const auto by_column = [&](const uint16_t* a, int f0, int kk) {
+  const auto by_column = [&](const uint16_t* a, int f0, int kk, int term) {
     const int r = kk * 32 + 8 * q + (i >> 2), c = f0 + (i & 3) * 4;
-    const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(in_lds<v4s>(a + small_at(r, c, np)));
-    const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(in_lds<v4s>(a + small_at(r + 4, c, np)));
+    const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(in_lds<v4s>(a + small_at(r, c, np) + term));
+    const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(in_lds<v4s>(a + small_at(r + 4, c, np) + term));
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   };
-  const auto multiply = [](v4f acc, const v8s (&a)[2], const v8s (&b)[2]) {
-    acc = mma<false>(b[0], a[0], acc);
-    acc = mma<false>(b[1], a[0], acc);
-    return mma<false>(b[0], a[1], acc);
-  };
-  // Of [64, 64] a wavefront has 16 rows by 32 columns; lane (q, i) row i, four columns from 4 q on.
+  // Of [64, 64] a wavefront has 16 rows by 32 columns; lane (q, i) row i, four columns from 4 q on.  Its sums are kept apart
+  // by term, so that no product waits for the one before.
   const int er = wave / 2 * 16, ec = wave % 2 * 32;
-  const auto put_e = [&](const v4f (&acc)[2], float mul, float diag) {
+  v4f acc[2];
+  const auto symmetric = [&](const uint16_t* a, int ld) {
+    v4f sum[2][3] = {};
+    for (int kk = 0; kk < ld / 32; ++kk) {
+      const v8s l0 = by_row(a, er, kk, ld, 0), l1 = by_row(a, er, kk, ld, 8);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const v8s r0 = by_row(a, ec + 16 * j, kk, ld, 0), r1 = by_row(a, ec + 16 * j, kk, ld, 8);
+        sum[j][0] = mma<false>(r0, l0, sum[j][0]);
+        sum[j][1] = mma<false>(r1, l0, sum[j][1]);
+        sum[j][2] = mma<false>(r0, l1, sum[j][2]);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) acc[j] = sum[j][0] + (sum[j][1] + sum[j][2]);
+  };
+  const auto put_e = [&](float mul, float diag) {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const int r = er + i, c = ec + j * 16 + 4 * q;
-      v4h hi, lo;
+      v4f v = acc[j] * mul;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float v = acc[j][e] * mul + (r == c + e ? diag : 0.0f);
-        const _Float16 h = (_Float16)v;
-        hi[e] = __builtin_bit_cast(unsigned short, h);
-        lo[e] = __builtin_bit_cast(unsigned short, (_Float16)(v - (float)h));
-      }
-      *in_lds<v4h>(E + small_at(r, c, SMALL_M)) = hi;
-      *in_lds<v4h>(E + e_term + small_at(r, c, SMALL_M)) = lo;
-    }
-  };
-  const auto symmetric = [&](const uint16_t* a, int term, int ld, v4f (&acc)[2]) {
-    acc[0] = acc[1] = v4f{};
-    for (int kk = 0; kk < ld / 32; ++kk) {
-      const v8s left[2] = {by_row(a, er, kk, ld), by_row(a + term, er, kk, ld)};
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const v8s right[2] = {by_row(a, ec + 16 * j, kk, ld), by_row(a + term, ec + 16 * j, kk, ld)};
-        acc[j] = multiply(acc[j], left, right);
-      }
+      for (int e = 0; e < 4; ++e)
+        if (r == c + e) v[e] += diag;
+      small_put4(E + small_at(r, c, SMALL_M), v);
     }
   };
 
+#pragma unroll 1
   for (int k = 0; k < p.steps; ++k) {
     const float a = p.coefficients[3 * k], b = p.coefficients[3 * k + 1], c = p.coefficients[3 * k + 2];
     const bool last = k + 1 == p.steps;
     constexpr float PER_GRAM = E_UNIT / (X_UNIT * X_UNIT);
-    v4f acc[2];
-    symmetric(X, x_term, np, acc);
+    symmetric(X, np);
     if (c != 0.0f) {      // E, then B = c E^2 + d (k_polar_symmetric)
-      put_e(acc, PER_GRAM, b / (2.0f * c) * E_UNIT);
+      put_e(PER_GRAM, b / (2.0f * c) * E_UNIT);
       __syncthreads();
-      symmetric(E, e_term, SMALL_M, acc);
+      symmetric(E, SMALL_M);
       __syncthreads();
-      put_e(acc, c / E_UNIT, (float)(((double)a - (double)b * b / (4.0 * c)) * E_UNIT));
+      put_e(c / E_UNIT, (float)(((double)a - (double)b * b / (4.0 * c)) * E_UNIT));
     } else {
-      put_e(acc, b * PER_GRAM, a * E_UNIT);
+      put_e(b * PER_GRAM, a * E_UNIT);
     }
     __syncthreads();
     // X <- B X, sixteen columns at a time: nobody else reads those
-    v8s B[4][2][2];
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int kk = 0; kk < 2; ++kk) {
-        B[t][kk][0] = by_row(E, t * 16, kk, SMALL_M);
-        B[t][kk][1] = by_row(E + e_term, t * 16, kk, SMALL_M);
-      }
+#pragma unroll 1
     for (int f0 = wave * 16; f0 < np; f0 += SMALL_NT / 64 * 16) {
       v8s x[2][2];
 #pragma unroll
       for (int kk = 0; kk < 2; ++kk) {
-        x[kk][0] = by_column(X, f0, kk);
-        x[kk][1] = by_column(X + x_term, f0, kk);
+        x[kk][0] = by_column(X, f0, kk, 0);
+        x[kk][1] = by_column(X, f0, kk, 8);
       }
       lds_done();
-#pragma unroll
+#pragma unroll 2
       for (int t = 0; t < 4; ++t) {
-        v4f o = {};
+        v4f sum[3] = {};
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk) o = multiply(o, B[t][kk], x[kk]);
+        for (int kk = 0; kk < 2; ++kk) {
+          const v8s b0 = by_row(E, t * 16, kk, SMALL_M, 0), b1 = by_row(E, t * 16, kk, SMALL_M, 8);
+          sum[0] = mma<false>(x[kk][0], b0, sum[0]);
+          sum[1] = mma<false>(x[kk][1], b0, sum[1]);
+          sum[2] = mma<false>(x[kk][0], b1, sum[2]);
+        }
+        const v4f o = (sum[0] + (sum[1] + sum[2])) * (1.0f / E_UNIT);
         const int r = t * 16 + i, col = f0 + 4 * q;
-        if (!last) {
-          v4h hi, lo;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float v = o[e] * (1.0f / E_UNIT);
-            const _Float16 h = (_Float16)v;
-            hi[e] = __builtin_bit_cast(unsigned short, h);
-            lo[e] = __builtin_bit_cast(unsigned short, (_Float16)(v - (float)h));
-          }
-          *in_lds<v4h>(X + small_at(r, col, np)) = hi;
-          *in_lds<v4h>(X + x_term + small_at(r, col, np)) = lo;
-          continue;
-        }
-        o *= 1.0f / (E_UNIT * X_UNIT);
-        const float step = p.finish.lr * mat.scale;
-        // four elements of one of the list's rows, or one of each of four
-        const int64_t at = mat.at + (tall ? (int64_t)col * cols + r : (int64_t)r * cols + col);
-        const int left = r < (tall ? cols : rows) ? (tall ? rows : cols) - col : 0;
-        if (!tall) {
-          if (p.finish.x) {
-            const v4f x0 = load4(p.finish.x, F32, at, left);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = x0[e] * p.finish.keep - step * o[e];
-            store4(p.finish.x, F32, at, left, o);
-          }
-          if (p.finish.out) store4(p.finish.out, p.finish.dtype, at, left, o);
-        } else {
-          v4f x0 = {};
-          if (p.finish.x) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (e < left) x0[e] = p.finish.x[at + (int64_t)e * cols];
-          }
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            if (e >= left) continue;
-            if (p.finish.x) {
-              o[e] = x0[e] * p.finish.keep - step * o[e];
-              p.finish.x[at + (int64_t)e * cols] = o[e];
-            }
-            if (p.finish.out) {
-              if (p.finish.dtype == F32) static_cast<float*>(p.finish.out)[at + (int64_t)e * cols] = o[e];
-              else static_cast<unsigned short*>(p.finish.out)[at + (int64_t)e * cols] = to_bits(o[e], p.finish.dtype == BF16);
-            }
-          }
-        }
+        if (last) *in_lds<v4f>(small_f32(X, r, col, np)) = o * (1.0f / X_UNIT);
+        else small_put4(X + small_at(r, col, np), o);
       }
     }
     __syncthreads();
+  }
+
+  const float step = p.finish.lr * mat.scale;
+  int r = tid / row_pieces, c4 = tid % row_pieces;
+#pragma unroll 2
+  for (int k = tid; k < pieces; k += SMALL_NT) {
+    const int c = c4 * 4, left = cols - c;
+    const int64_t at = mat.at + (int64_t)r * cols + c;
+    v4f o;
+    if (tall) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = *in_lds<const float>(small_f32(X, min(c + e, cols - 1), r, np));
+    } else {
+      o = *in_lds<const v4f>(small_f32(X, r, c, np));
+    }
+    if (p.finish.x) {
+      const v4f x = load4(p.finish.x, F32, at, left);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = x[e] * p.finish.keep - step * o[e];
+      store4(p.finish.x, F32, at, left, o);
+    }
+    if (p.finish.out) store4(p.finish.out, p.finish.dtype, at, left, o);
+    c4 += step_c;
+    r += step_r + (c4 >= row_pieces);
+    c4 -= c4 >= row_pieces ? row_pieces : 0;
   }
 }
 
