@@ -20,15 +20,9 @@ typedef unsigned short v4h_any __attribute__((ext_vector_type(4), aligned(2)));
 __device__ __forceinline__ float from_bits(unsigned short h, bool bf) {
   return bf ? __uint_as_float((unsigned)h << 16) : (float)__builtin_bit_cast(_Float16, h);
 }
-// to nearest, ties to even; NaN -> the format's canonical quiet NaN
+// to nearest, ties to even (a NaN stays one)
 __device__ __forceinline__ unsigned short to_bits(float x, bool bf) {
-  if (bf) {
-    const unsigned u = __float_as_uint(x);
-    if ((u & 0x7fffffffu) > 0x7f800000u) return 0x7fc0;
-    return (unsigned short)((u + 0x7fffu + ((u >> 16) & 1u)) >> 16);
-  }
-  if (x != x) return 0x7e00;
-  return __builtin_bit_cast(unsigned short, (_Float16)x);
+  return bf ? __builtin_bit_cast(unsigned short, (__bf16)x) : __builtin_bit_cast(unsigned short, (_Float16)x);
 }
 
 // Four values in a row from p + at on, of which those from `left` on do not exist (and read as zeros).
@@ -82,6 +76,52 @@ __device__ __forceinline__ void store4(void* p, int dtype, int64_t at, int left,
   }
 }
 
+// A tile's results to `out` [rows, cols], rows ld elements apart, from its row r0 and column c0 on: 128 bytes of a row by eight lanes
+// with 16-bit numbers, by sixteen (256 bytes) with binary32 ones.  BF: the 16-bit type, if dtype is not F32.
+template <class S, bool BF>
+__device__ __forceinline__ void store_tile(const v4f (&acc)[S::FM][S::FN], uint16_t* lds, void* out, int dtype, int64_t ld, int r0, int c0, int rows,
+                                           int cols) {
+  using R = Results<S>;
+  if (dtype == F32) {
+    R::by_rows(acc, lds, [&](int r, int c, v4f v) {
+      if (r0 + r < rows) store4(out, F32, (int64_t)(r0 + r) * ld + c0 + c, cols - c0 - c, v);
+    });
+    return;
+  }
+  R::visit(acc, lds, [&](const float* own, int tr, int tc) {
+    constexpr int EIGHTS = R::ROWS * R::WIDTH / 8, BATCH = EIGHTS / 64 < 4 ? EIGHTS / 64 : 4;
+    const int lane = threadIdx.x & 63;
+#pragma unroll 1
+    for (int k0 = lane; k0 < EIGHTS; k0 += BATCH * 64) {
+      v8s v[BATCH];
+#pragma unroll
+      for (int u = 0; u < BATCH; ++u) {
+        const int k = k0 + u * 64;
+        const float* const at = own + k / (R::WIDTH / 8) * R::STRIDE + k % (R::WIDTH / 8) * 8;
+        const v4f lo = *in_lds<const v4f>(at), hi = *in_lds<const v4f>(at + 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          v[u][e] = (short)to_bits(lo[e], BF);
+          v[u][e + 4] = (short)to_bits(hi[e], BF);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < BATCH; ++u) {
+        const int k = k0 + u * 64, r = r0 + tr + k / (R::WIDTH / 8), c = c0 + tc + k % (R::WIDTH / 8) * 8, left = cols - c;
+        if (r >= rows || left <= 0) continue;
+        uint16_t* const at = static_cast<uint16_t*>(out) + (int64_t)r * ld + c;
+        if (left >= 8) {
+          *reinterpret_cast<v8s_any*>(at) = v[u];
+        } else {
+#pragma unroll
+          for (int e = 0; e < 7; ++e)
+            if (e < left) at[e] = (uint16_t)v[u][e];
+        }
+      }
+    }
+  });
+}
+
 extern __shared__ __align__(1024) uint16_t lds_of_launch[];
 
 // ---- expert layers -------------------------------------------------------------------------------------------------
@@ -95,58 +135,53 @@ struct Groups {
   }
 };
 
-// The groups' tiles of BM rows, one after the other: every wavefront counts them, 64 groups at a time.  The host knows an
+// The groups' tiles of BM rows, one after the other, as every wavefront counts them, 64 groups at a time.  The host knows an
 // upper bound of their number alone.
-template <int BM>
-__device__ __forceinline__ int count_row_tiles(const Groups& gr) {
-  const int lane = threadIdx.x & 63;
-  int total = 0;
-  for (int g0 = 0; g0 < gr.n; g0 += 64) {
-    int lo = 0, hi = 0;
-    if (g0 + lane < gr.n) gr.range(g0 + lane, &lo, &hi);
-    int t = (hi - lo + BM - 1) / BM;
-#pragma unroll
-    for (int d = 32; d; d >>= 1) t += __shfl_xor(t, d);
-    total += t;
-  }
-  return __builtin_amdgcn_readfirstlane(total);
-}
-// Tile `tile` of them and of the `width` columns of tiles: its group's number, first row and number of rows, and its place
 struct RowTile {
-  int g, lo, rows, tm, tn;
+  int g, lo, rows, tm, tn;      // a tile's group, that group's first row and number of rows, and the tile's place among its tiles
 };
 template <int BM>
-__device__ __forceinline__ RowTile find_row_tile(const Groups& gr, int width, int tile) {
-  const int lane = threadIdx.x & 63;
-  RowTile out = {};
-  int before = 0;
-  for (int g0 = 0; g0 < gr.n; g0 += 64) {
-    int lo = 0, hi = 0;
+struct RowTiles {
+  int lo, hi, own, upto, total;      // of group `lane` (of the first 64): rows, tiles, and tiles up to and with it; tiles of all groups
+  __device__ __forceinline__ void look(const Groups& gr, int g0) {
+    const int lane = threadIdx.x & 63;
+    lo = hi = 0;
     if (g0 + lane < gr.n) gr.range(g0 + lane, &lo, &hi);
-    const int own = (hi - lo + BM - 1) / BM;
-    int upto = own;
+    upto = own = (hi - lo + BM - 1) / BM;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
       const int o = __shfl_up(upto, d);
       if (lane >= d) upto += o;
     }
-    const unsigned long long past = __ballot((before + upto) * width > tile);
-    if (past) {
-      const int l = __ffsll((long long)past) - 1;
-      const int tiles = __shfl(own, l), first = before + __shfl(upto, l) - tiles;
-      int tm, tn;
-      tile_in_bands(tile - first * width, tiles, width, &tm, &tn);
-      out.g = __builtin_amdgcn_readfirstlane(g0 + l);
-      out.lo = __builtin_amdgcn_readfirstlane(__shfl(lo, l));
-      out.rows = __builtin_amdgcn_readfirstlane(__shfl(hi, l)) - out.lo;
-      out.tm = __builtin_amdgcn_readfirstlane(tm);
-      out.tn = __builtin_amdgcn_readfirstlane(tn);
-      return out;
-    }
-    before += __shfl(upto, 63);
   }
-  return out;
-}
+  __device__ __forceinline__ explicit RowTiles(const Groups& gr) {
+    total = 0;
+    for (int g0 = (gr.n - 1) / 64 * 64; g0 >= 0; g0 -= 64) {      // (the first 64 last: they stay)
+      look(gr, g0);
+      total += __builtin_amdgcn_readlane(upto, 63);
+    }
+  }
+  // Tile `tile` of them and of the `width` columns of tiles; to be called once
+  __device__ __forceinline__ RowTile find(const Groups& gr, int width, int tile) {
+    RowTile out = {};
+    int before = 0;
+    for (int g0 = 0; g0 < gr.n; g0 += 64) {
+      if (g0) look(gr, g0);
+      const unsigned long long past = __ballot((before + upto) * width > tile);
+      if (past) {
+        const int l = __builtin_amdgcn_readfirstlane(__ffsll((long long)past) - 1);
+        const int tiles = __builtin_amdgcn_readlane(own, l), first = before + __builtin_amdgcn_readlane(upto, l) - tiles;
+        tile_in_bands(tile - first * width, tiles, width, &out.tm, &out.tn);
+        out.g = g0 + l;
+        out.lo = __builtin_amdgcn_readlane(lo, l);
+        out.rows = __builtin_amdgcn_readlane(hi, l) - out.lo;
+        return out;
+      }
+      before += __builtin_amdgcn_readlane(upto, 63);
+    }
+    return out;
+  }
+};
 
 // forward (x, W, y) and input_grad (dy, W transposed, dx): out[r] = a[r] W_g, a [rows, depth], out [rows, width].  FB: order
 // of W as an operand of `width` rows.
@@ -167,15 +202,14 @@ __device__ __forceinline__ void rows_tile(const RowsArgs& p, const RowTile& t, i
   const Operand a{p.a + t.lo * p.lda, 0, p.lda, t.rows, p.a_direct};
   const Operand b{p.w + t.g * p.w_stride, 0, p.ldw, p.width, p.w_direct};
   P::run(a, b, r0, c0, 0, p.depth, lds_of_launch, acc);
-  Results<S>::by_rows(acc, lds_of_launch, [&](int r, int c, v4f v) {
-    r += r0;
-    c += c0;
-    if (r < t.rows) store4(p.out, p.out_dtype, (t.lo + r) * p.ldo + c, p.width - c, v);
-  });
+  void* const out = static_cast<char*>(p.out) + t.lo * p.ldo * (p.out_dtype == F32 ? 4 : 2);
+  store_tile<S, BF>(acc, lds_of_launch, out, p.out_dtype, p.ldo, r0, c0, t.rows, p.width);
 }
 template <class S, bool BF, int FB, int MODE>
 __global__ __launch_bounds__(S::NT, 2) void k_experts_rows(RowsArgs p) {
-  const int width = (p.width + S::BN - 1) / S::BN, tiles = count_row_tiles<S::BM>(p.groups) * width;
+  const int width = (p.width + S::BN - 1) / S::BN;
+  RowTiles<S::BM> all(p.groups);
+  const int tiles = all.total * width;
   // A CU has one workgroup of 256 x 256 at a time.  Of the last round, if it would leave half the card or more idle, each tile is
   // split between two workgroups, or four.  (Measured with 1088 tiles, 4.25 rounds: TODO-ROUNDS.)
   const int rest = S::BM == 256 ? tiles % CUS : 0, parts = rest == 0 ? 1 : rest * 4 <= CUS ? 4 : rest * 2 <= CUS ? 2 : 1;
@@ -184,14 +218,14 @@ __global__ __launch_bounds__(S::NT, 2) void k_experts_rows(RowsArgs p) {
   if (id < before_rest) {
     const int tile = tile_of_workgroup(id, whole);
     if (tile < 0) return;
-    const RowTile t = find_row_tile<S::BM>(p.groups, width, tile);
+    const RowTile t = all.find(p.groups, width, tile);
     rows_tile<S, BF, FB, MODE>(p, t, t.tm * S::BM, t.tn * S::BN);
     return;
   }
   if constexpr (S::BM == 256) {
     const int part = id - before_rest;
     if (parts == 1 || part >= rest * parts) return;
-    const RowTile t = find_row_tile<256>(p.groups, width, whole + part / parts);
+    const RowTile t = all.find(p.groups, width, whole + part / parts);
     const int k = part % parts;
     if (parts == 4) rows_tile<Shape<128, 128, 64, 2, 4>, BF, FB, MODE>(p, t, t.tm * 256 + k / 2 * 128, t.tn * 256 + k % 2 * 128);
     else rows_tile<Shape<128, 256, 64, 2, 4>, BF, FB, MODE>(p, t, t.tm * 256 + k * 128, t.tn * 256);
@@ -216,9 +250,10 @@ __global__ __launch_bounds__(256, 2) void k_experts_few_rows(RowsArgs p) {
   using A = typename F::A;
   using B = typename F::B;
   const int width = (p.width + F::BN - 1) / F::BN;
-  const int tile = tile_of_workgroup(blockIdx.x, count_row_tiles<F::BM>(p.groups) * width);
+  RowTiles<F::BM> all(p.groups);
+  const int tile = tile_of_workgroup(blockIdx.x, all.total * width);
   if (tile < 0) return;
-  const RowTile t = find_row_tile<F::BM>(p.groups, width, tile);
+  const RowTile t = all.find(p.groups, width, tile);
   const Operand a{p.a + t.lo * p.lda, 0, p.lda, t.rows, p.a_direct};
   const Operand b{p.w + t.g * p.w_stride, 0, p.ldw, p.width, p.w_direct};
   const int r0 = t.tm * F::BM, c0 = t.tn * F::BN, lane = threadIdx.x & 63;
@@ -323,13 +358,21 @@ __global__ __launch_bounds__(S::NT, 2) void k_experts_weights(WeightsArgs p) {
   } else if (p.accumulate) {
     return;
   }
-  Results<S>::by_rows(acc, lds_of_launch, [&](int r, int c, v4f v) {
-    r += tm * S::BM;
-    c += tn * S::BN;
-    if (r >= p.height) return;
-    const int64_t at = g * p.out_stride + (int64_t)r * p.width + c;
-    if (p.accumulate) v += load4(p.out, F32, at, p.width - c);
-    store4(p.out, p.out_dtype, at, p.width - c, v);
+  if (!p.accumulate) {
+    void* const out = static_cast<char*>(p.out) + g * p.out_stride * (p.out_dtype == F32 ? 4 : 2);
+    store_tile<S, BF>(acc, lds_of_launch, out, p.out_dtype, p.width, tm * S::BM, tn * S::BN, p.height, p.width);
+    return;
+  }
+  float* const sums = static_cast<float*>(p.out) + g * p.out_stride;
+  Results<S>::visit(acc, lds_of_launch, [&](const float* own, int r0, int c0) {
+    r0 += tm * S::BM;
+    c0 += tn * S::BN;
+    Results<S>::template pass<true>(
+        own, r0, c0,
+        [&](int r, int c) { return r < p.height ? load4(sums, F32, (int64_t)r * p.width + c, p.width - c) : v4f{}; },
+        [&](int r, int c, v4f v, v4f before) {
+          if (r < p.height) store4(sums, F32, (int64_t)r * p.width + c, p.width - c, v + before);
+        });
   });
 }
 
