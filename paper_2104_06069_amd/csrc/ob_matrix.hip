@@ -43,7 +43,7 @@ struct Rate {
   int per_cu;
   double fixed, all, one;
 };
-constexpr Rate RATES[KINDS] = {{1, 7.0, 0.0251, 0.0251}, {2, 3.6, 0.0149, 0.0095}, {3, 1.8, 0.0080, 0.0055}, {1, 1.8, 0.0050, 0.0050}};
+constexpr Rate RATES[KINDS] = {{1, 5.5, 0.0251, 0.0251}, {2, 3.6, 0.0155, 0.0095}, {3, 1.8, 0.0100, 0.0055}, {1, 1.8, 0.0050, 0.0050}};
 // Time of `tiles` tiles of the given mean depth, if they are dealt evenly
 double tiles_time(int kind, double tiles, double depth) {
   const Rate& r = RATES[kind];
@@ -164,7 +164,9 @@ hipError_t allow_experts() {
   return e;
 }
 
-constexpr double FEW_ROWS = 16;      // rows a group (of those that can have one) up to which k_experts_few_rows is taken
+// Rows a group (of those that can have one) up to which k_experts_few_rows is taken, and with unaligned operands; us with it / with
+// 64 x 64 tiles: 64 rows of 8 experts of 1024 x 1024 8.5 / 13.0, 512 of 32 17.2 / 14.9; 200 of 6 of 555 x 999 8.4 / 11.2
+constexpr double FEW_ROWS = 12, FEW_ROWS_ANY = 36;
 constexpr int64_t MAX_LD = (int64_t)1 << 22;      // a tile's offsets are 32-bit
 
 ob_status rows_call(ob_experts_ctx* ctx, const void* a, int64_t lda, const void* w, const int32_t* offsets, int64_t rows,
@@ -197,7 +199,7 @@ ob_status rows_call(ob_experts_ctx* ctx, const void* a, int64_t lda, const void*
   // (a group's last tile is half full in the mean)
   const double groups = (double)std::min<int64_t>(c.num_groups, rows);
   const int kind = best_tile([&](int n) { return std::max(groups, rows / (double)n + 0.5 * groups) * (double)((width + n - 1) / n); }, (double)depth);
-  if (rows <= FEW_ROWS * groups) {
+  if (rows <= (p.a_direct && p.w_direct ? FEW_ROWS : FEW_ROWS_ANY) * groups) {
     const auto few = [&](auto mode) {
       if (c.dtype == OB_BF16) return strided ? launch_few_rows<true, KS, mode>(ctx, p, s) : launch_few_rows<true, KC, mode>(ctx, p, s);
       return strided ? launch_few_rows<false, KS, mode>(ctx, p, s) : launch_few_rows<false, KC, mode>(ctx, p, s);

@@ -76,15 +76,37 @@ __device__ __forceinline__ void store4(void* p, int dtype, int64_t at, int left,
   }
 }
 
+// store4 of binary32 values of which those before `from` belong to another tile
+__device__ __forceinline__ void store_from(void* p, int64_t at, int left, int from, v4f v) {
+  if (from <= 0) {
+    store4(p, F32, at, left, v);
+    return;
+  }
+#pragma unroll
+  for (int e = 1; e < 4; ++e)
+    if (e >= from && e < left) static_cast<float*>(p)[at + e] = v[e];
+}
+
+// Where tile t of `side` of a range of `size` starts.  With operands that go through registers the last tile is moved back to
+// end where the range does, so that its slabs exist as a whole; what it shares with the one before is computed twice, and stored by
+// that one.
+template <int MODE>
+__device__ __forceinline__ int tile_start(int t, int side, int size) {
+  return MODE == ANY ? min(t * side, max(size - side, 0)) : t * side;
+}
+
 // A tile's results to `out` [rows, cols], rows ld elements apart, from its row r0 and column c0 on: 128 bytes of a row by eight lanes
-// with 16-bit numbers, by sixteen (256 bytes) with binary32 ones.  BF: the 16-bit type, if dtype is not F32.
+// with 16-bit numbers, by sixteen (256 bytes) with binary32 ones.  Rows before row0 and columns before col0 are another
+// tile's.  BF: the 16-bit type, if dtype is not F32.
 template <class S, bool BF>
 __device__ __forceinline__ void store_tile(const v4f (&acc)[S::FM][S::FN], uint16_t* lds, void* out, int dtype, int64_t ld, int r0, int c0, int rows,
-                                           int cols) {
+                                           int cols, int row0, int col0) {
   using R = Results<S>;
   if (dtype == F32) {
     R::by_rows(acc, lds, [&](int r, int c, v4f v) {
-      if (r0 + r < rows) store4(out, F32, (int64_t)(r0 + r) * ld + c0 + c, cols - c0 - c, v);
+      r += r0;
+      c += c0;
+      if (r >= row0 && r < rows && c + 3 >= col0) store_from(out, (int64_t)r * ld + c, cols - c, col0 - c, v);
     });
     return;
   }
@@ -108,14 +130,14 @@ __device__ __forceinline__ void store_tile(const v4f (&acc)[S::FM][S::FN], uint1
 #pragma unroll
       for (int u = 0; u < BATCH; ++u) {
         const int k = k0 + u * 64, r = r0 + tr + k / (R::WIDTH / 8), c = c0 + tc + k % (R::WIDTH / 8) * 8, left = cols - c;
-        if (r >= rows || left <= 0) continue;
+        if (r < row0 || r >= rows || left <= 0 || c + 7 < col0) continue;
         uint16_t* const at = static_cast<uint16_t*>(out) + (int64_t)r * ld + c;
-        if (left >= 8) {
+        if (left >= 8 && c >= col0) {
           *reinterpret_cast<v8s_any*>(at) = v[u];
         } else {
 #pragma unroll
-          for (int e = 0; e < 7; ++e)
-            if (e < left) at[e] = (uint16_t)v[u][e];
+          for (int e = 0; e < 8; ++e)
+            if (e < left && c + e >= col0) at[e] = (uint16_t)v[u][e];
         }
       }
     }
@@ -198,12 +220,14 @@ template <class S, bool BF, int FB, int MODE>
 __device__ __forceinline__ void rows_tile(const RowsArgs& p, const RowTile& t, int r0, int c0) {
   using P = Product<S, BF, KC, FB, 1, 1, MODE>;
   if (r0 >= t.rows || c0 >= p.width) return;
+  const int col0 = c0;
+  if constexpr (FB == KS) c0 = tile_start<MODE>(c0 / S::BN, S::BN, p.width);
   typename P::Acc acc = {};
   const Operand a{p.a + t.lo * p.lda, 0, p.lda, t.rows, p.a_direct};
   const Operand b{p.w + t.g * p.w_stride, 0, p.ldw, p.width, p.w_direct};
   P::run(a, b, r0, c0, 0, p.depth, lds_of_launch, acc);
   void* const out = static_cast<char*>(p.out) + t.lo * p.ldo * (p.out_dtype == F32 ? 4 : 2);
-  store_tile<S, BF>(acc, lds_of_launch, out, p.out_dtype, p.ldo, r0, c0, t.rows, p.width);
+  store_tile<S, BF>(acc, lds_of_launch, out, p.out_dtype, p.ldo, r0, c0, t.rows, p.width, 0, col0);
 }
 template <class S, bool BF, int FB, int MODE>
 __global__ __launch_bounds__(S::NT, 2) void k_experts_rows(RowsArgs p) {
@@ -279,17 +303,17 @@ __global__ __launch_bounds__(256, 2) void k_experts_few_rows(RowsArgs p) {
   if constexpr (MODE == ANY) {
     typename A::Fetched va;
     typename B::Fetched vb;
-    if (n > 0) {
-      A::fetch(a, r0, column(0), p.depth, lane, va);
-      B::fetch(b, c0, column(0), p.depth, lane, vb);
-    }
+    const auto fetch = [&](int k) {
+      if (A::exists(a, r0, k, p.depth)) sa.fetch_whole(a, r0, k, lane, va);
+      else A::fetch(a, r0, k, p.depth, lane, va);
+      if (B::exists(b, c0, k, p.depth)) sb.fetch_whole(b, c0, k, lane, vb);
+      else B::fetch(b, c0, k, p.depth, lane, vb);
+    };
+    if (n > 0) fetch(column(0));
     for (int i = 0; i < n; ++i) {
       A::put(a, r0, column(i), p.depth, lane, va, own);
       B::put(b, c0, column(i), p.depth, lane, vb, own + F::BM * F::BK);
-      if (i + 1 < n) {
-        A::fetch(a, r0, column(i + 1), p.depth, lane, va);
-        B::fetch(b, c0, column(i + 1), p.depth, lane, vb);
-      }
+      if (i + 1 < n) fetch(column(i + 1));
       lds_done();
       multiply(own);
       lds_done();
@@ -351,27 +375,27 @@ __global__ __launch_bounds__(S::NT, 2) void k_experts_weights(WeightsArgs p) {
   int tm, tn, lo, hi;
   tile_in_bands(t, nm, nn, &tm, &tn);
   p.groups.range(g, &lo, &hi);
+  const int r0 = tile_start<MODE>(tm, S::BM, p.height), c0 = tile_start<MODE>(tn, S::BN, p.width), row0 = tm * S::BM, col0 = tn * S::BN;
   typename P::Acc acc = {};
   if (hi > lo) {
     const Operand a{p.a + lo * p.lda, 0, p.lda, p.height, p.a_direct}, b{p.b + lo * p.ldb, 0, p.ldb, p.width, p.b_direct};
-    P::run(a, b, tm * S::BM, tn * S::BN, 0, hi - lo, lds_of_launch, acc);
+    P::run(a, b, r0, c0, 0, hi - lo, lds_of_launch, acc);
   } else if (p.accumulate) {
     return;
   }
   if (!p.accumulate) {
     void* const out = static_cast<char*>(p.out) + g * p.out_stride * (p.out_dtype == F32 ? 4 : 2);
-    store_tile<S, BF>(acc, lds_of_launch, out, p.out_dtype, p.width, tm * S::BM, tn * S::BN, p.height, p.width);
+    store_tile<S, BF>(acc, lds_of_launch, out, p.out_dtype, p.width, r0, c0, p.height, p.width, row0, col0);
     return;
   }
   float* const sums = static_cast<float*>(p.out) + g * p.out_stride;
-  Results<S>::visit(acc, lds_of_launch, [&](const float* own, int r0, int c0) {
-    r0 += tm * S::BM;
-    c0 += tn * S::BN;
+  Results<S>::visit(acc, lds_of_launch, [&](const float* own, int tr, int tc) {
+    const auto mine = [&](int r, int c) { return r >= row0 && r < p.height && c + 3 >= col0; };
     Results<S>::template pass<true>(
-        own, r0, c0,
-        [&](int r, int c) { return r < p.height ? load4(sums, F32, (int64_t)r * p.width + c, p.width - c) : v4f{}; },
+        own, r0 + tr, c0 + tc,
+        [&](int r, int c) { return mine(r, c) ? load4(sums, F32, (int64_t)r * p.width + c, p.width - c) : v4f{}; },
         [&](int r, int c, v4f v, v4f before) {
-          if (r < p.height) store4(sums, F32, (int64_t)r * p.width + c, p.width - c, v + before);
+          if (mine(r, c)) store_from(sums, (int64_t)r * p.width + c, p.width - c, col0 - c, v + before);
         });
   });
 }

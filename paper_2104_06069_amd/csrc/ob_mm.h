@@ -93,8 +93,26 @@ struct Slab {
     }
   }
 
-  // Any slab, through registers: fetch() starts its loads, put() takes them to LDS.  Columns from K on are zeros.
+  // Through registers, from any address: fetch() starts a slab's loads, put() takes them to LDS.  Where all of the slab
+  // exists (KC: rows past the last repeat one that does), with the offsets of load():
   typedef v8s Fetched[PER];
+  __device__ static bool exists(const Operand& o, int r0, int k0, int K) { return k0 + BK <= K && (FORM == KC || r0 + BR <= o.rows); }
+  __device__ void fetch_whole(const Operand& o, int r0, int k0, int tid, Fetched& v) const {
+    if (WORK < NT && tid >= WORK) return;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      const uint16_t* src;
+      if constexpr (FORM == KC) src = o.p + (int64_t)r0 * o.ld + k0 + off[j];
+      else src = o.p + (int64_t)(k0 + j * STEP) * o.ld + r0 + off[j % OFFS];
+      v[j] = *reinterpret_cast<const v8s_any*>(src);
+    }
+  }
+  __device__ static void put_whole(const Fetched& v, uint16_t* lds, int tid) {
+    if (WORK < NT && tid >= WORK) return;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) *in_lds<v8s>(lds + (j * WORK + tid) * 8) = v[j];
+  }
+  // Any slab.  Columns from K on are zeros.
   // How many of the eight elements of piece j exist (8: all; 0 or less: none), and the width of a row in memory
   __device__ static int piece_left(const Operand& o, int r0, int k0, int K, int tid, int j, int* r, int* c) {
     const int row = tid / PIECES + j * STEP, at = (tid % PIECES ^ turn(row)) * 8;
@@ -312,7 +330,7 @@ struct Product {
               for (int j = 0; j < FN; ++j) acc[i][j] = mma<BF>(fb[y][j], fa[x][i], acc[i][j]);
           }
     };
-    if constexpr (MODE == ANY) through_registers(a, b, r0, c0, k0, end, n, team, lds, read, multiply);
+    if constexpr (MODE == ANY) through_registers(sa, sb, a, b, r0, c0, k0, end, n, team, lds, read, multiply);
     else if constexpr (S::TURNS) turns(n, lds, acc, load, read, multiply);
     else straight(n, wave, team, lds, load, read, multiply);
     if (MODE == TAIL && n * BK < K) {
@@ -379,24 +397,28 @@ struct Product {
   }
 
   template <class R, class M>
-  __device__ static __forceinline__ void through_registers(const Operand& a, const Operand& b, int r0, int c0, int k0, int end, int n, int team, uint16_t* lds,
+  __device__ static __forceinline__ void through_registers(const A& sa, const B& sb, const Operand& a, const Operand& b, int r0, int c0, int k0, int end, int n, int team, uint16_t* lds,
                                                            R read, M multiply) {
     const int tid = threadIdx.x;
     typename A::Fetched va;
     typename B::Fetched vb;
-    A::fetch(a, r0, k0, end, tid, va);
-    B::fetch(b, c0, k0, end, tid, vb);
+    const auto fetch = [&](int k) {
+      if (A::exists(a, r0, k, end)) sa.fetch_whole(a, r0, k, tid, va);
+      else A::fetch(a, r0, k, end, tid, va);
+      if (B::exists(b, c0, k, end)) sb.fetch_whole(b, c0, k, tid, vb);
+      else B::fetch(b, c0, k, end, tid, vb);
+    };
+    fetch(k0);
     for (int t = 0; t < n; ++t) {
       uint16_t* const s = lds + t % 2 * STAGE;      // nobody reads slab t - 2 after the barrier of t - 1
       const int k = k0 + t * BK;
-      A::put(a, r0, k, end, tid, va, s);
-      B::put(b, c0, k, end, tid, vb, s + TA * BM * BK);
+      if (A::exists(a, r0, k, end)) A::put_whole(va, s, tid);
+      else A::put(a, r0, k, end, tid, va, s);
+      if (B::exists(b, c0, k, end)) B::put_whole(vb, s + TA * BM * BK, tid);
+      else B::put(b, c0, k, end, tid, vb, s + TA * BM * BK);
       lds_done();
       group_barrier();
-      if (t + 1 < n) {
-        A::fetch(a, r0, k + BK, end, tid, va);
-        B::fetch(b, c0, k + BK, end, tid, vb);
-      }
+      if (t + 1 < n) fetch(k + BK);
       steps(s, team, read, multiply);
     }
     lds_done();
