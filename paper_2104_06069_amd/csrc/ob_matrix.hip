@@ -45,19 +45,23 @@ struct Rate {
 };
 constexpr Rate RATES[KINDS] = {{1, 5.5, 0.0251, 0.0251}, {2, 3.6, 0.0155, 0.0095}, {3, 1.8, 0.0100, 0.0055}, {1, 1.8, 0.0050, 0.0050}};
 // Time of `tiles` tiles of the given mean depth, if they are dealt evenly
-double tiles_time(int kind, double tiles, double depth) {
+double tiles_time(int kind, double tiles, double depth, bool split_rest = false) {
   const Rate& r = RATES[kind];
+  if (split_rest && kind == T256 && tiles > CUS) {      // (k_experts_rows: a last round of up to a quarter or half of the CUs)
+    const double rounds = std::floor(tiles / CUS), rest = tiles / CUS - rounds;
+    return (r.fixed + depth * r.all) * (rounds + (rest == 0 ? 0.0 : rest <= 0.25 ? 0.4 : rest <= 0.5 ? 0.65 : 1.0));
+  }
   const double a_cu = std::ceil(tiles / CUS), rounds = std::floor(a_cu / r.per_cu), rest = a_cu - rounds * r.per_cu;
   const double last = rest > 0 ? r.fixed + depth * (r.one + (r.all - r.one) * (rest - 1) / (r.per_cu - 1)) : 0.0;
   return rounds * (r.fixed + depth * r.all) + last;
 }
 // The kind whose tiles take the shortest, for `tiles(side)` tiles
 template <class F>
-int best_tile(F tiles, double depth) {
+int best_tile(F tiles, double depth, bool split_rest = false) {
   int best = T64;
   double least = 1e300;
   for (int kind = 0; kind < KINDS; ++kind) {
-    const double t = tiles_time(kind, tiles(side_of(kind)), depth);
+    const double t = tiles_time(kind, tiles(side_of(kind)), depth, split_rest);
     if (t < least) {
       least = t;
       best = kind;
@@ -98,6 +102,14 @@ hipError_t allow_lds(K* kernel, int bytes) {
 struct ob_experts_ctx {
   ob_experts_config cfg;
   int device = -1;
+  // weight_grad with more than one workgroup a tile of 64 x 64: the most of them there is room for
+  int parts = 1;
+  void* mem = nullptr;
+  size_t bytes = 0;
+  float* d_partial = nullptr;
+  ~ob_experts_ctx() {
+    if (mem) (void)hipFree(mem);
+  }
   std::string hip_err;
 };
 
@@ -125,9 +137,10 @@ ob_status launch_few_rows(ob_experts_ctx* ctx, const RowsArgs& p, hipStream_t st
 template <class S, bool BF, int MODE>
 ob_status launch_weights(ob_experts_ctx* ctx, const WeightsArgs& p, hipStream_t stream) {
   const int64_t tiles = (int64_t)((p.height + S::BM - 1) / S::BM) * ((p.width + S::BN - 1) / S::BN);      // of a group
-  const int64_t grid = (tiles + 7) / 8 * 8 * p.groups.n;
+  const int64_t grid = (tiles + 7) / 8 * 8 * p.groups.n * p.parts;
   if (grid > 0x7fffffff) return OB_ERR_SIZE;
   hipLaunchKernelGGL((k_experts_weights<S, BF, MODE>), dim3((unsigned)grid), dim3(S::NT), (Product<S, BF, KS, KS, 1, 1, MODE>::LDS_BYTES), stream, p);
+  if (p.parts > 1) hipLaunchKernelGGL((k_experts_join<BF, MODE>), dim3((unsigned)(tiles * p.groups.n)), dim3(BLOCK), 0, stream, p);
   return hip_ok(ctx, hipGetLastError(), "k_experts_weights") ? OB_OK : OB_ERR_HIP;
 }
 
@@ -198,7 +211,7 @@ ob_status rows_call(ob_experts_ctx* ctx, const void* a, int64_t lda, const void*
   const hipStream_t s = static_cast<hipStream_t>(hip_stream);
   // (a group's last tile is half full in the mean)
   const double groups = (double)std::min<int64_t>(c.num_groups, rows);
-  const int kind = best_tile([&](int n) { return std::max(groups, rows / (double)n + 0.5 * groups) * (double)((width + n - 1) / n); }, (double)depth);
+  const int kind = best_tile([&](int n) { return std::max(groups, rows / (double)n + 0.5 * groups) * (double)((width + n - 1) / n); }, (double)depth, true);
   if (rows <= (p.a_direct && p.w_direct ? FEW_ROWS : FEW_ROWS_ANY) * groups) {
     const auto few = [&](auto mode) {
       if (c.dtype == OB_BF16) return strided ? launch_few_rows<true, KS, mode>(ctx, p, s) : launch_few_rows<true, KC, mode>(ctx, p, s);
@@ -232,6 +245,13 @@ ob_status ob_experts_create(const ob_experts_config* cfg, ob_experts_ctx** out) 
   if (!ctx->cfg.w_stride) ctx->cfg.w_stride = cfg->k * cfg->n;
   hipError_t e = hipGetDevice(&ctx->device);
   if (e == hipSuccess) e = cfg->dtype == OB_BF16 ? allow_experts<true>() : allow_experts<false>();
+  const int64_t tiles = cfg->num_groups * ((cfg->k + 63) / 64) * ((cfg->n + 63) / 64);
+  if (e == hipSuccess && tiles < 2 * CUS && cfg->max_rows >= 256) {
+    ctx->parts = (int)std::min<int64_t>((2 * CUS + tiles - 1) / tiles, 32);
+    ctx->bytes = (size_t)tiles * ctx->parts * 64 * 64 * sizeof(float);
+    e = hipMalloc(&ctx->mem, ctx->bytes);
+    ctx->d_partial = static_cast<float*>(ctx->mem);
+  }
   if (e != hipSuccess) {
     delete ctx;
     return OB_ERR_HIP;
@@ -241,7 +261,7 @@ ob_status ob_experts_create(const ob_experts_config* cfg, ob_experts_ctx** out) 
 }
 
 void ob_experts_destroy(ob_experts_ctx* ctx) { delete ctx; }
-size_t ob_experts_workspace_bytes(const ob_experts_ctx*) { return 0; }
+size_t ob_experts_workspace_bytes(const ob_experts_ctx* ctx) { return ctx ? ctx->bytes : 0; }
 const char* ob_experts_last_hip_error(const ob_experts_ctx* ctx) { return ctx ? ctx->hip_err.c_str() : ""; }
 
 ob_status ob_experts_forward(ob_experts_ctx* ctx, const void* x, int64_t ldx, const void* w, const int32_t* offsets, int64_t rows,
@@ -279,8 +299,18 @@ ob_status ob_experts_weight_grad(ob_experts_ctx* ctx, const void* x, int64_t ldx
   p.a_direct = at16(p.a) && p.lda % 8 == 0 && p.height % 8 == 0;
   p.b_direct = at16(p.b) && p.ldb % 8 == 0 && p.width % 8 == 0;
   const hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  const int kind = best_tile([&](int n) { return (double)c.num_groups * ((p.height + n - 1) / n) * ((p.width + n - 1) / n); },
-                             (double)rows / c.num_groups);
+  const auto tiles = [&](int n) { return (double)c.num_groups * ((p.height + n - 1) / n) * ((p.width + n - 1) / n); };
+  const double depth = (double)rows / c.num_groups;
+  int kind = best_tile(tiles, depth);
+  // Few tiles of many rows: several workgroups each, as many as fill the card twice and have 128 rows or more.  Adding up
+  // takes about 4 us.
+  p.parts = 1;
+  p.partial = ctx->d_partial;
+  const int parts = (int)std::min({(double)ctx->parts, std::floor(depth / 128), std::ceil(2 * CUS / tiles(64))});
+  if (parts > 1 && 4.0 + tiles_time(T64, tiles(64) * parts, depth / parts) < tiles_time(kind, tiles(side_of(kind)), depth)) {
+    kind = T64;
+    p.parts = parts;
+  }
   return with_tile_and_mode(kind, p.a_direct && p.b_direct, [&](auto n, auto mode) {
     using S = Tile<n, 64>;
     return c.dtype == OB_BF16 ? launch_weights<S, true, mode>(ctx, p, s) : launch_weights<S, false, mode>(ctx, p, s);

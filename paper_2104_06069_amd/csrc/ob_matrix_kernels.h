@@ -355,33 +355,47 @@ __global__ __launch_bounds__(256, 2) void k_experts_few_rows(RowsArgs p) {
   if (r0 + r < t.rows) store4(p.out, p.out_dtype, (t.lo + r0 + r) * p.ldo + c0 + c, p.width - c0 - c, v);
 }
 
-// weight_grad: out_g = a_g^T b_g, a [rows, height], b [rows, width], out [height, width].
+// weight_grad: out_g = a_g^T b_g, a [rows, height], b [rows, width], out [height, width].  Where the tiles are too few for the card
+// each has `parts` workgroups, a share of the group's rows each: their sums go to `partial`, and k_experts_join adds them up.  (The
+// last one to arrive adding them up in the same launch was tried: making the others' sums visible across the dies took three
+// times as long as all the rest, 94 us in place of 33 without parts.)
 struct WeightsArgs {
   Groups groups;
   const uint16_t* a;
   const uint16_t* b;
   void* out;
+  float* partial;           // [groups * tiles][parts][BM][BN]
   int64_t lda, ldb, out_stride;
-  int height, width, out_dtype, accumulate;
+  int height, width, out_dtype, accumulate, parts;
   bool a_direct, b_direct;
 };
 template <class S, bool BF, int MODE>
 __global__ __launch_bounds__(S::NT, 2) void k_experts_weights(WeightsArgs p) {
   using P = Product<S, BF, KS, KS, 1, 1, MODE>;
+  using R = Results<S>;
   const int nm = (p.height + S::BM - 1) / S::BM, nn = (p.width + S::BN - 1) / S::BN;
   // Each die (tile_of_workgroup) gets an eighth of every group's tiles, whose cost goes with the group's rows.
-  const int share = (nm * nn + 7) / 8, place = blockIdx.x >> 3, g = place / share, t = (blockIdx.x & 7) * share + place % share;
+  const int share = (nm * nn + 7) / 8, all = blockIdx.x >> 3, part = all % p.parts, place = all / p.parts, g = place / share;
+  const int t = (blockIdx.x & 7) * share + place % share;
   if (g >= p.groups.n || t >= nm * nn) return;
   int tm, tn, lo, hi;
   tile_in_bands(t, nm, nn, &tm, &tn);
   p.groups.range(g, &lo, &hi);
   const int r0 = tile_start<MODE>(tm, S::BM, p.height), c0 = tile_start<MODE>(tn, S::BN, p.width), row0 = tm * S::BM, col0 = tn * S::BN;
   typename P::Acc acc = {};
-  if (hi > lo) {
-    const Operand a{p.a + lo * p.lda, 0, p.lda, p.height, p.a_direct}, b{p.b + lo * p.ldb, 0, p.ldb, p.width, p.b_direct};
-    P::run(a, b, r0, c0, 0, hi - lo, lds_of_launch, acc);
-  } else if (p.accumulate) {
+  const int each = ((hi - lo + p.parts - 1) / p.parts + S::BK - 1) / S::BK * S::BK, first = lo + part * each, rows = min(each, hi - first);
+  if (rows > 0) {
+    const Operand a{p.a + first * p.lda, 0, p.lda, p.height, p.a_direct}, b{p.b + first * p.ldb, 0, p.ldb, p.width, p.b_direct};
+    P::run(a, b, r0, c0, 0, rows, lds_of_launch, acc);
+  } else if (p.accumulate && p.parts == 1) {
     return;
+  }
+  if constexpr (S::BM == 64) {      // (larger tiles are not split)
+    if (p.parts > 1) {
+      float* const sums = p.partial + ((int64_t)(g * nm * nn + t) * p.parts + part) * (S::BM * S::BN);
+      R::by_rows(acc, lds_of_launch, [&](int r, int c, v4f v) { *reinterpret_cast<v4f*>(sums + r * S::BN + c) = v; });
+      return;
+    }
   }
   if (!p.accumulate) {
     void* const out = static_cast<char*>(p.out) + g * p.out_stride * (p.out_dtype == F32 ? 4 : 2);
@@ -389,15 +403,42 @@ __global__ __launch_bounds__(S::NT, 2) void k_experts_weights(WeightsArgs p) {
     return;
   }
   float* const sums = static_cast<float*>(p.out) + g * p.out_stride;
-  Results<S>::visit(acc, lds_of_launch, [&](const float* own, int tr, int tc) {
+  R::visit(acc, lds_of_launch, [&](const float* own, int tr, int tc) {
     const auto mine = [&](int r, int c) { return r >= row0 && r < p.height && c + 3 >= col0; };
-    Results<S>::template pass<true>(
+    R::template pass<true>(
         own, r0 + tr, c0 + tc,
         [&](int r, int c) { return mine(r, c) ? load4(sums, F32, (int64_t)r * p.width + c, p.width - c) : v4f{}; },
         [&](int r, int c, v4f v, v4f before) {
           if (mine(r, c)) store_from(sums, (int64_t)r * p.width + c, p.width - c, col0 - c, v + before);
         });
   });
+}
+
+// The parts' sums, in their order.  A workgroup a tile.
+template <bool BF, int MODE>
+__global__ __launch_bounds__(BLOCK) void k_experts_join(WeightsArgs p) {
+  constexpr int N = 64;
+  const int nm = (p.height + N - 1) / N, nn = (p.width + N - 1) / N, g = blockIdx.x / (nm * nn);
+  int tm, tn;
+  tile_in_bands(blockIdx.x - g * nm * nn, nm, nn, &tm, &tn);
+  const int r0 = tile_start<MODE>(tm, N, p.height), c0 = tile_start<MODE>(tn, N, p.width), row0 = tm * N, col0 = tn * N;
+  const float* const sums = p.partial + (int64_t)blockIdx.x * p.parts * (N * N);
+#pragma unroll
+  for (int u = 0; u < N * N / 4 / BLOCK; ++u) {
+    const int k = threadIdx.x + u * BLOCK, r = r0 + k / (N / 4), c = c0 + k % (N / 4) * 4;
+    if (r < row0 || r >= p.height || c + 3 < col0 || c >= p.width) continue;
+    const int64_t at = g * p.out_stride + (int64_t)r * p.width + c;
+    v4f v = {};
+    for (int j = 0; j < p.parts; ++j) v += *reinterpret_cast<const v4f*>(sums + j * (N * N) + k * 4);
+    if (p.accumulate) v += load4(p.out, F32, at, p.width - c);
+    if (p.out_dtype == F32) {
+      store_from(p.out, at, p.width - c, col0 - c, v);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (c + e >= col0 && c + e < p.width) static_cast<uint16_t*>(p.out)[at + e] = to_bits(v[e], BF);
+    }
+  }
 }
 
 // ---- orthogonalised update -----------------------------------------------------------------------------------------
