@@ -257,11 +257,11 @@ __global__ __launch_bounds__(S::NT, 2) void k_experts_rows(RowsArgs p) {
 }
 
 // The same for few rows a group, where what counts is how fast the weights of the groups that have any are read.  A workgroup has
-// 16 rows by 32 columns; its wavefronts share out the slabs of K, each with slabs of its own in LDS and no barriers, so that
-// up to 4 x 3 slabs are under way at once, and their sums are added in a fixed order at the end.
+// 16 rows by 32 columns (64 where a row of W in memory runs along them, 128 bytes of each at once); its wavefronts share out the slabs of K, each with slabs of its own in LDS and no barriers, so that
+// up to 4 x 3 (or 4 x 2) slabs are under way at once, and their sums are added in a fixed order at the end.
 template <bool BF, int FB, int MODE>
 struct FewRows {
-  static constexpr int BM = 16, BN = 32, BK = 64, WAVES = 4, STAGES = 3;
+  static constexpr int BM = 16, BN = FB == KS ? 64 : 32, BK = 64, WAVES = 4, STAGES = FB == KS ? 2 : 3;
   using A = Slab<KC, BM, BK, 64>;
   using B = Slab<FB, BN, BK, 64>;
   static constexpr int STAGE = (BM + BN) * BK, STRIDE = BN + 4;
@@ -287,13 +287,13 @@ __global__ __launch_bounds__(256, 2) void k_experts_few_rows(RowsArgs p) {
   B sb;
   sa.init(a, r0, lane);
   sb.init(b, c0, lane);
-  v4f acc[2] = {};
+  v4f acc[F::BN / 16] = {};
   const auto multiply = [&](const uint16_t* s) {
 #pragma unroll
     for (int kk = 0; kk < F::BK / 32; ++kk) {
       const v8s fa = A::fragment(s, 0, kk, lane);
 #pragma unroll
-      for (int j = 0; j < 2; ++j) acc[j] = mma<BF>(B::fragment(s + F::BM * F::BK, j * 16, kk, lane), fa, acc[j]);
+      for (int j = 0; j < F::BN / 16; ++j) acc[j] = mma<BF>(B::fragment(s + F::BM * F::BK, j * 16, kk, lane), fa, acc[j]);
     }
   };
   // slabs wave, wave + 4, ..
@@ -322,7 +322,7 @@ __global__ __launch_bounds__(256, 2) void k_experts_few_rows(RowsArgs p) {
     const auto load = [&](int i) {
       uint16_t* const s = own + i % F::STAGES * F::STAGE;
       sa.load(a, 0, r0, column(i), s, 0);
-      sb.load(b, 0, c0, column(i), s + F::BM * F::BK, 0);
+      sb.template load<true>(b, 0, c0, column(i), s + F::BM * F::BK, 0);
     };
 #pragma unroll
     for (int i = 0; i < F::STAGES; ++i)
@@ -344,7 +344,7 @@ __global__ __launch_bounds__(256, 2) void k_experts_few_rows(RowsArgs p) {
   }
   float* const sums = reinterpret_cast<float*>(own);
 #pragma unroll
-  for (int j = 0; j < 2; ++j) *in_lds<v4f>(sums + (lane & 15) * F::STRIDE + j * 16 + 4 * (lane >> 4)) = acc[j];
+  for (int j = 0; j < F::BN / 16; ++j) *in_lds<v4f>(sums + (lane & 15) * F::STRIDE + j * 16 + 4 * (lane >> 4)) = acc[j];
   __syncthreads();
   if (threadIdx.x >= F::BM * F::BN / 4) return;
   const int r = threadIdx.x / (F::BN / 4), c = threadIdx.x % (F::BN / 4) * 4;

@@ -81,6 +81,8 @@ struct Slab {
   }
 
   // A slab whose BK columns all exist, of an operand with `direct`: rows past the last repeat one that exists.
+  // ONCE: what is read by this workgroup alone (not kept in the caches).
+  template <bool ONCE = false>
   __device__ void load(const Operand& o, int term, int r0, int k0, uint16_t* lds, int wave) const {
     if (WORK < NT && wave >= WORK / 64) return;
     const uint16_t* const base = o.p + term * o.term;
@@ -89,7 +91,7 @@ struct Slab {
       const uint16_t* src;
       if constexpr (FORM == KC) src = base + (int64_t)r0 * o.ld + k0 + off[j];
       else src = base + (int64_t)(k0 + j * STEP) * o.ld + r0 + off[j % OFFS];
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, in_lds<void>(lds + wave * 512 + j * WORK * 8), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, in_lds<void>(lds + wave * 512 + j * WORK * 8), 16, 0, ONCE ? 2 : 0);
     }
   }
 

@@ -29,6 +29,9 @@ class ExpertLinear:
             raise ValueError("layout is 'kn' or 'nk', dtype torch.float16 or torch.bfloat16")
         self.w_shape = (self.groups, self.k, self.n) if layout == "kn" else (self.groups, self.n, self.k)
         self.w_stride = int(w_stride) or self.k * self.n
+        self._w_dense, self._offsets_shape = (self.w_stride, self.w_shape[2], 1), (self.groups + 1,)
+        self._index = torch.cuda.current_device()
+        self._forward, self._input_grad = ob.lib().ob_experts_forward, ob.lib().ob_experts_input_grad
         self.ctx = ob.ob_experts_create(self.groups, self.k, self.n, _OB_DTYPE[dtype], _LAYOUTS[layout], max_rows, w_stride)
 
     def close(self):
@@ -63,25 +66,35 @@ class ExpertLinear:
         if t.dtype != torch.int32 or t.dim() != 1 or t.numel() != self.groups + 1 or not t.is_contiguous() or t.device != self.device:
             raise ValueError(f"offsets: {self.groups + 1} adjacent int32 on {self.device}")
 
-    def _product(self, call, a, depth, width, w, offsets, out, out_dtype, names):
-        lda = self._rows(a, depth, (self.dtype,), names[0])
-        self._weights(w, (self.dtype,), "w")
-        self._offsets(offsets)
+    def _product(self, call, where, a, depth, width, w, offsets, out, out_dtype, names):
+        # (a token's product takes 5 us on the device: the common case is looked at as a whole, anything else piece by piece)
+        rows, lda = a.shape[0], depth
+        if not (a.dtype is self.dtype and w.dtype is self.dtype and offsets.dtype is torch.int32 and a.shape == (rows, depth)
+                and a.stride() == (depth, 1) and w.shape == self.w_shape and w.stride() == self._w_dense and offsets.shape == self._offsets_shape
+                and offsets.is_contiguous() and a.get_device() == w.get_device() == offsets.get_device() == self._index):
+            lda = self._rows(a, depth, (self.dtype,), names[0])
+            self._weights(w, (self.dtype,), "w")
+            self._offsets(offsets)
         if out is None:
-            out = torch.empty(a.shape[0], width, device=self.device, dtype=out_dtype or self.dtype)
-        ldo = self._rows(out, width, (self.dtype, torch.float32), names[1])
-        if out.shape[0] != a.shape[0]:
-            raise ValueError(f"{names[1]}: {a.shape[0]} rows")
-        call(self.ctx, a, lda, w, offsets, a.shape[0], out, ldo, _OB_DTYPE[out.dtype], _current_stream(self.device))
+            out = torch.empty((rows, width), device=self.device, dtype=out_dtype or self.dtype)
+            ldo = width
+        else:
+            ldo = self._rows(out, width, (self.dtype, torch.float32), names[1])
+            if out.shape[0] != rows:
+                raise ValueError(f"{names[1]}: {rows} rows")
+        status = call(self.ctx, a.data_ptr(), lda, w.data_ptr(), offsets.data_ptr(), rows, out.data_ptr(), ldo, _OB_DTYPE[out.dtype],
+                      _current_stream(self.device))
+        if status:
+            raise ob.ObLambError(status, where, ob.lib().ob_experts_last_hip_error(self.ctx).decode())
         return out
 
     def forward(self, x, w, offsets, out=None, out_dtype=None):
         """y[r] = x[r] W_g.  Rows that belong to no expert are not written."""
-        return self._product(ob.ob_experts_forward, x, self.k, self.n, w, offsets, out, out_dtype, ("x", "out"))
+        return self._product(self._forward, "ob_experts_forward", x, self.k, self.n, w, offsets, out, out_dtype, ("x", "out"))
 
     def input_grad(self, dy, w, offsets, out=None, out_dtype=None):
         """dx[r] = dy[r] W_g^T.  Rows that belong to no expert are not written."""
-        return self._product(ob.ob_experts_input_grad, dy, self.n, self.k, w, offsets, out, out_dtype, ("dy", "out"))
+        return self._product(self._input_grad, "ob_experts_input_grad", dy, self.n, self.k, w, offsets, out, out_dtype, ("dy", "out"))
 
     def weight_grad(self, x, dy, offsets, out=None, out_dtype=None, accumulate=False):
         """dW_g = x_g^T dy_g, or with accumulate (a float32 `out`) dW_g += x_g^T dy_g."""
