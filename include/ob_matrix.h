@@ -46,7 +46,7 @@ typedef struct ob_experts_config {
   int32_t w_layout;   /* OB_EXPERTS_KN or OB_EXPERTS_NK, of W and dW */
   int32_t reserved;   /* 0 */
   int64_t k, n;       /* 1 .. 2^20 each */
-  int64_t max_rows;   /* largest `rows` of a call: 0 .. 2^30 */
+  int64_t max_rows;   /* largest `rows` of a call: 0 .. 2^26 */
   int64_t w_stride;   /* elements from W_g to W_(g+1), and from dW_g to dW_(g+1); >= k * n, or 0 for k * n */
 } ob_experts_config;
 

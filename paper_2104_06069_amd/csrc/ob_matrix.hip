@@ -236,7 +236,7 @@ ob_status ob_experts_create(const ob_experts_config* cfg, ob_experts_ctx** out) 
   const int64_t most = (int64_t)1 << 20;
   if (cfg->num_groups < 1 || cfg->num_groups > 65536 || (cfg->dtype != OB_F16 && cfg->dtype != OB_BF16) ||
       (cfg->w_layout != OB_EXPERTS_KN && cfg->w_layout != OB_EXPERTS_NK) || cfg->reserved != 0 || cfg->k < 1 || cfg->k > most ||
-      cfg->n < 1 || cfg->n > most || cfg->max_rows < 0 || cfg->max_rows > ((int64_t)1 << 30) ||
+      cfg->n < 1 || cfg->n > most || cfg->max_rows < 0 || cfg->max_rows > ((int64_t)1 << 26) ||
       (cfg->w_stride != 0 && cfg->w_stride < cfg->k * cfg->n) || cfg->w_stride > ((int64_t)1 << 44))
     return OB_ERR_ARG;
   ob_experts_ctx* ctx = new (std::nothrow) ob_experts_ctx();

@@ -229,3 +229,41 @@ def test_refusals_of_the_python_class():
     from paper_2104_06069_amd import ObLambError
     with pytest.raises(ObLambError):
         op.forward(torch.cat([x, x]), w, offsets)      # more rows than max_rows
+
+
+@pytest.mark.parametrize("counts,k,n", [([3000, 10, 0, 2000], 64, 64), ([5000, 1], 128, 200), ([1, 4000, 700], 72, 70), ([2000], 33, 129)])
+@pytest.mark.parametrize("layout", ("kn", "nk"))
+def test_weight_gradients_of_few_tiles_and_many_rows(counts, k, n, layout):
+    """Several workgroups share the rows of a tile."""
+    x, dy, w, offsets = inputs(counts, k, n, torch.bfloat16, layout)
+    op = layer(len(counts), k, n, max_rows=x.shape[0], layout=layout)
+    mark = torch.full(op.w_shape, 77.0, device="cuda")
+    dw = op.weight_grad(x, dy, offsets, out=mark)
+    low = op.weight_grad(x, dy, offsets)
+    start = torch.randn(op.w_shape, device="cuda")
+    assert torch.equal(op.weight_grad(x, dy, offsets, out=start.clone(), accumulate=True), start + dw)
+    assert torch.equal(low, dw.to(torch.bfloat16))
+    assert torch.equal(op.weight_grad(x, dy, offsets, out_dtype=torch.float32), dw)
+    ends, xd, dyd = offsets.tolist(), x.double().cpu(), dy.double().cpu()
+    dwc = dw.cpu() if layout == "kn" else dw.cpu().transpose(1, 2)
+    for g, (a, b) in enumerate(zip(ends[:-1], ends[1:])):
+        near(dwc[g], xd[a:b].T @ dyd[a:b], xd[a:b].T.abs() @ dyd[a:b].abs(), b - a, f"dw of group {g}")
+
+
+def test_tables_that_are_none_at_any_row_count():
+    """Overlapping and reversed ranges in each kernel: nothing is read or written out of bounds (the results are not defined)."""
+    for rows, k, n in ((24, 64, 64), (600, 128, 136), (9000, 256, 512)):
+        x, dy, w, _ = inputs([rows], k, n, torch.bfloat16, "kn")
+        w = w.expand(4, k, n).contiguous()
+        op = layer(4, k, n, max_rows=rows)
+        for table in ([0, rows, 0, rows, 0], [rows, 0, rows, 5, 1], [-9, -3, rows + 7, rows, 1 << 30], [0, rows, rows, rows, rows]):
+            offsets = torch.tensor(table, dtype=torch.int32, device="cuda")
+            op.forward(x, w, offsets)
+            op.backward(x, dy, w, offsets)
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("counts,k,n", [([16384 - 300, 300], 64, 1024), ([4000, 2000, 96, 4000], 96, 2048), ([20000], 40, 520)])
+def test_last_round_of_large_tiles(counts, k, n):
+    """More tiles than the card has CUs, so that those of the last round are split."""
+    check(counts, k, n, torch.bfloat16, "kn")
