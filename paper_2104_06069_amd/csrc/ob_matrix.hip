@@ -325,7 +325,7 @@ namespace {
 // Matrices that go through the steps together, and the tiles of their products
 struct Part {
   bool follow_s = false;      // the way that follows S (ob_matrix_kernels.h); else step by step
-  int terms = 2;
+  int terms = 2, table = 0;
   int sym_tile = T64, apply_tile = T64;
   // tiles of X X^T, of the other symmetric products (the same ones, but not in the same order: only there depths differ by n)
   // and of B X
@@ -631,32 +631,37 @@ ob_status create(const ob_muon_config* cfg, ob_muon_ctx* ctx) {
     square.clear();
   }
   // 11 bits, step by step: 12.5 n / m + 2.5 (in m^3, 5 steps); 22 bits, following S with one S, which will do there: three
-  // times 1.5 n / m + 8.5, less from n = 3 m on, which is worth launches of its own where there is much of it.
+  // times 1.5 n / m + 8.5, less from n = 3 m on.  With 22 bits following S takes as many multiply-adds as step by step for
+  // n = m, and more launches and writes (8 of 1024 x 1024: 1010 and 787 us, 4 of 1024 x 4096: 895 and 1277).  Each of the
+  // two ways is worth launches of its own where there is much for it.
+  const bool fine = cfg->precision == OB_F32;
+  constexpr double MUCH = 1e10;
   std::vector<int> each[2];
-  double narrow = 0;
+  double work[2] = {};
   for (size_t i = 0; i < mats.size(); ++i) {
-    const bool f = cfg->precision == OB_F32 || mats[i].np >= 3 * mats[i].mp;
+    const bool f = mats[i].np >= (fine ? 1.5 : 3.0) * mats[i].mp;
     each[f].push_back((int)i);
-    if (f) narrow += (double)mats[i].mp * mats[i].mp * mats[i].np;
+    work[f] += (double)mats[i].mp * mats[i].mp * mats[i].np;
   }
-  if (cfg->precision == OB_F16 && narrow < 1e10) {
-    each[0].insert(each[0].end(), each[1].begin(), each[1].end());
-    each[1].clear();
+  if (work[1] < MUCH || (fine && work[0] < MUCH)) {
+    std::vector<int>& all = each[fine];
+    all.insert(all.end(), each[!fine].begin(), each[!fine].end());
+    each[!fine].clear();
   }
   std::vector<ListTile> tables[2][3];
   for (const int f : {1, 0}) {
     if (each[f].empty() || ctx->small_lds) continue;
     Part part;
-    part.terms = f ? 2 : 1;
-    part.sym_tile = product_tile(mats, each[f], true, f == 1);
-    part.apply_tile = product_tile(mats, each[f], false, f == 1);
+    part.terms = f || fine ? 2 : 1;
+    part.sym_tile = product_tile(mats, each[f], true, part.terms == 2);
+    part.apply_tile = product_tile(mats, each[f], false, part.terms == 2);
     for (const ProductKind k : {GRAM, SYMMETRIC, APPLY}) {
       tables[f][k] = product_tiles(mats, each[f], side_of(k == APPLY ? part.apply_tile : part.sym_tile), k);
       if (tables[f][k].size() > 0x7fffffff) return OB_ERR_SIZE;
       part.grid[k] = (int)tables[f][k].size();
     }
-    // With 22 bits following S takes fewer multiply-adds for n > m, but a launch more for every step but the first of each S
-    part.follow_s = f == 1 && (cfg->precision == OB_F16 || following_pays(ctx, mats, each[1], part));
+    part.follow_s = f == 1 && (!fine || following_pays(ctx, mats, each[1], part));
+    part.table = f;
     ctx->parts.push_back(part);
   }
   for (int kind = 0; kind < KINDS; ++kind) {
@@ -697,8 +702,8 @@ ob_status create(const ob_muon_config* cfg, ob_muon_ctx* ctx) {
                   hip_ok(ctx, hipMemcpy(ctx->d_square, square.data(), square.size() * sizeof(SquareTile), hipMemcpyHostToDevice), "hipMemcpy");
   for (Part& part : ctx->parts)
     for (const int k : {0, 1, 2}) {
-      const std::vector<ListTile>& table = tables[part.terms == 2][k];
-      part.d_tiles[k] = reinterpret_cast<ListTile*>(base + at_table[part.terms == 2][k]);
+      const std::vector<ListTile>& table = tables[part.table][k];
+      part.d_tiles[k] = reinterpret_cast<ListTile*>(base + at_table[part.table][k]);
       ok = ok && hip_ok(ctx, hipMemcpy(part.d_tiles[k], table.data(), table.size() * sizeof(ListTile), hipMemcpyHostToDevice), "hipMemcpy");
     }
   return ok ? OB_OK : OB_ERR_HIP;
