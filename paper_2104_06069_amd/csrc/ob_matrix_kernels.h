@@ -487,6 +487,16 @@ __device__ __forceinline__ void store_terms(uint16_t* plane, int64_t term, int64
   if constexpr (TERMS == 2) *reinterpret_cast<v4h*>(plane + term + at) = lo;
 }
 
+template <int TERMS>
+__device__ __forceinline__ void store_terms8(uint16_t* plane, int64_t term, int64_t at, v4f a, v4f b) {
+  v4h ha, la, hb, lb;
+  split4(a, &ha, &la);
+  split4(b, &hb, &lb);
+  typedef unsigned short v8u __attribute__((ext_vector_type(8)));
+  *reinterpret_cast<v8u*>(plane + at) = __builtin_shufflevector(ha, hb, 0, 1, 2, 3, 4, 5, 6, 7);
+  if constexpr (TERMS == 2) *reinterpret_cast<v8u*>(plane + term + at) = __builtin_shufflevector(la, lb, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
 // Two ways through the Newton-Schulz steps X <- B X, B = a + b S + c S^2, S = X X^T, of which the first two products of three
 // are symmetric: half their tiles are computed, each written on both sides of the diagonal.
 //
@@ -535,32 +545,40 @@ __global__ __launch_bounds__(S::NT, 2) void k_polar_symmetric(SymmetricArgs p) {
   uint16_t* const out = p.out[which] + t.e;
   const uint16_t* const add = which == 0 && p.add ? p.add + t.e : nullptr;
   const float mul = p.mul[which], diag = which == 0 ? p.diag : 0.0f;
-  // Element (r + e dr, c + e dc) is element e of the four from (r, c) on; all of them lie in a row of `out` (and of ADD), turned over
+  // Element (r + e dr, c + e dc) is element e of the eight from (r, c) on; all of them lie in a row of `out` (and of ADD), turned over
   // the diagonal where dr is 1.
   const auto half = [&](const float* own, int r0, int c0, auto rowwise) {
     constexpr int dr = rowwise ? 0 : 1, dc = rowwise ? 1 : 0;
     const auto at = [&](int r, int c) { return rowwise ? (int64_t)(tr + r) * mp + tc + c : (int64_t)(tc + c) * mp + tr + r; };
     const auto inside = [&](int r, int c) { return tr + r < mp && tc + c < mp; };
-    R::template pass<rowwise>(
+    using Eight = typename R::Eight;
+    R::template pass8<rowwise>(
         own, r0, c0,
         [&](int r, int c) {
-          v4f v = {};
+          Eight v = {};
           if (add && inside(r, c)) {
-            const v4h hi = *reinterpret_cast<const v4h*>(add + at(r, c));
-            v4h lo = {};
-            if constexpr (TERMS == 2) lo = *reinterpret_cast<const v4h*>(add + p.term + at(r, c));
+            const v8s hi = *reinterpret_cast<const v8s*>(add + at(r, c));
+            v8s lo = {};
+            if constexpr (TERMS == 2) lo = *reinterpret_cast<const v8s*>(add + p.term + at(r, c));
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = p.add_mul * (from_bits(hi[e], false) + from_bits(lo[e], false));
+            for (int e = 0; e < 4; ++e) {
+              v.a[e] = p.add_mul * (from_bits((unsigned short)hi[e], false) + from_bits((unsigned short)lo[e], false));
+              v.b[e] = p.add_mul * (from_bits((unsigned short)hi[e + 4], false) + from_bits((unsigned short)lo[e + 4], false));
+            }
           }
           return v;
         },
-        [&](int r, int c, v4f v, v4f w) {
+        [&](int r, int c, Eight v, Eight w) {
           if (!inside(r, c)) return;
-          v = v * mul + w;
+          v.a = v.a * mul + w.a;
+          v.b = v.b * mul + w.b;
+          const int off = (tc + c) - (tr + r);      // (0: the first of the eight is on the diagonal)
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (tr + r + e * dr == tc + c + e * dc) v[e] += diag;
-          store_terms<TERMS>(out, p.term, at(r, c), v);
+          for (int e = 0; e < 4; ++e) {
+            if (off + e * (dc - dr) == 0) v.a[e] += diag;
+            if (off + (e + 4) * (dc - dr) == 0) v.b[e] += diag;
+          }
+          store_terms8<TERMS>(out, p.term, at(r, c), v.a, v.b);
         });
   };
   R::visit(acc, lds_of_launch, [&](const float* own, int r0, int c0) {
@@ -599,10 +617,13 @@ __global__ __launch_bounds__(S::NT, 2) void k_polar_apply(ApplyArgs p) {
   const int tr = t.tm * S::BM, tc = t.tn * S::BN;
   P::run(a, b, tr, tc, 0, t.mp, lds_of_launch, acc);
   if constexpr (!LAST) {
-    R::by_rows(acc, lds_of_launch, [&](int r, int c, v4f v) {
-      r += tr;
-      c += tc;
-      if (r < t.mp && c < t.np) store_terms<2>(p.out + t.x, p.x_term, (int64_t)r * t.np + c, v * p.mul);
+    using Eight = typename R::Eight;
+    R::visit(acc, lds_of_launch, [&](const float* own, int r0, int c0) {
+      R::template pass8<true>(
+          own, tr + r0, tc + c0, [](int, int) { return Eight{}; },
+          [&](int r, int c, Eight v, Eight) {
+            if (r < t.mp && c < t.np) store_terms8<2>(p.out + t.x, p.x_term, (int64_t)r * t.np + c, v.a * p.mul, v.b * p.mul);
+          });
     });
   } else {
     const Matrix& m = p.mats[t.mat];

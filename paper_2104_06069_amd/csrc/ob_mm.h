@@ -249,6 +249,45 @@ struct Results {
     }
   }
 
+  // The same for eight adjacent elements at a time; values and before()'s are pairs of v4f.
+  struct Eight {
+    v4f a, b;
+  };
+  template <bool ROWWISE, class F, class G>
+  __device__ static __forceinline__ void pass8(const float* own, int r0, int c0, F before, G after) {
+    constexpr int EACH = ROWS * WIDTH / 512, BATCH = EACH < 2 ? EACH : 2;
+    static_assert(EACH >= 1, "a piece for every lane");
+    const int lane = threadIdx.x & 63;
+#pragma unroll 1
+    for (int k0 = lane; k0 < EACH * 64; k0 += BATCH * 64) {
+      Eight v[BATCH], w[BATCH];
+#pragma unroll
+      for (int u = 0; u < BATCH; ++u) {
+        const int k = k0 + u * 64;
+        if constexpr (ROWWISE) {
+          const int r = k / (WIDTH / 8), c = k % (WIDTH / 8) * 8;
+          v[u].a = *in_lds<const v4f>(own + r * STRIDE + c);
+          v[u].b = *in_lds<const v4f>(own + r * STRIDE + c + 4);
+          w[u] = before(r0 + r, c0 + c);
+        } else {
+          const int c = k / (ROWS / 8), r = k % (ROWS / 8) * 8;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            v[u].a[e] = *in_lds<const float>(own + (r + e) * STRIDE + c);
+            v[u].b[e] = *in_lds<const float>(own + (r + e + 4) * STRIDE + c);
+          }
+          w[u] = before(r0 + r, c0 + c);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < BATCH; ++u) {
+        const int k = k0 + u * 64;
+        if constexpr (ROWWISE) after(r0 + k / (WIDTH / 8), c0 + k % (WIDTH / 8) * 8, v[u], w[u]);
+        else after(r0 + k % (ROWS / 8) * 8, c0 + k / (ROWS / 8), v[u], w[u]);
+      }
+    }
+  }
+
   // by(own, r0, c0): what to do with `own`, the rows r0 .. and columns c0 .. of the tile that this wavefront has turned (see
   // pass()).  To be called after Product::run, whose last barrier ends the reads of LDS.
   template <class F>
