@@ -10,8 +10,9 @@
 // 128 x 64 of it and reads 12 KB of LDS for each 32 columns of K, 768 of the 1024 cycles that the eight wavefronts' matrix
 // instructions take.  The wavefronts are therefore two groups that take turns, half a step apart: while one reads its
 // operands from LDS (and starts the loads of the next K slab from memory straight into LDS), the other has the matrix
-// cores.  Measured at 8192^3 with binary16 operands: 1130 to 1190 TFLOP/s (the library's product of the same: 1405), with
-// two terms 1370 to 1425 TFLOP/s of matrix instructions (three products out of each two slabs read); 128 x 128 tiles 960.
+// cores.  Measured at 8192^3: 1190 to 1310 TFLOP/s with bfloat16 operands (the library's product of the same: 1314), with
+// two terms 1370 to 1495 TFLOP/s of matrix instructions (three products out of each two slabs read); 128 x 128 tiles of four
+// wavefronts 1130 and 1090, 64 x 64 ones 760.
 //
 // LDS holds 16-byte pieces in the order in which the loads bring them.  Which piece of its row a lane fetches is permuted
 // by the row's number, so that the reads below do not meet in the same banks.
