@@ -522,8 +522,10 @@ void step_by_step(ob_muon_ctx* ctx, const Part& part, const Finish& finish, hipS
     const float a = ctx->coefficients[3 * k], b = ctx->coefficients[3 * k + 1], c = ctx->coefficients[3 * k + 2];
     const float per_gram = E_UNIT / (X_UNIT * X_UNIT);
     SymmetricArgs g{part.d_tiles[GRAM], ctx->d_x[k & 1], {}, nullptr, {E}, ctx->x_plane, ctx->e_plane, {per_gram}, 0.0f, 0.0f};
+    Shifted form = {};
     if (c != 0.0f) {
-      g.diag = b / (2.0f * c) * E_UNIT;
+      form = shifted(a, b, c);
+      g.diag = -form.t * E_UNIT;
     } else {      // B = a + b S from the first product alone
       g.out[0] = B;
       g.mul[0] = b * per_gram;
@@ -531,8 +533,8 @@ void step_by_step(ob_muon_ctx* ctx, const Part& part, const Finish& finish, hipS
     }
     symmetric<TERMS, true>(part, g, 1, stream);
     if (c != 0.0f) {
-      const float d = (float)(((double)a - (double)b * b / (4.0 * c)) * E_UNIT);
-      symmetric<TERMS, false>(part, SymmetricArgs{part.d_tiles[SYMMETRIC], E, {E}, nullptr, {B}, 0, ctx->e_plane, {c / E_UNIT}, 0.0f, d}, 1, stream);
+      symmetric<TERMS, false>(part, SymmetricArgs{part.d_tiles[SYMMETRIC], E, {E}, form.linear != 0.0f ? E : nullptr, {B}, 0, ctx->e_plane, {c / E_UNIT},
+                                                  form.linear, form.constant * E_UNIT}, 1, stream);
     }
     apply<TERMS>(part, ApplyArgs{part.d_tiles[APPLY], ctx->d_mats, B, ctx->d_x[k & 1], ctx->d_x[(k & 1) ^ 1], ctx->e_plane, ctx->x_plane, 1.0f / E_UNIT, finish},
                  k + 1 == ctx->steps, stream);

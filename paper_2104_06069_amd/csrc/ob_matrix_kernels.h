@@ -512,8 +512,19 @@ __device__ __forceinline__ void store_terms8(uint16_t* plane, int64_t term, int6
 //
 // With 11 bits for the [m, m] matrices those errors would be 1e-1, so there the plain order stays: with c != 0,
 // a + b S + c S^2 = c E^2 + d, E = S - t, t = -b / 2c, d = a - b^2 / 4c, one product E E^T and nothing to read beside it, and
-// where the singular values end up (S near 1) E is small, and so is what its rounding costs.  X keeps two terms: rounding it
-// to 11 bits would drown the small singular vectors of a matrix of low rank (3e-2 in place of 2e-3).
+// where the singular values end up (S near 1) E is small, and so is what its rounding costs.  A c that is small beside b would
+// put t, and with it E's rounding errors, far beyond S; outside of [0, 2], which S ends in the middle of, t is 1 and E is read
+// once more for the term that is left, (b + 2 c t) E.  X keeps two terms: rounding it to 11 bits would drown the small singular
+// vectors of a matrix of low rank (3e-2 in place of 2e-3).
+struct Shifted {      // a + b S + c S^2 = c E^2 + linear E + constant, E = S - t
+  float t, linear, constant;
+};
+__host__ __device__ inline Shifted shifted(float a, float b, float c) {
+  const double vertex = -(double)b / (2.0 * c);
+  const bool there = vertex >= 0.0 && vertex <= 2.0;
+  const double t = there ? vertex : 1.0;
+  return Shifted{(float)t, there ? 0.0f : (float)(b + 2.0 * c * t), (float)(a + t * (b + c * t))};
+}
 
 // One or two products of [mp, mp] results over the list, of which those with j == blockIdx.y: out = mul A B^T + add_mul ADD +
 // diag on the diagonal.
@@ -871,7 +882,7 @@ __global__ __launch_bounds__(SMALL_NT, 2) void k_polar_small(SmallArgs p) {
   // Of [64, 64] a wavefront has 16 rows by 32 columns; lane (q, i) row i, four columns from 4 q on.  Its sums are kept apart
   // by term, so that no product waits for the one before.
   const int er = wave / 2 * 16, ec = wave % 2 * 32;
-  v4f acc[2];
+  v4f acc[2], own[2] = {};      // sums, and of E what this wavefront wrote
   const auto symmetric = [&](const uint16_t* a, int ld) {
     v4f sum[2][3] = {};
     for (int kk = 0; kk < ld / 32; ++kk) {
@@ -887,14 +898,16 @@ __global__ __launch_bounds__(SMALL_NT, 2) void k_polar_small(SmallArgs p) {
 #pragma unroll
     for (int j = 0; j < 2; ++j) acc[j] = sum[j][0] + (sum[j][1] + sum[j][2]);
   };
-  const auto put_e = [&](float mul, float diag) {
+  const auto put_e = [&](float mul, float linear, float diag) {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const int r = er + i, c = ec + j * 16 + 4 * q;
       v4f v = acc[j] * mul;
+      if (linear != 0.0f) v += own[j] * linear;
 #pragma unroll
       for (int e = 0; e < 4; ++e)
         if (r == c + e) v[e] += diag;
+      own[j] = v;
       small_put4(E + small_at(r, c, SMALL_M), v);
     }
   };
@@ -905,14 +918,15 @@ __global__ __launch_bounds__(SMALL_NT, 2) void k_polar_small(SmallArgs p) {
     const bool last = k + 1 == p.steps;
     constexpr float PER_GRAM = E_UNIT / (X_UNIT * X_UNIT);
     symmetric(X, np);
-    if (c != 0.0f) {      // E, then B = c E^2 + d (k_polar_symmetric)
-      put_e(PER_GRAM, b / (2.0f * c) * E_UNIT);
+    if (c != 0.0f) {      // E, then B
+      const Shifted form = shifted(a, b, c);
+      put_e(PER_GRAM, 0.0f, -form.t * E_UNIT);
       __syncthreads();
       symmetric(E, SMALL_M);
       __syncthreads();
-      put_e(c / E_UNIT, (float)(((double)a - (double)b * b / (4.0 * c)) * E_UNIT));
+      put_e(c / E_UNIT, form.linear, form.constant * E_UNIT);
     } else {
-      put_e(b * PER_GRAM, a * E_UNIT);
+      put_e(b * PER_GRAM, 0.0f, a * E_UNIT);
     }
     __syncthreads();
     // X <- B X, sixteen columns at a time: nobody else reads those

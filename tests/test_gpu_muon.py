@@ -113,6 +113,19 @@ def test_coefficients(steps, coefficients, precision):
         assert off(out[a:b].view(r, c), definition(src[a:b].view(r, c), steps, coefficients)) <= BOUND[precision] * max(1, steps / 5)
 
 
+@pytest.mark.parametrize("coefficients", [(1.5, -0.5, 1e-6), (1.4, -0.45, 0.05), (0.5, 0.3, 0.2), (1.2, 0.1, -0.3)])
+@pytest.mark.parametrize("shapes", ([(60, 64), (64, 30)], [(100, 130), (90, 64)], [(300, 1100), (257, 255)]))
+@pytest.mark.parametrize("precision", (torch.float32, torch.float16))
+def test_vertex_of_the_polynomial_anywhere(precision, shapes, coefficients):
+    """-b / 2c far beyond the singular values' squares, close behind them, and below zero.  The bounds as above: with a shift
+    within [0, 2] every rounded term stays below 1.5."""
+    offsets, rows = layout(shapes)
+    src = flat_of(shapes, seed=9)
+    out = muon(offsets, rows, precision=precision, coefficients=coefficients, own_state=False).orthogonalize(src.cuda())
+    for (r, c), a, b in zip(shapes, offsets[:-1], offsets[1:]):
+        assert off(out[a:b].view(r, c), definition(src[a:b].view(r, c), 5, coefficients)) <= BOUND[precision], (r, c)
+
+
 def test_singular_values_and_vectors():
     """On a diagonal matrix every singular value becomes what the scalar polynomial makes of it, small ones as well."""
     s = 10.0 ** -np.linspace(0.0, 3.0, 50)
