@@ -208,7 +208,10 @@ struct RowTiles {
 };
 
 // forward (x, W, y) and input_grad (dy, W transposed, dx): out[r] = a[r] W_g, a [rows, depth], out [rows, width].  FB: order
-// of W as an operand of `width` rows.
+// of W as an operand of `width` rows.  Tiles of 256 are bounded by the matrix instructions, and by their results, which all CUs
+// write at about the same time: 32768 rows over 16 groups, 8192 deep, 2048 wide in 1.25 ms, 880 TFLOP/s; 16384 over 8, 1024 deep,
+// 4096 wide in 165 us, 830.  Tiles of 64 are for calls with too few of those, which the latency of their slabs bounds: 4096 rows
+// over 16 groups, 2048 deep, 512 wide in 29 us, 300 TFLOP/s.
 struct RowsArgs {
   Groups groups;
   const uint16_t* a;
@@ -259,8 +262,10 @@ __global__ __launch_bounds__(S::NT, 2) void k_experts_rows(RowsArgs p) {
 }
 
 // The same for few rows a group, where what counts is how fast the weights of the groups that have any are read.  A workgroup has
-// 16 rows by 32 columns (64 where a row of W in memory runs along them, 128 bytes of each at once); its wavefronts share out the slabs of K, each with slabs of its own in LDS and no barriers, so that
-// up to 4 x 3 (or 4 x 2) slabs are under way at once, and their sums are added in a fixed order at the end.
+// 16 rows by 32 columns (64 where a row of W in memory runs along them, 128 bytes of each at once); its wavefronts share out the
+// slabs of K, each with slabs of its own in LDS and no barriers, so that up to 4 x 3 (or 4 x 2) slabs are under way at once, and
+// their sums are added in a fixed order at the end.  Reading W bounds it: 256 rows over 64 groups of 2048 x 1024 in 45.5 us, 5.9
+// TB/s; with 2 rows of a 1024 x 4096 group, 4.6 us, the one trip to memory.
 template <bool BF, int FB, int MODE>
 struct FewRows {
   static constexpr int BM = 16, BN = FB == KS ? 64 : 32, BK = 64, WAVES = 4, STAGES = FB == KS ? 2 : 3;
@@ -361,7 +366,9 @@ __global__ __launch_bounds__(256, 2) void k_experts_few_rows(RowsArgs p) {
 // weight_grad: out_g = a_g^T b_g, a [rows, height], b [rows, width], out [height, width].  Where the tiles are too few for the card
 // each has `parts` workgroups, a share of the group's rows each: their sums go to `partial`, and k_experts_join adds them up.  (The
 // last one to arrive adding them up in the same launch was tried: making the others' sums visible across the dies took three
-// times as long as all the rest, 94 us in place of 33 without parts.)
+// times as long as all the rest, 94 us in place of 33 without parts.)  Both operands are read across their rows in LDS.  Bounded by
+// the matrix instructions, 32768 rows over 16 groups of 2048 x 8192 in 1.29 ms, 850 TFLOP/s; with few rows by writing out: 4096 over
+// 16 of 512 x 2048, binary32, in 26 us, 2.6 TB/s in one burst.
 struct WeightsArgs {
   Groups groups;
   const uint16_t* a;
@@ -527,7 +534,9 @@ __host__ __device__ inline Shifted shifted(float a, float b, float c) {
 }
 
 // One or two products of [mp, mp] results over the list, of which those with j == blockIdx.y: out = mul A B^T + add_mul ADD +
-// diag on the diagonal.
+// diag on the diagonal.  48 matrices with m = 1024, 22 bits, half their tiles: X X^T with n = 4096 in 637 us, 1210 TFLOP/s of
+// matrix instructions, which bound it; the products 1024 deep in 226 us, 850 TFLOP/s, the matrix units busy half the time: the
+// results, on both sides of the diagonal, are written by all CUs at about the same time.
 struct SymmetricArgs {
   const ListTile* tiles;
   const uint16_t* a;           // X, or [mp, mp]
@@ -606,7 +615,8 @@ struct Finish {
   float lr, keep;           // keep = 1 - lr * weight_decay
 };
 
-// X' = mul B X, or with LAST what becomes of it
+// X' = mul B X, or with LAST what becomes of it.  Bounded as the symmetric products: 48 of [1024, 1024] by [1024, 4096], 22 bits,
+// in 1.03 ms, 1200 TFLOP/s of matrix instructions; with the update of binary32 parameters 1.34 ms.
 struct ApplyArgs {
   const ListTile* tiles;
   const Matrix* mats;
@@ -693,7 +703,8 @@ __device__ __forceinline__ v4f direction4(const Direction& d, v4f g, v4f m) {
   return u;
 }
 
-// m <- beta m + (1 - beta) scale g, and the sum of u's squares over each tile, in binary64.
+// m <- beta m + (1 - beta) scale g, and the sum of u's squares over each tile, in binary64.  Bounded by HBM: 302M elements with
+// binary32 gradients in 670 us, 5.4 TB/s.
 __global__ __launch_bounds__(BLOCK) void k_muon_moments(const SquareTile* tiles, const Matrix* mats, Direction d, float* m_out, double* sums) {
   const SquareTile t = tiles[blockIdx.x];
   const Matrix& mat = mats[t.mat];
@@ -742,7 +753,8 @@ __global__ __launch_bounds__(BLOCK) void k_muon_norms(const Matrix* mats, const 
 }
 
 // X = u / (norm + eps), transposed for tall matrices, zeros around it.  inv == NULL: every workgroup adds up its matrix's sums
-// itself, which for matrices of few tiles takes less than a launch.
+// itself, which for matrices of few tiles takes less than a launch.  Bounded by HBM: 302M elements of m and g into two terms in 700
+// us, 5.2 TB/s.
 __global__ __launch_bounds__(BLOCK) void k_muon_pack(const SquareTile* tiles, const Matrix* mats, Direction d, const float* inv, const double* sums,
                                                      float eps, uint16_t* x, int64_t term) {
   __shared__ float turned[SIDE][SIDE + 1];
