@@ -267,3 +267,27 @@ def test_tables_that_are_none_at_any_row_count():
 def test_last_round_of_large_tiles(counts, k, n):
     """More tiles than the card has CUs, so that those of the last round are split."""
     check(counts, k, n, torch.bfloat16, "kn")
+
+
+@pytest.mark.parametrize("rows,k,ld", [(270_000, 8200, 8200), (700, 64, (1 << 22) - 8), (700, 64, (1 << 22) - 5)])
+def test_rows_beyond_32_bits(rows, k, ld):
+    """The last group's rows lie more than 2^31 elements behind the first ones."""
+    n, last = 24, 40
+    assert (rows - last) * ld > 2 ** 31
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    def wide():
+        return torch.empty(rows, ld, dtype=torch.bfloat16, device="cuda")[:, :k]
+    x, dx = wide(), wide()
+    x.normal_(generator=gen)
+    dy = torch.randn(rows, n, generator=gen, device="cuda", dtype=torch.bfloat16)
+    w = torch.randn(2, k, n, generator=gen, device="cuda", dtype=torch.bfloat16)
+    offsets = torch.tensor([0, rows - last, rows], dtype=torch.int32, device="cuda")
+    op = layer(2, k, n, max_rows=rows)
+    y, dw = op.forward(x, w, offsets), op.weight_grad(x, dy, offsets)
+    op.input_grad(dy, w, offsets, out=dx)
+    for a, b, g in ((0, last, 0), (rows - 2 * last, rows - last, 0), (rows - last, rows, 1)):      # (first rows, last of group 0, group 1)
+        xd, dyd, wd = x[a:b].double().cpu(), dy[a:b].double().cpu(), w[g].double().cpu()
+        near(y[a:b], xd @ wd, xd.abs() @ wd.abs(), k, f"y from row {a}")
+        near(dx[a:b], dyd @ wd.T, dyd.abs() @ wd.T.abs(), n, f"dx from row {a}")
+    near(dw[1], xd.T @ dyd, xd.T.abs() @ dyd.abs(), last, "dw of the last group")
+    op.close()

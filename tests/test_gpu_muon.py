@@ -369,3 +369,22 @@ def test_wide_and_square_matrices_in_one_list(precision):
                 X = QUINTIC[0] * X + (QUINTIC[1] * S + QUINTIC[2] * S @ S) @ X
             want = (X.T if r > c else X).cpu()
             assert off(out[a:b].view(r, c), want) <= BOUND[precision]
+
+
+@pytest.mark.parametrize("shape", [(60, 70), (200, 130)])
+def test_matrices_beyond_32_bits(shape):
+    """The second matrix begins more than 2^32 elements into the list."""
+    gap, size = 2 ** 32 + 5, shape[0] * shape[1]
+    offsets, rows = np.array([0, size, size + gap, 2 * size + gap], dtype=np.int64), [shape[0], 0, shape[0]]
+    src = torch.zeros(2 * size + gap, dtype=torch.bfloat16, device="cuda")
+    want = []
+    for seed, a in ((11, 0), (12, size + gap)):
+        part = flat_of([shape], seed=seed).to(torch.bfloat16)
+        src[a:a + size] = part.cuda()
+        want.append(definition(part.view(shape)))
+    opt = muon(offsets, rows, own_state=False)
+    out = opt.orthogonalize(src, torch.zeros_like(src))
+    assert off(out[:size].view(shape), want[0]) <= BOUND[torch.float32] + ROUNDING[torch.bfloat16]
+    assert off(out[size + gap:].view(shape), want[1]) <= BOUND[torch.float32] + ROUNDING[torch.bfloat16]
+    assert not out[size:size + gap].any()
+    opt.close()
