@@ -18,6 +18,13 @@ from .step import _OB_DTYPE, _current_stream
 _LAYOUTS = {"kn": ob.OB_EXPERTS_KN, "nk": ob.OB_EXPERTS_NK}
 
 
+def _adjacent(t):
+    """Whether each row's elements follow each other and no row overlaps the next.  Of a single row only the distance to the next one
+    is free."""
+    rows, width = t.shape
+    return rows == 0 or ((width < 2 or t.stride(1) == 1) and (rows < 2 or t.stride(0) >= width))
+
+
 class ExpertLinear:
     def __init__(self, num_groups, k, n, dtype=torch.bfloat16, max_rows=1 << 20, layout="kn", w_stride=0, device="cuda:0"):
         """layout: "kn", W is [num_groups, k, n], or "nk", [num_groups, n, k].  w_stride: elements from one expert's weights
@@ -50,7 +57,7 @@ class ExpertLinear:
         if t.dim() != 2 or t.shape[1] != width or t.dtype not in dtypes or t.device != self.device:
             raise ValueError(f"{what}: a [rows, {width}] tensor of {' or '.join(map(str, dtypes))} on {self.device}, not "
                              f"{tuple(t.shape)} of {t.dtype} on {t.device}")
-        if t.shape[0] > 1 and ((width > 1 and t.stride(1) != 1) or t.stride(0) < width):
+        if not _adjacent(t):
             raise ValueError(f"{what}: rows of adjacent elements that do not overlap")
         return t.stride(0) if t.shape[0] > 1 else width
 
@@ -131,7 +138,7 @@ class _Apply(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dy):
         x, w, offsets = ctx.saved_tensors
-        dy = dy if dy.dim() == 2 and (dy.shape[0] < 2 or (dy.stride(1) == 1 and dy.stride(0) >= dy.shape[1])) else dy.contiguous()
+        dy = dy if _adjacent(dy) else dy.contiguous()      # (a sum's gradient is one element, seen as all of them)
         dx = ctx.layer.input_grad(dy, w, offsets) if ctx.needs_input_grad[0] else None
         dw = ctx.layer.weight_grad(x, dy, offsets) if ctx.needs_input_grad[1] else None
         return dx, dw, None, None

@@ -1,0 +1,125 @@
+"""What ExpertLinear hands to the library's calls, without a device: the calls are stood in for by ones that read and write the same
+addresses on the host."""
+import ctypes
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+
+def at(address, rows, width, ld, dtype):
+    """[rows, width] elements from an address on, rows ld elements apart."""
+    count = (rows - 1) * ld + width if rows and width else 0
+    size = torch.empty(0, dtype=dtype).element_size()
+    flat = torch.frombuffer((ctypes.c_char * max(count * size, 1)).from_address(address), dtype=dtype, count=count) if count else torch.empty(0, dtype=dtype)
+    return flat.as_strided((rows, width), (ld, 1)) if count else flat.view(rows, width)
+
+
+@pytest.fixture
+def host_layer(monkeypatch):
+    """-> a function that makes an ExpertLinear whose products run on the host."""
+    from paper_2104_06069_amd import binding as ob
+    from paper_2104_06069_amd import experts
+    types = {v: k for k, v in experts._OB_DTYPE.items()}
+    layers = {}
+
+    def groups_of(layer, offsets, rows):
+        ends = at(offsets, 1, layer.groups + 1, layer.groups + 1, torch.int32)[0].clamp(0, rows).tolist()
+        return enumerate(zip(ends[:-1], ends[1:]))
+
+    def weights(layer, address, dtype):
+        _, r, c = layer.w_shape
+        flat = at(address, 1, (layer.groups - 1) * layer.w_stride + r * c, 1, dtype)[0]
+        return flat.as_strided(layer.w_shape, (layer.w_stride, c, 1))
+
+    def rows_call(transposed):
+        def call(ctx, a, lda, w, offsets, rows, out, ldo, out_dtype, stream):
+            layer = layers[ctx]
+            depth, width = (layer.n, layer.k) if transposed else (layer.k, layer.n)
+            x, y, wv = at(a, rows, depth, lda, layer.dtype), at(out, rows, width, ldo, types[out_dtype]), weights(layer, w, layer.dtype)
+            for g, (lo, hi) in groups_of(layer, offsets, rows):
+                m = wv[g] if layer.layout == "kn" else wv[g].T
+                y[lo:hi] = (x[lo:hi].double() @ (m.T if transposed else m).double()).to(y.dtype)
+            return 0
+        return call
+
+    def weight_grad(ctx, x, ldx, dy, lddy, offsets, rows, dw, dw_dtype, accumulate=False, stream=None):
+        layer = layers[ctx]
+        xv, dv = at(x.data_ptr(), rows, layer.k, ldx, layer.dtype), at(dy.data_ptr(), rows, layer.n, lddy, layer.dtype)
+        out = weights(layer, dw.data_ptr(), types[dw_dtype])
+        for g, (lo, hi) in groups_of(layer, offsets.data_ptr(), rows):
+            p = xv[lo:hi].double().T @ dv[lo:hi].double()
+            p = p if layer.layout == "kn" else p.T
+            out[g] = (out[g].double() + p if accumulate else p).to(out.dtype)
+
+    class Lib:
+        ob_experts_forward, ob_experts_input_grad = staticmethod(rows_call(False)), staticmethod(rows_call(True))
+
+    def create(*args):
+        return len(layers) + 1
+    monkeypatch.setattr(ob, "lib", lambda: Lib)
+    monkeypatch.setattr(ob, "ob_experts_create", create)
+    monkeypatch.setattr(ob, "ob_experts_destroy", lambda ctx: None)
+    monkeypatch.setattr(ob, "ob_experts_weight_grad", weight_grad)
+    monkeypatch.setattr(experts, "_current_stream", lambda device: 0)
+    monkeypatch.setattr(torch.cuda, "set_device", lambda device: None)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: -1)       # (a host tensor's get_device())
+    monkeypatch.setattr(torch.cuda, "synchronize", lambda device=None: None)
+
+    def make(groups, k, n, **kw):
+        layer = experts.ExpertLinear(groups, k, n, device="cpu", **kw)
+        layers[layer.ctx] = layer
+        return layer
+    return make
+
+
+def whole(*shape, seed=0, dtype=torch.bfloat16):
+    """Small whole numbers: every sum is exact."""
+    return torch.randint(-3, 4, shape, generator=torch.Generator().manual_seed(seed)).to(dtype)
+
+
+def table(*ends):
+    return torch.tensor(ends, dtype=torch.int32)
+
+
+def test_the_stand_in_computes_the_products(host_layer):
+    for layout in ("kn", "nk"):
+        op = host_layer(2, 8, 4, layout=layout)
+        x, dy, w = whole(5, 8), whole(5, 4, seed=1), whole(*op.w_shape, seed=2)
+        m = w if layout == "kn" else w.transpose(1, 2)
+        y, (dx, dw) = op.forward(x, w, table(0, 2, 5)), op.backward(x, dy, w, table(0, 2, 5), dw_dtype=torch.float32)
+        for g, (a, b) in enumerate(((0, 2), (2, 5))):
+            assert torch.equal(y[a:b].float(), x[a:b].float() @ m[g].float()) and torch.equal(dx[a:b].float(), dy[a:b].float() @ m[g].float().T)
+            p = x[a:b].float().T @ dy[a:b].float()
+            assert torch.equal(dw[g], p if layout == "kn" else p.T)
+
+
+def test_one_row_of_elements_that_are_not_adjacent_is_refused(host_layer):
+    """Of one row only the distance to the next one is free, not the distance between its elements."""
+    op = host_layer(1, 8, 4)
+    x, dy, w, offsets = whole(1, 8), whole(1, 4, seed=1), whole(1, 8, 4, seed=2), table(0, 1)
+    apart = {n: (whole(n, 3, seed=3).T[:1], whole(1, 2 * n, seed=4)[:, ::2], whole(1, 1, seed=5).expand(1, n)) for n in (8, 4)}
+    for bad in apart[8]:
+        for call in (lambda: op.forward(bad, w, offsets), lambda: op.weight_grad(bad, dy, offsets), lambda: op.input_grad(dy, w, offsets, out=bad)):
+            with pytest.raises(ValueError):
+                call()
+    for bad in apart[4]:
+        for call in (lambda: op.input_grad(bad, w, offsets), lambda: op.weight_grad(x, bad, offsets), lambda: op.forward(x, w, offsets, out=bad)):
+            with pytest.raises(ValueError):
+                call()
+    # a row of a wider matrix is one of adjacent elements, and so is a single element
+    wide = whole(3, 20, seed=6)[1:2, 5:13]
+    assert torch.equal(op.forward(wide, w, offsets), op.forward(wide.clone(), w, offsets))
+    one = host_layer(1, 1, 4)
+    column = whole(3, 5, seed=7)[1:2, 2:3]
+    assert torch.equal(one.forward(column, w[:, :1].contiguous(), offsets), (column.float() * w[0, :1].float()).to(torch.bfloat16))
+
+
+@pytest.mark.parametrize("rows", (1, 2))
+def test_a_gradient_that_is_one_number(host_layer, rows):
+    """The gradient of a sum has one element in memory, whatever its shape."""
+    op = host_layer(1, 8, 4)
+    x, w = whole(rows, 8).requires_grad_(), whole(1, 8, 4, seed=2).requires_grad_()
+    op(x, w, table(0, rows)).sum().backward()
+    assert torch.equal(x.grad.float(), w[0].detach().float().sum(1).expand(rows, 8))
+    assert torch.equal(w.grad[0].float(), x.detach().float().sum(0)[:, None].expand(8, 4))

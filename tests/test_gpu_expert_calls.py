@@ -1,0 +1,43 @@
+"""ExpertLinear's calls and their autograd form on the device, where tests/test_expert_calls.py has stand-ins for the kernels.  Operands are
+small whole numbers, so that every sum is exact."""
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+def layer(*args, **kw):
+    from paper_2104_06069_amd.experts import ExpertLinear
+    return ExpertLinear(*args, **kw)
+
+
+def whole(*shape, seed=0, dtype=torch.bfloat16):
+    return torch.randint(-3, 4, shape, generator=torch.Generator().manual_seed(seed)).to(dtype).cuda()
+
+
+def table(*ends):
+    return torch.tensor(ends, dtype=torch.int32).cuda()
+
+
+@pytest.mark.parametrize("rows", (1, 2))
+@pytest.mark.parametrize("layout", ("kn", "nk"))
+def test_a_gradient_that_is_one_number(layout, rows):
+    """The gradient of a sum has one element in memory, whatever its shape."""
+    op = layer(1, 72, 40, max_rows=rows, layout=layout)
+    x, w = whole(rows, 72).requires_grad_(), whole(*op.w_shape, seed=2).requires_grad_()
+    op(x, w, table(0, rows)).sum().backward()
+    m = w[0].detach() if layout == "kn" else w[0].detach().T
+    assert torch.equal(x.grad.float(), m.float().sum(1).expand(rows, 72))
+    dw = x.detach().float().sum(0)[:, None].expand(72, 40)
+    assert torch.equal(w.grad[0].float(), dw if layout == "kn" else dw.T)
+
+
+def test_one_row_of_elements_that_are_not_adjacent_is_refused():
+    op = layer(1, 72, 40, max_rows=1)
+    x, w, offsets = whole(72, 3, seed=3), whole(1, 72, 40, seed=2), table(0, 1)
+    with pytest.raises(ValueError):
+        op.forward(x.T[:1], w, offsets)
+    with pytest.raises(ValueError):
+        op.forward(x.T[:1].contiguous(), w, offsets, out=whole(40, 3).T[:1])
+    wide = whole(3, 100, seed=6)[1:2, 5:77]
+    assert torch.equal(op.forward(wide, w, offsets), op.forward(wide.clone(), w, offsets))
