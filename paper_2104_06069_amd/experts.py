@@ -8,7 +8,7 @@ weight gradients can go straight into a view of the flat gradient that those rea
     y = layer.forward(x, w, offsets)
     dx, dw = layer.backward(x, dy, w, offsets, dw=flat_grad[a:b].view(groups, k, n))
 
-or, with torch's autograd, y = layer(x, w, offsets).
+or, with torch's autograd, y = layer(x, w, offsets), where rows that belong to no expert are zeros and get none of a gradient.
 """
 import torch
 
@@ -121,7 +121,7 @@ class ExpertLinear:
         return out
 
     def backward(self, x, dy, w, offsets, dw=None, dw_dtype=None):
-        """-> (dx, dW)"""
+        """-> (dx, dW).  Rows of dx that belong to no expert are not written."""
         return self.input_grad(dy, w, offsets), self.weight_grad(x, dy, offsets, out=dw, out_dtype=dw_dtype)
 
     def __call__(self, x, w, offsets):
@@ -133,12 +133,13 @@ class _Apply(torch.autograd.Function):
     def forward(ctx, x, w, offsets, layer):
         ctx.save_for_backward(x, w, offsets)
         ctx.layer = layer
-        return layer.forward(x, w, offsets)
+        # (rows of no expert are not written: they are zeros, and so are their gradients)
+        return layer.forward(x, w, offsets, out=x.new_zeros(x.shape[0], layer.n))
 
     @staticmethod
     def backward(ctx, dy):
         x, w, offsets = ctx.saved_tensors
         dy = dy if _adjacent(dy) else dy.contiguous()      # (a sum's gradient is one element, seen as all of them)
-        dx = ctx.layer.input_grad(dy, w, offsets) if ctx.needs_input_grad[0] else None
+        dx = ctx.layer.input_grad(dy, w, offsets, out=torch.zeros_like(x, memory_format=torch.contiguous_format)) if ctx.needs_input_grad[0] else None
         dw = ctx.layer.weight_grad(x, dy, offsets) if ctx.needs_input_grad[1] else None
         return dx, dw, None, None

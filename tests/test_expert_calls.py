@@ -123,3 +123,25 @@ def test_a_gradient_that_is_one_number(host_layer, rows):
     op(x, w, table(0, rows)).sum().backward()
     assert torch.equal(x.grad.float(), w[0].detach().float().sum(1).expand(rows, 8))
     assert torch.equal(w.grad[0].float(), x.detach().float().sum(0)[:, None].expand(8, 4))
+
+
+@pytest.fixture
+def marked_memory():
+    """Memory that nobody has written yet holds NaNs."""
+    torch.use_deterministic_algorithms(True)
+    assert torch.utils.deterministic.fill_uninitialized_memory and torch.isnan(torch.empty(1)).all()
+    yield
+    torch.use_deterministic_algorithms(False)
+
+
+def test_rows_of_no_expert_through_autograd(host_layer, marked_memory):
+    """They have no product and no gradient: zeros, not what the allocator left."""
+    op = host_layer(2, 8, 4)
+    x, w = whole(9, 8).requires_grad_(), whole(2, 8, 4, seed=2).requires_grad_()
+    y = op(x, w, table(2, 4, 6))
+    inside = torch.zeros(9, dtype=torch.bool)
+    inside[2:6] = True
+    assert (y[~inside] == 0).all() and torch.isfinite(y).all()
+    y.backward(whole(9, 4, seed=3))
+    assert (x.grad[~inside] == 0).all() and torch.equal(x.grad[2:4].float(), whole(9, 4, seed=3)[2:4].float() @ w[0].detach().float().T)
+    assert torch.equal(w.grad[1].float(), x.detach()[4:6].float().T @ whole(9, 4, seed=3)[4:6].float())

@@ -41,3 +41,27 @@ def test_one_row_of_elements_that_are_not_adjacent_is_refused():
         op.forward(x.T[:1].contiguous(), w, offsets, out=whole(40, 3).T[:1])
     wide = whole(3, 100, seed=6)[1:2, 5:77]
     assert torch.equal(op.forward(wide, w, offsets), op.forward(wide.clone(), w, offsets))
+
+
+@pytest.fixture
+def marked_memory():
+    """Memory that nobody has written yet holds NaNs."""
+    torch.use_deterministic_algorithms(True)
+    assert torch.utils.deterministic.fill_uninitialized_memory and torch.isnan(torch.empty(1, device="cuda")).all()
+    yield
+    torch.use_deterministic_algorithms(False)
+
+
+@pytest.mark.parametrize("rows", (9, 300))
+def test_rows_of_no_expert_through_autograd(marked_memory, rows):
+    """They have no product and no gradient: zeros, not what the allocator left."""
+    op = layer(2, 72, 40, max_rows=rows)
+    x, w, dy = whole(rows, 72).requires_grad_(), whole(2, 72, 40, seed=2).requires_grad_(), whole(rows, 40, seed=3)
+    y = op(x, w, table(2, 4, rows - 3))
+    inside = torch.zeros(rows, dtype=torch.bool, device="cuda")
+    inside[2:rows - 3] = True
+    assert (y[~inside] == 0).all() and torch.isfinite(y).all()
+    y.backward(dy)
+    assert (x.grad[~inside] == 0).all() and torch.isfinite(x.grad).all()
+    assert torch.equal(x.grad[2:4], (dy[2:4].float() @ w[0].detach().float().T).to(torch.bfloat16))
+    assert torch.equal(w.grad[1], (x.detach()[4:rows - 3].float().T @ dy[4:rows - 3].float()).to(torch.bfloat16))
