@@ -11,6 +11,7 @@ weight gradients can go straight into a view of the flat gradient that those rea
 or, with torch's autograd, y = layer(x, w, offsets), where rows that belong to no expert are zeros and get none of a gradient.
 """
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as ob
 from .step import _OB_DTYPE, _current_stream
@@ -137,6 +138,7 @@ class _Apply(torch.autograd.Function):
         return layer.forward(x, w, offsets, out=x.new_zeros(x.shape[0], layer.n))
 
     @staticmethod
+    @once_differentiable      # (what the calls write has no graph: a derivative of it raises)
     def backward(ctx, dy):
         x, w, offsets = ctx.saved_tensors
         dy = dy if _adjacent(dy) else dy.contiguous()      # (a sum's gradient is one element, seen as all of them)

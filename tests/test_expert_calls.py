@@ -145,3 +145,13 @@ def test_rows_of_no_expert_through_autograd(host_layer, marked_memory):
     y.backward(whole(9, 4, seed=3))
     assert (x.grad[~inside] == 0).all() and torch.equal(x.grad[2:4].float(), whole(9, 4, seed=3)[2:4].float() @ w[0].detach().float().T)
     assert torch.equal(w.grad[1].float(), x.detach()[4:6].float().T @ whole(9, 4, seed=3)[4:6].float())
+
+
+def test_second_derivatives_are_refused(host_layer):
+    """The gradients are kernels' results that autograd knows nothing about: asking for theirs is an error, not a missing term."""
+    op = host_layer(1, 8, 4)
+    x, w = whole(3, 8).requires_grad_(), whole(1, 8, 4, seed=2).requires_grad_()
+    loss = op(x, w, table(0, 3)).float().square().sum()
+    dx, = torch.autograd.grad(loss, x, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        (loss + dx.float().square().sum()).backward()
