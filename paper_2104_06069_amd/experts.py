@@ -113,9 +113,7 @@ class ExpertLinear:
         if out is None:
             if accumulate:
                 raise ValueError("accumulate needs an out to add to")
-            if self.w_stride != self.k * self.n:
-                raise ValueError("weights with gaps between them need an out")
-            out = torch.empty(self.w_shape, device=self.device, dtype=out_dtype or self.dtype)
+            out = torch.empty_strided(self.w_shape, self._w_dense, device=self.device, dtype=out_dtype or self.dtype)      # (gaps as between W's)
         self._weights(out, (torch.float32,) if accumulate else (self.dtype, torch.float32), "out")
         ob.ob_experts_weight_grad(self.ctx, x, ldx, dy, lddy, offsets, x.shape[0], out, _OB_DTYPE[out.dtype], accumulate,
                                   _current_stream(self.device))

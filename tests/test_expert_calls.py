@@ -155,3 +155,17 @@ def test_second_derivatives_are_refused(host_layer):
     dx, = torch.autograd.grad(loss, x, create_graph=True)
     with pytest.raises(RuntimeError, match="once_differentiable"):
         (loss + dx.float().square().sum()).backward()
+
+
+def test_autograd_with_other_tensors_between_the_weights(host_layer):
+    """w_stride beyond k * n, as in a flat list where something lies between one expert's weights and the next one's."""
+    op = host_layer(2, 8, 4, w_stride=40)
+    flat = whole(80, seed=2).requires_grad_()
+    view = flat.as_strided((2, 8, 4), (40, 4, 1), 5)
+    x, dy = whole(5, 8).requires_grad_(), whole(5, 4, seed=3)
+    op(x, view, table(0, 2, 5)).backward(dy)
+    want = torch.zeros(80)
+    for g, (a, b) in enumerate(((0, 2), (2, 5))):
+        assert torch.equal(x.grad[a:b].float(), dy[a:b].float() @ view[g].detach().float().T)
+        want[5 + 40 * g:5 + 40 * g + 32] = (x.detach()[a:b].float().T @ dy[a:b].float()).reshape(-1)
+    assert torch.equal(flat.grad.float(), want)

@@ -65,3 +65,26 @@ def test_rows_of_no_expert_through_autograd(marked_memory, rows):
     assert (x.grad[~inside] == 0).all() and torch.isfinite(x.grad).all()
     assert torch.equal(x.grad[2:4], (dy[2:4].float() @ w[0].detach().float().T).to(torch.bfloat16))
     assert torch.equal(w.grad[1], (x.detach()[4:rows - 3].float().T @ dy[4:rows - 3].float()).to(torch.bfloat16))
+
+
+def test_autograd_with_other_tensors_between_the_weights():
+    """w_stride beyond k * n, as in a flat list where something lies between one expert's weights and the next one's."""
+    op = layer(2, 24, 40, max_rows=50, w_stride=1000)
+    flat = whole(2000, seed=2).requires_grad_()
+    view = flat.as_strided((2, 24, 40), (1000, 40, 1), 5)
+    x, dy = whole(50, 24).requires_grad_(), whole(50, 40, seed=3)
+    op(x, view, table(0, 20, 50)).backward(dy)
+    want = torch.zeros(2000, device="cuda")
+    for g, (a, b) in enumerate(((0, 20), (20, 50))):
+        assert torch.equal(x.grad[a:b], (dy[a:b].float() @ view[g].detach().float().T).to(torch.bfloat16))
+        want[5 + 1000 * g:965 + 1000 * g] = (x.detach()[a:b].float().T @ dy[a:b].float()).reshape(-1)
+    assert torch.equal(flat.grad, want.to(torch.bfloat16))
+
+
+def test_second_derivatives_are_refused():
+    op = layer(1, 24, 40, max_rows=3)
+    x, w = whole(3, 24).requires_grad_(), whole(1, 24, 40, seed=2).requires_grad_()
+    loss = op(x, w, table(0, 3)).float().square().sum()
+    dx, = torch.autograd.grad(loss, x, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        (loss + dx.float().square().sum()).backward()
