@@ -351,7 +351,7 @@ struct ob_muon_ctx {
   Matrix* d_mats = nullptr;
   SquareTile* d_square = nullptr;
   double* d_sums = nullptr;
-  float* d_inv = nullptr;
+  Inverse* d_inv = nullptr;
   uint16_t* d_x[2] = {nullptr, nullptr};
   uint16_t* d_e[5] = {};                // S or E, B, Y, and two of Q
   std::string hip_err;
@@ -686,7 +686,7 @@ ob_status create(const ob_muon_config* cfg, ob_muon_ctx* ctx) {
   size_t at_table[2][3];
   for (const int f : {0, 1})
     for (const int k : {0, 1, 2}) at_table[f][k] = place(room<ListTile>(tables[f][k].size()));
-  const size_t at_sums = place(room<double>(square.size())), at_inv = place(room<float>(mats.size()));
+  const size_t at_sums = place(room<double>(square.size())), at_inv = place(room<Inverse>(mats.size()));
   const size_t at_x0 = place(room<uint16_t>(2 * xs)), at_x1 = place(room<uint16_t>(2 * xs));
   size_t at_e[5];
   for (size_t& at : at_e) at = place(room<uint16_t>(2 * es));
@@ -696,7 +696,7 @@ ob_status create(const ob_muon_config* cfg, ob_muon_ctx* ctx) {
   ctx->d_mats = reinterpret_cast<Matrix*>(base + at_mats);
   ctx->d_square = reinterpret_cast<SquareTile*>(base + at_square);
   ctx->d_sums = reinterpret_cast<double*>(base + at_sums);
-  ctx->d_inv = reinterpret_cast<float*>(base + at_inv);
+  ctx->d_inv = reinterpret_cast<Inverse*>(base + at_inv);
   ctx->d_x[0] = reinterpret_cast<uint16_t*>(base + at_x0);
   ctx->d_x[1] = reinterpret_cast<uint16_t*>(base + at_x1);
   for (int i = 0; i < 5; ++i) ctx->d_e[i] = reinterpret_cast<uint16_t*>(base + at_e[i]);

@@ -736,8 +736,18 @@ __global__ __launch_bounds__(BLOCK) void k_muon_moments(const SquareTile* tiles,
   if (threadIdx.x == 0) sums[blockIdx.x] = (part[0] + part[1]) + (part[2] + part[3]);
 }
 
-// X_UNIT / (norm + eps) of a matrix, in every thread of a workgroup
-__device__ __forceinline__ float inverse_norm(const Matrix& m, const double* sums, float eps) {
+// X_UNIT / (norm + eps) as two factors: their product need not be a normal binary32 number, the first is a power of two that makes the
+// second one, and 1 for all but the smallest and the largest of norms.
+struct Inverse {
+  float first, second;
+};
+__device__ __forceinline__ Inverse inverse_of(double squares, float eps) {
+  const double d = sqrt(squares) + (double)eps;
+  const float first = d < 0x1p-100 ? 0x1p100f : d > 0x1p130 ? 0x1p-30f : 1.0f;
+  return Inverse{first, (float)((double)X_UNIT / (d * (double)first))};
+}
+// That of a matrix, in every thread of a workgroup
+__device__ __forceinline__ Inverse inverse_norm(const Matrix& m, const double* sums, float eps) {
   double s = 0.0;
   for (int i = threadIdx.x; i < m.tiles; i += BLOCK) s += sums[m.tile0 + i];
   __shared__ double part[BLOCK / 64];
@@ -745,22 +755,22 @@ __device__ __forceinline__ float inverse_norm(const Matrix& m, const double* sum
   for (int k = 32; k; k >>= 1) s += __shfl_xor(s, k);
   if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
   __syncthreads();
-  return (float)((double)X_UNIT / (sqrt((part[0] + part[1]) + (part[2] + part[3])) + (double)eps));
+  return inverse_of((part[0] + part[1]) + (part[2] + part[3]), eps);
 }
-__global__ __launch_bounds__(BLOCK) void k_muon_norms(const Matrix* mats, const double* sums, float eps, float* inv) {
-  const float f = inverse_norm(mats[blockIdx.x], sums, eps);
+__global__ __launch_bounds__(BLOCK) void k_muon_norms(const Matrix* mats, const double* sums, float eps, Inverse* inv) {
+  const Inverse f = inverse_norm(mats[blockIdx.x], sums, eps);
   if (threadIdx.x == 0) inv[blockIdx.x] = f;
 }
 
 // X = u / (norm + eps), transposed for tall matrices, zeros around it.  inv == NULL: every workgroup adds up its matrix's sums
 // itself, which for matrices of few tiles takes less than a launch.  Bounded by HBM: 302M elements of m and g into two terms in 700
 // us, 5.2 TB/s.
-__global__ __launch_bounds__(BLOCK) void k_muon_pack(const SquareTile* tiles, const Matrix* mats, Direction d, const float* inv, const double* sums,
+__global__ __launch_bounds__(BLOCK) void k_muon_pack(const SquareTile* tiles, const Matrix* mats, Direction d, const Inverse* inv, const double* sums,
                                                      float eps, uint16_t* x, int64_t term) {
   __shared__ float turned[SIDE][SIDE + 1];
   const SquareTile t = tiles[blockIdx.x];
   const Matrix& mat = mats[t.mat];
-  const float f = inv ? inv[t.mat] : inverse_norm(mat, sums, eps);
+  const Inverse f = inv ? inv[t.mat] : inverse_norm(mat, sums, eps);
 #pragma unroll
   for (int j = 0; j < SIDE / 16; ++j) {
     const int y = threadIdx.x / 16 + 16 * j, z = threadIdx.x % 16 * 4, r = t.row0 + y, c = t.col0 + z;
@@ -773,7 +783,7 @@ __global__ __launch_bounds__(BLOCK) void k_muon_pack(const SquareTile* tiles, co
       if (d.m) m = load4(d.m, F32, at, left);
       const v4f u = direction4(d, g, m);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = e < left ? u[e] * f : 0.0f;
+      for (int e = 0; e < 4; ++e) v[e] = e < left ? u[e] * f.first * f.second : 0.0f;
     }
     if (!mat.tall) {
       store_terms<2>(x + mat.x, term, (int64_t)r * mat.np + c, v);
@@ -871,12 +881,12 @@ __global__ __launch_bounds__(SMALL_NT, 2) void k_polar_small(SmallArgs p) {
   s = 0.0;
 #pragma unroll
   for (int k = 0; k < SMALL_NT / 64; ++k) s += part[k];
-  const float f = (float)((double)X_UNIT / (sqrt(s) + (double)p.eps));
+  const Inverse f = inverse_of(s, p.eps);
   for (int k = tid; k < SMALL_M * np / 8; k += SMALL_NT) {      // eights of X, wherever they are
     uint16_t* const at = X + 16 * k;
     const v4f u0 = *in_lds<const v4f>(at), u1 = *in_lds<const v4f>(at + 8);
-    small_put4(at, u0 * f);
-    small_put4(at + 4, u1 * f);
+    small_put4(at, u0 * f.first * f.second);
+    small_put4(at + 4, u1 * f.first * f.second);
   }
   __syncthreads();
 
