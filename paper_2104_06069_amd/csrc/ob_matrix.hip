@@ -5,7 +5,6 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
-#include <limits>
 #include <new>
 #include <string>
 #include <type_traits>
@@ -18,11 +17,6 @@ using namespace obm;
 
 namespace {
 
-// Tiles of the products: 256 x 256 (eight wavefronts, one workgroup on a CU), 128 x 128 and 64 x 64 (four).  Slabs of 64
-// columns, or with two terms of 32: the same LDS.  DEEP: 64 x 64 with two teams of wavefronts, slabs of 64 columns and 128 KB of
-// them, for launches of which a CU has one workgroup at most.
-enum TileKind { T256, T128, T64, DEEP, KINDS };
-constexpr int side_of(int kind) { return kind == T256 ? 256 : kind == T128 ? 128 : 64; }
 template <int KIND, int BK>
 using Tile = Shape<side_of(KIND), side_of(KIND), KIND == DEEP ? 64 : BK, 2, KIND == T256 ? 4 : 2,
                    KIND == DEEP ? (BK == 32 ? 4 : 8) : KIND == T64 ? 3 : 2, KIND == DEEP ? 2 : 1>;
@@ -35,39 +29,6 @@ auto with_tile(int kind, F f) {
     case T64: return f(std::integral_constant<int, T64>{});
     default: return f(std::integral_constant<int, DEEP>{});
   }
-}
-
-// What a CU takes for as many tiles of a kind as it runs at once, in microseconds: `fixed` for loading the first slabs and for
-// the results, and for each column of K with all of them, or with one alone.  Measured at 8192 x 8192 by 512 to 8192, bfloat16.
-struct Rate {
-  int per_cu;
-  double fixed, all, one;
-};
-constexpr Rate RATES[KINDS] = {{1, 5.5, 0.0251, 0.0251}, {2, 3.6, 0.0155, 0.0095}, {3, 1.8, 0.0100, 0.0055}, {1, 1.8, 0.0050, 0.0050}};
-// Time of `tiles` tiles of the given mean depth, if they are dealt evenly
-double tiles_time(int kind, double tiles, double depth, bool split_rest = false) {
-  const Rate& r = RATES[kind];
-  if (split_rest && kind == T256 && tiles > CUS) {      // (k_experts_rows: a last round of up to a quarter or half of the CUs)
-    const double rounds = std::floor(tiles / CUS), rest = tiles / CUS - rounds;
-    return (r.fixed + depth * r.all) * (rounds + (rest == 0 ? 0.0 : rest <= 0.25 ? 0.4 : rest <= 0.5 ? 0.65 : 1.0));
-  }
-  const double a_cu = std::ceil(tiles / CUS), rounds = std::floor(a_cu / r.per_cu), rest = a_cu - rounds * r.per_cu;
-  const double last = rest > 0 ? r.fixed + depth * (r.one + (r.all - r.one) * (rest - 1) / (r.per_cu - 1)) : 0.0;
-  return rounds * (r.fixed + depth * r.all) + last;
-}
-// The kind whose tiles take the shortest, for `tiles(side)` tiles
-template <class F>
-int best_tile(F tiles, double depth, bool split_rest = false) {
-  int best = T64;
-  double least = 1e300;
-  for (int kind = 0; kind < KINDS; ++kind) {
-    const double t = tiles_time(kind, tiles(side_of(kind)), depth, split_rest);
-    if (t < least) {
-      least = t;
-      best = kind;
-    }
-  }
-  return best;
 }
 
 inline int elem_size(int dtype) { return dtype == OB_F32 ? 4 : 2; }
@@ -144,11 +105,11 @@ ob_status launch_weights(ob_experts_ctx* ctx, const WeightsArgs& p, hipStream_t 
   return hip_ok(ctx, hipGetLastError(), "k_experts_weights") ? OB_OK : OB_ERR_HIP;
 }
 
-// f(kind, mode): operands that are not `direct` have tiles of 128 or 64, whose loads are waited for at each slab (ob_mm.h)
+// f(kind, mode), for a kind of kind_of()
 template <class F>
 auto with_tile_and_mode(int kind, bool direct, F f) {
   if (!direct) {
-    if (kind == T256 || kind == T128) return f(std::integral_constant<int, T128>{}, std::integral_constant<int, ANY>{});
+    if (kind == T128) return f(std::integral_constant<int, T128>{}, std::integral_constant<int, ANY>{});
     return f(std::integral_constant<int, T64>{}, std::integral_constant<int, ANY>{});
   }
   return with_tile(kind, [&](auto n) { return f(n, std::integral_constant<int, TAIL>{}); });
@@ -166,7 +127,7 @@ hipError_t allow_experts() {
   for (int kind = 0; kind < KINDS; ++kind)
     for (const bool direct : {false, true}) {
       if (e != hipSuccess) return e;
-      e = with_tile_and_mode(kind, direct, [&](auto n, auto mode) {
+      e = with_tile_and_mode(kind_of(kind, direct), direct, [&](auto n, auto mode) {
         using S = Tile<n, 64>;
         hipError_t e = allow_lds(k_experts_rows<S, BF, KC, mode>, Product<S, BF, KC, KC, 1, 1, mode>::LDS_BYTES);
         if (e == hipSuccess) e = allow_lds(k_experts_rows<S, BF, KS, mode>, Product<S, BF, KC, KS, 1, 1, mode>::LDS_BYTES);
@@ -177,9 +138,6 @@ hipError_t allow_experts() {
   return e;
 }
 
-// Rows a group (of those that can have one) up to which k_experts_few_rows is taken, and with unaligned operands; us with it / with
-// 64 x 64 tiles: 64 rows of 8 experts of 1024 x 1024 8.5 / 13.0, 512 of 32 17.2 / 14.9; 200 of 6 of 555 x 999 8.4 / 11.2
-constexpr double FEW_ROWS = 12, FEW_ROWS_ANY = 36;
 constexpr int64_t MAX_LD = (int64_t)1 << 22;      // a tile's offsets are 32-bit
 
 ob_status rows_call(ob_experts_ctx* ctx, const void* a, int64_t lda, const void* w, const int32_t* offsets, int64_t rows,
@@ -209,17 +167,16 @@ ob_status rows_call(ob_experts_ctx* ctx, const void* a, int64_t lda, const void*
   p.a_direct = at16(a) && lda % 8 == 0;
   p.w_direct = at16(w) && p.ldw % 8 == 0 && c.w_stride % 8 == 0 && (!strided || width % 8 == 0);
   const hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  // (a group's last tile is half full in the mean)
-  const double groups = (double)std::min<int64_t>(c.num_groups, rows);
-  const int kind = best_tile([&](int n) { return std::max(groups, rows / (double)n + 0.5 * groups) * (double)((width + n - 1) / n); }, (double)depth, true);
-  if (rows <= (p.a_direct && p.w_direct ? FEW_ROWS : FEW_ROWS_ANY) * groups) {
+  const bool direct = p.a_direct && p.w_direct;
+  const RowsPlan plan = rows_plan(c.num_groups, rows, depth, width, direct);
+  if (plan.few) {
     const auto few = [&](auto mode) {
       if (c.dtype == OB_BF16) return strided ? launch_few_rows<true, KS, mode>(ctx, p, s) : launch_few_rows<true, KC, mode>(ctx, p, s);
       return strided ? launch_few_rows<false, KS, mode>(ctx, p, s) : launch_few_rows<false, KC, mode>(ctx, p, s);
     };
-    return p.a_direct && p.w_direct ? few(std::integral_constant<int, TAIL>{}) : few(std::integral_constant<int, ANY>{});
+    return direct ? few(std::integral_constant<int, TAIL>{}) : few(std::integral_constant<int, ANY>{});
   }
-  return with_tile_and_mode(kind, p.a_direct && p.w_direct, [&](auto n, auto mode) {
+  return with_tile_and_mode(plan.kind, direct, [&](auto n, auto mode) {
     using S = Tile<n, 64>;
     if (c.dtype == OB_BF16) return strided ? launch_rows<S, true, KS, mode>(ctx, p, s) : launch_rows<S, true, KC, mode>(ctx, p, s);
     return strided ? launch_rows<S, false, KS, mode>(ctx, p, s) : launch_rows<S, false, KC, mode>(ctx, p, s);
@@ -245,9 +202,9 @@ ob_status ob_experts_create(const ob_experts_config* cfg, ob_experts_ctx** out) 
   if (!ctx->cfg.w_stride) ctx->cfg.w_stride = cfg->k * cfg->n;
   hipError_t e = hipGetDevice(&ctx->device);
   if (e == hipSuccess) e = cfg->dtype == OB_BF16 ? allow_experts<true>() : allow_experts<false>();
-  const int64_t tiles = cfg->num_groups * ((cfg->k + 63) / 64) * ((cfg->n + 63) / 64);
-  if (e == hipSuccess && tiles < 2 * CUS && cfg->max_rows >= 256) {
-    ctx->parts = (int)std::min<int64_t>((2 * CUS + tiles - 1) / tiles, 32);
+  ctx->parts = most_parts(cfg->num_groups, cfg->k, cfg->n, cfg->max_rows);
+  if (e == hipSuccess && ctx->parts > 1) {
+    const int64_t tiles = cfg->num_groups * ((cfg->k + 63) / 64) * ((cfg->n + 63) / 64);
     ctx->bytes = (size_t)tiles * ctx->parts * 64 * 64 * sizeof(float);
     e = hipMalloc(&ctx->mem, ctx->bytes);
     ctx->d_partial = static_cast<float*>(ctx->mem);
@@ -299,19 +256,11 @@ ob_status ob_experts_weight_grad(ob_experts_ctx* ctx, const void* x, int64_t ldx
   p.a_direct = at16(p.a) && p.lda % 8 == 0 && p.height % 8 == 0;
   p.b_direct = at16(p.b) && p.ldb % 8 == 0 && p.width % 8 == 0;
   const hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  const auto tiles = [&](int n) { return (double)c.num_groups * ((p.height + n - 1) / n) * ((p.width + n - 1) / n); };
-  const double depth = (double)rows / c.num_groups;
-  int kind = best_tile(tiles, depth);
-  // Few tiles of many rows: several workgroups each, as many as fill the card twice and have 128 rows or more.  Adding up
-  // takes about 4 us.
-  p.parts = 1;
+  const bool direct = p.a_direct && p.b_direct;
+  const WeightsPlan plan = weights_plan(c.num_groups, rows, p.height, p.width, ctx->parts, direct);
+  p.parts = plan.parts;
   p.partial = ctx->d_partial;
-  const int parts = (int)std::min({(double)ctx->parts, std::floor(depth / 128), std::ceil(2 * CUS / tiles(64))});
-  if (parts > 1 && 4.0 + tiles_time(T64, tiles(64) * parts, depth / parts) < tiles_time(kind, tiles(side_of(kind)), depth)) {
-    kind = T64;
-    p.parts = parts;
-  }
-  return with_tile_and_mode(kind, p.a_direct && p.b_direct, [&](auto n, auto mode) {
+  return with_tile_and_mode(plan.kind, direct, [&](auto n, auto mode) {
     using S = Tile<n, 64>;
     return c.dtype == OB_BF16 ? launch_weights<S, true, mode>(ctx, p, s) : launch_weights<S, false, mode>(ctx, p, s);
   });
@@ -320,21 +269,6 @@ ob_status ob_experts_weight_grad(ob_experts_ctx* ctx, const void* x, int64_t ldx
 }  // extern "C"
 
 // ---- orthogonalised update -----------------------------------------------------------------------------------------
-namespace {
-
-// Matrices that go through the steps together, and the tiles of their products
-struct Part {
-  bool follow_s = false;      // the way that follows S (ob_matrix_kernels.h); else step by step
-  int terms = 2, table = 0;
-  int sym_tile = T64, apply_tile = T64;
-  // tiles of X X^T, of the other symmetric products (the same ones, but not in the same order: only there depths differ by n)
-  // and of B X
-  int grid[3] = {0, 0, 0};
-  ListTile* d_tiles[3] = {nullptr, nullptr, nullptr};
-};
-
-}  // namespace
-
 struct ob_muon_ctx {
   int device = -1;
   int steps = 0, nesterov = 0, precision = OB_F32;
@@ -362,67 +296,6 @@ struct ob_muon_ctx {
 
 namespace {
 
-// Tiles of a product over the list, dealt to the eight dies: workgroup id runs on die id % 8, so that place id of the table
-// is place id / 8 of that die's queue.  Up to 4 x 8 neighbouring tiles of a matrix (what a die runs at once) stay together;
-// the dearest go first, each to the queue that has the least to do.
-struct Unit {
-  double cost;
-  int mat, tm0, tm1, tn0, tn1;
-};
-std::vector<ListTile> deal(const std::vector<Matrix>& mats, std::vector<Unit> units, bool upper) {
-  std::stable_sort(units.begin(), units.end(), [](const Unit& a, const Unit& b) { return a.cost > b.cost; });
-  std::vector<ListTile> queue[8];
-  double load[8] = {};
-  for (const Unit& u : units) {
-    const int q = (int)(std::min_element(load, load + 8) - load);
-    for (int tn = u.tn0; tn < u.tn1; ++tn)
-      for (int tm = u.tm0; tm < u.tm1; ++tm) {
-        if (upper && tn < tm) continue;
-        queue[q].push_back(ListTile{mats[u.mat].x, mats[u.mat].e, mats[u.mat].mp, mats[u.mat].np, u.mat, (short)tm, (short)tn});
-        load[q] += u.cost;
-      }
-  }
-  size_t longest = 0;
-  for (const auto& q : queue) longest = std::max(longest, q.size());
-  std::vector<ListTile> table(8 * longest, ListTile{});
-  for (int q = 0; q < 8; ++q)
-    for (size_t i = 0; i < queue[q].size(); ++i) table[8 * i + q] = queue[q][i];
-  return table;
-}
-
-enum ProductKind { GRAM, SYMMETRIC, APPLY };
-std::vector<ListTile> product_tiles(const std::vector<Matrix>& mats, const std::vector<int>& part, int side, ProductKind product) {
-  const bool symmetric = product != APPLY;
-  std::vector<Unit> units;
-  for (const int i : part) {
-    const int nm = (mats[i].mp + side - 1) / side, nn = symmetric ? nm : (mats[i].np + side - 1) / side;
-    const double cost = (double)(product == GRAM ? mats[i].np : mats[i].mp);
-    for (int a = 0; a < nm; a += 4)
-      for (int b = 0; b < nn; b += 8) {
-        if (symmetric && std::min(b + 8, nn) <= a) continue;
-        units.push_back(Unit{cost, i, a, std::min(a + 4, nm), b, std::min(b + 8, nn)});
-      }
-  }
-  return deal(mats, std::move(units), symmetric);
-}
-
-int product_tile(const std::vector<Matrix>& mats, const std::vector<int>& part, bool symmetric, bool two_terms) {
-  double depth = 0, elements = 0;      // of the products' K, weighted by what is computed of them
-  for (const int i : part) {
-    const double out = symmetric ? 0.5 * mats[i].mp * mats[i].mp : (double)mats[i].mp * mats[i].np;
-    depth += out * mats[i].mp;
-    elements += out;
-  }
-  return best_tile([&](int n) {
-    double tiles = 0;
-    for (const int i : part) {
-      const double nm = (mats[i].mp + n - 1) / n, nn = (mats[i].np + n - 1) / n;
-      tiles += symmetric ? 0.5 * nm * (nm + 1) : nm * nn;
-    }
-    return tiles;
-  }, (two_terms ? 3.0 : symmetric ? 1.0 : 2.0) * depth / elements);      // products of terms
-}
-
 template <class T>
 size_t room(size_t count) {
   return (std::max<size_t>(count * sizeof(T), 1) + 1023) / 1024 * 1024;
@@ -444,7 +317,7 @@ void symmetric(const Part& part, const SymmetricArgs& a, int products, hipStream
   with_tile(part.sym_tile, [&](auto n) {
     using S = Tile<n, TERMS == 2 ? 32 : 64>;
     using P = Product<S, false, KC, KC, TERMS, TERMS, WHOLE>;
-    hipLaunchKernelGGL((k_polar_symmetric<S, TERMS, FROM_X>), dim3(part.grid[FROM_X ? GRAM : SYMMETRIC], products), dim3(S::NT), P::LDS_BYTES, s, a);
+    hipLaunchKernelGGL((k_polar_symmetric<S, TERMS, FROM_X>), dim3((unsigned)part.tiles[FROM_X ? GRAM : SYMMETRIC].size(), products), dim3(S::NT), P::LDS_BYTES, s, a);
   });
 }
 template <int TERMS>
@@ -452,22 +325,9 @@ void apply(const Part& part, const ApplyArgs& a, bool last, hipStream_t s) {
   with_tile(part.apply_tile, [&](auto n) {
     using S = Tile<n, 32>;
     using P = Product<S, false, KC, KS, TERMS, 2, WHOLE>;
-    if (last) hipLaunchKernelGGL((k_polar_apply<S, TERMS, true>), dim3(part.grid[APPLY]), dim3(S::NT), P::LDS_BYTES, s, a);
-    else hipLaunchKernelGGL((k_polar_apply<S, TERMS, false>), dim3(part.grid[APPLY]), dim3(S::NT), P::LDS_BYTES, s, a);
+    if (last) hipLaunchKernelGGL((k_polar_apply<S, TERMS, true>), dim3((unsigned)part.tiles[APPLY].size()), dim3(S::NT), P::LDS_BYTES, s, a);
+    else hipLaunchKernelGGL((k_polar_apply<S, TERMS, false>), dim3((unsigned)part.tiles[APPLY].size()), dim3(S::NT), P::LDS_BYTES, s, a);
   });
-}
-
-// Steps that follow one S: the growth of a singular value's square up to the last of them (ob_matrix_kernels.h) is at most
-// 2^8, or 2^15 where an error of 2e-3 will do
-int steps_from(const ob_muon_ctx* ctx, int k) {
-  const int first = k;
-  double growth = 1.0;
-  for (; k < ctx->steps; ++k) {
-    if (k > first && growth > (ctx->precision == OB_F32 ? 256.0 : 32768.0)) break;
-    const double a = ctx->coefficients[3 * k];
-    growth *= std::max(1.0, a * a);
-  }
-  return k - first;
 }
 
 void follow_s(ob_muon_ctx* ctx, const Part& part, const Finish& finish, hipStream_t stream) {
@@ -475,7 +335,7 @@ void follow_s(ob_muon_ctx* ctx, const Part& part, const Finish& finish, hipStrea
   uint16_t* const Y = ctx->d_e[2];
   int cur = 0;
   for (int first = 0, n; first < ctx->steps; first += n) {
-    n = steps_from(ctx, first);
+    n = steps_from(ctx->coefficients, ctx->precision == OB_F32, first);
     SymmetricArgs g{part.d_tiles[GRAM], ctx->d_x[cur], {}, nullptr, {S}, ctx->x_plane, ctx->e_plane, {S_UNIT / (X_UNIT * X_UNIT)}, 0.0f, 0.0f};
     symmetric<2, true>(part, g, 1, stream);
     double most = 1.0;      // what Q's elements can come to
@@ -561,27 +421,6 @@ ob_status run_list(ob_muon_ctx* ctx, Direction d, float* m_out, const Finish& fi
   return hip_ok(ctx, hipGetLastError(), "the orthogonaliser's kernels") ? OB_OK : OB_ERR_HIP;
 }
 
-// Whether following S takes less than going step by step, both with 22 bits, by the tiles' times and LAUNCH a launch
-bool following_pays(const ob_muon_ctx* ctx, const std::vector<Matrix>& mats, const std::vector<int>& list, const Part& part) {
-  constexpr double LAUNCH = 3.0;      // us, from the end of one kernel to the start of the next one's loads
-  double depth[3] = {}, out[3] = {};
-  for (const int i : list)
-    for (const ProductKind k : {GRAM, SYMMETRIC, APPLY}) {
-      const double n = k == APPLY ? (double)mats[i].mp * mats[i].np : 0.5 * mats[i].mp * mats[i].mp;
-      out[k] += n;
-      depth[k] += n * (k == GRAM ? mats[i].np : mats[i].mp);
-    }
-  double t[3];
-  for (const ProductKind k : {GRAM, SYMMETRIC, APPLY})
-    t[k] = LAUNCH + tiles_time(k == APPLY ? part.apply_tile : part.sym_tile, part.grid[k], 3.0 * depth[k] / out[k]);
-  double followed = 0;
-  for (int k = 0, n; k < ctx->steps; k += n) {
-    n = steps_from(ctx, k);
-    followed += t[GRAM] + t[APPLY] + t[SYMMETRIC] * (n + (n - 1)) + (t[SYMMETRIC] - LAUNCH) * 2 * (n - 1) + LAUNCH * n;
-  }
-  return followed < ctx->steps * (t[GRAM] + t[SYMMETRIC] + t[APPLY]);
-}
-
 ob_status create(const ob_muon_config* cfg, ob_muon_ctx* ctx) {
   ctx->steps = cfg->steps;
   ctx->nesterov = cfg->nesterov != 0;
@@ -632,40 +471,10 @@ ob_status create(const ob_muon_config* cfg, ob_muon_ctx* ctx) {
     xs = es = 0;      // no working matrices outside of LDS
     square.clear();
   }
-  // 11 bits, step by step: 12.5 n / m + 2.5 (in m^3, 5 steps); 22 bits, following S with one S, which will do there: three
-  // times 1.5 n / m + 8.5, less from n = 3 m on.  With 22 bits following S takes as many multiply-adds as step by step for
-  // n = m, and more launches and writes (8 of 1024 x 1024: 1010 and 787 us, 4 of 1024 x 4096: 895 and 1277).  Each of the
-  // two ways is worth launches of its own where there is much for it.
-  const bool fine = cfg->precision == OB_F32;
-  constexpr double MUCH = 1e10;
-  std::vector<int> each[2];
-  double work[2] = {};
-  for (size_t i = 0; i < mats.size(); ++i) {
-    const bool f = mats[i].np >= (fine ? 1.5 : 3.0) * mats[i].mp;
-    each[f].push_back((int)i);
-    work[f] += (double)mats[i].mp * mats[i].mp * mats[i].np;
-  }
-  if (work[1] < MUCH || (fine && work[0] < MUCH)) {
-    std::vector<int>& all = each[fine];
-    all.insert(all.end(), each[!fine].begin(), each[!fine].end());
-    each[!fine].clear();
-  }
-  std::vector<ListTile> tables[2][3];
-  for (const int f : {1, 0}) {
-    if (each[f].empty() || ctx->small_lds) continue;
-    Part part;
-    part.terms = f || fine ? 2 : 1;
-    part.sym_tile = product_tile(mats, each[f], true, part.terms == 2);
-    part.apply_tile = product_tile(mats, each[f], false, part.terms == 2);
-    for (const ProductKind k : {GRAM, SYMMETRIC, APPLY}) {
-      tables[f][k] = product_tiles(mats, each[f], side_of(k == APPLY ? part.apply_tile : part.sym_tile), k);
-      if (tables[f][k].size() > 0x7fffffff) return OB_ERR_SIZE;
-      part.grid[k] = (int)tables[f][k].size();
-    }
-    part.follow_s = f == 1 && (!fine || following_pays(ctx, mats, each[1], part));
-    part.table = f;
-    ctx->parts.push_back(part);
-  }
+  if (!ctx->small_lds) ctx->parts = parts_of(mats, ctx->coefficients, cfg->precision == OB_F32);
+  for (const Part& part : ctx->parts)
+    for (const auto& table : part.tiles)
+      if (table.size() > 0x7fffffff) return OB_ERR_SIZE;
   for (int kind = 0; kind < KINDS; ++kind) {
     hipError_t e = with_tile(kind, [&](auto n) { return allow_muon<n, 2>(); });
     if (e == hipSuccess) e = with_tile(kind, [&](auto n) { return allow_muon<n, 1>(); });
@@ -683,9 +492,9 @@ ob_status create(const ob_muon_config* cfg, ob_muon_ctx* ctx) {
     return at;
   };
   const size_t at_mats = place(room<Matrix>(mats.size())), at_square = place(room<SquareTile>(square.size()));
-  size_t at_table[2][3];
-  for (const int f : {0, 1})
-    for (const int k : {0, 1, 2}) at_table[f][k] = place(room<ListTile>(tables[f][k].size()));
+  std::vector<size_t> at_table;
+  for (const Part& part : ctx->parts)
+    for (const auto& table : part.tiles) at_table.push_back(place(room<ListTile>(table.size())));
   const size_t at_sums = place(room<double>(square.size())), at_inv = place(room<Inverse>(mats.size()));
   const size_t at_x0 = place(room<uint16_t>(2 * xs)), at_x1 = place(room<uint16_t>(2 * xs));
   size_t at_e[5];
@@ -702,11 +511,11 @@ ob_status create(const ob_muon_config* cfg, ob_muon_ctx* ctx) {
   for (int i = 0; i < 5; ++i) ctx->d_e[i] = reinterpret_cast<uint16_t*>(base + at_e[i]);
   bool ok = hip_ok(ctx, hipMemcpy(ctx->d_mats, mats.data(), mats.size() * sizeof(Matrix), hipMemcpyHostToDevice), "hipMemcpy") &&
                   hip_ok(ctx, hipMemcpy(ctx->d_square, square.data(), square.size() * sizeof(SquareTile), hipMemcpyHostToDevice), "hipMemcpy");
+  size_t next = 0;
   for (Part& part : ctx->parts)
     for (const int k : {0, 1, 2}) {
-      const std::vector<ListTile>& table = tables[part.table][k];
-      part.d_tiles[k] = reinterpret_cast<ListTile*>(base + at_table[part.table][k]);
-      ok = ok && hip_ok(ctx, hipMemcpy(part.d_tiles[k], table.data(), table.size() * sizeof(ListTile), hipMemcpyHostToDevice), "hipMemcpy");
+      part.d_tiles[k] = reinterpret_cast<ListTile*>(base + at_table[next++]);
+      ok = ok && hip_ok(ctx, hipMemcpy(part.d_tiles[k], part.tiles[k].data(), part.tiles[k].size() * sizeof(ListTile), hipMemcpyHostToDevice), "hipMemcpy");
     }
   return ok ? OB_OK : OB_ERR_HIP;
 }

@@ -3,13 +3,12 @@
 
 #include <type_traits>
 
+#include "ob_matrix_plan.h"
 #include "ob_mm.h"
 
 namespace obm {
 
-constexpr int CUS = 256;        // of an MI355X
 constexpr int BLOCK = 256;      // threads of the element-wise kernels
-constexpr int SIDE = 64;        // side of their tiles, and what the sides of the working matrices are multiples of
 
 enum { F32 = 0, F16 = 1, BF16 = 2 };      // ob_dtype
 
@@ -452,26 +451,10 @@ __global__ __launch_bounds__(BLOCK) void k_experts_join(WeightsArgs p) {
 }
 
 // ---- orthogonalised update -----------------------------------------------------------------------------------------
-// A matrix of the list, and its working matrices: X [mp, np], and those of [mp, mp], binary16, mp and np the sides m <= n
-// rounded up to multiples of SIDE.  Zeros around X stay zeros: every product keeps them.
-struct Matrix {
-  int64_t at;          // in the flat buffers
-  int64_t x, e;        // in a plane of X, and of a [mp, mp] matrix
-  int rows, cols, mp, np;
-  int tall;            // more rows than columns: X is the transpose
-  int tile0, tiles;    // its element-wise tiles
-  float scale;
-};
 // Working matrices hold X * 2^12 and S, Y * 2^12, E and B * 2^8 (and Q times a power of two for what the coefficients can
 // make of it), so that second terms of common elements are normal binary16 numbers: X's elements are about 1 / sqrt(m n) and
 // S's 1 / m at first.
 constexpr float X_UNIT = 4096.0f, S_UNIT = 4096.0f, E_UNIT = 256.0f;
-
-struct ListTile {      // of a product, with what it needs of its matrix; mp == 0: none
-  int64_t x, e;
-  int mp, np, mat;
-  short tm, tn;
-};
 
 // v as a sum of two binary16 numbers.  Both have to come from the same binary32 number: left to itself the compiler may form the
 // first from a product before that is rounded to binary32 (v_fma_mixlo_f16), and the second from the rounded one, which puts
@@ -806,7 +789,7 @@ __global__ __launch_bounds__(BLOCK) void k_muon_pack(const SquareTile* tiles, co
 // gradient to the updated parameters, step by step with 22 bits (in both precisions: it is not the multiply-adds that
 // count here, but the fifteen products' latency).  12 matrices of 64 x 64 to 256 x 64 with momentum and update: 40 us, in which a step
 // takes 2.8 us and 0.6 for every 64 columns more (its binary16 pairs cost as much as its products); 74 us with tiles.
-constexpr int SMALL_M = 64, SMALL_N = 512, SMALL_NT = 512, MAX_STEPS = 64;
+constexpr int SMALL_NT = 512, MAX_STEPS = 64;
 struct SmallArgs {
   const Matrix* mats;
   Direction d;
