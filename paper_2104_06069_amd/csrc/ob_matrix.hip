@@ -481,7 +481,7 @@ ob_status create(const ob_muon_config* cfg, ob_muon_ctx* ctx) {
     if (!hip_ok(ctx, e, "hipFuncSetAttribute")) return OB_ERR_HIP;
   }
   ctx->mats = (int)mats.size();
-  for (const Matrix& m : mats) ctx->norms = ctx->norms || m.tiles > 64;
+  ctx->norms = norms_apart(mats);
   ctx->square_tiles = (int)square.size();
   ctx->x_plane = xs;
   ctx->e_plane = es;

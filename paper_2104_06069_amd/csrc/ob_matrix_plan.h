@@ -110,6 +110,14 @@ struct ListTile {      // of a product, with what it needs of its matrix; mp == 
 
 constexpr int SMALL_M = 64, SMALL_N = 512;      // k_polar_small: lists of which no matrix is larger
 
+// Whether the norms get a launch of their own (k_muon_norms) instead of being added up by every workgroup of k_muon_pack.  us of a call in 11 bits
+// with it / without: 4 matrices of 256 tiles 321 / 316, 12 of 256 335 / 327, 4 of 1024 708 / 706, one of 16384 (8192 x 8192) 13753 / 13909,
+// (1024 x 65536) 1207 / 1315.
+constexpr int NORMS_APART = 256;
+inline bool norms_apart(const std::vector<Matrix>& mats) {
+  return std::any_of(mats.begin(), mats.end(), [](const Matrix& m) { return m.tiles > NORMS_APART; });
+}
+
 // Tiles of a product over the list, dealt to the eight dies: workgroup id runs on die id % 8, so that place id of the table
 // is place id / 8 of that die's queue.  Up to 4 x 8 neighbouring tiles of a matrix (what a die runs at once) stay together;
 // the dearest go first, each to the queue that has the least to do.
