@@ -1,4 +1,8 @@
 // Kernels of the matrix operators (include/ob_matrix.h), on the tiles of ob_mm.h.  Included by ob_matrix.hip only.
+//
+// Times stated beside the kernels are calls among others of their kind, timed by events; those of single kernels of the
+// orthogonalised update, marked P, are medians under the profiler, where they come out up to 17% longer (the two large gradients of
+// an expert layer 2.54 ms there, 2.26 ms without).
 #pragma once
 
 #include <type_traits>
@@ -208,9 +212,9 @@ struct RowTiles {
 
 // forward (x, W, y) and input_grad (dy, W transposed, dx): out[r] = a[r] W_g, a [rows, depth], out [rows, width].  FB: order
 // of W as an operand of `width` rows.  Tiles of 256 are bounded by the matrix instructions, and by their results, which all CUs
-// write at about the same time: 32768 rows over 16 groups, 8192 deep, 2048 wide in 1.25 ms, 880 TFLOP/s; 16384 over 8, 1024 deep,
-// 4096 wide in 165 us, 830.  Tiles of 64 are for calls with too few of those, which the latency of their slabs bounds: 4096 rows
-// over 16 groups, 2048 deep, 512 wide in 29 us, 300 TFLOP/s.
+// write at about the same time: 32768 rows over 16 groups, 8192 deep, 2048 wide in 1.07 ms, 1025 TFLOP/s; 16384 over 8, 1024 deep,
+// 4096 wide in 176 us, 780.  Tiles of 64 are for calls with too few of those, which the latency of their slabs bounds: 4096 rows
+// over 16 groups, 2048 deep, 512 wide in 28 us, 305 TFLOP/s.
 struct RowsArgs {
   Groups groups;
   const uint16_t* a;
@@ -366,8 +370,8 @@ __global__ __launch_bounds__(256, 2) void k_experts_few_rows(RowsArgs p) {
 // each has `parts` workgroups, a share of the group's rows each: their sums go to `partial`, and k_experts_join adds them up.  (The
 // last one to arrive adding them up in the same launch was tried: making the others' sums visible across the dies took three
 // times as long as all the rest, 94 us in place of 33 without parts.)  Both operands are read across their rows in LDS.  Bounded by
-// the matrix instructions, 32768 rows over 16 groups of 2048 x 8192 in 1.29 ms, 850 TFLOP/s; with few rows by writing out: 4096 over
-// 16 of 512 x 2048, binary32, in 26 us, 2.6 TB/s in one burst.
+// the matrix instructions, 32768 rows over 16 groups of 2048 x 8192 in 1.13 ms, 970 TFLOP/s; with few rows by writing out: 4096 over
+// 16 of 512 x 2048, binary32, in 27 us, 2.5 TB/s in one burst.
 struct WeightsArgs {
   Groups groups;
   const uint16_t* a;
@@ -497,7 +501,7 @@ __device__ __forceinline__ void store_terms8(uint16_t* plane, int64_t term, int6
 // grow by a^2 a step; so S is formed from X again after steps that together make more than 2^8 of it.  The usual 5 steps
 // are 3 and 2: of multiply-adds, in m^3, 3 n / m + 7 in place of 7.5 n / m + 2.5, the same for n = m, 19 in place of 32.5
 // for n = 4 m.
-// In the 2-norm over the matrix 2e-6 to 3e-6 off for matrices of normal numbers, 1.6e-5 for a sixteenth of the rank with 1%
+// In the 2-norm over the matrix 1e-6 to 3e-6 off for matrices of normal numbers, 1.6e-5 for a sixteenth of the rank with 1%
 // noise (binary32 products in the plain order: 1e-6 to 2e-6, and 1.7e-5); with one S for all 5 steps 3e-5 and 2e-3.
 //
 // With 11 bits for the [m, m] matrices those errors would be 1e-1, so there the plain order stays: with c != 0,
@@ -517,8 +521,8 @@ __host__ __device__ inline Shifted shifted(float a, float b, float c) {
 }
 
 // One or two products of [mp, mp] results over the list, of which those with j == blockIdx.y: out = mul A B^T + add_mul ADD +
-// diag on the diagonal.  48 matrices with m = 1024, 22 bits, half their tiles: X X^T with n = 4096 in 637 us, 1210 TFLOP/s of
-// matrix instructions, which bound it; the products 1024 deep in 226 us, 850 TFLOP/s, the matrix units busy half the time: the
+// diag on the diagonal.  48 matrices with m = 1024, 22 bits, half their tiles: X X^T with n = 4096 in 637 us (P), 1210 TFLOP/s of
+// matrix instructions, which bound it; the products 1024 deep in 226 us (P), 850 TFLOP/s, the matrix units busy half the time: the
 // results, on both sides of the diagonal, are written by all CUs at about the same time.
 struct SymmetricArgs {
   const ListTile* tiles;
@@ -599,7 +603,7 @@ struct Finish {
 };
 
 // X' = mul B X, or with LAST what becomes of it.  Bounded as the symmetric products: 48 of [1024, 1024] by [1024, 4096], 22 bits,
-// in 1.03 ms, 1200 TFLOP/s of matrix instructions; with the update of binary32 parameters 1.34 ms.
+// in 1.03 ms (P), 1200 TFLOP/s of matrix instructions; with the update of binary32 parameters 1.34 ms (P).
 struct ApplyArgs {
   const ListTile* tiles;
   const Matrix* mats;
@@ -687,7 +691,7 @@ __device__ __forceinline__ v4f direction4(const Direction& d, v4f g, v4f m) {
 }
 
 // m <- beta m + (1 - beta) scale g, and the sum of u's squares over each tile, in binary64.  Bounded by HBM: 302M elements with
-// binary32 gradients in 670 us, 5.4 TB/s.
+// binary32 gradients in 670 us (P), 5.4 TB/s.
 __global__ __launch_bounds__(BLOCK) void k_muon_moments(const SquareTile* tiles, const Matrix* mats, Direction d, float* m_out, double* sums) {
   const SquareTile t = tiles[blockIdx.x];
   const Matrix& mat = mats[t.mat];
@@ -746,8 +750,8 @@ __global__ __launch_bounds__(BLOCK) void k_muon_norms(const Matrix* mats, const 
 }
 
 // X = u / (norm + eps), transposed for tall matrices, zeros around it.  inv == NULL: every workgroup adds up its matrix's sums
-// itself, which for matrices of few tiles takes less than a launch.  Bounded by HBM: 302M elements of m and g into two terms in 700
-// us, 5.2 TB/s.
+// itself, which for matrices of few tiles takes less than a launch (norms_apart).  Bounded by HBM: 302M elements of m and g into two
+// terms in 700 us (P), 5.2 TB/s.
 __global__ __launch_bounds__(BLOCK) void k_muon_pack(const SquareTile* tiles, const Matrix* mats, Direction d, const Inverse* inv, const double* sums,
                                                      float eps, uint16_t* x, int64_t term) {
   __shared__ float turned[SIDE][SIDE + 1];
@@ -787,8 +791,11 @@ __global__ __launch_bounds__(BLOCK) void k_muon_pack(const SquareTile* tiles, co
 
 // A whole list of small matrices (m <= 64, n <= 512) in one launch, a workgroup each: X stays in LDS as two terms from the
 // gradient to the updated parameters, step by step with 22 bits (in both precisions: it is not the multiply-adds that
-// count here, but the fifteen products' latency).  12 matrices of 64 x 64 to 256 x 64 with momentum and update: 40 us, in which a step
-// takes 2.8 us and 0.6 for every 64 columns more (its binary16 pairs cost as much as its products); 74 us with tiles.
+// count here, but the fifteen products' latency).  12 matrices of 64 x 64 to 256 x 64 with momentum and update: 41 us, of
+// which about 17 are the way in and out, in trips to memory that wait for each other; a step takes 2.8 us and 0.6 for every 64 columns more (its
+// binary16 pairs cost as much as its products).  74 us with tiles, and less than those at every size measured, us in one launch /
+// with tiles of 22 bits / of 11: 12 of 64 x 64 19 / 61 / 56, 12 of 64 x 512 62 / 78 / 66, one of it 61 / 73 / 61, 2048 of 64 x 64 99 / 243 / 188,
+// 2048 of 64 x 512 595 / 821 / 954.
 constexpr int SMALL_NT = 512, MAX_STEPS = 64;
 struct SmallArgs {
   const Matrix* mats;

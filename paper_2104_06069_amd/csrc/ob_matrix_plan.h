@@ -108,7 +108,7 @@ struct ListTile {      // of a product, with what it needs of its matrix; mp == 
   short tm, tn;
 };
 
-constexpr int SMALL_M = 64, SMALL_N = 512;      // k_polar_small: lists of which no matrix is larger
+constexpr int SMALL_M = 64, SMALL_N = 512;      // k_polar_small (where both sides' times are): lists of which no matrix is larger
 
 // Whether the norms get a launch of their own (k_muon_norms) instead of being added up by every workgroup of k_muon_pack.  us of a call in 11 bits
 // with it / without: 4 matrices of 256 tiles 321 / 316, 12 of 256 335 / 327, 4 of 1024 708 / 706, one of 16384 (8192 x 8192) 13753 / 13909,
@@ -229,8 +229,13 @@ inline bool following_pays(const std::vector<Matrix>& mats, const std::vector<fl
 // 11 bits, step by step: 12.5 n / m + 2.5 (in m^3, 5 steps); 22 bits, following S with one S, which will do there: three
 // times 1.5 n / m + 8.5, less from n = 3 m on.  With 22 bits following S takes as many multiply-adds as step by step for
 // n = m, and more launches and writes (8 of 1024 x 1024: 1010 and 787 us, 4 of 1024 x 4096: 895 and 1277).  Each of the
-// two ways is worth launches of its own where there is much for it.
-constexpr double MUCH = 1e10;      // of m m n
+// two ways is worth launches of its own where there is much for it: MUCH, of m m n, for the wide ones, and with 22 bits for the
+// others too.  us apart / together: 22 bits, four [m, m] to one [m, 4 m], 4.3e9 of each 852 / 720 (m = 1024) and 781 / 719 (512),
+// 8.6e9 1243 / 1124 and 1263 / 1450, 1.3e10 1601 / 1918, 1.7e10 1990 / 2156 and 2431 / 2829.  11 bits, wide ones following S / all step by
+// step: [1024, 4096], 8.6e9 877 / 873 (beside [1024, 1024]), 1.7e10 711 / 594, 5.2e10 1473 / 1531, 2.1e11 5638 / 6014; n = 8 m, 2.6e10
+// 726 / 911, 1e11 2008 / 2878; n = 3 m, [768, 2304], 3.3e10 2529 / 2211.  (So at 11 bits n = 3 m and 4 m lose up to a fifth between 1e10 and
+// 5e10, and n = 8 m gains as much.)
+constexpr double MUCH = 1e10;
 inline std::vector<Part> parts_of(const std::vector<Matrix>& mats, const std::vector<float>& coefficients, bool fine) {
   std::vector<int> each[2];
   double work[2] = {};

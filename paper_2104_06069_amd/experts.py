@@ -29,7 +29,8 @@ def _adjacent(t):
 class ExpertLinear:
     def __init__(self, num_groups, k, n, dtype=torch.bfloat16, max_rows=1 << 20, layout="kn", w_stride=0, device="cuda:0"):
         """layout: "kn", W is [num_groups, k, n], or "nk", [num_groups, n, k].  w_stride: elements from one expert's weights
-        to the next one's (0: they follow each other)."""
+        to the next one's (0: they follow each other).  Weight gradients share the object's workspace: calls on one object, those of
+        autograd among them, must not overlap in time; on several streams, each has to wait for the one before."""
         self.device = torch.device(device)
         torch.cuda.set_device(self.device)
         self.groups, self.k, self.n, self.dtype, self.layout = int(num_groups), int(k), int(n), dtype, layout
