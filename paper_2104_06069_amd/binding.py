@@ -67,6 +67,23 @@ class ObMuonConfig(C.Structure):
                 ("weight_decay", C.c_float), ("nesterov", C.c_int32), ("precision", C.c_int32)]
 
 
+# include/ob_layer.h
+OB_E4M3, OB_E5M2 = 0, 1
+OB_BLOCK_ROWS, OB_BLOCK_SQUARE = 0, 1
+
+
+class ObNormConfig(C.Structure):
+    _fields_ = [("n", C.c_int64), ("dtype", C.c_int32), ("res_dtype", C.c_int32), ("weight_dtype", C.c_int32), ("eps", C.c_float)]
+
+
+class ObLinear8Config(C.Structure):
+    _fields_ = [("k", C.c_int64), ("n", C.c_int64), ("max_rows", C.c_int64)]
+
+
+class ObClipConfig(C.Structure):
+    _fields_ = [("num_layers", C.c_int64), ("layer_offsets", C.POINTER(C.c_int64)), ("eps", C.c_float), ("grad_scale", C.c_float)]
+
+
 def lib_path():
     return os.path.join(_PKG, "lib", "libonebitlamb.so")
 
@@ -125,6 +142,27 @@ def lib():
             "ob_lamb_profile_enable": (C.c_int, [vp, C.c_int]),
             "ob_lamb_profile_read": (i32, [vp, i32, C.POINTER(C.c_char_p), C.POINTER(C.c_double),
                                            C.POINTER(i64)]),
+            "ob_norm_create": (C.c_int, [C.POINTER(ObNormConfig), C.POINTER(vp)]),
+            "ob_norm_destroy": (None, [vp]),
+            "ob_norm_workspace_bytes": (C.c_size_t, [vp]),
+            "ob_norm_last_hip_error": (C.c_char_p, [vp]),
+            "ob_norm_forward": (C.c_int, [vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, i32, vp, vp]),
+            "ob_norm_backward": (C.c_int, [vp, vp, i64, vp, i64, vp, vp, vp, i64, i64, vp, i64, vp, i32, vp]),
+            "ob_linear8_create": (C.c_int, [C.POINTER(ObLinear8Config), C.POINTER(vp)]),
+            "ob_linear8_destroy": (None, [vp]),
+            "ob_linear8_workspace_bytes": (C.c_size_t, [vp]),
+            "ob_linear8_last_hip_error": (C.c_char_p, [vp]),
+            "ob_linear8_quantize": (C.c_int, [vp, vp, C.c_int, i64, i64, i64, i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp]),
+            "ob_linear8_forward": (C.c_int, [vp, vp, i64, vp, i64, i32, vp, i64, vp, i64, i64, vp, i64, C.c_int, vp]),
+            "ob_linear8_input_grad": (C.c_int, [vp, vp, i64, vp, i64, i32, vp, i64, vp, i64, i64, vp, i64, C.c_int, vp]),
+            "ob_linear8_weight_grad": (C.c_int, [vp, vp, i64, vp, i64, i32, vp, i64, vp, i64, i64, vp, i64, C.c_int, i32, vp]),
+            "ob_clip_create": (C.c_int, [C.POINTER(ObClipConfig), C.POINTER(vp)]),
+            "ob_clip_destroy": (None, [vp]),
+            "ob_clip_workspace_bytes": (C.c_size_t, [vp]),
+            "ob_clip_last_hip_error": (C.c_char_p, [vp]),
+            "ob_clip_norm": (C.c_int, [vp, vp, C.c_int, vp, vp, vp]),
+            "ob_clip_apply": (C.c_int, [vp, vp, C.c_int, vp, f, vp, C.c_int, vp]),
+            "ob_clip_norm_apply": (C.c_int, [vp, vp, C.c_int, f, vp, vp, vp, C.c_int, vp]),
             "ob_experts_create": (C.c_int, [C.POINTER(ObExpertsConfig), C.POINTER(vp)]),
             "ob_experts_destroy": (None, [vp]),
             "ob_experts_workspace_bytes": (C.c_size_t, [vp]),
@@ -502,3 +540,114 @@ def ob_muon_step(ctx, x, m, grad, grad_dtype, grad_scale, lr, x_lp=None, x_dtype
     L = lib()
     _check_matrix(L.ob_muon_step(ctx, _addr(x), _addr(m), _addr(grad), grad_dtype, grad_scale, lr, _addr(x_lp), x_dtype, _addr(stream)),
                   ctx, "ob_muon_step", L.ob_muon_last_hip_error)
+
+
+# ---- operators of a layer in 8 bits and of the flat gradient (include/ob_layer.h) ------------------
+def _create(call, cfg, where):
+    out = C.c_void_p()
+    st = call(C.byref(cfg), C.byref(out))
+    if st != OB_OK:
+        raise ObLambError(st, where)
+    return out
+
+
+def ob_norm_create(n, dtype, res_dtype, weight_dtype=OB_F32, eps=1e-6):
+    """-> opaque context handle (on the current HIP device)."""
+    return _create(lib().ob_norm_create, ObNormConfig(int(n), int(dtype), int(res_dtype), int(weight_dtype), float(eps)), "ob_norm_create")
+
+
+def ob_norm_destroy(ctx):
+    lib().ob_norm_destroy(ctx)
+
+
+def ob_norm_workspace_bytes(ctx):
+    return int(lib().ob_norm_workspace_bytes(ctx))
+
+
+def ob_norm_forward(ctx, x, ldx, residual, ldr, weight, rows, h, ldh, y, ldy, data, ld, scales, ld_scales, format, rstd, stream=None):
+    L = lib()
+    _check_matrix(L.ob_norm_forward(ctx, _addr(x), ldx, _addr(residual), ldr, _addr(weight), rows, _addr(h), ldh, _addr(y), ldy, _addr(data), ld,
+                                    _addr(scales), ld_scales, format, _addr(rstd), _addr(stream)),
+                  ctx, "ob_norm_forward", L.ob_norm_last_hip_error)
+
+
+def ob_norm_backward(ctx, dy, lddy, h, ldh, rstd, weight, dres, lddres, rows, dh, lddh, dweight, accumulate=False, stream=None):
+    L = lib()
+    _check_matrix(L.ob_norm_backward(ctx, _addr(dy), lddy, _addr(h), ldh, _addr(rstd), _addr(weight), _addr(dres), lddres, rows, _addr(dh), lddh,
+                                     _addr(dweight), int(bool(accumulate)), _addr(stream)),
+                  ctx, "ob_norm_backward", L.ob_norm_last_hip_error)
+
+
+def ob_linear8_create(k, n, max_rows=1 << 22):
+    """-> opaque context handle (on the current HIP device)."""
+    return _create(lib().ob_linear8_create, ObLinear8Config(int(k), int(n), int(max_rows)), "ob_linear8_create")
+
+
+def ob_linear8_destroy(ctx):
+    lib().ob_linear8_destroy(ctx)
+
+
+def ob_linear8_workspace_bytes(ctx):
+    return int(lib().ob_linear8_workspace_bytes(ctx))
+
+
+def ob_linear8_quantize(ctx, src, src_dtype, lds, rows, cols, form, format, format_t, data, ld, scales, ld_scales, data_t, ld_t, scales_t, ld_scales_t,
+                        stream=None):
+    L = lib()
+    _check_matrix(L.ob_linear8_quantize(ctx, _addr(src), src_dtype, lds, rows, cols, form, format, format_t, _addr(data), ld, _addr(scales), ld_scales,
+                                        _addr(data_t), ld_t, _addr(scales_t), ld_scales_t, _addr(stream)),
+                  ctx, "ob_linear8_quantize", L.ob_linear8_last_hip_error)
+
+
+def ob_linear8_forward(ctx, x, ldx, x_scales, ldx_scales, x_format, w, ldw, w_scales, ldw_scales, rows, y, ldy, y_dtype, stream=None):
+    L = lib()
+    _check_matrix(L.ob_linear8_forward(ctx, _addr(x), ldx, _addr(x_scales), ldx_scales, x_format, _addr(w), ldw, _addr(w_scales), ldw_scales, rows,
+                                       _addr(y), ldy, y_dtype, _addr(stream)),
+                  ctx, "ob_linear8_forward", L.ob_linear8_last_hip_error)
+
+
+def ob_linear8_input_grad(ctx, dy, lddy, dy_scales, lddy_scales, dy_format, w_t, ldw_t, w_t_scales, ldw_t_scales, rows, dx, lddx, dx_dtype, stream=None):
+    L = lib()
+    _check_matrix(L.ob_linear8_input_grad(ctx, _addr(dy), lddy, _addr(dy_scales), lddy_scales, dy_format, _addr(w_t), ldw_t, _addr(w_t_scales),
+                                          ldw_t_scales, rows, _addr(dx), lddx, dx_dtype, _addr(stream)),
+                  ctx, "ob_linear8_input_grad", L.ob_linear8_last_hip_error)
+
+
+def ob_linear8_weight_grad(ctx, dy_t, lddy_t, dy_t_scales, lddy_t_scales, dy_format, x_t, ldx_t, x_t_scales, ldx_t_scales, rows, dw, lddw, dw_dtype,
+                           accumulate=False, stream=None):
+    L = lib()
+    _check_matrix(L.ob_linear8_weight_grad(ctx, _addr(dy_t), lddy_t, _addr(dy_t_scales), lddy_t_scales, dy_format, _addr(x_t), ldx_t, _addr(x_t_scales),
+                                           ldx_t_scales, rows, _addr(dw), lddw, dw_dtype, int(bool(accumulate)), _addr(stream)),
+                  ctx, "ob_linear8_weight_grad", L.ob_linear8_last_hip_error)
+
+
+def ob_clip_create(layer_offsets, eps=1e-6, grad_scale=1.0):
+    """-> opaque context handle (on the current HIP device)."""
+    offs = [int(o) for o in layer_offsets]
+    return _create(lib().ob_clip_create, ObClipConfig(len(offs) - 1, (C.c_int64 * len(offs))(*offs), float(eps), float(grad_scale)), "ob_clip_create")
+
+
+def ob_clip_destroy(ctx):
+    lib().ob_clip_destroy(ctx)
+
+
+def ob_clip_workspace_bytes(ctx):
+    return int(lib().ob_clip_workspace_bytes(ctx))
+
+
+def ob_clip_norm(ctx, grad, grad_dtype, norm, layer_norms=None, stream=None):
+    L = lib()
+    _check_matrix(L.ob_clip_norm(ctx, _addr(grad), grad_dtype, _addr(norm), _addr(layer_norms), _addr(stream)), ctx, "ob_clip_norm",
+                  L.ob_clip_last_hip_error)
+
+
+def ob_clip_apply(ctx, grad, grad_dtype, norm, max_norm, out, out_dtype, stream=None):
+    L = lib()
+    _check_matrix(L.ob_clip_apply(ctx, _addr(grad), grad_dtype, _addr(norm), max_norm, _addr(out), out_dtype, _addr(stream)), ctx, "ob_clip_apply",
+                  L.ob_clip_last_hip_error)
+
+
+def ob_clip_norm_apply(ctx, grad, grad_dtype, max_norm, norm, layer_norms, out, out_dtype, stream=None):
+    L = lib()
+    _check_matrix(L.ob_clip_norm_apply(ctx, _addr(grad), grad_dtype, max_norm, _addr(norm), _addr(layer_norms), _addr(out), out_dtype, _addr(stream)),
+                  ctx, "ob_clip_norm_apply", L.ob_clip_last_hip_error)

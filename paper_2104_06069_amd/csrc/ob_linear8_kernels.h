@@ -1,0 +1,173 @@
+// Kernels of the linear layer in 8 bits (include/ob_layer.h), on the tiles of ob_mm8.h.  Included by ob_linear8.hip only.
+#pragma once
+
+#include "ob_mm8.h"
+
+namespace obl {
+
+// ---- to 8 bits -----------------------------------------------------------------------------------------------------
+struct QuantizeArgs {
+  const void* src;
+  int64_t lds;
+  int rows, cols, format, format_t;
+  uint8_t *data, *scales, *data_t, *scales_t;
+  int64_t ld, ld_scales, ld_t, ld_scales_t;
+};
+
+// Bytes of numbers from `left` on are zeros
+__device__ __forceinline__ v2i bytes_before(v2i q, int left) {
+  if (left >= 8) return q;
+  const unsigned long long keep = left <= 0 ? 0 : ~0ull >> (64 - 8 * left);
+  q.x &= (int)(unsigned)keep;
+  q.y &= (int)(unsigned)(keep >> 32);
+  return q;
+}
+
+// A workgroup takes 128 x 128 numbers, a thread eight adjacent rows by eight adjacent columns of them: a row's block is that of
+// sixteen adjacent lanes, a column's that of sixteen lanes one from each group of those, four in a wavefront.  The transposed
+// bytes are turned in LDS, so that both results go out 128 bytes of a row at a time.
+template <int DTYPE, bool SQUARE>
+__global__ __launch_bounds__(256) void k_quantize8(QuantizeArgs p) {
+  constexpr int PITCH = BLOCK8 + 16;
+  __shared__ __align__(16) uint8_t turned[BLOCK8 * PITCH];
+  __shared__ unsigned most_of[4][BLOCK8];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, rg = tid >> 4, cg = tid & 15;
+  const int r0 = blockIdx.y * BLOCK8, c0 = blockIdx.x * BLOCK8, left = p.cols - c0 - cg * 8, below = p.rows - r0 - rg * 8;
+  float v[8][8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) load8<DTYPE>(p.src, (int64_t)(r0 + rg * 8 + i) * p.lds + c0 + cg * 8, i < below ? left : 0, v[i]);
+  unsigned row_most[8], col_most[8] = {};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    row_most[i] = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const unsigned m = magnitude(v[i][e]);
+      row_most[i] = max(row_most[i], m);
+      col_most[e] = max(col_most[e], m);
+    }
+  }
+  if constexpr (SQUARE) {
+    unsigned m = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) m = max(m, col_most[e]);
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) m = max(m, (unsigned)__shfl_xor((int)m, d));
+    if (lane == 0) most_of[wave][0] = m;
+    __syncthreads();
+    m = max(max(most_of[0][0], most_of[1][0]), max(most_of[2][0], most_of[3][0]));
+#pragma unroll
+    for (int e = 0; e < 8; ++e) row_most[e] = col_most[e] = m;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int d = 8; d >= 1; d >>= 1) row_most[i] = max(row_most[i], (unsigned)__shfl_xor((int)row_most[i], d));
+    if (p.data_t) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+#pragma unroll
+        for (int d = 32; d >= 16; d >>= 1) col_most[e] = max(col_most[e], (unsigned)__shfl_xor((int)col_most[e], d));
+        if (lane < 16) most_of[wave][cg * 8 + e] = col_most[e];
+      }
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int c = cg * 8 + e;
+        col_most[e] = max(max(most_of[0][c], most_of[1][c]), max(most_of[2][c], most_of[3][c]));
+      }
+    }
+  }
+  if (p.data) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int byte = scale_byte(row_most[i], p.format);
+      const v2i q = bytes_before(bytes8(v[i], inverse_scale(byte), p.format), left);
+      if (i < below) {
+        const int64_t row = r0 + rg * 8 + i;
+        *reinterpret_cast<v2i*>(p.data + row * p.ld + c0 + cg * 8) = q;
+        if (cg == 0 && (!SQUARE || (rg == 0 && i == 0))) p.scales[(SQUARE ? row / BLOCK8 : row) * p.ld_scales + blockIdx.x] = (uint8_t)byte;
+      }
+    }
+  }
+  if (p.data_t) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int byte = scale_byte(col_most[e], p.format_t);
+      float w[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i] = v[i][e];
+      *reinterpret_cast<v2i*>(turned + (cg * 8 + e) * PITCH + rg * 8) = bytes_before(bytes8(w, inverse_scale(byte), p.format_t), below);
+      if (rg == 0 && e < left) {
+        const int64_t col = c0 + cg * 8 + e;
+        if (!SQUARE) p.scales_t[col * p.ld_scales_t + blockIdx.y] = (uint8_t)byte;
+        else if (cg == 0 && e == 0) p.scales_t[col / BLOCK8 * p.ld_scales_t + blockIdx.y] = (uint8_t)byte;
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int col = j * 32 + tid / 8, at = tid % 8 * 16;
+      if (c0 + col < p.cols) *reinterpret_cast<v4i*>(p.data_t + (int64_t)(c0 + col) * p.ld_t + r0 + at) = *reinterpret_cast<const v4i*>(turned + col * PITCH + at);
+    }
+  }
+}
+
+// ---- products --------------------------------------------------------------------------------------------------------
+struct Product8Args {
+  Operand8 a, b;
+  void* out;
+  float* partial;      // [parts, rows, cols], with parts > 1
+  int64_t ldo;
+  int slabs, parts, out_dtype;
+  bool accumulate;
+};
+
+extern __shared__ __align__(1024) uint16_t lds_of_product8[];
+
+template <class S, int FORMAT, bool WIDE>
+__global__ __launch_bounds__(S::NT, 2) void k_product8(Product8Args p) {
+  using P = Product8<S, FORMAT, WIDE>;
+  const int nm = (p.a.rows + S::BM - 1) / S::BM, nn = (p.b.rows + S::BN - 1) / S::BN, tiles = nm * nn;
+  const int at = tile_of_workgroup(blockIdx.x, tiles * p.parts);
+  if (at < 0) return;
+  int tm, tn;
+  tile_in_bands(at % tiles, nm, nn, &tm, &tn);
+  const int part = at / tiles, first = (int)((int64_t)p.slabs * part / p.parts), end = (int)((int64_t)p.slabs * (part + 1) / p.parts);
+  const int r0 = tm * S::BM, c0 = tn * S::BN;
+  typename P::Acc acc = {};
+  P::run(p.a, p.b, r0, c0, first, end - first, lds_of_product8, acc);
+  const int rows = p.a.rows, cols = p.b.rows;
+  if (p.parts > 1) {
+    store_tile<S, true>(acc, lds_of_product8, p.partial + (int64_t)part * rows * cols, F32, cols, r0, c0, rows, cols, 0, 0);
+  } else if constexpr (WIDE) {
+    if (p.accumulate) {
+      Results<S>::by_rows(acc, lds_of_product8, [&](int r, int c, v4f v) {
+        r += r0;
+        c += c0;
+        if (r < rows) store4(p.out, F32, (int64_t)r * p.ldo + c, cols - c, v + load4(p.out, F32, (int64_t)r * p.ldo + c, cols - c));
+      });
+    } else {
+      store_tile<S, true>(acc, lds_of_product8, p.out, F32, p.ldo, r0, c0, rows, cols, 0, 0);
+    }
+  } else if (p.out_dtype == BF16) {
+    store_tile<S, true>(acc, lds_of_product8, p.out, BF16, p.ldo, r0, c0, rows, cols, 0, 0);
+  } else {
+    store_tile<S, false>(acc, lds_of_product8, p.out, F16, p.ldo, r0, c0, rows, cols, 0, 0);
+  }
+}
+
+// The parts of a product's sums, in their order
+__global__ __launch_bounds__(256) void k_product8_join(Product8Args p) {
+  const int64_t rows = p.a.rows, cols = p.b.rows, fours = (cols + 3) / 4;
+  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (at >= rows * fours) return;
+  const int64_t r = at / fours, c = at % fours * 4;
+  const int left = (int)min(cols - c, (int64_t)4);
+  v4f sum = load4(p.partial, F32, r * cols + c, left);
+  for (int k = 1; k < p.parts; ++k) sum += load4(p.partial, F32, (k * rows + r) * cols + c, left);
+  if (p.accumulate) sum += load4(p.out, F32, r * p.ldo + c, left);
+  store4(p.out, p.out_dtype, r * p.ldo + c, left, sum);
+}
+
+}  // namespace obl

@@ -1,5 +1,5 @@
 // Core of the matrix operators (gfx950): one workgroup's tile of C = A B^T with 16-bit operands and binary32
-// accumulation, on the matrix cores.  Included by ob_matrix.hip only.
+// accumulation, on the matrix cores.
 //
 // An operand is a matrix of `rows` rows (the tile's M or N side) and K columns, in one of two orders: KC, element (r, k)
 // at p[r * ld + k], or KS, element (r, k) at p[k * ld + r].  It has one or two terms (planes `term` elements apart): with

@@ -1,0 +1,136 @@
+// libonebitlamb: host side of the root-mean-square norm (include/ob_layer.h) -- contexts, argument validation and launches.  The
+// kernels live in ob_norm_kernels.h.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <new>
+#include <type_traits>
+
+#include "ob_host.h"
+#include "ob_layer.h"
+#include "ob_norm_kernels.h"
+
+using namespace obl;
+
+struct ob_norm_ctx {
+  ob_norm_config cfg;
+  int device = -1;
+  int most_parts = 1;      // workgroups of k_norm_backward that there is room for
+  size_t bytes = 0;
+  float* d_partial = nullptr;
+  std::string hip_err;
+  ~ob_norm_ctx() {
+    if (d_partial) (void)hipFree(d_partial);
+  }
+};
+
+namespace {
+
+constexpr int64_t MOST_N = 16384, MOST_LD = (int64_t)1 << 31;
+
+template <int V>
+using Int = std::integral_constant<int, V>;
+
+// f(type of x, type of h, threads of a row, pieces of a thread)
+template <int X, int H, class F>
+ob_status with_size(int64_t n, F f) {
+  if (n <= 512) return f(Int<X>{}, Int<H>{}, Int<64>{}, Int<1>{});
+  if (n <= 1024) return f(Int<X>{}, Int<H>{}, Int<64>{}, Int<2>{});
+  if (n <= 2048) return f(Int<X>{}, Int<H>{}, Int<64>{}, Int<4>{});
+  if (n <= 4096) return f(Int<X>{}, Int<H>{}, Int<256>{}, Int<2>{});
+  if (n <= 8192) return f(Int<X>{}, Int<H>{}, Int<256>{}, Int<4>{});
+  return f(Int<X>{}, Int<H>{}, Int<512>{}, Int<4>{});
+}
+template <class F>
+ob_status with_kernel(const ob_norm_config& c, F f) {
+  if (c.dtype == OB_F32) return with_size<F32, F32>(c.n, f);
+  if (c.dtype == OB_F16) return c.res_dtype == OB_F32 ? with_size<F16, F32>(c.n, f) : with_size<F16, F16>(c.n, f);
+  return c.res_dtype == OB_F32 ? with_size<BF16, F32>(c.n, f) : with_size<BF16, BF16>(c.n, f);
+}
+
+// rows of T threads that a workgroup of k_norm_backward has at a time
+int sets_of(int64_t n) { return n <= 2048 ? 8 : n <= 8192 ? 2 : 1; }
+
+bool rows_wrong(int64_t ld, int64_t n) { return ld < n || ld >= MOST_LD; }
+
+}  // namespace
+
+extern "C" {
+
+ob_status ob_norm_create(const ob_norm_config* cfg, ob_norm_ctx** out) {
+  if (!cfg || !out) return OB_ERR_NULL;
+  *out = nullptr;
+  if (cfg->n < 1 || cfg->n > MOST_N || !any_dtype(cfg->dtype) || (cfg->res_dtype != cfg->dtype && cfg->res_dtype != OB_F32) ||
+      !any_dtype(cfg->weight_dtype) || !(cfg->eps >= 0) || !std::isfinite(cfg->eps))
+    return OB_ERR_ARG;
+  ob_norm_ctx* ctx = new (std::nothrow) ob_norm_ctx();
+  if (!ctx) return OB_ERR_ARG;
+  ctx->cfg = *cfg;
+  hipError_t e = hipGetDevice(&ctx->device);
+  ctx->most_parts = cfg->n <= 8192 ? 512 : 256;
+  ctx->bytes = (size_t)ctx->most_parts * cfg->n * sizeof(float);
+  if (e == hipSuccess) e = hipMalloc(&ctx->d_partial, ctx->bytes);
+  if (e != hipSuccess) {
+    delete ctx;
+    return OB_ERR_HIP;
+  }
+  *out = ctx;
+  return OB_OK;
+}
+
+void ob_norm_destroy(ob_norm_ctx* ctx) { delete ctx; }
+size_t ob_norm_workspace_bytes(const ob_norm_ctx* ctx) { return ctx ? ctx->bytes : 0; }
+const char* ob_norm_last_hip_error(const ob_norm_ctx* ctx) { return ctx ? ctx->hip_err.c_str() : ""; }
+
+ob_status ob_norm_forward(ob_norm_ctx* ctx, const void* x, int64_t ldx, const void* residual, int64_t ldr, const void* weight, int64_t rows,
+                          void* h, int64_t ldh, void* y, int64_t ldy, void* data, int64_t ld, void* scales, int64_t ld_scales, int32_t format,
+                          float* rstd, void* hip_stream) {
+  if (!ctx) return OB_ERR_NULL;
+  const ob_norm_config& c = ctx->cfg;
+  const int64_t blocks = (c.n + BLOCK8 - 1) / BLOCK8;
+  if (rows < 0 || rows > 0x7fffffff || rows_wrong(ldx, c.n) || (residual && (rows_wrong(ldr, c.n) || rows_wrong(ldh, c.n))) ||
+      (y && rows_wrong(ldy, c.n)) || (data && (ld % BLOCK8 || rows_wrong(ld, c.n) || ld_scales % 4 || rows_wrong(ld_scales, blocks))) ||
+      (data && format != OB_E4M3 && format != OB_E5M2))
+    return OB_ERR_ARG;
+  if (!on_device(ctx->device)) return OB_ERR_ARG;
+  if (!rows) return OB_OK;
+  if (!x || (residual && !h) || (!y && !data) || (data && !scales)) return OB_ERR_NULL;
+  if (off_element(x, c.dtype) || off_element(residual, c.res_dtype) || (residual && off_element(h, c.res_dtype)) || off_element(weight, c.weight_dtype) ||
+      off_element(y, c.dtype) || off(data, 16) || (data && off(scales, 4)) || off(rstd, 4))
+    return OB_ERR_ALIGN;
+  NormArgs p{x, residual, weight, h, y, static_cast<uint8_t*>(data), static_cast<uint8_t*>(scales), rstd, ldx, ldr, ldh, ldy, ld, ld_scales,
+             (int)rows, (int)c.n, c.weight_dtype, format, c.eps};
+  return with_kernel(c, [&](auto X, auto H, auto T, auto C) {
+    constexpr int NT = T < 256 ? 256 : T;
+    hipLaunchKernelGGL((k_norm_forward<X, H, T, C>), dim3((unsigned)((rows + NT / T - 1) / (NT / T))), dim3(NT), 0, static_cast<hipStream_t>(hip_stream), p);
+    return hip_ok(ctx, hipGetLastError(), "k_norm_forward") ? OB_OK : OB_ERR_HIP;
+  });
+}
+
+ob_status ob_norm_backward(ob_norm_ctx* ctx, const void* dy, int64_t lddy, const void* h, int64_t ldh, const float* rstd, const void* weight,
+                           const void* dres, int64_t lddres, int64_t rows, void* dh, int64_t lddh, float* dweight, int32_t accumulate, void* hip_stream) {
+  if (!ctx) return OB_ERR_NULL;
+  const ob_norm_config& c = ctx->cfg;
+  if (rows < 0 || rows > 0x7fffffff || rows_wrong(lddy, c.n) || rows_wrong(ldh, c.n) || (dres && rows_wrong(lddres, c.n)) || (dh && rows_wrong(lddh, c.n)))
+    return OB_ERR_ARG;
+  if (!on_device(ctx->device)) return OB_ERR_ARG;
+  if (!dh && !dweight) return OB_ERR_NULL;
+  if (rows && (!dy || !h || !rstd)) return OB_ERR_NULL;
+  if (off_element(dy, c.dtype) || off_element(h, c.res_dtype) || off(rstd, 4) || off_element(weight, c.weight_dtype) || off_element(dres, c.res_dtype) ||
+      off_element(dh, c.res_dtype) || off(dweight, 4))
+    return OB_ERR_ALIGN;
+  const int sets = sets_of(c.n);
+  const int parts = (int)std::max<int64_t>(std::min<int64_t>((rows + sets - 1) / sets, ctx->most_parts), 1);
+  NormGradArgs p{dy, h, weight, dres, rstd, dh, dweight, ctx->d_partial, lddy, ldh, lddres, lddh, (int)rows, (int)c.n, c.weight_dtype, accumulate != 0};
+  if (!rows && !dweight) return OB_OK;      // (without rows one workgroup writes zeros to dweight, or adds them)
+  const hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  return with_kernel(c, [&](auto X, auto H, auto T, auto C) {
+    hipLaunchKernelGGL((k_norm_backward<X, H, T, C>), dim3((unsigned)parts), dim3(norm_grad_threads<T>()), 0, s, p);
+    if (dweight && parts > 1)
+      hipLaunchKernelGGL(k_norm_join, dim3((unsigned)((c.n + 63) / 64)), dim3(256), 0, s, ctx->d_partial, parts, (int)c.n, p.accumulate, dweight);
+    return hip_ok(ctx, hipGetLastError(), "k_norm_backward") ? OB_OK : OB_ERR_HIP;
+  });
+}
+
+}  // extern "C"
