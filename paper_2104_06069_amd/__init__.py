@@ -20,8 +20,8 @@ from .binding import (  # noqa: F401
     OB_EXPERTS_KN, OB_EXPERTS_NK, ObExpertsConfig, ObMuonConfig, ob_experts_create, ob_experts_destroy, ob_experts_forward,
     ob_experts_input_grad, ob_experts_weight_grad, ob_experts_workspace_bytes, ob_muon_create, ob_muon_destroy,
     ob_muon_orthogonalize, ob_muon_step, ob_muon_workspace_bytes,
-    OB_E4M3, OB_E5M2, OB_BLOCK_ROWS, OB_BLOCK_SQUARE, ObNormConfig, ObLinear8Config, ObClipConfig, ob_norm_create, ob_norm_destroy,
+    OB_E4M3, OB_E5M2, OB_BLOCK_ROWS, OB_BLOCK_SQUARE, OB_LINEAR8_FEW_ROWS, ObNormConfig, ObLinear8Config, ObClipConfig, ob_norm_create, ob_norm_destroy,
     ob_norm_workspace_bytes, ob_norm_forward, ob_norm_backward, ob_linear8_create, ob_linear8_destroy, ob_linear8_workspace_bytes,
-    ob_linear8_quantize, ob_linear8_forward, ob_linear8_input_grad, ob_linear8_weight_grad, ob_clip_create, ob_clip_destroy,
+    ob_linear8_quantize, ob_linear8_forward, ob_linear8_forward_few, ob_linear8_input_grad, ob_linear8_weight_grad, ob_clip_create, ob_clip_destroy,
     ob_clip_workspace_bytes, ob_clip_norm, ob_clip_apply, ob_clip_norm_apply,
 )

@@ -70,6 +70,7 @@ class ObMuonConfig(C.Structure):
 # include/ob_layer.h
 OB_E4M3, OB_E5M2 = 0, 1
 OB_BLOCK_ROWS, OB_BLOCK_SQUARE = 0, 1
+OB_LINEAR8_FEW_ROWS = 16
 
 
 class ObNormConfig(C.Structure):
@@ -154,6 +155,7 @@ def lib():
             "ob_linear8_last_hip_error": (C.c_char_p, [vp]),
             "ob_linear8_quantize": (C.c_int, [vp, vp, C.c_int, i64, i64, i64, i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp]),
             "ob_linear8_forward": (C.c_int, [vp, vp, i64, vp, i64, i32, vp, i64, vp, i64, i64, vp, i64, C.c_int, vp]),
+            "ob_linear8_forward_few": (C.c_int, [vp, vp, C.c_int, i64, i32, vp, i64, vp, i64, i64, vp, i64, C.c_int, vp]),
             "ob_linear8_input_grad": (C.c_int, [vp, vp, i64, vp, i64, i32, vp, i64, vp, i64, i64, vp, i64, C.c_int, vp]),
             "ob_linear8_weight_grad": (C.c_int, [vp, vp, i64, vp, i64, i32, vp, i64, vp, i64, i64, vp, i64, C.c_int, i32, vp]),
             "ob_clip_create": (C.c_int, [C.POINTER(ObClipConfig), C.POINTER(vp)]),
@@ -604,6 +606,13 @@ def ob_linear8_forward(ctx, x, ldx, x_scales, ldx_scales, x_format, w, ldw, w_sc
     _check_matrix(L.ob_linear8_forward(ctx, _addr(x), ldx, _addr(x_scales), ldx_scales, x_format, _addr(w), ldw, _addr(w_scales), ldw_scales, rows,
                                        _addr(y), ldy, y_dtype, _addr(stream)),
                   ctx, "ob_linear8_forward", L.ob_linear8_last_hip_error)
+
+
+def ob_linear8_forward_few(ctx, x, x_dtype, ldx, x_format, w, ldw, w_scales, ldw_scales, rows, y, ldy, y_dtype, stream=None):
+    L = lib()
+    _check_matrix(L.ob_linear8_forward_few(ctx, _addr(x), x_dtype, ldx, x_format, _addr(w), ldw, _addr(w_scales), ldw_scales, rows, _addr(y), ldy, y_dtype,
+                                           _addr(stream)),
+                  ctx, "ob_linear8_forward_few", L.ob_linear8_last_hip_error)
 
 
 def ob_linear8_input_grad(ctx, dy, lddy, dy_scales, lddy_scales, dy_format, w_t, ldw_t, w_t_scales, ldw_t_scales, rows, dx, lddx, dx_dtype, stream=None):

@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <new>
+#include <type_traits>
 
 #include "ob_host.h"
 #include "ob_layer.h"
@@ -26,7 +27,9 @@ namespace {
 
 constexpr int64_t MOST = (int64_t)1 << 22;      // rows, columns and distances between rows: a tile's offsets are 32-bit
 
-using Tile8 = Shape<64, 64, 64, 2, 2, 3>;
+// Tiles by their side (ob_linear8_plan.h)
+template <int KIND>
+using Tile8 = std::conditional_t<KIND == W256, Shape<256, 256, 64, 2, 4>, std::conditional_t<KIND == W128, Shape<128, 128, 64, 2, 2>, Shape<64, 64, 64, 2, 2, 3>>>;
 
 template <class S, int FORMAT, bool WIDE>
 ob_status launch_product(ob_linear8_ctx* ctx, const Product8Args& p, hipStream_t s) {
@@ -40,10 +43,43 @@ ob_status launch_product(ob_linear8_ctx* ctx, const Product8Args& p, hipStream_t
   return hip_ok(ctx, hipGetLastError(), "k_product8") ? OB_OK : OB_ERR_HIP;
 }
 
-template <int FORMAT>
+// f(kind, format, wide)
+template <class F>
+auto with_product(int kind, int format, bool wide, F f) {
+  const auto with_kind = [&](auto format, auto wide) {
+    if (kind == W256) return f(std::integral_constant<int, W256>{}, format, wide);
+    if (kind == W128) return f(std::integral_constant<int, W128>{}, format, wide);
+    return f(std::integral_constant<int, W64>{}, format, wide);
+  };
+  const auto with_format = [&](auto format) { return wide ? with_kind(format, std::true_type{}) : with_kind(format, std::false_type{}); };
+  return format == OB_E4M3 ? with_format(std::integral_constant<int, E4M3>{}) : with_format(std::integral_constant<int, E5M2>{});
+}
+
 hipError_t allow_products() {
-  const hipError_t e = allow_lds(k_product8<Tile8, FORMAT, false>, Product8<Tile8, FORMAT, false>::LDS_BYTES);
-  return e == hipSuccess ? allow_lds(k_product8<Tile8, FORMAT, true>, Product8<Tile8, FORMAT, true>::LDS_BYTES) : e;
+  hipError_t e = hipSuccess;
+  for (int kind = 0; kind < KINDS8; ++kind)
+    for (const int format : {E4M3, E5M2})
+      for (const bool wide : {false, true})
+        if (e == hipSuccess)
+          e = with_product(kind, format, wide, [](auto k, auto f, auto w) { return allow_lds(k_product8<Tile8<k>, f, w>, Product8<Tile8<k>, f, w>::LDS_BYTES); });
+  return e;
+}
+
+template <int R, int DTYPE, bool WIDE>
+void launch_few(const FewArgs& f, hipStream_t s) {
+  const FewPlan8 plan = few_plan8(f.p.b.rows, f.p.slabs);
+  const dim3 grid((unsigned)((f.p.b.rows + plan.columns - 1) / plan.columns));
+  if (plan.columns == 32) hipLaunchKernelGGL((k_product8_few<R, 2, 8, DTYPE, WIDE>), grid, dim3(512), 0, s, f);
+  else if (plan.waves == 8) hipLaunchKernelGGL((k_product8_few<R, 1, 8, DTYPE, WIDE>), grid, dim3(512), 0, s, f);
+  else hipLaunchKernelGGL((k_product8_few<R, 1, 16, DTYPE, WIDE>), grid, dim3(1024), 0, s, f);
+}
+template <bool WIDE>
+void launch_few(const FewArgs& f, int x_dtype, hipStream_t s) {
+  if (x_dtype == OB_F32) launch_few<1, F32, WIDE>(f, s);
+  else if (x_dtype == OB_F16) launch_few<1, F16, WIDE>(f, s);
+  else if (x_dtype == OB_BF16) launch_few<1, BF16, WIDE>(f, s);
+  else if (f.p.a.rows <= 16) launch_few<1, NONE, WIDE>(f, s);
+  else launch_few<2, NONE, WIDE>(f, s);
 }
 
 struct Given {      // an operand as a call has it
@@ -74,11 +110,17 @@ ob_status product(ob_linear8_ctx* ctx, const Given& a, int format, const Given& 
   p.slabs = (int)((depth + BLOCK8 - 1) / BLOCK8);
   p.out_dtype = out_dtype;
   p.accumulate = accumulate;
-  const Plan8 plan = plan8(rows, cols, p.slabs);
-  p.parts = plan.parts;
   const hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  if (out_dtype == OB_F32) return format == OB_E4M3 ? launch_product<Tile8, E4M3, true>(ctx, p, s) : launch_product<Tile8, E5M2, true>(ctx, p, s);
-  return format == OB_E4M3 ? launch_product<Tile8, E4M3, false>(ctx, p, s) : launch_product<Tile8, E5M2, false>(ctx, p, s);
+  if (few8(rows, p.slabs)) {
+    p.parts = 1;
+    const FewArgs f{p, nullptr, 0, (int)depth, format};
+    if (out_dtype == OB_F32) launch_few<true>(f, NONE, s);
+    else launch_few<false>(f, NONE, s);
+    return hip_ok(ctx, hipGetLastError(), "k_product8_few") ? OB_OK : OB_ERR_HIP;
+  }
+  const Plan8 plan = plan8(rows, cols, p.slabs, out_dtype == OB_F32);
+  p.parts = plan.parts;
+  return with_product(plan.kind, format, out_dtype == OB_F32, [&](auto k, auto f, auto w) { return launch_product<Tile8<k>, f, w>(ctx, p, s); });
 }
 
 template <int DTYPE>
@@ -101,8 +143,7 @@ ob_status ob_linear8_create(const ob_linear8_config* cfg, ob_linear8_ctx** out) 
   if (!ctx) return OB_ERR_ARG;
   ctx->cfg = *cfg;
   hipError_t e = hipGetDevice(&ctx->device);
-  if (e == hipSuccess) e = allow_products<E4M3>();
-  if (e == hipSuccess) e = allow_products<E5M2>();
+  if (e == hipSuccess) e = allow_products();
   ctx->bytes = (size_t)WORKSPACE8;
   if (e == hipSuccess) e = hipMalloc(&ctx->d_partial, ctx->bytes);
   if (e != hipSuccess) {
@@ -146,6 +187,38 @@ ob_status ob_linear8_forward(ob_linear8_ctx* ctx, const void* x, int64_t ldx, co
   if (rows < 0 || rows > ctx->cfg.max_rows) return OB_ERR_ARG;
   return product(ctx, Given{x, ldx, x_scales, ldx_scales}, x_format, Given{w, ldw, w_scales, ldw_scales}, true, rows, ctx->cfg.n, ctx->cfg.k, y, ldy, y_dtype,
                  false, hip_stream);
+}
+
+ob_status ob_linear8_forward_few(ob_linear8_ctx* ctx, const void* x, ob_dtype x_dtype, int64_t ldx, int32_t x_format, const void* w, int64_t ldw,
+                                 const void* w_scales, int64_t ldw_scales, int64_t rows, void* y, int64_t ldy, ob_dtype y_dtype, void* hip_stream) {
+  if (!ctx) return OB_ERR_NULL;
+  const int64_t k = ctx->cfg.k, n = ctx->cfg.n;
+  const Given g{w, ldw, w_scales, ldw_scales};
+  if (rows < 0 || rows > ctx->cfg.max_rows || ldx < k || ldx > MOST || wrong(g, k) || ldy < n || ldy > MOST || !any_dtype(x_dtype) || !any_dtype(y_dtype) ||
+      (x_format != OB_E4M3 && x_format != OB_E5M2))
+    return OB_ERR_ARG;
+  if (rows > OB_LINEAR8_FEW_ROWS) return OB_ERR_SIZE;
+  if (!on_device(ctx->device)) return OB_ERR_ARG;
+  if (!rows) return OB_OK;
+  if (!x || !w || !w_scales || !y) return OB_ERR_NULL;
+  if (off_element(x, x_dtype) || misplaced(g) || off_element(y, y_dtype)) return OB_ERR_ALIGN;
+  FewArgs f;
+  f.p.a = Operand8{nullptr, nullptr, 0, 0, (int)rows, 0};
+  f.p.b = Operand8{static_cast<const uint8_t*>(w), static_cast<const uint8_t*>(w_scales), ldw, ldw_scales, (int)n, 7};
+  f.p.out = y;
+  f.p.partial = nullptr;
+  f.p.ldo = ldy;
+  f.p.slabs = (int)((k + BLOCK8 - 1) / BLOCK8);
+  f.p.parts = 1;
+  f.p.out_dtype = y_dtype;
+  f.p.accumulate = false;
+  f.x = x;
+  f.ldx = ldx;
+  f.k = (int)k;
+  f.format = x_format;
+  if (y_dtype == OB_F32) launch_few<true>(f, x_dtype, static_cast<hipStream_t>(hip_stream));
+  else launch_few<false>(f, x_dtype, static_cast<hipStream_t>(hip_stream));
+  return hip_ok(ctx, hipGetLastError(), "k_product8_few") ? OB_OK : OB_ERR_HIP;
 }
 
 ob_status ob_linear8_input_grad(ob_linear8_ctx* ctx, const void* dy, int64_t lddy, const void* dy_scales, int64_t lddy_scales, int32_t dy_format, const void* w_t,

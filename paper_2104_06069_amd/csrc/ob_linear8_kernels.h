@@ -136,7 +136,7 @@ __global__ __launch_bounds__(S::NT, 2) void k_product8(Product8Args p) {
   const int part = at / tiles, first = (int)((int64_t)p.slabs * part / p.parts), end = (int)((int64_t)p.slabs * (part + 1) / p.parts);
   const int r0 = tm * S::BM, c0 = tn * S::BN;
   typename P::Acc acc = {};
-  P::run(p.a, p.b, r0, c0, first, end - first, lds_of_product8, acc);
+  P::run(p.a, p.b, r0, c0, first, end - first, reinterpret_cast<uint8_t*>(lds_of_product8), acc);
   const int rows = p.a.rows, cols = p.b.rows;
   if (p.parts > 1) {
     store_tile<S, true>(acc, lds_of_product8, p.partial + (int64_t)part * rows * cols, F32, cols, r0, c0, rows, cols, 0, 0);
@@ -168,6 +168,126 @@ __global__ __launch_bounds__(256) void k_product8_join(Product8Args p) {
   for (int k = 1; k < p.parts; ++k) sum += load4(p.partial, F32, (k * rows + r) * cols + c, left);
   if (p.accumulate) sum += load4(p.out, F32, r * p.ldo + c, left);
   store4(p.out, p.out_dtype, r * p.ldo + c, left, sum);
+}
+
+// The same for a few rows, where what counts is how fast the other operand is read.  A workgroup has up to 16 R rows and 16 J columns, its
+// wavefronts share out the slabs of K and load each operand's 32 bytes a lane straight into registers, two slabs under way at once; their sums
+// are added in a fixed order at the end.
+struct FewArgs {
+  Product8Args p;
+  const void* x;      // where a is not in 8 bits yet (up to 16 rows): every workgroup makes it so itself, as k_quantize8 does
+  int64_t ldx;
+  int k, format;      // columns of x; a's format
+};
+
+// A lane's pieces q and q + 4 of a row's block, in 8 bits, and the block's scale
+template <int DTYPE>
+__device__ __forceinline__ void quantized_fragment(const FewArgs& f, int row, int slab, int lane, v8i& to, int& scale) {
+  float v[4][8];
+  unsigned most = 0;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const int at = slab * BLOCK8 + (lane >> 4) * 16 + (u & 1) * 8 + (u >> 1) * 64;
+    load8<DTYPE>(f.x, row * f.ldx + at, f.k - at, v[u]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) most = max(most, magnitude(v[u][e]));
+  }
+#pragma unroll
+  for (int d = 32; d >= 16; d >>= 1) most = max(most, (unsigned)__shfl_xor((int)most, d));
+  scale = scale_byte(most, f.format);
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const int at = slab * BLOCK8 + (lane >> 4) * 16 + (u & 1) * 8 + (u >> 1) * 64;
+    const v2i q = bytes_before(bytes8(v[u], inverse_scale(scale), f.format), f.k - at);
+    to[u * 2] = q.x;
+    to[u * 2 + 1] = q.y;
+  }
+}
+
+constexpr int NONE = 3;      // (of types: a is in 8 bits)
+template <int R, int J, int WAVES, int DTYPE, bool WIDE>
+__global__ __launch_bounds__(WAVES * 64) void k_product8_few(FewArgs f) {
+  constexpr int STRIDE = 16 * J + 4, AHEAD = 2;
+  __shared__ __align__(16) float sums[WAVES][16 * R * STRIDE];
+  const Product8Args& p = f.p;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, q = lane >> 4;
+  const int c0 = blockIdx.x * 16 * J, rows = p.a.rows, cols = p.b.rows;
+  const uint8_t *a[R], *b[J], *sa[R], *sb[J];
+  int row[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    row[r] = min(r * 16 + i, rows - 1);
+    a[r] = p.a.p + row[r] * p.a.ld + q * 16;
+    sa[r] = p.a.scales + (row[r] >> p.a.shift) * p.a.ld_scales;
+  }
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    const int c = min(c0 + j * 16 + i, cols - 1);
+    b[j] = p.b.p + c * p.b.ld + q * 16;
+    sb[j] = p.b.scales + (c >> p.b.shift) * p.b.ld_scales;
+  }
+  const auto fragment = [](const uint8_t* at) {
+    const v4i lo = *reinterpret_cast<const v4i*>(at), hi = *reinterpret_cast<const v4i*>(at + 64);
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  v4f acc[R][J] = {};
+  for (int t0 = wave; t0 < p.slabs; t0 += WAVES * AHEAD) {
+    v8i fa[AHEAD][R], fb[AHEAD][J];
+    int ea[AHEAD][R], eb[AHEAD][J];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      const int t = min(t0 + u * WAVES, p.slabs - 1);
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        fb[u][j] = fragment(b[j] + (int64_t)t * BLOCK8);
+        eb[u][j] = sb[j][t];
+      }
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        if constexpr (DTYPE == NONE) {
+          fa[u][r] = fragment(a[r] + (int64_t)t * BLOCK8);
+          ea[u][r] = sa[r][t];
+        }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      if (t0 + u * WAVES >= p.slabs) break;
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        if constexpr (DTYPE != NONE) quantized_fragment<DTYPE>(f, row[r], t0 + u * WAVES, lane, fa[u][r], ea[u][r]);
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+          if constexpr (!WIDE) {
+            acc[r][j] = f.format == E4M3 ? mma8<E4M3>(fb[u][j], eb[u][j], fa[u][r], ea[u][r], acc[r][j]) : mma8<E5M2>(fb[u][j], eb[u][j], fa[u][r], ea[u][r], acc[r][j]);
+          } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const v8s wb = widened<E4M3>(fb[u][j][2 * k], fb[u][j][2 * k + 1], scale_value(eb[u][j]));
+              const v8s wa = f.format == E4M3 ? widened<E4M3>(fa[u][r][2 * k], fa[u][r][2 * k + 1], scale_value(ea[u][r]))
+                                              : widened<E5M2>(fa[u][r][2 * k], fa[u][r][2 * k + 1], scale_value(ea[u][r]));
+              acc[r][j] = mma<true>(wb, wa, acc[r][j]);
+            }
+          }
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int j = 0; j < J; ++j) *reinterpret_cast<v4f*>(&sums[wave][(r * 16 + i) * STRIDE + j * 16 + q * 4]) = acc[r][j];
+  __syncthreads();
+  for (int at = threadIdx.x; at < R * 16 * 4 * J; at += WAVES * 64) {
+    const int r = at / (4 * J), c = at % (4 * J) * 4, left = cols - c0 - c;
+    if (r >= rows || left <= 0) continue;
+    v4f v = *reinterpret_cast<const v4f*>(&sums[0][r * STRIDE + c]);
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) v += *reinterpret_cast<const v4f*>(&sums[w][r * STRIDE + c]);
+    const int64_t to = r * p.ldo + c0 + c;
+    if (p.accumulate) v += load4(p.out, F32, to, left);
+    store4(p.out, p.out_dtype, to, left, v);
+  }
 }
 
 }  // namespace obl

@@ -3,21 +3,66 @@
 #pragma once
 
 #include <algorithm>
+#include <cmath>
 #include <cstdint>
 
 namespace obl {
 
+constexpr int CUS8 = 256;                              // of an MI355X
 constexpr int64_t WORKSPACE8 = (int64_t)32 << 20;      // bytes of partial sums
 
+// Tiles of 256 x 256 (eight wavefronts, one workgroup on a CU), 128 x 128 and 64 x 64 (four)
+enum { W256, W128, W64, KINDS8 };
+constexpr int side8(int kind) { return kind == W256 ? 256 : kind == W128 ? 128 : 64; }
+
+// What a CU takes for as many tiles of a kind as it runs at once, in microseconds: `fixed` for loading the first slabs and for
+// the results, and for each slab of K with all of them, or with one alone.  Measured at 512 to 4096 rows and columns by 1024 to
+// 4096, for 16-bit and for binary32 results.
+struct Rate8 {
+  int per_cu;
+  double fixed, all, one;
+};
+constexpr Rate8 RATES8[2][KINDS8] = {{{1, 5.3, 1.80, 1.60}, {2, 3.8, 1.00, 0.65}, {3, 3.8, 0.55, 0.32}},
+                                     {{1, 8.3, 3.30, 2.82}, {2, 4.7, 1.75, 1.00}, {3, 3.5, 0.89, 0.53}}};
+inline double tiles_time8(int kind, bool wide, double tiles, double slabs) {
+  const Rate8& r = RATES8[wide][kind];
+  const double a_cu = std::ceil(tiles / CUS8), rounds = std::floor(a_cu / r.per_cu), rest = a_cu - rounds * r.per_cu;
+  const double last = rest > 0 ? r.fixed + slabs * (r.one + (r.all - r.one) * (rest - 1) / std::max(r.per_cu - 1, 1)) : 0.0;
+  return rounds * (r.fixed + slabs * r.all) + last;
+}
+
 struct Plan8 {
-  int parts;      // workgroups that share a tile's slabs of K
+  int kind, parts;      // parts: workgroups that share a tile's slabs of K
 };
 
-inline Plan8 plan8(int64_t rows, int64_t cols, int64_t slabs) {
-  const int64_t tiles = ((rows + 63) / 64) * ((cols + 63) / 64);
-  // Few tiles of many slabs: several workgroups each, as many as fill the card three times and have eight slabs or more
-  const int64_t parts = std::min({(768 + tiles - 1) / tiles, slabs / 8, WORKSPACE8 / 4 / (rows * cols)});
-  return Plan8{tiles < 384 && parts > 1 ? (int)parts : 1};
+// Few rows: k_product8_few, whose workgroups have all of the rows and 16 or 32 columns, and read all of the rows each.  Microseconds
+// with it / with tiles, the host's call of 6.3 included: 1 row of 8192 x 2048 6.2 / 7.8, 32 rows 6.6 / 7.9, 33 rows 10.2 / 7.9; 1 row of
+// 2048 x 8192 7.0 / 11.0, 16 rows 11.2 / 12.8, 32 rows 16.6 / 13.0; 1 row of 8192 x 8192 12.9 / 14.8, 16 rows 20.1 / 15.1.
+constexpr bool few8(int64_t rows, int64_t slabs) { return rows <= 32 && rows * slabs <= 512; }
+struct FewPlan8 {
+  int columns, waves;      // 16 or 32; 8 or 16
+};
+inline FewPlan8 few_plan8(int64_t cols, int64_t slabs) {
+  if (cols >= 32 * CUS8 && slabs < 64) return FewPlan8{32, 8};
+  return FewPlan8{16, slabs > 16 ? 16 : 8};
+}
+
+// The kind and number of parts that take the shortest.  Adding parts up takes 3 us and their bytes' way to memory and back.
+inline Plan8 plan8(int64_t rows, int64_t cols, int64_t slabs, bool wide) {
+  Plan8 best{W64, 1};
+  double least = 1e300;
+  for (int kind = 0; kind < KINDS8; ++kind) {
+    const double tiles = (double)((rows + side8(kind) - 1) / side8(kind)) * (double)((cols + side8(kind) - 1) / side8(kind));
+    for (int64_t parts = 1; parts == 1 || (parts <= slabs / 2 && parts <= 64 && tiles * parts <= 4 * CUS8 && parts * rows * cols * 4 <= WORKSPACE8); parts *= 2) {
+      const double join = parts > 1 ? 3.0 + (double)(rows * cols) * 4 * (parts + 1) / 4e6 : 0.0;
+      const double t = tiles_time8(kind, wide || parts > 1, tiles * parts, (double)((slabs + parts - 1) / parts)) + join;
+      if (t < least) {
+        least = t;
+        best = Plan8{kind, (int)parts};
+      }
+    }
+  }
+  return best;
 }
 
 }  // namespace obl

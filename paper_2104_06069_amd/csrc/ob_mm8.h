@@ -7,9 +7,9 @@
 //   lose nothing before binary32 (7e-8 at K = 8192): half the rate.
 //
 // An operand's rows are K bytes, K a multiple of 128 and zeros behind the matrix, so that a slab of 128 columns is always whole.  In
-// LDS it lies as a slab of 64 16-bit numbers does (Slab, ob_mm.h): what a lane gets are pieces q and q + 4 of its row in place of 2 q
-// and 2 q + 1, of both operands alike, and of one block.  Beside a slab lie the scales of its rows, four bytes each, for the four
-// slabs of a group.
+// LDS a row of it is eight pieces of 16 bytes, in an order permuted by the row's number so that lanes that read the same piece of
+// their rows meet in no bank.  Lane (q, i) of a product gets pieces q and q + 4 of its row, for both operands alike.  Beside a slab lie the scales of
+// its rows, four bytes each, for the four slabs of a group.
 #pragma once
 
 #include <type_traits>
@@ -23,6 +23,32 @@ struct Operand8 {
   const uint8_t *p, *scales;
   int64_t ld, ld_scales;
   int rows, shift;      // rows >= 1; row r has the scales of scale row r >> shift
+};
+
+// Memory from p on, as the loads that go straight to LDS take it: an offset for each lane and one for all, 32 bits each
+typedef __amdgpu_buffer_rsrc_t Buffer;
+__device__ __forceinline__ Buffer buffer_of(const uint8_t* p, int64_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, (int)bytes, 0x00027000);
+}
+
+// BR rows of a slab, brought into LDS by NT threads
+template <int BR, int NT>
+struct Rows8 {
+  static constexpr int PER = BR * 8 / NT, STEP = NT / 8;      // pieces a thread fetches, rows between them
+  static_assert(PER * NT == BR * 8 && STEP % 8 == 0, "whole passes, of the same permutation");
+  Buffer memory;
+  int off[PER];
+
+  __device__ void init(const Operand8& o, int r0, int tid) {
+    memory = buffer_of(o.p + (int64_t)r0 * o.ld, min(o.rows - r0, BR) * o.ld);
+    const int row = tid / 8, at = ((tid % 8) ^ (row & 7)) * 16;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) off[j] = min(row + j * STEP, o.rows - 1 - r0) * (int)o.ld + at;      // (rows past the last repeat one that exists)
+  }
+  __device__ void load(int slab, uint8_t* lds, int wave) const {
+#pragma unroll
+    for (int j = 0; j < PER; ++j) __builtin_amdgcn_raw_ptr_buffer_load_lds(memory, in_lds<void>(lds + wave * 1024 + j * NT * 16), 16, off[j], slab * BLOCK8, 0, 0);
+  }
 };
 
 // B's numbers are e4m3
@@ -46,54 +72,50 @@ __device__ __forceinline__ float scale_value(int byte) { return __uint_as_float(
 
 template <class S, int FORMAT, bool WIDE>
 struct Product8 {
-  static constexpr int BM = S::BM, BN = S::BN, BK = 64, FM = S::FM, FN = S::FN;      // (BK in pairs of bytes)
-  static_assert(S::BK == BK && S::TEAMS == 1, "slabs of a block");
-  using A = Slab<KC, BM, BK, S::NT>;
-  using B = Slab<KC, BN, BK, S::NT>;
-  static constexpr int SCALE_WAVES = (BM + BN) / 64, SCALES = (BM + BN) * BK;      // where a slab's scales begin
+  static constexpr int BM = S::BM, BN = S::BN, FM = S::FM, FN = S::FN;
+  static_assert(S::BK * 2 == BLOCK8 && S::TEAMS == 1, "slabs of a block");      // (BK of pairs of bytes)
+  using A = Rows8<BM, S::NT>;
+  using B = Rows8<BN, S::NT>;
+  static constexpr int SCALE_WAVES = (BM + BN) / 64, SCALES = (BM + BN) * BLOCK8;      // where a slab's scales begin
   static_assert(SCALE_WAVES <= S::WAVES, "a row's scales for each lane");
-  static constexpr int STAGE = (BM + BN) * (BK + 2);
-  static constexpr int LDS_BYTES = S::STAGES * STAGE * 2 > Results<S>::LDS_BYTES ? S::STAGES * STAGE * 2 : Results<S>::LDS_BYTES;
+  static constexpr int STAGE = (BM + BN) * (BLOCK8 + 4);
+  static constexpr int LDS_BYTES = S::STAGES * STAGE > Results<S>::LDS_BYTES ? S::STAGES * STAGE : Results<S>::LDS_BYTES;
   typedef v4f Acc[FM][FN];
 
   // Slabs t0 .. t0 + n - 1 of K.  The layout of acc is Product's.
-  __device__ static void run(const Operand8& oa, const Operand8& ob, int r0, int c0, int t0, int n, uint16_t* lds, Acc& acc) {
+  __device__ static void run(const Operand8& a, const Operand8& b, int r0, int c0, int t0, int n, uint8_t* lds, Acc& acc) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / S::WN, wn = wave % S::WN;
-    const Operand a{reinterpret_cast<const uint16_t*>(oa.p), 0, oa.ld / 2, oa.rows, true};
-    const Operand b{reinterpret_cast<const uint16_t*>(ob.p), 0, ob.ld / 2, ob.rows, true};
     A sa;
     B sb;
     sa.init(a, r0, tid);
     sb.init(b, c0, tid);
-    const Operand8& own = wave < BM / 64 ? oa : ob;
-    const int of = wave < BM / 64 ? r0 + tid : c0 + tid - BM;
-    const uint8_t* const scales = own.scales + (int64_t)(min(of, own.rows - 1) >> own.shift) * own.ld_scales;
+    const Operand8& own = wave < BM / 64 ? a : b;
+    const int first = wave < BM / 64 ? r0 + wave * 64 : c0 + wave * 64 - BM;      // of this wavefront's rows of scales
+    const int scale0 = first < own.rows ? first >> own.shift : 0;
+    const Buffer scales = buffer_of(own.scales + scale0 * own.ld_scales, (((own.rows - 1) >> own.shift) + 1 - scale0) * own.ld_scales);
+    const int scale_off = ((min(first + lane, own.rows - 1) >> own.shift) - scale0) * (int)own.ld_scales;
     const auto load = [&](int t) {
-      uint16_t* const s = lds + t % S::STAGES * STAGE;
-      sa.load(a, 0, r0, (t0 + t) * BK, s, wave);
-      sb.load(b, 0, c0, (t0 + t) * BK, s + BM * BK, wave);
-      if (wave < SCALE_WAVES)
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(scales + (t0 + t) / 4 * 4), in_lds<void>(s + SCALES + wave * 128), 4, 0, 0);
+      uint8_t* const s = lds + t % S::STAGES * STAGE;
+      sa.load(t0 + t, s, wave);
+      sb.load(t0 + t, s + BM * BLOCK8, wave);
+      if (wave < SCALE_WAVES) __builtin_amdgcn_raw_ptr_buffer_load_lds(scales, in_lds<void>(s + SCALES + wave * 256), 4, scale_off, (t0 + t) / 4 * 4, 0, 0);
     };
-    const auto fragment = [&](const uint16_t* s, int row) {
-      const v8s lo = A::fragment(s, row, 0, lane), hi = A::fragment(s, row, 1, lane);      // (the same for B: it goes by BK alone)
-      return __builtin_bit_cast(v8i, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13, 14, 15));
+    // Where a lane's pieces q and q + 4 of its row, and that row's scales, lie in a slab; fragments are 16 rows apart
+    const int i = lane & 15, row_a = wm * (BM / S::WM) + i, row_b = BM + wn * (BN / S::WN) + i, piece = ((lane >> 4) ^ (i & 7)) * 16;
+    const int a_lo = row_a * BLOCK8 + piece, a_hi = row_a * BLOCK8 + (piece ^ 64), b_lo = row_b * BLOCK8 + piece, b_hi = row_b * BLOCK8 + (piece ^ 64);
+    const auto base = in_lds<uint8_t>(lds);
+    const auto read = [&](int lo, int hi, int row, int slab, int f, int t, v8i& to, int& e) {
+      const int s = slab * STAGE;
+      const v4i x = *(__attribute__((address_space(3))) const v4i*)(base + (s + lo) + f * 16 * BLOCK8);
+      const v4i y = *(__attribute__((address_space(3))) const v4i*)(base + (s + hi) + f * 16 * BLOCK8);
+      to = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+      e = *(base + (s + SCALES + row * 4 + ((t0 + t) & 3)) + f * 64);
     };
-    const auto scale = [&](const uint16_t* s, int row, int t) {
-      return (int)*in_lds<const uint8_t>(reinterpret_cast<const uint8_t*>(s + SCALES) + (row + (lane & 15)) * 4 + ((t0 + t) & 3));
-    };
-    const auto read_a = [&](const uint16_t* s, int i, int t, v8i& f, int& e) {
-      const int row = wm * (BM / S::WM) + i * 16;
-      f = fragment(s, row);
-      e = scale(s, row, t);
-    };
-    const auto read_b = [&](const uint16_t* s, int j, int t, v8i& f, int& e) {
-      const int row = wn * (BN / S::WN) + j * 16;
-      f = fragment(s + BM * BK, row);
-      e = scale(s, BM + row, t);
-    };
-    straight(n, wave, lds, load, read_a, read_b, acc);
+    const auto read_a = [&](int slab, int f, int t, v8i& to, int& e) { read(a_lo, a_hi, row_a, slab, f, t, to, e); };
+    const auto read_b = [&](int slab, int f, int t, v8i& to, int& e) { read(b_lo, b_hi, row_b, slab, f, t, to, e); };
+    if constexpr (S::TURNS) turns(n, load, read_a, read_b, acc);
+    else straight(n, wave, load, read_a, read_b, acc);
   }
 
  private:
@@ -122,9 +144,8 @@ struct Product8 {
   }
 
   template <class L, class RA, class RB>
-  __device__ static __forceinline__ void straight(int n, int wave, uint16_t* lds, L load, RA read_a, RB read_b, Acc& acc) {
+  __device__ static __forceinline__ void straight(int n, int wave, L load, RA read_a, RB read_b, Acc& acc) {
     constexpr int AHEAD = S::STAGES - 1, LOADS = A::PER + B::PER;      // loads of a slab, one more for scales
-    static_assert(A::WORK == S::NT && B::WORK == S::NT, "of all wavefronts");
 #pragma unroll
     for (int t = 0; t < AHEAD; ++t)
       if (t < n) load(t);
@@ -134,7 +155,7 @@ struct Product8 {
       else loads_left<LOADS * (AHEAD - 1)>();
       group_barrier();      // slab t is there, and nobody reads slab t - 1 any more
       if (t + AHEAD < n) load(t + AHEAD);
-      const uint16_t* const s = lds + t % S::STAGES * STAGE;
+      const int s = t % S::STAGES;
       v8i fa[FM], fb[FN];
       int ea[FM], eb[FN];
 #pragma unroll
@@ -145,6 +166,55 @@ struct Product8 {
     }
     lds_done();
     group_barrier();
+  }
+
+  // Product's turns, two a slab: each with half of a wavefront's rows, the first with its columns' operands for both.
+  template <class L, class RA, class RB>
+  __device__ static __forceinline__ void turns(int n, L load, RA read_a, RB read_b, Acc& acc) {
+    const bool second = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) >= S::WAVES / 2;
+    constexpr int HALF = FM / 2;
+    if (n > 0) {
+      load(0);
+      loads_done();
+      group_barrier();
+      if (second) {
+        if (n > 1) load(1);
+        group_barrier();
+      }
+      for (int t = 0; t < n; ++t) {
+        const int s = t & 1;
+        v8i fa[HALF], fb[FN];
+        int ea[HALF], eb[FN];
+#pragma unroll
+        for (int j = 0; j < FN; ++j) read_b(s, j, t, fb[j], eb[j]);
+#pragma unroll
+        for (int i = 0; i < HALF; ++i) read_a(s, i, t, fa[i], ea[i]);
+        if (!second && t + 1 < n) load(t + 1);
+        lds_done();
+        group_barrier();
+        __builtin_amdgcn_s_setprio(1);
+        multiply<0, HALF>(fa, ea, fb, eb, acc);
+        // (here, and not behind the barrier beside the second half's: both halves' operands do not fit in registers)
+#pragma unroll
+        for (int i = 0; i < HALF; ++i)
+#pragma unroll
+          for (int j = 0; j < FN; ++j) asm volatile("" : "+v"(acc[i][j]));
+        __builtin_amdgcn_s_setprio(0);
+        group_barrier();
+#pragma unroll
+        for (int i = 0; i < HALF; ++i) read_a(s, HALF + i, t, fa[i], ea[i]);
+        if (second) loads_done();
+        else lds_done();
+        group_barrier();
+        if (second && t + 2 < n) load(t + 2);
+        __builtin_amdgcn_s_setprio(1);
+        multiply<HALF, HALF>(fa, ea, fb, eb, acc);
+        __builtin_amdgcn_s_setprio(0);
+        if (!second) loads_done();
+        group_barrier();
+      }
+      if (!second) group_barrier();
+    }
   }
 };
 

@@ -235,3 +235,24 @@ def test_refusals():
             op(*args)
     with pytest.raises(RuntimeError):
         op(64, 32, max_rows=4).forward(x, w8)
+
+
+@pytest.mark.parametrize("rows,k,n", [(1, 1024, 4096), (1, 100, 72), (3, 9000, 40), (16, 2048, 9000), (7, 130, 8200), (16, 500, 300), (15, 3000, 16), (31, 2100, 8192),
+                                      (32, 130, 20), (50, 2500, 33), (64, 700, 8200)])
+@pytest.mark.parametrize("dtype", (BF, F16, F32))
+def test_few_rows(rows, k, n, dtype):
+    """One token and a few: from x itself and from its 8 bits, the same."""
+    layer = op(k, n, dtype=dtype)
+    x, w = numbers(rows, k, dtype, 1, pitch=5), numbers(n, k, BF, 3)
+    w8 = layer.quantize_weight(w)
+    x8 = layer.quantize(x)
+    y = layer.forward(x, w8)
+    product_near(y, values(x8), values(w8.w), k, "y")
+    assert torch.equal(layer.forward(x8, w8), y)
+    assert torch.equal(layer.forward(layer.quantize(x, E5M2), w8), layer.forward(layer.quantize(x, E5M2), w8))
+    dy = numbers(rows, n, dtype, 4)
+    product_near(layer.input_grad(dy, w8), values(layer.quantize(dy)), values(w8.w).T, n, "dx")
+    if rows < 40:      # a weight gradient of few rows of W
+        few = op(k, rows, dtype=dtype)
+        xs, g = numbers(300, k, dtype, 5), numbers(300, rows, dtype, 6)
+        product_near(few.weight_grad(xs, g), values(few._quantize(g, "dy", rows, None, E4M3)[1]), values(few._quantize(xs, "x", k, None, E4M3)[1]), 300, "dw")
