@@ -32,25 +32,42 @@ constexpr int64_t MOST_N = 16384, MOST_LD = (int64_t)1 << 31;
 template <int V>
 using Int = std::integral_constant<int, V>;
 
-// f(type of x, type of h, threads of a row, pieces of a thread)
-template <int X, int H, class F>
-ob_status with_size(int64_t n, F f) {
-  if (n <= 512) return f(Int<X>{}, Int<H>{}, Int<64>{}, Int<1>{});
-  if (n <= 1024) return f(Int<X>{}, Int<H>{}, Int<64>{}, Int<2>{});
-  if (n <= 2048) return f(Int<X>{}, Int<H>{}, Int<64>{}, Int<4>{});
-  if (n <= 4096) return f(Int<X>{}, Int<H>{}, Int<256>{}, Int<2>{});
-  if (n <= 8192) return f(Int<X>{}, Int<H>{}, Int<256>{}, Int<4>{});
-  return f(Int<X>{}, Int<H>{}, Int<512>{}, Int<4>{});
-}
+// f(type of x, type of h)
 template <class F>
-ob_status with_kernel(const ob_norm_config& c, F f) {
-  if (c.dtype == OB_F32) return with_size<F32, F32>(c.n, f);
-  if (c.dtype == OB_F16) return c.res_dtype == OB_F32 ? with_size<F16, F32>(c.n, f) : with_size<F16, F16>(c.n, f);
-  return c.res_dtype == OB_F32 ? with_size<BF16, F32>(c.n, f) : with_size<BF16, BF16>(c.n, f);
+ob_status with_types(const ob_norm_config& c, F f) {
+  if (c.dtype == OB_F32) return f(Int<F32>{}, Int<F32>{});
+  if (c.dtype == OB_F16) return c.res_dtype == OB_F32 ? f(Int<F16>{}, Int<F32>{}) : f(Int<F16>{}, Int<F16>{});
+  return c.res_dtype == OB_F32 ? f(Int<BF16>{}, Int<F32>{}) : f(Int<BF16>{}, Int<BF16>{});
 }
 
-// rows of T threads that a workgroup of k_norm_backward has at a time
-int sets_of(int64_t n) { return n <= 2048 ? 8 : n <= 8192 ? 2 : 1; }
+// f(threads of a row, pieces of a thread): one piece each where a workgroup has threads for that, so that a row is one trip to
+// memory and many rows are under way (forward 16384 x 2048: 42.8 us, four pieces of a wavefront 44.4; backward 57.9, four pieces 95).
+// What the weight's gradient takes of the registers speaks for wavefronts of their own with rows up to 1024 (32768 rows: the same time as
+// with two wavefronts a row), and above 8192 there are not threads enough.
+template <class F>
+ob_status with_forward_size(int64_t n, F f) {
+  if (n <= 512) return f(Int<64>{}, Int<1>{});
+  if (n <= 1024) return f(Int<128>{}, Int<1>{});
+  if (n <= 2048) return f(Int<256>{}, Int<1>{});
+  if (n <= 4096) return f(Int<512>{}, Int<1>{});
+  if (n <= 8192) return f(Int<1024>{}, Int<1>{});
+  return f(Int<512>{}, Int<4>{});
+}
+template <class F>
+ob_status with_backward_size(int64_t n, F f) {
+  if (n <= 512) return f(Int<64>{}, Int<1>{});
+  if (n <= 1024) return f(Int<64>{}, Int<2>{});
+  if (n <= 2048) return f(Int<256>{}, Int<1>{});
+  if (n <= 4096) return f(Int<512>{}, Int<1>{});
+  if (n <= 8192) return f(Int<1024>{}, Int<1>{});
+  return f(Int<512>{}, Int<4>{});
+}
+
+// rows that a workgroup of k_norm_backward has at a time
+int sets_of(int64_t n) { return n <= 1024 ? 8 : n <= 2048 ? 2 : 1; }
+// and workgroups of it, as many as the card runs at once (16384 x 2048 with 256 / 512 / 768 / 1024 of them: 81.4 / 62.3 / 57.9 / 68.9 us; 32768 x 1024,
+// where two wavefronts' registers less fit: 512 / 768: 61.8 / 74.4)
+int parts_of(int64_t n) { return n <= 512 || (n > 1024 && n <= 4096) ? 768 : 512; }
 
 bool rows_wrong(int64_t ld, int64_t n) { return ld < n || ld >= MOST_LD; }
 
@@ -68,7 +85,7 @@ ob_status ob_norm_create(const ob_norm_config* cfg, ob_norm_ctx** out) {
   if (!ctx) return OB_ERR_ARG;
   ctx->cfg = *cfg;
   hipError_t e = hipGetDevice(&ctx->device);
-  ctx->most_parts = cfg->n <= 8192 ? 512 : 256;
+  ctx->most_parts = parts_of(cfg->n);
   ctx->bytes = (size_t)ctx->most_parts * cfg->n * sizeof(float);
   if (e == hipSuccess) e = hipMalloc(&ctx->d_partial, ctx->bytes);
   if (e != hipSuccess) {
@@ -101,10 +118,12 @@ ob_status ob_norm_forward(ob_norm_ctx* ctx, const void* x, int64_t ldx, const vo
     return OB_ERR_ALIGN;
   NormArgs p{x, residual, weight, h, y, static_cast<uint8_t*>(data), static_cast<uint8_t*>(scales), rstd, ldx, ldr, ldh, ldy, ld, ld_scales,
              (int)rows, (int)c.n, c.weight_dtype, format, c.eps};
-  return with_kernel(c, [&](auto X, auto H, auto T, auto C) {
-    constexpr int NT = T < 256 ? 256 : T;
-    hipLaunchKernelGGL((k_norm_forward<X, H, T, C>), dim3((unsigned)((rows + NT / T - 1) / (NT / T))), dim3(NT), 0, static_cast<hipStream_t>(hip_stream), p);
-    return hip_ok(ctx, hipGetLastError(), "k_norm_forward") ? OB_OK : OB_ERR_HIP;
+  return with_types(c, [&](auto X, auto H) {
+    return with_forward_size(c.n, [&](auto T, auto C) {
+      constexpr int NT = T < 256 ? 256 : T;
+      hipLaunchKernelGGL((k_norm_forward<X, H, T, C>), dim3((unsigned)((rows + NT / T - 1) / (NT / T))), dim3(NT), 0, static_cast<hipStream_t>(hip_stream), p);
+      return hip_ok(ctx, hipGetLastError(), "k_norm_forward") ? OB_OK : OB_ERR_HIP;
+    });
   });
 }
 
@@ -125,11 +144,13 @@ ob_status ob_norm_backward(ob_norm_ctx* ctx, const void* dy, int64_t lddy, const
   NormGradArgs p{dy, h, weight, dres, rstd, dh, dweight, ctx->d_partial, lddy, ldh, lddres, lddh, (int)rows, (int)c.n, c.weight_dtype, accumulate != 0};
   if (!rows && !dweight) return OB_OK;      // (without rows one workgroup writes zeros to dweight, or adds them)
   const hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  return with_kernel(c, [&](auto X, auto H, auto T, auto C) {
-    hipLaunchKernelGGL((k_norm_backward<X, H, T, C>), dim3((unsigned)parts), dim3(norm_grad_threads<T>()), 0, s, p);
-    if (dweight && parts > 1)
-      hipLaunchKernelGGL(k_norm_join, dim3((unsigned)((c.n + 63) / 64)), dim3(256), 0, s, ctx->d_partial, parts, (int)c.n, p.accumulate, dweight);
-    return hip_ok(ctx, hipGetLastError(), "k_norm_backward") ? OB_OK : OB_ERR_HIP;
+  return with_types(c, [&](auto X, auto H) {
+    return with_backward_size(c.n, [&](auto T, auto C) {
+      hipLaunchKernelGGL((k_norm_backward<X, H, T, C>), dim3((unsigned)parts), dim3(norm_grad_threads<T>()), 0, s, p);
+      if (dweight && parts > 1)
+        hipLaunchKernelGGL(k_norm_join, dim3((unsigned)((c.n + 63) / 64)), dim3(SHARES * 64), 0, s, ctx->d_partial, parts, (int)c.n, p.accumulate, dweight);
+      return hip_ok(ctx, hipGetLastError(), "k_norm_backward") ? OB_OK : OB_ERR_HIP;
+    });
   });
 }
 

@@ -47,16 +47,32 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void k_norm_forward(NormArgs p) 
   const int64_t row = (int64_t)blockIdx.x * (NT / T) + threadIdx.x / T;
   const bool there = row < p.rows;
   if (T <= 64 && !there) return;
-  float h[C][8], sum = 0;
+  // Every load is under way before the first sum; the weights too, where there are registers for them.
+  constexpr bool EARLY = C <= 2;
+  Raw8<X> x[C];
+  Raw8<H> r[C];
+  float w[EARLY ? C : 1][8], h[C][8], sum = 0;
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     const int at = (c * T + t) * 8, left = there ? p.n - at : 0;
-    load8<X>(p.x, row * p.ldx + at, left, h[c]);
-    if (p.residual) {
-      float r[8];
-      load8<H>(p.residual, row * p.ldr + at, left, r);
+    x[c].load(p.x, row * p.ldx + at, left);
+    if (p.residual) r[c].load(p.residual, row * p.ldr + at, left);
+  }
+  if constexpr (EARLY) {
+    if (p.weight) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) h[c][e] = as_stored<H>(h[c][e] + r[e]);
+      for (int c = 0; c < C; ++c) load8_any(p.weight, p.weight_dtype, (c * T + t) * 8, p.n - (c * T + t) * 8, w[c]);
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int at = (c * T + t) * 8, left = there ? p.n - at : 0;
+    x[c].values(h[c]);
+    if (p.residual) {
+      float v[8];
+      r[c].values(v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) h[c][e] = as_stored<H>(h[c][e] + v[e]);
       if (left > 0) store8<H>(p.h, row * p.ldh + at, left, h[c]);
     }
 #pragma unroll
@@ -69,14 +85,15 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void k_norm_forward(NormArgs p) 
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     const int at = (c * T + t) * 8, left = p.n - at;
-    float w[8];
-    if (p.weight) load8_any(p.weight, p.weight_dtype, at, left, w);
+    if constexpr (!EARLY) {
+      if (p.weight) load8_any(p.weight, p.weight_dtype, at, left, w[0]);
+    }
     float y[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) y[e] = h[c][e] * rstd;
     if (p.weight) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = y[e] * w[e];
+      for (int e = 0; e < 8; ++e) y[e] = y[e] * w[EARLY ? c : 0][e];
     }
     if (p.y && left > 0) store8<X>(p.y, row * p.ldy + at, left, y);
     if (p.data) {
@@ -117,7 +134,7 @@ template <int X, int H, int T, int C>
 __global__ __launch_bounds__(norm_grad_threads<T>()) void k_norm_backward(NormGradArgs p) {
   constexpr int NT = norm_grad_threads<T>(), SETS = NT / T;      // rows at a time
   __shared__ float part[2][NT / 64];
-  __shared__ float sums[T * 8];
+  __shared__ float sums[SETS > 1 ? T * 8 : 1];
   const int t = threadIdx.x % T, set = threadIdx.x / T;
   float dw[C][8] = {};
   int turn = 0;
@@ -125,39 +142,69 @@ __global__ __launch_bounds__(norm_grad_threads<T>()) void k_norm_backward(NormGr
     const int64_t row = first + set;
     const bool there = row < p.rows;
     const float rstd = there ? p.rstd[row] : 0.0f;
-    float g[C][8], xhat[C][8], dot = 0;
+    // (Across the sum the row stays as memory has it, and is unpacked twice: half the registers of its values.)
+    Raw8<X> dy[C];
+    Raw8<H> h[C], dres[C];
+    float dot = 0;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       const int at = (c * T + t) * 8, left = there ? p.n - at : 0;
-      load8<X>(p.dy, row * p.lddy + at, left, g[c]);
-      load8<H>(p.h, row * p.ldh + at, left, xhat[c]);
-      float w[8];
-      if (p.weight) load8_any(p.weight, p.weight_dtype, at, p.n - at, w);
+      dy[c].load(p.dy, row * p.lddy + at, left);
+      h[c].load(p.h, row * p.ldh + at, left);
+    }
+    if (p.dres) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        xhat[c][e] = e < left ? xhat[c][e] * rstd : 0.0f;      // (rstd may be no finite number)
-        dw[c][e] += g[c][e] * xhat[c][e];
-        if (p.weight) g[c][e] = g[c][e] * w[e];
-        dot += g[c][e] * xhat[c][e];
-      }
+      for (int c = 0; c < C; ++c) dres[c].load(p.dres, row * p.lddres + (c * T + t) * 8, there ? p.n - (c * T + t) * 8 : 0);
+    }
+    const auto unpack = [&](int c, float (&g)[8], float (&xhat)[8]) {
+      dy[c].values(g);
+      h[c].values(xhat);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) xhat[e] = e < p.n - (c * T + t) * 8 ? xhat[e] * rstd : 0.0f;      // (rstd may be no finite number)
+    };
+    const void* weight = p.weight;
+    const auto weigh = [&](int c, float (&g)[8]) {
+      float w[8];
+      if (!weight) return;
+      load8_any(weight, p.weight_dtype, (c * T + t) * 8, p.n - (c * T + t) * 8, w);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) g[e] = g[e] * w[e];
+    };
+    asm volatile("" : "+s"(weight));      // (read for each row, from the nearest cache, and not held in registers)
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      float g[8], xhat[8];
+      unpack(c, g, xhat);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) dw[c][e] += g[e] * xhat[e];
+      weigh(c, g);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) dot += g[e] * xhat[e];
     }
     if (!p.dh) continue;      // (the same for all of them)
     dot = row_sum<T>(dot, part[turn]) / (float)p.n;
     if (!there) continue;
+    asm volatile("" : "+s"(weight));
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      dy[c].forget();
+      h[c].forget();
+    }
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       const int at = (c * T + t) * 8, left = p.n - at;
       if (left <= 0) continue;
-      float d[8];
+      float g[8], xhat[8], r[8];
+      unpack(c, g, xhat);
+      weigh(c, g);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) d[e] = rstd * (g[c][e] - xhat[c][e] * dot);
+      for (int e = 0; e < 8; ++e) g[e] = rstd * (g[e] - xhat[e] * dot);
       if (p.dres) {
-        float r[8];
-        load8<H>(p.dres, row * p.lddres + at, left, r);
+        dres[c].values(r);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) d[e] += r[e];
+        for (int e = 0; e < 8; ++e) g[e] += r[e];
       }
-      store8<H>(p.dh, row * p.lddh + at, left, d);
+      store8<H>(p.dh, row * p.lddh + at, left, g);
     }
   }
   if (!p.dweight) return;
@@ -193,18 +240,23 @@ __global__ __launch_bounds__(norm_grad_threads<T>()) void k_norm_backward(NormGr
   }
 }
 
-// dweight[j] = sum over the workgroups, in their order: 64 columns a workgroup, four shares of the sums, then those four.
-__global__ __launch_bounds__(256) void k_norm_join(const float* partial, int parts, int n, int accumulate, float* dweight) {
-  __shared__ float share[4][64];
+// dweight[j] = sum over the workgroups, in their order: 64 columns a workgroup, SHARES shares of the sums, then those.
+constexpr int SHARES = 16;
+__global__ __launch_bounds__(SHARES * 64) void k_norm_join(const float* partial, int parts, int n, int accumulate, float* dweight) {
+  __shared__ float share[SHARES][64];
   const int lane = threadIdx.x & 63, w = threadIdx.x / 64, j = blockIdx.x * 64 + lane;
   float s = 0;
-  const int each = (parts + 3) / 4, end = min(parts, (w + 1) * each);
-  if (j < n)
+  const int each = (parts + SHARES - 1) / SHARES, end = min(parts, (w + 1) * each);
+  if (j < n) {
+#pragma unroll 8
     for (int g = w * each; g < end; ++g) s += partial[(int64_t)g * n + j];
+  }
   share[w][lane] = s;
   __syncthreads();
   if (w == 0 && j < n) {
-    s = ((share[0][lane] + share[1][lane]) + share[2][lane]) + share[3][lane];
+    s = share[0][lane];
+#pragma unroll
+    for (int k = 1; k < SHARES; ++k) s += share[k][lane];
     dweight[j] = accumulate ? dweight[j] + s : s;
   }
 }

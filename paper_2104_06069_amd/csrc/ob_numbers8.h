@@ -44,19 +44,13 @@ __device__ __forceinline__ v2i bytes8(const float (&v)[8], float inv, int format
   return r;
 }
 
-// Eight adjacent elements of one type, of which those from `left` on do not exist (and read as zeros)
+// Eight adjacent elements of one type as memory has them.  Those from `left` on do not exist and read as zeros.
 template <int DTYPE>
-__device__ __forceinline__ void load8(const void* p, int64_t at, int left, float (&v)[8]) {
-  if constexpr (DTYPE == F32) {
-    const v4f lo = load4(p, F32, at, left), hi = load4(p, F32, at + 4, left - 4);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      v[e] = lo[e];
-      v[e + 4] = hi[e];
-    }
-  } else {
+struct Raw8 {
+  v8s h;
+  __device__ __forceinline__ void load(const void* p, int64_t at, int left) {
     const uint16_t* const s = static_cast<const uint16_t*>(p) + at;
-    v8s h = {};
+    h = v8s{};
     if (left >= 8) {
       h = *reinterpret_cast<const v8s_any*>(s);
     } else {
@@ -64,9 +58,34 @@ __device__ __forceinline__ void load8(const void* p, int64_t at, int left, float
       for (int e = 0; e < 7; ++e)
         if (e < left) h[e] = (short)s[e];
     }
+  }
+  __device__ __forceinline__ void values(float (&v)[8]) const {
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = from_bits((unsigned short)h[e], DTYPE == BF16);
   }
+  __device__ __forceinline__ void forget() { asm volatile("" : "+v"(h)); }      // (what was made of it before is made again)
+};
+template <>
+struct Raw8<F32> {
+  v4f lo, hi;
+  __device__ __forceinline__ void load(const void* p, int64_t at, int left) {
+    lo = load4(p, F32, at, left);
+    hi = load4(p, F32, at + 4, left - 4);
+  }
+  __device__ __forceinline__ void values(float (&v)[8]) const {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[e] = lo[e];
+      v[e + 4] = hi[e];
+    }
+  }
+  __device__ __forceinline__ void forget() {}
+};
+template <int DTYPE>
+__device__ __forceinline__ void load8(const void* p, int64_t at, int left, float (&v)[8]) {
+  Raw8<DTYPE> r;
+  r.load(p, at, left);
+  r.values(v);
 }
 template <int DTYPE>
 __device__ __forceinline__ void store8(void* p, int64_t at, int left, const float (&v)[8]) {

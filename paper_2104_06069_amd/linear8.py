@@ -39,6 +39,7 @@ class Linear8:
         format_of(grad_format)
         if dtype not in _OB_DTYPE:
             raise ValueError("dtype is torch.float32, torch.float16 or torch.bfloat16")
+        self._few = ob.lib().ob_linear8_forward_few
         self.ctx = ob.ob_linear8_create(self.k, self.n, max_rows)
         # rows whose numbers the product itself makes 8 bits (one launch): few, or short ones, up to 512 blocks of 128 in all
         self._few_rows = min(ob.OB_LINEAR8_FEW_ROWS, 512 // ((self.k + 127) // 128))
@@ -104,8 +105,10 @@ class Linear8:
         if not isinstance(x, Matrix8) and x.dim() == 2 and x.shape[0] <= self._few_rows:
             rows, ldx = x.shape[0], rows_of(x, self.k, _TYPES, self.device, "x")
             out, ldo = self._out(out, rows, self.n, out_dtype or self.dtype, _TYPES)
-            ob.ob_linear8_forward_few(self.ctx, x, _OB_DTYPE[x.dtype], ldx, ob.OB_E4M3, *w8.w.address(), rows, out, ldo, _OB_DTYPE[out.dtype],
-                                      _current_stream(self.device))
+            status = self._few(self.ctx, x.data_ptr(), _OB_DTYPE[x.dtype], ldx, ob.OB_E4M3, *w8.w.address(), rows, out.data_ptr(), ldo, _OB_DTYPE[out.dtype],
+                               _current_stream(self.device))
+            if status:
+                raise ob.ObLambError(status, "ob_linear8_forward_few", ob.lib().ob_linear8_last_hip_error(self.ctx).decode())
             return out
         m = self._matrix(x, self.k, _E4M3, "x")
         out, ldo = self._out(out, m.rows, self.n, out_dtype or self.dtype, _TYPES)

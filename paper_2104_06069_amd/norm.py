@@ -27,6 +27,7 @@ class RMSNorm:
         self.ctx = None
         if dtype not in _OB_DTYPE or self.residual_dtype not in (dtype, torch.float32) or weight_dtype not in _OB_DTYPE:
             raise ValueError("types are torch.float32, torch.float16 and torch.bfloat16; the residual's is dtype or torch.float32")
+        self._index, self._call = torch.cuda.current_device(), ob.lib().ob_norm_forward
         self.ctx = ob.ob_norm_create(self.n, _OB_DTYPE[dtype], _OB_DTYPE[self.residual_dtype], _OB_DTYPE[weight_dtype], eps)
 
     def close(self):
@@ -54,35 +55,47 @@ class RMSNorm:
         if t is not None and (t.dtype != self.weight_dtype or tuple(t.shape) != (self.n,) or not t.is_contiguous() or t.device != self.device):
             raise ValueError(f"weight: {self.n} adjacent {self.weight_dtype} on {self.device}")
 
-    def _forward(self, x, weight, residual, h, y, ldy, m8):
-        ldx, rows = rows_of(x, self.n, (self.dtype,), self.device, "x"), x.shape[0]
-        self._weight(weight)
-        ldr = ldh = self.n
+    def _forward(self, x, weight, residual, h, y, want_y, format):
+        # (a token's norm takes 3 us on the device: the common case is looked at as a whole, anything else piece by piece)
+        n, rows = self.n, x.shape[0]
+        dense, ldr, ldh, ldy = (rows, n), n, n, n
+        if x.dtype is self.dtype and x.shape == dense and x.is_contiguous() and x.get_device() == self._index:
+            ldx = n
+        else:
+            ldx = rows_of(x, n, (self.dtype,), self.device, "x")
+        if weight is not None and not (weight.dtype is self.weight_dtype and weight.shape == (n,) and weight.is_contiguous() and weight.get_device() == self._index):
+            self._weight(weight)
         if residual is None:
             if h is not None:
                 raise ValueError("h is x where there is no residual")
         else:
-            residual, ldr = self._like(residual, rows, self.residual_dtype, "residual")
+            if not (residual.dtype is self.residual_dtype and residual.shape == dense and residual.is_contiguous() and residual.get_device() == self._index):
+                residual, ldr = self._like(residual, rows, self.residual_dtype, "residual")
             h, ldh = self._like(h, rows, self.residual_dtype, "h")
+        if want_y:
+            y, ldy = self._like(y, rows, self.dtype, "out")
+        m8, data, ld, scales, ld_scales, code = None, None, 0, None, 0, 0
+        if format is not None:
+            code = format_of(format)
+            m8 = Matrix8(rows, n, format, self.device)
+            data, ld, scales, ld_scales = m8.address()
         rstd = torch.empty(rows, device=self.device, dtype=torch.float32)
-        data, ld, scales, ld_scales = (None, 0, None, 0) if m8 is None else m8.address()
-        ob.ob_norm_forward(self.ctx, x, ldx, residual, ldr, weight, rows, h, ldh, y, ldy, data, ld, scales, ld_scales,
-                           ob.OB_E4M3 if m8 is None else format_of(m8.dtype), rstd, _current_stream(self.device))
-        return (x if residual is None else h), rstd
+        status = self._call(self.ctx, x.data_ptr(), ldx, None if residual is None else residual.data_ptr(), ldr, None if weight is None else weight.data_ptr(), rows,
+                            None if h is None else h.data_ptr(), ldh, y.data_ptr() if want_y else None, ldy, data, ld, scales, ld_scales, code, rstd.data_ptr(),
+                            _current_stream(self.device))
+        if status:
+            raise ob.ObLambError(status, "ob_norm_forward", ob.lib().ob_norm_last_hip_error(self.ctx).decode())
+        return y, m8, (x if residual is None else h), rstd
 
     def forward(self, x, weight=None, residual=None, h=None, out=None):
         """-> (y, h, rstd).  h: where x + residual goes (default: a new tensor); it may be residual itself, or x if their types are
         one.  Without a residual, h is x."""
-        y, ldy = self._like(out, x.shape[0], self.dtype, "out")
-        h, rstd = self._forward(x, weight, residual, h, y, ldy, None)
+        y, _, h, rstd = self._forward(x, weight, residual, h, out, True, None)
         return y, h, rstd
 
     def forward8(self, x, weight=None, residual=None, h=None, out=None, format=torch.float8_e4m3fn):
         """-> (y as a Matrix8, h, rstd).  out: where y goes in x's type too, for a weight gradient that reads it later."""
-        format_of(format)
-        y, ldy = (None, 0) if out is None else self._like(out, x.shape[0], self.dtype, "out")
-        m8 = Matrix8(x.shape[0], self.n, format, self.device)
-        h, rstd = self._forward(x, weight, residual, h, y, ldy, m8)
+        _, m8, h, rstd = self._forward(x, weight, residual, h, out, out is not None, format)
         return m8, h, rstd
 
     def backward(self, dy, h, rstd, weight=None, dres=None, dweight=None, accumulate=False, out=None):
