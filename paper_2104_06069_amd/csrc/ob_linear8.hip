@@ -28,8 +28,9 @@ namespace {
 constexpr int64_t MOST = (int64_t)1 << 22;      // rows, columns and distances between rows: a tile's offsets are 32-bit
 
 // Tiles by their side (ob_linear8_plan.h)
-template <int KIND>
-using Tile8 = std::conditional_t<KIND == W256, Shape<256, 256, 64, 2, 4>, std::conditional_t<KIND == W128, Shape<128, 128, 64, 2, 2>, Shape<64, 64, 64, 2, 2, 3>>>;
+template <int KIND, bool WIDE>
+using Tile8 = std::conditional_t<KIND == W256, std::conditional_t<WIDE, Shape<256, 256, 64, 2, 4>, Shape<256, 256, 64, 2, 2>>, 
+                                 std::conditional_t<KIND == W128, Shape<128, 128, 64, 2, 2>, Shape<64, 64, 64, 2, 2, 3>>>;
 
 template <class S, int FORMAT, bool WIDE>
 ob_status launch_product(ob_linear8_ctx* ctx, const Product8Args& p, hipStream_t s) {
@@ -61,7 +62,7 @@ hipError_t allow_products() {
     for (const int format : {E4M3, E5M2})
       for (const bool wide : {false, true})
         if (e == hipSuccess)
-          e = with_product(kind, format, wide, [](auto k, auto f, auto w) { return allow_lds(k_product8<Tile8<k>, f, w>, Product8<Tile8<k>, f, w>::LDS_BYTES); });
+          e = with_product(kind, format, wide, [](auto k, auto f, auto w) { return allow_lds(k_product8<Tile8<k, w>, f, w>, Product8<Tile8<k, w>, f, w>::LDS_BYTES); });
   return e;
 }
 
@@ -120,7 +121,7 @@ ob_status product(ob_linear8_ctx* ctx, const Given& a, int format, const Given& 
   }
   const Plan8 plan = plan8(rows, cols, p.slabs, out_dtype == OB_F32);
   p.parts = plan.parts;
-  return with_product(plan.kind, format, out_dtype == OB_F32, [&](auto k, auto f, auto w) { return launch_product<Tile8<k>, f, w>(ctx, p, s); });
+  return with_product(plan.kind, format, out_dtype == OB_F32, [&](auto k, auto f, auto w) { return launch_product<Tile8<k, w>, f, w>(ctx, p, s); });
 }
 
 template <int DTYPE>

@@ -126,7 +126,7 @@ struct Product8Args {
 extern __shared__ __align__(1024) uint16_t lds_of_product8[];
 
 template <class S, int FORMAT, bool WIDE>
-__global__ __launch_bounds__(S::NT, 2) void k_product8(Product8Args p) {
+__global__ __launch_bounds__(S::NT, S::BM == 256 && S::WAVES == 4 ? 1 : 2) void k_product8(Product8Args p) {
   using P = Product8<S, FORMAT, WIDE>;
   const int nm = (p.a.rows + S::BM - 1) / S::BM, nn = (p.b.rows + S::BN - 1) / S::BN, tiles = nm * nn;
   const int at = tile_of_workgroup(blockIdx.x, tiles * p.parts);

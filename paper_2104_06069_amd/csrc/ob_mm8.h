@@ -45,9 +45,8 @@ struct Rows8 {
 #pragma unroll
     for (int j = 0; j < PER; ++j) off[j] = min(row + j * STEP, o.rows - 1 - r0) * (int)o.ld + at;      // (rows past the last repeat one that exists)
   }
-  __device__ void load(int slab, uint8_t* lds, int wave) const {
-#pragma unroll
-    for (int j = 0; j < PER; ++j) __builtin_amdgcn_raw_ptr_buffer_load_lds(memory, in_lds<void>(lds + wave * 1024 + j * NT * 16), 16, off[j], slab * BLOCK8, 0, 0);
+  __device__ __forceinline__ void load(int slab, uint8_t* lds, int wave, int j) const {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(memory, in_lds<void>(lds + wave * 1024 + j * NT * 16), 16, off[j], slab * BLOCK8, 0, 0);
   }
 };
 
@@ -76,8 +75,10 @@ struct Product8 {
   static_assert(S::BK * 2 == BLOCK8 && S::TEAMS == 1, "slabs of a block");      // (BK of pairs of bytes)
   using A = Rows8<BM, S::NT>;
   using B = Rows8<BN, S::NT>;
-  static constexpr int SCALE_WAVES = (BM + BN) / 64, SCALES = (BM + BN) * BLOCK8;      // where a slab's scales begin
-  static_assert(SCALE_WAVES <= S::WAVES, "a row's scales for each lane");
+  static constexpr int SCALE_WAVES = (BM + BN) / 64, SCALES = (BM + BN) * BLOCK8;      // (64 rows' scales a load); where a slab's scales begin
+  static constexpr int SCALE_LOADS = SCALE_WAVES > S::WAVES ? SCALE_WAVES / S::WAVES : 1;
+  static constexpr int LOADS = A::PER + B::PER + SCALE_LOADS;      // of a slab (without the last one, where only some wavefronts have scales)
+  static constexpr bool FLOW = S::WAVES == 4 && BM == 256 && !WIDE;      // flow() below
   static constexpr int STAGE = (BM + BN) * (BLOCK8 + 4);
   static constexpr int LDS_BYTES = S::STAGES * STAGE > Results<S>::LDS_BYTES ? S::STAGES * STAGE : Results<S>::LDS_BYTES;
   typedef v4f Acc[FM][FN];
@@ -90,16 +91,30 @@ struct Product8 {
     B sb;
     sa.init(a, r0, tid);
     sb.init(b, c0, tid);
-    const Operand8& own = wave < BM / 64 ? a : b;
-    const int first = wave < BM / 64 ? r0 + wave * 64 : c0 + wave * 64 - BM;      // of this wavefront's rows of scales
-    const int scale0 = first < own.rows ? first >> own.shift : 0;
-    const Buffer scales = buffer_of(own.scales + scale0 * own.ld_scales, (((own.rows - 1) >> own.shift) + 1 - scale0) * own.ld_scales);
-    const int scale_off = ((min(first + lane, own.rows - 1) >> own.shift) - scale0) * (int)own.ld_scales;
-    const auto load = [&](int t) {
+    Buffer scales[SCALE_LOADS];
+    int scale_off[SCALE_LOADS];
+#pragma unroll
+    for (int u = 0; u < SCALE_LOADS; ++u) {
+      const int at = wave + u * S::WAVES;
+      const Operand8& own = at < BM / 64 ? a : b;
+      const int first = at < BM / 64 ? r0 + at * 64 : c0 + at * 64 - BM;      // of this load's rows
+      const int scale0 = first < own.rows ? first >> own.shift : 0;
+      scales[u] = buffer_of(own.scales + scale0 * own.ld_scales, (((own.rows - 1) >> own.shift) + 1 - scale0) * own.ld_scales);
+      scale_off[u] = ((min(first + lane, own.rows - 1) >> own.shift) - scale0) * (int)own.ld_scales;
+    }
+    // Load k of a slab's LOADS
+    const auto load_one = [&](int t, int k) {
       uint8_t* const s = lds + t % S::STAGES * STAGE;
-      sa.load(t0 + t, s, wave);
-      sb.load(t0 + t, s + BM * BLOCK8, wave);
-      if (wave < SCALE_WAVES) __builtin_amdgcn_raw_ptr_buffer_load_lds(scales, in_lds<void>(s + SCALES + wave * 256), 4, scale_off, (t0 + t) / 4 * 4, 0, 0);
+      const int slab = FLOW ? min(t0 + t, t0 + n - 1) : t0 + t;      // (flow() has no branches: what it loads behind the last slab is not used)
+      if (k < A::PER) sa.load(slab, s, wave, k);
+      else if (k < A::PER + B::PER) sb.load(slab, s + BM * BLOCK8, wave, k - A::PER);
+      else if (SCALE_WAVES >= S::WAVES || wave < SCALE_WAVES)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(scales[k - A::PER - B::PER], in_lds<void>(s + SCALES + (wave + (k - A::PER - B::PER) * S::WAVES) * 256), 4,
+                                                 scale_off[k - A::PER - B::PER], slab / 4 * 4, 0, 0);
+    };
+    const auto load = [&](int t) {
+#pragma unroll
+      for (int k = 0; k < LOADS; ++k) load_one(t, k);
     };
     // Where a lane's pieces q and q + 4 of its row, and that row's scales, lie in a slab; fragments are 16 rows apart
     const int i = lane & 15, row_a = wm * (BM / S::WM) + i, row_b = BM + wn * (BN / S::WN) + i, piece = ((lane >> 4) ^ (i & 7)) * 16;
@@ -114,7 +129,8 @@ struct Product8 {
     };
     const auto read_a = [&](int slab, int f, int t, v8i& to, int& e) { read(a_lo, a_hi, row_a, slab, f, t, to, e); };
     const auto read_b = [&](int slab, int f, int t, v8i& to, int& e) { read(b_lo, b_hi, row_b, slab, f, t, to, e); };
-    if constexpr (S::TURNS) turns(n, load, read_a, read_b, acc);
+    if constexpr (FLOW) flow(n, load, load_one, read_a, read_b, acc);
+    else if constexpr (S::TURNS) turns(n, load, read_a, read_b, acc);
     else straight(n, wave, load, read_a, read_b, acc);
   }
 
@@ -145,14 +161,14 @@ struct Product8 {
 
   template <class L, class RA, class RB>
   __device__ static __forceinline__ void straight(int n, int wave, L load, RA read_a, RB read_b, Acc& acc) {
-    constexpr int AHEAD = S::STAGES - 1, LOADS = A::PER + B::PER;      // loads of a slab, one more for scales
+    constexpr int AHEAD = S::STAGES - 1;
 #pragma unroll
     for (int t = 0; t < AHEAD; ++t)
       if (t < n) load(t);
     for (int t = 0; t < n; ++t) {
       if (AHEAD == 1 || t + AHEAD > n) loads_done();
-      else if (wave < SCALE_WAVES) loads_left<(LOADS + 1) * (AHEAD - 1)>();
-      else loads_left<LOADS * (AHEAD - 1)>();
+      else if (wave < SCALE_WAVES) loads_left<LOADS * (AHEAD - 1)>();
+      else loads_left<(LOADS - 1) * (AHEAD - 1)>();
       group_barrier();      // slab t is there, and nobody reads slab t - 1 any more
       if (t + AHEAD < n) load(t + AHEAD);
       const int s = t % S::STAGES;
@@ -215,6 +231,55 @@ struct Product8 {
       }
       if (!second) group_barrier();
     }
+  }
+
+  // One wavefront on a SIMD, which goes through its columns' fragments one after the other, with all of its rows': beside the products of one
+  // column it reads the next column's operand from LDS, and beside those of the last one, row by row as they are done with, the next
+  // slab's.  Before the last column every wavefront has read all that it needs of slab t, and slab t + 1 has come: one barrier a slab, and slab
+  // t + 2 is loaded where slab t was, in the next four columns, a load for every second product: a CU takes loads at 64 bytes a cycle, and a
+  // wavefront that has to wait for its turn at them issues no products (all of a slab's loads at once: 56 cycles a product in place of ..).
+  template <class L, class L1, class RA, class RB>
+  __device__ static __forceinline__ void flow(int n, L load, L1 load_one, RA read_a, RB read_b, Acc& acc) {
+    static_assert(FN % 2 == 0 && !WIDE, "the next slab's first column goes where this slab's was");
+    constexpr int COLUMNS = 4, EACH = (LOADS + COLUMNS - 1) / COLUMNS;
+    static_assert(EACH <= FM && COLUMNS <= FN, "a load behind a product");
+    if (n <= 0) return;
+    v8i fa[FM], fb[2];
+    int ea[FM], eb[2];
+    load(0);
+    loads_done();
+    group_barrier();
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) load_one(1, k);
+    read_b(0, 0, 0, fb[0], eb[0]);
+#pragma unroll
+    for (int i = 0; i < FM; ++i) read_a(0, i, 0, fa[i], ea[i]);
+#pragma unroll 1
+    for (int t = 0; t < n; ++t) {
+      const int s = t & 1;
+#pragma unroll
+      for (int j = 0; j < FN; ++j) {
+        const bool last = j == FN - 1;
+        const int part = last ? 0 : j + 1;      // of the loads of slab t + 2 or t + 1
+        if (last) {
+          loads_done();
+          group_barrier();
+        }
+        if (last) read_b(s ^ 1, 0, t + 1, fb[0], eb[0]);
+        else read_b(s, j + 1, t, fb[(j + 1) & 1], eb[(j + 1) & 1]);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+          acc[i][j] = mma8<FORMAT>(fb[j & 1], eb[j & 1], fa[i], ea[i], acc[i][j]);
+          if (last) read_a(s ^ 1, i, t + 1, fa[i], ea[i]);
+          const int k0 = part * EACH + i * EACH / FM, k1 = part * EACH + (i + 1) * EACH / FM;
+          if (part < COLUMNS && k0 < k1 && k0 < LOADS) load_one(last ? t + 2 : t + 1, k0);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    }
+    loads_done();
+    group_barrier();
   }
 };
 
