@@ -2,6 +2,7 @@
 // kernels live in ob_linear8_kernels.h and ob_mm8.h.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <new>
 #include <type_traits>
 
@@ -28,9 +29,15 @@ namespace {
 constexpr int64_t MOST = (int64_t)1 << 22;      // rows, columns and distances between rows: a tile's offsets are 32-bit
 
 // Tiles by their side (ob_linear8_plan.h)
-template <int KIND, bool WIDE>
-using Tile8 = std::conditional_t<KIND == W256, std::conditional_t<WIDE, Shape<256, 256, 64, 2, 4>, Shape<256, 256, 64, 2, 2>>, 
-                                 std::conditional_t<KIND == W128, Shape<128, 128, 64, 2, 2>, Shape<64, 64, 64, 2, 2, 3>>>;
+template <int KIND>
+using Tile8 = std::conditional_t<KIND == W256, Shape<256, 256, 64, 2, 4>, std::conditional_t<KIND == W128, Shape<128, 128, 64, 2, 2>, Shape<64, 64, 64, 2, 2, 3>>>;
+
+template <int FORMAT, bool BF>
+ob_status launch_flow(ob_linear8_ctx* ctx, const Product8Args& p, hipStream_t s) {
+  const int64_t tiles = (int64_t)((p.a.rows + 255) / 256) * ((p.b.rows + 255) / 256);
+  hipLaunchKernelGGL((k_product8_flow<FORMAT, BF>), dim3((unsigned)std::min<int64_t>((tiles + 7) / 8 * 8, CUS8)), dim3(256), (Flow8<FORMAT, BF>::LDS_BYTES), s, p);
+  return hip_ok(ctx, hipGetLastError(), "k_product8_flow") ? OB_OK : OB_ERR_HIP;
+}
 
 template <class S, int FORMAT, bool WIDE>
 ob_status launch_product(ob_linear8_ctx* ctx, const Product8Args& p, hipStream_t s) {
@@ -62,7 +69,14 @@ hipError_t allow_products() {
     for (const int format : {E4M3, E5M2})
       for (const bool wide : {false, true})
         if (e == hipSuccess)
-          e = with_product(kind, format, wide, [](auto k, auto f, auto w) { return allow_lds(k_product8<Tile8<k, w>, f, w>, Product8<Tile8<k, w>, f, w>::LDS_BYTES); });
+          e = with_product(kind, format, wide, [](auto k, auto f, auto w) { return allow_lds(k_product8<Tile8<k>, f, w>, Product8<Tile8<k>, f, w>::LDS_BYTES); });
+  const auto flow = [&](auto format, auto bf) {
+    if (e == hipSuccess) e = allow_lds(k_product8_flow<format, bf>, Flow8<format, bf>::LDS_BYTES);
+  };
+  flow(std::integral_constant<int, E4M3>{}, std::true_type{});
+  flow(std::integral_constant<int, E4M3>{}, std::false_type{});
+  flow(std::integral_constant<int, E5M2>{}, std::true_type{});
+  flow(std::integral_constant<int, E5M2>{}, std::false_type{});
   return e;
 }
 
@@ -119,9 +133,14 @@ ob_status product(ob_linear8_ctx* ctx, const Given& a, int format, const Given& 
     else launch_few<false>(f, NONE, s);
     return hip_ok(ctx, hipGetLastError(), "k_product8_few") ? OB_OK : OB_ERR_HIP;
   }
-  const Plan8 plan = plan8(rows, cols, p.slabs, out_dtype == OB_F32);
+  const bool wide = out_dtype == OB_F32, eights = cols % 8 == 0 && ldo % 8 == 0 && !off(out, 16) && ldo <= ((int64_t)1 << 21);
+  const Plan8 plan = plan8(rows, cols, p.slabs, wide, !wide && eights && p.slabs >= 2);
   p.parts = plan.parts;
-  return with_product(plan.kind, format, out_dtype == OB_F32, [&](auto k, auto f, auto w) { return launch_product<Tile8<k, w>, f, w>(ctx, p, s); });
+  if (plan.kind == FLOW256) {
+    if (format == OB_E4M3) return out_dtype == OB_BF16 ? launch_flow<E4M3, true>(ctx, p, s) : launch_flow<E4M3, false>(ctx, p, s);
+    return out_dtype == OB_BF16 ? launch_flow<E5M2, true>(ctx, p, s) : launch_flow<E5M2, false>(ctx, p, s);
+  }
+  return with_product(plan.kind, format, wide, [&](auto k, auto f, auto w) { return launch_product<Tile8<k>, f, w>(ctx, p, s); });
 }
 
 template <int DTYPE>

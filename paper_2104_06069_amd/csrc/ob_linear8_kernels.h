@@ -126,7 +126,7 @@ struct Product8Args {
 extern __shared__ __align__(1024) uint16_t lds_of_product8[];
 
 template <class S, int FORMAT, bool WIDE>
-__global__ __launch_bounds__(S::NT, S::BM == 256 && S::WAVES == 4 ? 1 : 2) void k_product8(Product8Args p) {
+__global__ __launch_bounds__(S::NT, 2) void k_product8(Product8Args p) {
   using P = Product8<S, FORMAT, WIDE>;
   const int nm = (p.a.rows + S::BM - 1) / S::BM, nn = (p.b.rows + S::BN - 1) / S::BN, tiles = nm * nn;
   const int at = tile_of_workgroup(blockIdx.x, tiles * p.parts);
@@ -155,6 +155,24 @@ __global__ __launch_bounds__(S::NT, S::BM == 256 && S::WAVES == 4 ? 1 : 2) void 
   } else {
     store_tile<S, false>(acc, lds_of_product8, p.out, F16, p.ldo, r0, c0, rows, cols, 0, 0);
   }
+}
+
+// Workgroups that stay (Flow8): tiles id, id + gridDim.x, ..
+template <int FORMAT, bool BF>
+__global__ __launch_bounds__(256, 1) void k_product8_flow(Product8Args p) {
+  const int nm = (p.a.rows + 255) / 256, nn = (p.b.rows + 255) / 256, tiles = nm * nn, per = (tiles + 7) / 8;
+  int id = blockIdx.x;
+  Flow8<FORMAT, BF>::run(p.a, p.b, p.slabs, p.out, p.ldo, reinterpret_cast<uint8_t*>(lds_of_product8), [&](int* r, int* c) {
+    for (*r = *c = -1; id >> 3 < per; id += gridDim.x) {
+      const int t = tile_of_workgroup(id, tiles);
+      if (t < 0) continue;
+      tile_in_bands(t, nm, nn, r, c);
+      *r *= 256;
+      *c *= 256;
+      id += gridDim.x;
+      return;
+    }
+  });
 }
 
 // The parts of a product's sums, in their order

@@ -50,6 +50,20 @@ struct Rows8 {
   }
 };
 
+// The scales of 64 rows, a lane each, for the group of four slabs that a slab is in
+struct Scales8 {
+  Buffer memory;
+  int off;
+  __device__ void init(const uint8_t* scales, int64_t ld, int rows, int shift, int first, int lane) {
+    const int scale0 = first < rows ? first >> shift : 0, high = min(((rows - 1) >> shift) + 1 - scale0, 64);      // (rows of scales)
+    memory = buffer_of(scales + scale0 * ld, high * ld);
+    off = ((min(first + lane, rows - 1) >> shift) - scale0) * (int)ld;
+  }
+  __device__ __forceinline__ void load(int slab, uint8_t* lds) const {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(memory, in_lds<void>(lds), 4, off, slab / 4 * 4, 0, 0);
+  }
+};
+
 // B's numbers are e4m3
 template <int FORMAT>
 __device__ __forceinline__ v4f mma8(v8i b, int scale_b, v8i a, int scale_a, v4f c) {
@@ -76,9 +90,7 @@ struct Product8 {
   using A = Rows8<BM, S::NT>;
   using B = Rows8<BN, S::NT>;
   static constexpr int SCALE_WAVES = (BM + BN) / 64, SCALES = (BM + BN) * BLOCK8;      // (64 rows' scales a load); where a slab's scales begin
-  static constexpr int SCALE_LOADS = SCALE_WAVES > S::WAVES ? SCALE_WAVES / S::WAVES : 1;
-  static constexpr int LOADS = A::PER + B::PER + SCALE_LOADS;      // of a slab (without the last one, where only some wavefronts have scales)
-  static constexpr bool FLOW = S::WAVES == 4 && BM == 256 && !WIDE;      // flow() below
+  static_assert(SCALE_WAVES <= S::WAVES, "a row's scales for each lane");
   static constexpr int STAGE = (BM + BN) * (BLOCK8 + 4);
   static constexpr int LDS_BYTES = S::STAGES * STAGE > Results<S>::LDS_BYTES ? S::STAGES * STAGE : Results<S>::LDS_BYTES;
   typedef v4f Acc[FM][FN];
@@ -91,30 +103,17 @@ struct Product8 {
     B sb;
     sa.init(a, r0, tid);
     sb.init(b, c0, tid);
-    Buffer scales[SCALE_LOADS];
-    int scale_off[SCALE_LOADS];
-#pragma unroll
-    for (int u = 0; u < SCALE_LOADS; ++u) {
-      const int at = wave + u * S::WAVES;
-      const Operand8& own = at < BM / 64 ? a : b;
-      const int first = at < BM / 64 ? r0 + at * 64 : c0 + at * 64 - BM;      // of this load's rows
-      const int scale0 = first < own.rows ? first >> own.shift : 0;
-      scales[u] = buffer_of(own.scales + scale0 * own.ld_scales, (((own.rows - 1) >> own.shift) + 1 - scale0) * own.ld_scales);
-      scale_off[u] = ((min(first + lane, own.rows - 1) >> own.shift) - scale0) * (int)own.ld_scales;
-    }
-    // Load k of a slab's LOADS
-    const auto load_one = [&](int t, int k) {
-      uint8_t* const s = lds + t % S::STAGES * STAGE;
-      const int slab = FLOW ? min(t0 + t, t0 + n - 1) : t0 + t;      // (flow() has no branches: what it loads behind the last slab is not used)
-      if (k < A::PER) sa.load(slab, s, wave, k);
-      else if (k < A::PER + B::PER) sb.load(slab, s + BM * BLOCK8, wave, k - A::PER);
-      else if (SCALE_WAVES >= S::WAVES || wave < SCALE_WAVES)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(scales[k - A::PER - B::PER], in_lds<void>(s + SCALES + (wave + (k - A::PER - B::PER) * S::WAVES) * 256), 4,
-                                                 scale_off[k - A::PER - B::PER], slab / 4 * 4, 0, 0);
-    };
+    const bool of_a = wave < BM / 64;
+    Scales8 scales;
+    scales.init(of_a ? a.scales : b.scales, of_a ? a.ld_scales : b.ld_scales, of_a ? a.rows : b.rows, of_a ? a.shift : b.shift,
+                of_a ? r0 + wave * 64 : c0 + wave * 64 - BM, lane);
     const auto load = [&](int t) {
+      uint8_t* const s = lds + t % S::STAGES * STAGE;
 #pragma unroll
-      for (int k = 0; k < LOADS; ++k) load_one(t, k);
+      for (int j = 0; j < A::PER; ++j) sa.load(t0 + t, s, wave, j);
+#pragma unroll
+      for (int j = 0; j < B::PER; ++j) sb.load(t0 + t, s + BM * BLOCK8, wave, j);
+      if (wave < SCALE_WAVES) scales.load(t0 + t, s + SCALES + wave * 256);
     };
     // Where a lane's pieces q and q + 4 of its row, and that row's scales, lie in a slab; fragments are 16 rows apart
     const int i = lane & 15, row_a = wm * (BM / S::WM) + i, row_b = BM + wn * (BN / S::WN) + i, piece = ((lane >> 4) ^ (i & 7)) * 16;
@@ -129,8 +128,7 @@ struct Product8 {
     };
     const auto read_a = [&](int slab, int f, int t, v8i& to, int& e) { read(a_lo, a_hi, row_a, slab, f, t, to, e); };
     const auto read_b = [&](int slab, int f, int t, v8i& to, int& e) { read(b_lo, b_hi, row_b, slab, f, t, to, e); };
-    if constexpr (FLOW) flow(n, load, load_one, read_a, read_b, acc);
-    else if constexpr (S::TURNS) turns(n, load, read_a, read_b, acc);
+    if constexpr (S::TURNS) turns(n, load, read_a, read_b, acc);
     else straight(n, wave, load, read_a, read_b, acc);
   }
 
@@ -161,14 +159,14 @@ struct Product8 {
 
   template <class L, class RA, class RB>
   __device__ static __forceinline__ void straight(int n, int wave, L load, RA read_a, RB read_b, Acc& acc) {
-    constexpr int AHEAD = S::STAGES - 1;
+    constexpr int AHEAD = S::STAGES - 1, LOADS = A::PER + B::PER;      // loads of a slab, one more for scales
 #pragma unroll
     for (int t = 0; t < AHEAD; ++t)
       if (t < n) load(t);
     for (int t = 0; t < n; ++t) {
       if (AHEAD == 1 || t + AHEAD > n) loads_done();
-      else if (wave < SCALE_WAVES) loads_left<LOADS * (AHEAD - 1)>();
-      else loads_left<(LOADS - 1) * (AHEAD - 1)>();
+      else if (wave < SCALE_WAVES) loads_left<(LOADS + 1) * (AHEAD - 1)>();
+      else loads_left<LOADS * (AHEAD - 1)>();
       group_barrier();      // slab t is there, and nobody reads slab t - 1 any more
       if (t + AHEAD < n) load(t + AHEAD);
       const int s = t % S::STAGES;
@@ -232,54 +230,159 @@ struct Product8 {
       if (!second) group_barrier();
     }
   }
+};
 
-  // One wavefront on a SIMD, which goes through its columns' fragments one after the other, with all of its rows': beside the products of one
-  // column it reads the next column's operand from LDS, and beside those of the last one, row by row as they are done with, the next
-  // slab's.  Before the last column every wavefront has read all that it needs of slab t, and slab t + 1 has come: one barrier a slab, and slab
-  // t + 2 is loaded where slab t was, in the next four columns, a load for every second product: a CU takes loads at 64 bytes a cycle, and a
-  // wavefront that has to wait for its turn at them issues no products (all of a slab's loads at once: 56 cycles a product in place of ..).
-  template <class L, class L1, class RA, class RB>
-  __device__ static __forceinline__ void flow(int n, L load, L1 load_one, RA read_a, RB read_b, Acc& acc) {
-    static_assert(FN % 2 == 0 && !WIDE, "the next slab's first column goes where this slab's was");
-    constexpr int COLUMNS = 4, EACH = (LOADS + COLUMNS - 1) / COLUMNS;
-    static_assert(EACH <= FM && COLUMNS <= FN, "a load behind a product");
-    if (n <= 0) return;
+// Many tiles of 256 x 256, 16-bit results of adjacent eights, K of two slabs or more: workgroups that stay, one on a CU, and go from tile to
+// tile without a pause in their loads.  A wavefront has a SIMD for itself and 128 x 128 of a tile.  It goes through its columns'
+// fragments one after the other, with all of its rows': beside the products of one column it reads the next column's operand from LDS, and
+// beside those of the last one, row by row as they are done with, the next slab's rows.  So A's part of a slab is done with when its
+// columns begin, and the first half of B's when they are half through, and what is free is loaded again at once, for the slab after the
+// next, which may be the next tile's: at Q, before column 3, A and the first columns; at P, before the last column, scales and the last
+// columns.  Each is waited for a slab and a half after that, at the P or Q before it is read.  Loads are spread over the products: a
+// wavefront that waits for its turn at the CU's loads issues no products (all of a slab's at once: 56 cycles a product in place of 44).
+// Results go out while the next tile's products run: nothing waits for them but their own turn in the count of loads.
+template <int FORMAT, bool BF>
+struct Flow8 {
+  static constexpr int BM = 256, BN = 256, NT = 256, FM = 8, FN = 8;
+  using A = Rows8<BM, NT>;
+  using B = Rows8<BN, NT>;
+  static constexpr int SCALES = (BM + BN) * BLOCK8, STAGE = SCALES + (BM + BN) * 4;
+  static constexpr int PITCH = 272, RESULTS = 16 * PITCH, LDS_BYTES = 2 * STAGE + 4 * RESULTS;      // (16 rows of 128 results a wavefront, four banks apart)
+  static_assert(A::PER == 8 && B::PER == 8, "the loads below");
+  static constexpr int STORES = FM * 4;      // of a tile, whatever part of it exists
+
+  struct Loads {      // of a tile, by a wavefront
+    A a;
+    B b;
+    Scales8 sa, sb;
+    __device__ void aim(const Operand8& oa, const Operand8& ob, int r0, int c0, int tid) {
+      const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+      a.init(oa, r0, tid);
+      b.init(ob, c0, tid);
+      sa.init(oa.scales, oa.ld_scales, oa.rows, oa.shift, r0 + wave * 64, lane);
+      sb.init(ob.scales, ob.ld_scales, ob.rows, ob.shift, c0 + wave * 64, lane);
+    }
+    // At Q: A, and columns 0 to 3 of both halves; at P: scales, and columns 4 to 7 of both
+    __device__ __forceinline__ void at_q(int k, int slab, uint8_t* s, int wave) const {
+      if (k < 8) a.load(slab, s, wave, k);
+      else b.load(slab, s + BM * BLOCK8, wave, k < 10 ? k - 8 : k - 6);
+    }
+    __device__ __forceinline__ void at_p(int k, int slab, uint8_t* s, int wave) const {
+      if (k == 0) sa.load(slab, s + SCALES + wave * 256);
+      else if (k == 1) sb.load(slab, s + SCALES + (4 + wave) * 256);
+      else b.load(slab, s + BM * BLOCK8, wave, k < 4 ? k : k + 2);
+    }
+  };
+
+  // next(id) is the next tile's place, or none: {row, column}, row < 0
+  template <class NEXT>
+  __device__ static __forceinline__ void run(const Operand8& oa, const Operand8& ob, int n, void* out, int64_t ldo, uint8_t* lds, NEXT next) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave / 2, wn = wave % 2, i16 = lane & 15, q = lane >> 4;
+    int r0, c0, r1, c1;      // of the tile, and of the next one
+    next(&r0, &c0);
+    if (r0 < 0) return;
+    Loads loads;
+    loads.aim(oa, ob, r0, c0, tid);
+
+    const int row_a = wm * 128 + i16, row_b = BM + wn * 128 + i16, piece = (q ^ (i16 & 7)) * 16;
+    const int a_lo = row_a * BLOCK8 + piece, a_hi = row_a * BLOCK8 + (piece ^ 64), b_lo = row_b * BLOCK8 + piece, b_hi = row_b * BLOCK8 + (piece ^ 64);
+    const auto base = in_lds<uint8_t>(lds);
+    const auto read = [&](int lo, int hi, int row, int stage, int f, int slab, v8i& to, int& e) {
+      const int s = stage * STAGE;
+      const v4i x = *(__attribute__((address_space(3))) const v4i*)(base + (s + lo) + f * 16 * BLOCK8);
+      const v4i y = *(__attribute__((address_space(3))) const v4i*)(base + (s + hi) + f * 16 * BLOCK8);
+      to = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+      e = *(base + (s + SCALES + row * 4 + (slab & 3)) + f * 64);
+    };
     v8i fa[FM], fb[2];
     int ea[FM], eb[2];
-    load(0);
-    loads_done();
-    group_barrier();
 #pragma unroll
-    for (int k = 0; k < EACH; ++k) load_one(1, k);
-    read_b(0, 0, 0, fb[0], eb[0]);
+    for (int t = 0; t < 2; ++t) {
 #pragma unroll
-    for (int i = 0; i < FM; ++i) read_a(0, i, 0, fa[i], ea[i]);
-#pragma unroll 1
-    for (int t = 0; t < n; ++t) {
-      const int s = t & 1;
+      for (int k = 0; k < 12; ++k) loads.at_q(k, t, lds + t * STAGE, wave);
 #pragma unroll
-      for (int j = 0; j < FN; ++j) {
-        const bool last = j == FN - 1;
-        const int part = last ? 0 : j + 1;      // of the loads of slab t + 2 or t + 1
-        if (last) {
-          loads_done();
-          group_barrier();
-        }
-        if (last) read_b(s ^ 1, 0, t + 1, fb[0], eb[0]);
-        else read_b(s, j + 1, t, fb[(j + 1) & 1], eb[(j + 1) & 1]);
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int i = 0; i < FM; ++i) {
-          acc[i][j] = mma8<FORMAT>(fb[j & 1], eb[j & 1], fa[i], ea[i], acc[i][j]);
-          if (last) read_a(s ^ 1, i, t + 1, fa[i], ea[i]);
-          const int k0 = part * EACH + i * EACH / FM, k1 = part * EACH + (i + 1) * EACH / FM;
-          if (part < COLUMNS && k0 < k1 && k0 < LOADS) load_one(last ? t + 2 : t + 1, k0);
-          __builtin_amdgcn_sched_barrier(0);
-        }
-      }
+      for (int k = 0; k < 6; ++k) loads.at_p(k, t, lds + t * STAGE, wave);
     }
     loads_done();
     group_barrier();
+    read(b_lo, b_hi, row_b, 0, 0, 0, fb[0], eb[0]);
+#pragma unroll
+    for (int i = 0; i < FM; ++i) read(a_lo, a_hi, row_a, 0, i, 0, fa[i], ea[i]);
+    int stage = 0;
+    while (true) {
+      v4f acc[FM][FN] = {};
+      next(&r1, &c1);
+      // AFTER: of a tile's first slab, behind the stores of the tile before (before the first tile everything has been waited for)
+      const auto slab = [&](int t, auto after) {
+        constexpr int BEHIND = decltype(after)::value ? STORES : 0;
+        if (t + 2 == n && r1 >= 0) loads.aim(oa, ob, r1, c1, tid);
+        const int one = t + 1 < n ? t + 1 : 0, two = t + 2 < n ? t + 2 : t + 2 - n;      // the slabs after this one, in their tile
+        uint8_t* const here = lds + stage * STAGE;
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+          const bool last = j == FN - 1;
+          if (j == 3) {
+            loads_left<18 + BEHIND>();      // (this slab's P: behind it the next slab's Q and P)
+            group_barrier();
+          }
+          if (last) {
+            loads_left<16 + BEHIND>();      // (the next slab's Q and scales: behind them its columns and the Q after that)
+            group_barrier();
+          }
+          if (last) read(b_lo, b_hi, row_b, stage ^ 1, 0, one, fb[0], eb[0]);
+          else read(b_lo, b_hi, row_b, stage, j + 1, t, fb[(j + 1) & 1], eb[(j + 1) & 1]);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int i = 0; i < FM; ++i) {
+            acc[i][j] = mma8<FORMAT>(fb[j & 1], eb[j & 1], fa[i], ea[i], acc[i][j]);
+            if (last) read(a_lo, a_hi, row_a, stage ^ 1, i, one, fa[i], ea[i]);
+            if (j >= 3 && j < 7 && i % 3 == 0) loads.at_q((j - 3) * 3 + i / 3, two, here, wave);
+            if (last && i < 6) loads.at_p(i, two, here, wave);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+        stage ^= 1;
+      };
+      slab(0, std::true_type{});
+#pragma unroll 1
+      for (int t = 1; t < n; ++t) slab(t, std::false_type{});
+      store(acc, oa.rows, ob.rows, out, ldo, r0, c0, lds + 2 * STAGE + wave * RESULTS, wm, wn, lane);
+      if (r1 < 0) break;
+      r0 = r1;
+      c0 = c1;
+    }
+    loads_done();      // (what was loaded behind the last tile's end)
+  }
+
+ private:
+  // A wavefront's results, sixteen rows at a time turned in LDS to 256 bytes of a row by sixteen lanes.  Always STORES stores: what lies outside
+  // of the matrix has an offset outside of the buffer and is dropped.
+  __device__ static __forceinline__ void store(const v4f (&acc)[FM][FN], int rows, int cols, void* out, int64_t ldo, int r0, int c0, uint8_t* own, int wm, int wn,
+                                               int lane) {
+    asm volatile("" : "+v"(lane));      // (offsets are made here, and not held through the products)
+    const int high = min(rows - r0, BM), wide = min(cols - c0, BN);
+    const Buffer to = buffer_of(static_cast<uint8_t*>(out) + (r0 * ldo + c0) * 2, ((high - 1) * ldo + wide) * 2);
+    const auto mine = in_lds<uint8_t>(own);
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+#pragma unroll
+      for (int j = 0; j < FN; ++j) {
+        v4f v = acc[i][j];
+        asm volatile("" : "+a"(v)::"memory");      // (from where the products left it, and not before its turn: there are registers for sixteen rows)
+        v4h h;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) h[e] = to_bits(v[e], BF);
+        *(__attribute__((address_space(3))) v2i*)(mine + (lane & 15) * PITCH + j * 32 + (lane >> 4) * 8) = __builtin_bit_cast(v2i, h);
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int row = u * 4 + (lane >> 4), piece = lane & 15, r = wm * 128 + i * 16 + row, c = wn * 128 + piece * 8;
+        const v4i v = *(__attribute__((address_space(3))) const v4i*)(mine + row * PITCH + piece * 16);
+        const int at = r < high && c < wide ? (r * (int)ldo + c) * 2 : 0x7ffffff0;
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(unsigned __attribute__((ext_vector_type(4))), v), to, at, 0, 0);
+      }
+    }
   }
 };
 

@@ -256,3 +256,22 @@ def test_few_rows(rows, k, n, dtype):
         few = op(k, rows, dtype=dtype)
         xs, g = numbers(300, k, dtype, 5), numbers(300, rows, dtype, 6)
         product_near(few.weight_grad(xs, g), values(few._quantize(g, "dy", rows, None, E4M3)[1]), values(few._quantize(xs, "x", k, None, E4M3)[1]), 300, "dw")
+
+
+@pytest.mark.parametrize("rows,k,n", [(4096, 512, 2048), (5000, 300, 4200), (20000, 400, 1032), (4097, 300, 4097), (2100, 1000, 3000), (600, 4100, 2056), (3000, 130, 3000), (70, 5000, 70)])
+@pytest.mark.parametrize("dtype", (BF, F16, F32))
+def test_many_tiles(rows, k, n, dtype):
+    """Sizes that take every kind of tile, several for a workgroup, and sums in parts; sums in 64 bits on the device."""
+    layer = op(k, n, dtype=dtype)
+    x, w = numbers(rows, k, BF, 1) / 64, numbers(n, k, BF, 3) / 64
+    w8, x8 = layer.quantize_weight(w), layer.quantize(x)
+    wide = torch.full((rows + 2, n + 8), 7.0, device="cuda", dtype=dtype)
+    y = layer.forward(x8, w8, out=wide[1:rows + 1, :n])
+    assert (wide[0] == 7).all() and (wide[rows + 1:] == 7).all() and (wide[:, n:] == 7).all()
+    a, b = values(x8).cuda(), values(w8.w).cuda()
+    want, size = a @ b.T, a.abs() @ b.abs().T
+    bound = (k * 2.0 ** -23 + (0.0 if dtype == F32 else 2.0 ** -10)) * size + HALF[dtype] * want.abs() + LOWEST[dtype]
+    got, beyond = y.double(), want.abs() + bound >= 65520 if dtype == F16 else torch.zeros_like(want, dtype=torch.bool)
+    assert (((got - want).abs() <= bound) | beyond).all()
+    assert (got[~beyond] - want[~beyond]).norm() / want[~beyond].norm() <= HALF[dtype] + (2e-6 if dtype == F32 else 1e-4)
+    assert torch.equal(layer.forward(x8, w8), y)
