@@ -27,6 +27,7 @@ class GradClip:
         self.N = int(layer_offsets[-1])
         self.ctx = ob.ob_clip_create(layer_offsets, eps, grad_scale)
         self.layer_norms = torch.zeros(len(layer_offsets) - 1, device=self.device)
+        self._call, self._layer_norms = ob.lib().ob_clip_norm_apply, self.layer_norms.data_ptr()
 
     def close(self):
         if self.ctx is not None:
@@ -65,8 +66,11 @@ class GradClip:
 
     def clip(self, grad, max_norm, out=None):
         """norm() and apply() in one call; -> the norm [1] before."""
-        out = self._flat(grad, "grad") if out is None else self._flat(out, "out")
+        self._flat(grad, "grad")
+        out = grad if out is None else self._flat(out, "out")
         norm = self._one()
-        ob.ob_clip_norm_apply(self.ctx, self._flat(grad, "grad"), _OB_DTYPE[grad.dtype], max_norm, norm, self.layer_norms, out, _OB_DTYPE[out.dtype],
-                              _current_stream(self.device))
+        status = self._call(self.ctx, grad.data_ptr(), _OB_DTYPE[grad.dtype], max_norm, norm.data_ptr(), self._layer_norms, out.data_ptr(), _OB_DTYPE[out.dtype],
+                            _current_stream(self.device))
+        if status:
+            raise ob.ObLambError(status, "ob_clip_norm_apply", ob.lib().ob_clip_last_hip_error(self.ctx).decode())
         return norm

@@ -14,11 +14,12 @@ import torch
 from torch.autograd.function import once_differentiable
 
 from . import binding as ob
-from .matrix8 import Matrix8, adjacent, format_of, rows_of
+from .matrix8 import FORMATS, Matrix8, adjacent, format_of, rows_of
 from .step import _OB_DTYPE, _current_stream
 
 _TYPES = tuple(_OB_DTYPE)
 _E4M3 = torch.float8_e4m3fn
+_NO_MATRIX = (None, 0, None, 0)
 
 
 class Weight8(NamedTuple):
@@ -39,7 +40,9 @@ class Linear8:
         format_of(grad_format)
         if dtype not in _OB_DTYPE:
             raise ValueError("dtype is torch.float32, torch.float16 or torch.bfloat16")
-        self._few = ob.lib().ob_linear8_forward_few
+        L = ob.lib()
+        self._calls = L.ob_linear8_quantize, L.ob_linear8_forward, L.ob_linear8_input_grad, L.ob_linear8_weight_grad, L.ob_linear8_forward_few
+        self._index = torch.cuda.current_device()
         self.ctx = ob.ob_linear8_create(self.k, self.n, max_rows)
         # rows whose numbers the product itself makes 8 bits (one launch): few, or short ones, up to 512 blocks of 128 in all
         self._few_rows = min(ob.OB_LINEAR8_FEW_ROWS, 512 // ((self.k + 127) // 128))
@@ -56,15 +59,27 @@ class Linear8:
         except Exception:
             pass
 
+    # (A small layer's calls take 5 to 10 us on the device each: the common cases are looked at as a whole, anything else piece by piece, and
+    # the library is called without a stop in between.)
+    def _check(self, status, where):
+        if status:
+            raise ob.ObLambError(status, where, ob.lib().ob_linear8_last_hip_error(self.ctx).decode())
+
+    def _rows(self, t, width, what):
+        """The distance between t's rows"""
+        if t.dim() == 2 and t.shape[1] == width and t.dtype in _OB_DTYPE and t.is_contiguous() and t.get_device() == self._index:
+            return width
+        return rows_of(t, width, _TYPES, self.device, what)
+
     def _quantize(self, t, what, width, rows_format=None, cols_format=None, square=False):
         """-> (t, t transposed) in the given formats, None where that is None"""
-        ld, (rows, cols) = rows_of(t, width, _TYPES, self.device, what), t.shape
+        ld, (rows, cols) = self._rows(t, width, what), t.shape
         m = None if rows_format is None else Matrix8(rows, cols, rows_format, self.device, square)
         mt = None if cols_format is None else Matrix8(cols, rows, cols_format, self.device, square)
-        ob.ob_linear8_quantize(self.ctx, t, _OB_DTYPE[t.dtype], ld, rows, cols, ob.OB_BLOCK_SQUARE if square else ob.OB_BLOCK_ROWS,
-                               ob.OB_E4M3 if m is None else format_of(rows_format), ob.OB_E4M3 if mt is None else format_of(cols_format),
-                               *((None, 0, None, 0) if m is None else m.address()), *((None, 0, None, 0) if mt is None else mt.address()),
-                               _current_stream(self.device))
+        self._check(self._calls[0](self.ctx, t.data_ptr(), _OB_DTYPE[t.dtype], ld, rows, cols, ob.OB_BLOCK_SQUARE if square else ob.OB_BLOCK_ROWS,
+                                   0 if m is None else FORMATS[rows_format], 0 if mt is None else FORMATS[cols_format],
+                                   *(_NO_MATRIX if m is None else m.address()), *(_NO_MATRIX if mt is None else mt.address()), _current_stream(self.device)),
+                    "ob_linear8_quantize")
         return m, mt
 
     def quantize(self, t, format=_E4M3):
@@ -103,16 +118,15 @@ class Linear8:
         """y = x W^T; x is quantised to e4m3 unless it is a Matrix8."""
         self._weight(w8)
         if not isinstance(x, Matrix8) and x.dim() == 2 and x.shape[0] <= self._few_rows:
-            rows, ldx = x.shape[0], rows_of(x, self.k, _TYPES, self.device, "x")
+            rows, ldx = x.shape[0], self._rows(x, self.k, "x")
             out, ldo = self._out(out, rows, self.n, out_dtype or self.dtype, _TYPES)
-            status = self._few(self.ctx, x.data_ptr(), _OB_DTYPE[x.dtype], ldx, ob.OB_E4M3, *w8.w.address(), rows, out.data_ptr(), ldo, _OB_DTYPE[out.dtype],
-                               _current_stream(self.device))
-            if status:
-                raise ob.ObLambError(status, "ob_linear8_forward_few", ob.lib().ob_linear8_last_hip_error(self.ctx).decode())
+            self._check(self._calls[4](self.ctx, x.data_ptr(), _OB_DTYPE[x.dtype], ldx, ob.OB_E4M3, *w8.w.address(), rows, out.data_ptr(), ldo,
+                                       _OB_DTYPE[out.dtype], _current_stream(self.device)), "ob_linear8_forward_few")
             return out
         m = self._matrix(x, self.k, _E4M3, "x")
         out, ldo = self._out(out, m.rows, self.n, out_dtype or self.dtype, _TYPES)
-        ob.ob_linear8_forward(self.ctx, *m.address(), format_of(m.dtype), *w8.w.address(), m.rows, out, ldo, _OB_DTYPE[out.dtype], _current_stream(self.device))
+        self._check(self._calls[1](self.ctx, *m.address(), FORMATS[m.dtype], *w8.w.address(), m.rows, out.data_ptr(), ldo, _OB_DTYPE[out.dtype],
+                                   _current_stream(self.device)), "ob_linear8_forward")
         return out
 
     def input_grad(self, dy, w8, out=None, out_dtype=None):
@@ -120,8 +134,8 @@ class Linear8:
         self._weight(w8)
         m = self._matrix(dy, self.n, self.grad_format, "dy")
         out, ldo = self._out(out, m.rows, self.k, out_dtype or self.dtype, _TYPES)
-        ob.ob_linear8_input_grad(self.ctx, *m.address(), format_of(m.dtype), *w8.transposed.address(), m.rows, out, ldo, _OB_DTYPE[out.dtype],
-                                 _current_stream(self.device))
+        self._check(self._calls[2](self.ctx, *m.address(), FORMATS[m.dtype], *w8.transposed.address(), m.rows, out.data_ptr(), ldo, _OB_DTYPE[out.dtype],
+                                   _current_stream(self.device)), "ob_linear8_input_grad")
         return out
 
     def weight_grad(self, x, dy, out=None, out_dtype=torch.float32, accumulate=False):
@@ -135,8 +149,8 @@ class Linear8:
         if accumulate and out is None:
             raise ValueError("accumulate needs an out to add to")
         out, ldo = self._out(out, self.n, self.k, out_dtype, (torch.float32,) if accumulate else _TYPES)
-        ob.ob_linear8_weight_grad(self.ctx, *dy_t.address(), format_of(dy_t.dtype), *x_t.address(), x.shape[0], out, ldo, _OB_DTYPE[out.dtype], accumulate,
-                                  _current_stream(self.device))
+        self._check(self._calls[3](self.ctx, *dy_t.address(), FORMATS[dy_t.dtype], *x_t.address(), x.shape[0], out.data_ptr(), ldo, _OB_DTYPE[out.dtype],
+                                   bool(accumulate), _current_stream(self.device)), "ob_linear8_weight_grad")
         return out
 
     def backward(self, x, dy, w8, dw=None, dw_dtype=torch.float32, accumulate=False):

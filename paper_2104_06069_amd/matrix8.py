@@ -37,9 +37,9 @@ class Matrix8:
 
     def __init__(self, rows, cols, dtype, device, square=False):
         self.rows, self.cols, self.dtype, self.square, self.device = rows, cols, dtype, square, device
-        blocks = (cols + 127) // 128
-        self.ld, self.ld_scales = blocks * 128, (blocks + 3) // 4 * 4
-        self.buffer = torch.empty(rows * self.ld + ((rows + 127) // 128 if square else rows) * self.ld_scales, dtype=torch.uint8, device=device)
+        blocks = cols + 127 >> 7
+        self.ld, self.ld_scales = blocks << 7, blocks + 3 & ~3
+        self.buffer = torch.empty(rows * self.ld + (rows + 127 >> 7 if square else rows) * self.ld_scales, dtype=torch.uint8, device=device)
 
     @property
     def data(self):
