@@ -14,16 +14,22 @@ struct Segment {
   int32_t len, layer;
 };
 
+// 16 bytes of elements, read past the caches, which hold nothing of a large gradient until it comes around again (302 M binary32 numbers: norm 208
+// us without, 187 with; clipped 642 and 591)
 template <int DTYPE>
-struct Piece {      // 16 bytes of elements
+struct Piece {
   static constexpr int N = DTYPE == F32 ? 4 : 8;
   __device__ static __forceinline__ void load(const void* p, int64_t at, int64_t left, float (&v)[N]) {
     if constexpr (DTYPE == F32) {
-      const v4f w = load4(p, F32, at, (int)min(left, (int64_t)4));
+      const v4f w = left >= 4 ? __builtin_nontemporal_load(reinterpret_cast<const v4f_any*>(static_cast<const float*>(p) + at)) : load4(p, F32, at, (int)left);
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] = w[e];
+    } else if (left >= 8) {
+      const v8s h = __builtin_nontemporal_load(reinterpret_cast<const v8s_any*>(static_cast<const uint16_t*>(p) + at));
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = from_bits((unsigned short)h[e], DTYPE == BF16);
     } else {
-      load8<DTYPE>(p, at, (int)min(left, (int64_t)8), v);
+      load8<DTYPE>(p, at, (int)left, v);
     }
   }
 };
