@@ -1,0 +1,51 @@
+"""What the compiler made of the kernels of a layer's operators, which results show rarely or not at all: built for gfx950, no device."""
+import os
+import re
+import shutil
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module", params=("ob_norm", "ob_linear8", "ob_clip"))
+def text(request, tmp_path_factory):
+    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+    if not (os.path.exists(hipcc) or shutil.which(hipcc)):
+        pytest.skip("no hipcc")
+    asm = tmp_path_factory.mktemp("asm") / "m.s"
+    subprocess.run([hipcc, "-O3", "--offload-arch=gfx950", "--offload-device-only", "-S", "-std=c++17", "-ffp-contract=off", "-Xclang",
+                    "-target-feature", "-Xclang", "-packed-fp32-ops", "-I", os.path.join(ROOT, "include"),
+                    os.path.join(ROOT, "paper_2104_06069_amd", "csrc", request.param + ".hip"), "-o", str(asm)], check=True, capture_output=True)
+    return request.param, asm.read_text()
+
+
+def test_no_memory_for_spills_and_no_packed_binary32(text):
+    name, text = text
+    counts = re.findall(r"\.name:\s+(_ZN3obl\w+).*?\.private_segment_fixed_size:\s+(\d+).*?\.vgpr_spill_count:\s+(\d+)", text, re.S)
+    assert len(counts) >= {"ob_norm": 50, "ob_linear8": 40, "ob_clip": 20}[name]
+    assert [c for c in counts if c[1:] != ("0", "0")] == []
+    assert not re.findall(r"v_pk_(?:add|mul|fma)_f32", text)
+
+
+def function(text, part):
+    start = re.search(r"^(_ZN3obl\w*" + part + r"\w*):", text, re.M)
+    return text[start.end():text.index(".Lfunc_end", start.end())]
+
+
+def test_stores_are_counted_with_the_loads(text):
+    """k_product8_flow waits for loads by how many loads and stores are behind them: a tile's 32 stores are stores whatever part of the tile exists,
+    in one piece without branches, and its loop has 18 loads a slab."""
+    name, text = text
+    if name != "ob_linear8":
+        pytest.skip("of the products")
+    for variant in ("k_product8_flowILi0ELb1", "k_product8_flowILi1ELb0"):
+        code = [line.split(";")[0].strip() for line in function(text, variant).split("\n")]
+        code = [line for line in code if line]
+        stores = [i for i, line in enumerate(code) if line.startswith("buffer_store")]
+        assert len(stores) == 32
+        assert not [line for line in code[stores[0]:stores[-1]] if line.startswith((".LBB", "s_cbranch", "s_branch", "scratch", "global"))]
+        assert len([line for line in code if line.startswith("v_mfma")]) == 2 * 64
+        assert len([line for line in code if line.startswith("buffer_load") and "lds" in line]) == 36 + 2 * 18
+        assert not [line for line in code if line.startswith(("scratch", "global_load", "flat_"))]
