@@ -59,21 +59,26 @@ class RMSNorm:
         # (a token's norm takes 3 us on the device: the common case is looked at as a whole, anything else piece by piece)
         n, rows = self.n, x.shape[0]
         dense, ldr, ldh, ldy = (rows, n), n, n, n
-        if x.dtype is self.dtype and x.shape == dense and x.is_contiguous() and x.get_device() == self._index:
-            ldx = n
-        else:
-            ldx = rows_of(x, n, (self.dtype,), self.device, "x")
+        whole = x.dtype is self.dtype and x.shape == dense and x.is_contiguous() and x.get_device() == self._index
+        ldx = n if whole else rows_of(x, n, (self.dtype,), self.device, "x")
         if weight is not None and not (weight.dtype is self.weight_dtype and weight.shape == (n,) and weight.is_contiguous() and weight.get_device() == self._index):
             self._weight(weight)
         if residual is None:
             if h is not None:
                 raise ValueError("h is x where there is no residual")
         else:
-            if not (residual.dtype is self.residual_dtype and residual.shape == dense and residual.is_contiguous() and residual.get_device() == self._index):
+            if residual.dtype is self.residual_dtype and residual.shape == dense and residual.is_contiguous() and residual.get_device() == self._index:
+                if h is None:
+                    h = torch.empty_like(residual)
+            else:
                 residual, ldr = self._like(residual, rows, self.residual_dtype, "residual")
-            h, ldh = self._like(h, rows, self.residual_dtype, "h")
+            if h is None or h.shape != dense or h.dtype is not self.residual_dtype or not h.is_contiguous() or h.get_device() != self._index:
+                h, ldh = self._like(h, rows, self.residual_dtype, "h")
         if want_y:
-            y, ldy = self._like(y, rows, self.dtype, "out")
+            if y is None and whole:
+                y = torch.empty_like(x)
+            else:
+                y, ldy = self._like(y, rows, self.dtype, "out")
         m8, data, ld, scales, ld_scales, code = None, None, 0, None, 0, 0
         if format is not None:
             code = format_of(format)
