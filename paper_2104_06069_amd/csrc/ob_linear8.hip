@@ -32,10 +32,10 @@ constexpr int64_t MOST = (int64_t)1 << 22;      // rows, columns and distances b
 template <int KIND>
 using Tile8 = std::conditional_t<KIND == W256, Shape<256, 256, 64, 2, 4>, std::conditional_t<KIND == W128, Shape<128, 128, 64, 2, 2>, Shape<64, 64, 64, 2, 2, 3>>>;
 
-template <int FORMAT, bool BF>
+template <int FORMAT, int OUT>
 ob_status launch_flow(ob_linear8_ctx* ctx, const Product8Args& p, hipStream_t s) {
   const int64_t tiles = (int64_t)((p.a.rows + 255) / 256) * ((p.b.rows + 255) / 256);
-  hipLaunchKernelGGL((k_product8_flow<FORMAT, BF>), dim3((unsigned)std::min<int64_t>((tiles + 7) / 8 * 8, CUS8)), dim3(256), (Flow8<FORMAT, BF>::LDS_BYTES), s, p);
+  hipLaunchKernelGGL((k_product8_flow<FORMAT, OUT>), dim3((unsigned)std::min<int64_t>((tiles + 7) / 8 * 8, CUS8)), dim3(256), (Flow8<FORMAT, OUT>::LDS_BYTES), s, p);
   return hip_ok(ctx, hipGetLastError(), "k_product8_flow") ? OB_OK : OB_ERR_HIP;
 }
 
@@ -63,6 +63,17 @@ auto with_product(int kind, int format, bool wide, F f) {
   return format == OB_E4M3 ? with_format(std::integral_constant<int, E4M3>{}) : with_format(std::integral_constant<int, E5M2>{});
 }
 
+// f(format, type of the results)
+template <class F>
+auto with_flow(int format, int out, F f) {
+  const auto with_out = [&](auto format) {
+    if (out == OB_F32) return f(format, std::integral_constant<int, F32>{});
+    if (out == OB_F16) return f(format, std::integral_constant<int, F16>{});
+    return f(format, std::integral_constant<int, BF16>{});
+  };
+  return format == OB_E4M3 ? with_out(std::integral_constant<int, E4M3>{}) : with_out(std::integral_constant<int, E5M2>{});
+}
+
 hipError_t allow_products() {
   hipError_t e = hipSuccess;
   for (int kind = 0; kind < KINDS8; ++kind)
@@ -70,13 +81,9 @@ hipError_t allow_products() {
       for (const bool wide : {false, true})
         if (e == hipSuccess)
           e = with_product(kind, format, wide, [](auto k, auto f, auto w) { return allow_lds(k_product8<Tile8<k>, f, w>, Product8<Tile8<k>, f, w>::LDS_BYTES); });
-  const auto flow = [&](auto format, auto bf) {
-    if (e == hipSuccess) e = allow_lds(k_product8_flow<format, bf>, Flow8<format, bf>::LDS_BYTES);
-  };
-  flow(std::integral_constant<int, E4M3>{}, std::true_type{});
-  flow(std::integral_constant<int, E4M3>{}, std::false_type{});
-  flow(std::integral_constant<int, E5M2>{}, std::true_type{});
-  flow(std::integral_constant<int, E5M2>{}, std::false_type{});
+  for (const int format : {E4M3, E5M2})
+    for (const int out : {F32, F16, BF16})
+      if (e == hipSuccess) e = with_flow(format, out, [](auto f, auto o) { return allow_lds(k_product8_flow<f, o>, Flow8<f, o>::LDS_BYTES); });
   return e;
 }
 
@@ -133,13 +140,10 @@ ob_status product(ob_linear8_ctx* ctx, const Given& a, int format, const Given& 
     else launch_few<false>(f, NONE, s);
     return hip_ok(ctx, hipGetLastError(), "k_product8_few") ? OB_OK : OB_ERR_HIP;
   }
-  const bool wide = out_dtype == OB_F32, eights = cols % 8 == 0 && ldo % 8 == 0 && !off(out, 16) && ldo <= ((int64_t)1 << 21);
-  const Plan8 plan = plan8(rows, cols, p.slabs, wide, !wide && eights && p.slabs >= 2);
+  const bool wide = out_dtype == OB_F32, eights = cols % 8 == 0 && ldo % 8 == 0 && !off(out, 16) && ldo <= ((int64_t)1 << 20);
+  const Plan8 plan = plan8(rows, cols, p.slabs, wide, eights && !accumulate && p.slabs >= 2);
   p.parts = plan.parts;
-  if (plan.kind == FLOW256) {
-    if (format == OB_E4M3) return out_dtype == OB_BF16 ? launch_flow<E4M3, true>(ctx, p, s) : launch_flow<E4M3, false>(ctx, p, s);
-    return out_dtype == OB_BF16 ? launch_flow<E5M2, true>(ctx, p, s) : launch_flow<E5M2, false>(ctx, p, s);
-  }
+  if (plan.kind == FLOW256) return with_flow(format, out_dtype, [&](auto f, auto o) { return launch_flow<f, o>(ctx, p, s); });
   return with_product(plan.kind, format, wide, [&](auto k, auto f, auto w) { return launch_product<Tile8<k>, f, w>(ctx, p, s); });
 }
 

@@ -158,11 +158,11 @@ __global__ __launch_bounds__(S::NT, 2) void k_product8(Product8Args p) {
 }
 
 // Workgroups that stay (Flow8): tiles id, id + gridDim.x, ..
-template <int FORMAT, bool BF>
+template <int FORMAT, int OUT>
 __global__ __launch_bounds__(256, 1) void k_product8_flow(Product8Args p) {
   const int nm = (p.a.rows + 255) / 256, nn = (p.b.rows + 255) / 256, tiles = nm * nn, per = (tiles + 7) / 8;
   int id = blockIdx.x;
-  Flow8<FORMAT, BF>::run(p.a, p.b, p.slabs, p.out, p.ldo, reinterpret_cast<uint8_t*>(lds_of_product8), [&](int* r, int* c) {
+  Flow8<FORMAT, OUT>::run(p.a, p.b, p.slabs, p.out, p.ldo, reinterpret_cast<uint8_t*>(lds_of_product8), [&](int* r, int* c) {
     for (*r = *c = -1; id >> 3 < per; id += gridDim.x) {
       const int t = tile_of_workgroup(id, tiles);
       if (t < 0) continue;

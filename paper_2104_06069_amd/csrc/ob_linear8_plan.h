@@ -12,7 +12,7 @@ constexpr int CUS8 = 256;                              // of an MI355X
 constexpr int64_t WORKSPACE8 = (int64_t)32 << 20;      // bytes of partial sums
 
 // Tiles of 256 x 256 (eight wavefronts, one workgroup on a CU), 128 x 128 and 64 x 64 (four).  FLOW256: 256 x 256 by workgroups that stay
-// (Flow8), for 16-bit results that it can store.
+// (Flow8), for results that it can store.
 enum { W256, W128, W64, KINDS8, FLOW256 = KINDS8 };
 constexpr int side8(int kind) { return kind == W256 || kind == FLOW256 ? 256 : kind == W128 ? 128 : 64; }
 
@@ -26,8 +26,12 @@ struct Rate8 {
 constexpr Rate8 RATES8[2][KINDS8] = {{{1, 5.3, 1.80, 1.60}, {2, 3.8, 1.00, 0.65}, {3, 3.8, 0.55, 0.32}},
                                      {{1, 8.3, 3.30, 2.82}, {2, 4.7, 1.75, 1.00}, {3, 3.5, 0.89, 0.53}}};
 inline double tiles_time8(int kind, bool wide, double tiles, double slabs) {
-  // (a tile after the other: 16384 x 8192 by 2048 226 us, 8192^3 417 us; 32 tiles alone, 2048 deep, 23.7 us)
-  if (kind == FLOW256) return 6.0 + std::ceil(tiles / CUS8) * (1.9 + slabs * (1.1 + 0.48 * std::min(tiles / CUS8, 1.0)));
+  // (a tile after the other: 16384 x 8192 by 2048 226 us, 8192^3 417 us; 32 tiles alone, 2048 deep, 23.7 us; binary32 results: 8192 x 2048 by
+  // 32768 675 us, 32768 x 8192 by 2048 800, alone 47.2)
+  if (kind == FLOW256) {
+    const double full = std::min(tiles / CUS8, 1.0), rounds = std::ceil(tiles / CUS8);
+    return wide ? 8.0 + rounds * (8.0 + slabs * (2.26 + 0.35 * full)) : 6.0 + rounds * (1.9 + slabs * (1.1 + 0.48 * full));
+  }
   const Rate8& r = RATES8[wide][kind];
   const double a_cu = std::ceil(tiles / CUS8), rounds = std::floor(a_cu / r.per_cu), rest = a_cu - rounds * r.per_cu;
   const double last = rest > 0 ? r.fixed + slabs * (r.one + (r.all - r.one) * (rest - 1) / std::max(r.per_cu - 1, 1)) : 0.0;

@@ -232,7 +232,7 @@ struct Product8 {
   }
 };
 
-// Many tiles of 256 x 256, 16-bit results of adjacent eights, K of two slabs or more: workgroups that stay, one on a CU, and go from tile to
+// Many tiles of 256 x 256, results of adjacent eights, K of two slabs or more: workgroups that stay, one on a CU, and go from tile to
 // tile without a pause in their loads.  A wavefront has a SIMD for itself and 128 x 128 of a tile.  It goes through its columns'
 // fragments one after the other, with all of its rows': beside the products of one column it reads the next column's operand from LDS, and
 // beside those of the last one, row by row as they are done with, the next slab's rows.  So A's part of a slab is done with when its
@@ -241,15 +241,20 @@ struct Product8 {
 // columns.  Each is waited for a slab and a half after that, at the P or Q before it is read.  Loads are spread over the products: a
 // wavefront that waits for its turn at the CU's loads issues no products (all of a slab's at once: 56 cycles a product in place of 44).
 // Results go out while the next tile's products run: nothing waits for them but their own turn in the count of loads.
-template <int FORMAT, bool BF>
+//   16-bit results   8192^3 in 417 us, 2.63 PFLOP/s (the library's product with one scale for each matrix: 2.62 to 2.71); 16384 x 8192 by 2048 226 us
+//   binary32         a row's operand is made bfloat16 once a slab, a column's once a column: 8192 x 2048 by 32768 in 675 us, 1.63 PFLOP/s (the
+//                    library's bfloat16 product at 8192^3: 1.31); with two rows' products in turn, which need more registers, 730
+template <int FORMAT, int OUT>
 struct Flow8 {
+  static constexpr bool WIDE = OUT == F32;
   static constexpr int BM = 256, BN = 256, NT = 256, FM = 8, FN = 8;
   using A = Rows8<BM, NT>;
   using B = Rows8<BN, NT>;
   static constexpr int SCALES = (BM + BN) * BLOCK8, STAGE = SCALES + (BM + BN) * 4;
   static constexpr int PITCH = 272, RESULTS = 16 * PITCH, LDS_BYTES = 2 * STAGE + 4 * RESULTS;      // (16 rows of 128 results a wavefront, four banks apart)
   static_assert(A::PER == 8 && B::PER == 8, "the loads below");
-  static constexpr int STORES = FM * 4;      // of a tile, whatever part of it exists
+  static constexpr int STORES = WIDE ? FM * FN : FM * 4;      // of a tile, whatever part of it exists
+  static constexpr int BEHIND = STORES < 45 ? STORES : 45;    // (a count of loads goes up to 63)
 
   struct Loads {      // of a tile, by a wavefront
     A a;
@@ -295,8 +300,6 @@ struct Flow8 {
       to = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
       e = *(base + (s + SCALES + row * 4 + (slab & 3)) + f * 64);
     };
-    v8i fa[FM], fb[2];
-    int ea[FM], eb[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
 #pragma unroll
@@ -306,16 +309,41 @@ struct Flow8 {
     }
     loads_done();
     group_barrier();
+    // Operands: WIDE, made bfloat16 once for a slab (A) and for a column (B), from what was read two rows of products, or a column, before
+    constexpr int RAW_A = WIDE ? 3 : FM;
+    v8i fa[RAW_A], fb[2];
+    int ea[RAW_A], eb[2];
+    v8s wa[WIDE ? FM : 1][4], wb[WIDE ? 2 : 1][4];
+    const auto widen_a = [&](int i) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) wa[WIDE ? i : 0][k] = widened<FORMAT>(fa[i % RAW_A][2 * k], fa[i % RAW_A][2 * k + 1], scale_value(ea[i % RAW_A]));
+    };
+    const auto widen_b = [&](int j, int k) { wb[WIDE ? j & 1 : 0][k] = widened<E4M3>(fb[j & 1][2 * k], fb[j & 1][2 * k + 1], scale_value(eb[j & 1])); };
+    const auto multiply = [&](int i, int j, v4f& acc) {
+      if constexpr (!WIDE) {
+        acc = mma8<FORMAT>(fb[j & 1], eb[j & 1], fa[i], ea[i], acc);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) acc = mma<true>(wb[j & 1][k], wa[i][k], acc);
+      }
+    };
     read(b_lo, b_hi, row_b, 0, 0, 0, fb[0], eb[0]);
 #pragma unroll
-    for (int i = 0; i < FM; ++i) read(a_lo, a_hi, row_a, 0, i, 0, fa[i], ea[i]);
+    for (int i = 0; i < FM; ++i) {
+      read(a_lo, a_hi, row_a, 0, i, 0, fa[i % RAW_A], ea[i % RAW_A]);
+      if (WIDE && i < FM - 2) widen_a(i);
+    }
+    if constexpr (WIDE) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) widen_b(0, k);
+    }
     int stage = 0;
     while (true) {
       v4f acc[FM][FN] = {};
       next(&r1, &c1);
       // AFTER: of a tile's first slab, behind the stores of the tile before (before the first tile everything has been waited for)
       const auto slab = [&](int t, auto after) {
-        constexpr int BEHIND = decltype(after)::value ? STORES : 0;
+        constexpr int MORE = decltype(after)::value ? BEHIND : 0;
         if (t + 2 == n && r1 >= 0) loads.aim(oa, ob, r1, c1, tid);
         const int one = t + 1 < n ? t + 1 : 0, two = t + 2 < n ? t + 2 : t + 2 - n;      // the slabs after this one, in their tile
         uint8_t* const here = lds + stage * STAGE;
@@ -323,11 +351,11 @@ struct Flow8 {
         for (int j = 0; j < FN; ++j) {
           const bool last = j == FN - 1;
           if (j == 3) {
-            loads_left<18 + BEHIND>();      // (this slab's P: behind it the next slab's Q and P)
+            loads_left<18 + MORE>();      // (this slab's P: behind it the next slab's Q and P)
             group_barrier();
           }
           if (last) {
-            loads_left<16 + BEHIND>();      // (the next slab's Q and scales: behind them its columns and the Q after that)
+            loads_left<16 + MORE>();      // (the next slab's Q and scales: behind them its columns and the Q after that)
             group_barrier();
           }
           if (last) read(b_lo, b_hi, row_b, stage ^ 1, 0, one, fb[0], eb[0]);
@@ -335,8 +363,11 @@ struct Flow8 {
           __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
           for (int i = 0; i < FM; ++i) {
-            acc[i][j] = mma8<FORMAT>(fb[j & 1], eb[j & 1], fa[i], ea[i], acc[i][j]);
-            if (last) read(a_lo, a_hi, row_a, stage ^ 1, i, one, fa[i], ea[i]);
+            if (WIDE && j == 0 && i < 2) widen_a(FM - 2 + i);
+            multiply(i, j, acc[i][j]);
+            if (WIDE && last && i >= 2) widen_a(i - 2);
+            if (last) read(a_lo, a_hi, row_a, stage ^ 1, i, one, fa[i % RAW_A], ea[i % RAW_A]);
+            if (WIDE && i >= 4) widen_b(j + 1, i - 4);
             if (j >= 3 && j < 7 && i % 3 == 0) loads.at_q((j - 3) * 3 + i / 3, two, here, wave);
             if (last && i < 6) loads.at_p(i, two, here, wave);
             __builtin_amdgcn_sched_barrier(0);
@@ -362,6 +393,20 @@ struct Flow8 {
                                                int lane) {
     asm volatile("" : "+v"(lane));      // (offsets are made here, and not held through the products)
     const int high = min(rows - r0, BM), wide = min(cols - c0, BN);
+    if constexpr (WIDE) {
+      const Buffer to = buffer_of(static_cast<uint8_t*>(out) + (r0 * ldo + c0) * 4, ((high - 1) * ldo + wide) * 4);
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+          v4f v = acc[i][j];
+          asm volatile("" : "+a"(v)::"memory");
+          const int r = wm * 128 + i * 16 + (lane & 15), c = wn * 128 + j * 16 + (lane >> 4) * 4;
+          const int at = r < high && c < wide ? (r * (int)ldo + c) * 4 : 0x7ffffff0;
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(unsigned __attribute__((ext_vector_type(4))), v), to, at, 0, 0);
+        }
+      return;
+    }
     const Buffer to = buffer_of(static_cast<uint8_t*>(out) + (r0 * ldo + c0) * 2, ((high - 1) * ldo + wide) * 2);
     const auto mine = in_lds<uint8_t>(own);
 #pragma unroll
@@ -372,7 +417,7 @@ struct Flow8 {
         asm volatile("" : "+a"(v)::"memory");      // (from where the products left it, and not before its turn: there are registers for sixteen rows)
         v4h h;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) h[e] = to_bits(v[e], BF);
+        for (int e = 0; e < 4; ++e) h[e] = to_bits(v[e], OUT == BF16);
         *(__attribute__((address_space(3))) v2i*)(mine + (lane & 15) * PITCH + j * 32 + (lane >> 4) * 8) = __builtin_bit_cast(v2i, h);
       }
 #pragma unroll

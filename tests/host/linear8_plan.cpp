@@ -18,7 +18,7 @@ int main() {
       std::printf("few %d %d\n", p.columns, p.waves);
       continue;
     }
-    const Plan8 p = plan8(rows, cols, slabs, wide, !wide && eights && slabs >= 2);
+    const Plan8 p = plan8(rows, cols, slabs, wide, eights && slabs >= 2);
     if (p.parts < 1 || p.parts > (slabs > 1 ? slabs : 1) || (p.parts > 1 && (p.kind == FLOW256 || p.parts * rows * cols * 4 > WORKSPACE8))) abort();
     std::printf("%s %d\n", names[p.kind], p.parts);
   }

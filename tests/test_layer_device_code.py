@@ -34,18 +34,18 @@ def function(text, part):
     return text[start.end():text.index(".Lfunc_end", start.end())]
 
 
-def test_stores_are_counted_with_the_loads(text):
-    """k_product8_flow waits for loads by how many loads and stores are behind them: a tile's 32 stores are stores whatever part of the tile exists,
-    in one piece without branches, and its loop has 18 loads a slab."""
+@pytest.mark.parametrize("variant,stores,products", [("ILi0ELi2", 32, 64), ("ILi1ELi1", 32, 64), ("ILi0ELi0", 64, 256), ("ILi1ELi0", 64, 256)])
+def test_stores_are_counted_with_the_loads(text, variant, stores, products):
+    """k_product8_flow waits for loads by how many loads and stores are behind them: a tile's stores are as many whatever part of the tile exists, in
+    one piece without branches, its loop has 18 loads a slab, and nothing else goes to memory."""
     name, text = text
     if name != "ob_linear8":
         pytest.skip("of the products")
-    for variant in ("k_product8_flowILi0ELb1", "k_product8_flowILi1ELb0"):
-        code = [line.split(";")[0].strip() for line in function(text, variant).split("\n")]
-        code = [line for line in code if line]
-        stores = [i for i, line in enumerate(code) if line.startswith("buffer_store")]
-        assert len(stores) == 32
-        assert not [line for line in code[stores[0]:stores[-1]] if line.startswith((".LBB", "s_cbranch", "s_branch", "scratch", "global"))]
-        assert len([line for line in code if line.startswith("v_mfma")]) == 2 * 64
-        assert len([line for line in code if line.startswith("buffer_load") and "lds" in line]) == 36 + 2 * 18
-        assert not [line for line in code if line.startswith(("scratch", "global_load", "flat_"))]
+    code = [line.split(";")[0].strip() for line in function(text, "k_product8_flow" + variant).split("\n")]
+    code = [line for line in code if line]
+    at = [i for i, line in enumerate(code) if line.startswith("buffer_store")]
+    assert len(at) == stores
+    assert not [line for line in code[at[0]:at[-1]] if line.startswith((".LBB", "s_cbranch", "s_branch", "buffer_load"))]
+    assert len([line for line in code if line.startswith("v_mfma")]) == 2 * products
+    assert len([line for line in code if line.startswith("buffer_load") and "lds" in line]) == 36 + 2 * 18
+    assert not [line for line in code if line.startswith(("scratch", "global_", "flat_"))]
