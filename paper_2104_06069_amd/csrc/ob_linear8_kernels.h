@@ -25,11 +25,11 @@ __device__ __forceinline__ v2i bytes_before(v2i q, int left) {
 
 // A workgroup takes 128 x 128 numbers, a thread eight adjacent rows by eight adjacent columns of them: a row's block is that of
 // sixteen adjacent lanes, a column's that of sixteen lanes one from each group of those, four in a wavefront.  The transposed
-// bytes are turned in LDS, so that both results go out 128 bytes of a row at a time.
+// bytes are turned in LDS, so that both results go out 128 bytes of a row at a time; there the 16-byte pieces of a column are permuted by the
+// column's number, or the lanes of a row would meet in one bank.
 template <int DTYPE, bool SQUARE>
 __global__ __launch_bounds__(256) void k_quantize8(QuantizeArgs p) {
-  constexpr int PITCH = BLOCK8 + 16;
-  __shared__ __align__(16) uint8_t turned[BLOCK8 * PITCH];
+  __shared__ __align__(16) uint8_t turned[BLOCK8 * BLOCK8];
   __shared__ unsigned most_of[4][BLOCK8];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, rg = tid >> 4, cg = tid & 15;
   const int r0 = blockIdx.y * BLOCK8, c0 = blockIdx.x * BLOCK8, left = p.cols - c0 - cg * 8, below = p.rows - r0 - rg * 8;
@@ -97,7 +97,7 @@ __global__ __launch_bounds__(256) void k_quantize8(QuantizeArgs p) {
       float w[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) w[i] = v[i][e];
-      *reinterpret_cast<v2i*>(turned + (cg * 8 + e) * PITCH + rg * 8) = bytes_before(bytes8(w, inverse_scale(byte), p.format_t), below);
+      *reinterpret_cast<v2i*>(turned + (cg * 8 + e) * BLOCK8 + (rg / 2 ^ (cg & 7)) * 16 + rg % 2 * 8) = bytes_before(bytes8(w, inverse_scale(byte), p.format_t), below);
       if (rg == 0 && e < left) {
         const int64_t col = c0 + cg * 8 + e;
         if (!SQUARE) p.scales_t[col * p.ld_scales_t + blockIdx.y] = (uint8_t)byte;
@@ -107,8 +107,9 @@ __global__ __launch_bounds__(256) void k_quantize8(QuantizeArgs p) {
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int col = j * 32 + tid / 8, at = tid % 8 * 16;
-      if (c0 + col < p.cols) *reinterpret_cast<v4i*>(p.data_t + (int64_t)(c0 + col) * p.ld_t + r0 + at) = *reinterpret_cast<const v4i*>(turned + col * PITCH + at);
+      const int col = j * 32 + tid / 8, piece = tid % 8;
+      if (c0 + col < p.cols)
+        *reinterpret_cast<v4i*>(p.data_t + (int64_t)(c0 + col) * p.ld_t + r0 + piece * 16) = *reinterpret_cast<const v4i*>(turned + col * BLOCK8 + (piece ^ (col >> 3 & 7)) * 16);
     }
   }
 }
