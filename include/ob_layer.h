@@ -45,7 +45,8 @@ enum { OB_BLOCK_ROWS = 0, OB_BLOCK_SQUARE = 1 };
  *   backward   g = dy weight, xhat = h rstd
  *              dh = dres + rstd (g - xhat mean(g xhat))          (dres NULL: 0), rounded to h's type
  *              dweight = sum over rows of dy xhat                 (+= with accumulate)
- * on rows of n numbers, in binary32, with y and xhat those of the rounded h.  dh is the gradient of x and of the residual.
+ * on rows of n numbers, in binary32, with y and xhat those of the rounded h.  dh is the gradient of x and of the residual.  A row of zeros with
+ * eps = 0 gives NaNs; a row with an infinity has rstd 0, zeros, and a NaN where the infinity was; one with a NaN gives NaNs.
  */
 typedef struct ob_norm_ctx ob_norm_ctx; /* opaque */
 
@@ -132,8 +133,8 @@ ob_status ob_linear8_weight_grad(ob_linear8_ctx* ctx, const void* dy_t, int64_t 
 typedef struct ob_clip_ctx ob_clip_ctx; /* opaque */
 
 typedef struct ob_clip_config {
-  int64_t num_layers;            /* >= 1 */
-  const int64_t* layer_offsets;  /* HOST, copied; up to 2^40 elements */
+  int64_t num_layers;            /* 1 .. 2^22 */
+  const int64_t* layer_offsets;  /* HOST, copied; up to 2^35 elements */
   float eps;                     /* >= 0, finite */
   float grad_scale;              /* > 0, finite: the inverse loss scale */
 } ob_clip_config;

@@ -93,13 +93,13 @@ ob_status ob_clip_create(const ob_clip_config* cfg, ob_clip_ctx** out) {
   if (!cfg || !out) return OB_ERR_NULL;
   *out = nullptr;
   if (!cfg->layer_offsets) return OB_ERR_NULL;
-  if (cfg->num_layers < 1 || cfg->num_layers > ((int64_t)1 << 28) || !(cfg->eps >= 0) || !std::isfinite(cfg->eps) || !(cfg->grad_scale > 0) ||
+  if (cfg->num_layers < 1 || cfg->num_layers > ((int64_t)1 << 22) || !(cfg->eps >= 0) || !std::isfinite(cfg->eps) || !(cfg->grad_scale > 0) ||
       !std::isfinite(cfg->grad_scale) || cfg->layer_offsets[0] != 0)
     return OB_ERR_ARG;
   for (int64_t l = 0; l < cfg->num_layers; ++l)
     if (cfg->layer_offsets[l + 1] < cfg->layer_offsets[l]) return OB_ERR_ARG;
   const int64_t n = cfg->layer_offsets[cfg->num_layers];
-  if (n > ((int64_t)1 << 40)) return OB_ERR_ARG;
+  if (n > ((int64_t)1 << 35)) return OB_ERR_ARG;
   ob_clip_ctx* ctx = nullptr;
   try {
     ctx = new ob_clip_ctx();
@@ -107,9 +107,10 @@ ob_status ob_clip_create(const ob_clip_config* cfg, ob_clip_ctx** out) {
     ctx->layers = (int)cfg->num_layers;
     ctx->eps = cfg->eps;
     ctx->grad_scale = cfg->grad_scale;
-    // Segments of 2048 elements, or twice as many as long as there would be over 4096 of them
+    // Segments of 2048 elements, or twice as many as long as there would be over 4096 of them; from 32768 elements on, over 2^22 (a grid
+    // counts its threads in 32 bits, and a tensor's last segment may be a short one)
     int64_t span = 2048;
-    while (span < (1 << 30) && (span < 32768 ? n / span > 4096 : n / span > ((int64_t)1 << 26))) span *= 2;
+    while (n / span > (span < 32768 ? 4096 : (int64_t)1 << 22)) span *= 2;
     std::vector<Segment> segments;
     std::vector<int> first;
     first.reserve(cfg->num_layers + 1);

@@ -42,7 +42,7 @@ ob_status launch_flow(ob_linear8_ctx* ctx, const Product8Args& p, hipStream_t s)
 template <class S, int FORMAT, bool WIDE>
 ob_status launch_product(ob_linear8_ctx* ctx, const Product8Args& p, hipStream_t s) {
   const int64_t tiles = (int64_t)((p.a.rows + S::BM - 1) / S::BM) * ((p.b.rows + S::BN - 1) / S::BN) * p.parts;
-  if (tiles > 0x7ffffff0) return OB_ERR_SIZE;
+  if ((tiles + 8) * S::NT > 0x7fffffff) return OB_ERR_SIZE;      // (a grid counts its threads in 32 bits)
   hipLaunchKernelGGL((k_product8<S, FORMAT, WIDE>), dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(S::NT), (Product8<S, FORMAT, WIDE>::LDS_BYTES), s, p);
   if (p.parts > 1) {
     const int64_t fours = (int64_t)p.a.rows * ((p.b.rows + 3) / 4);

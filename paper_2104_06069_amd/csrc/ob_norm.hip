@@ -118,10 +118,23 @@ ob_status ob_norm_forward(ob_norm_ctx* ctx, const void* x, int64_t ldx, const vo
     return OB_ERR_ALIGN;
   NormArgs p{x, residual, weight, h, y, static_cast<uint8_t*>(data), static_cast<uint8_t*>(scales), rstd, ldx, ldr, ldh, ldy, ld, ld_scales,
              (int)rows, (int)c.n, c.weight_dtype, format, c.eps};
+  const auto part = [](auto* from, int64_t rows, int64_t ld, int size) { return from ? reinterpret_cast<decltype(from)>((uintptr_t)from + rows * ld * size) : nullptr; };
   return with_types(c, [&](auto X, auto H) {
     return with_forward_size(c.n, [&](auto T, auto C) {
       constexpr int NT = T < 256 ? 256 : T;
-      hipLaunchKernelGGL((k_norm_forward<X, H, T, C>), dim3((unsigned)((rows + NT / T - 1) / (NT / T))), dim3(NT), 0, static_cast<hipStream_t>(hip_stream), p);
+      constexpr int64_t MOST = ((int64_t)1 << 31) / T;      // rows of a launch: a grid counts its threads in 32 bits
+      for (int64_t first = 0; first < rows; first += MOST) {
+        NormArgs q = p;
+        q.rows = (int)std::min(MOST, rows - first);
+        q.x = part(p.x, first, ldx, elem_size(c.dtype));
+        q.residual = part(p.residual, first, ldr, elem_size(c.res_dtype));
+        q.h = part(p.h, first, ldh, elem_size(c.res_dtype));
+        q.y = part(p.y, first, ldy, elem_size(c.dtype));
+        q.data = part(p.data, first, ld, 1);
+        q.scales = part(p.scales, first, ld_scales, 1);
+        q.rstd = part(p.rstd, first, 1, 4);
+        hipLaunchKernelGGL((k_norm_forward<X, H, T, C>), dim3((unsigned)((q.rows + NT / T - 1) / (NT / T))), dim3(NT), 0, static_cast<hipStream_t>(hip_stream), q);
+      }
       return hip_ok(ctx, hipGetLastError(), "k_norm_forward") ? OB_OK : OB_ERR_HIP;
     });
   });

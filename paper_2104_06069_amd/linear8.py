@@ -73,6 +73,8 @@ class Linear8:
 
     def _quantize(self, t, what, width, rows_format=None, cols_format=None, square=False):
         """-> (t, t transposed) in the given formats, None where that is None"""
+        if not isinstance(t, torch.Tensor):
+            raise ValueError(f"{what}: a tensor, not {type(t).__name__}")
         ld, (rows, cols) = self._rows(t, width, what), t.shape
         m = None if rows_format is None else Matrix8(rows, cols, rows_format, self.device, square)
         mt = None if cols_format is None else Matrix8(cols, rows, cols_format, self.device, square)
@@ -85,8 +87,8 @@ class Linear8:
     def quantize(self, t, format=_E4M3):
         """t [rows, any width] in 8 bits, a scale for each 128 columns of a row."""
         format_of(format)
-        if t.dim() != 2:
-            raise ValueError("t: [rows, width]")
+        if not isinstance(t, torch.Tensor) or t.dim() != 2:
+            raise ValueError("t: a [rows, width] tensor")
         return self._quantize(t, "t", t.shape[1], rows_format=format)[0]
 
     def quantize_weight(self, w):
@@ -111,8 +113,11 @@ class Linear8:
         return out, ld
 
     def _weight(self, w8):
-        if not isinstance(w8, Weight8) or (w8.w.rows, w8.w.cols) != (self.n, self.k) or w8.w.device != self.device:
-            raise ValueError(f"w8: the Weight8 of a [{self.n}, {self.k}] tensor on {self.device}")
+        if isinstance(w8, Weight8):
+            w, t = w8
+            if w.rows == t.cols == self.n and w.cols == t.rows == self.k and w.square and t.square and w.dtype is t.dtype is _E4M3 and w.device == t.device == self.device:
+                return
+        raise ValueError(f"w8: the Weight8 of a [{self.n}, {self.k}] tensor on {self.device}")
 
     def forward(self, x, w8, out=None, out_dtype=None):
         """y = x W^T; x is quantised to e4m3 unless it is a Matrix8."""
@@ -143,8 +148,8 @@ class Linear8:
         return self._weight_grad(x, dy, self._quantize(dy, "dy", self.n, cols_format=self.grad_format)[1], out, out_dtype, accumulate)
 
     def _weight_grad(self, x, dy, dy_t, out, out_dtype, accumulate):
-        if x.shape[0] != dy.shape[0]:
-            raise ValueError("x and dy: one row each")
+        if not isinstance(x, torch.Tensor) or x.shape[:1] != dy.shape[:1]:
+            raise ValueError("x and dy: tensors of one row each")
         x_t = self._quantize(x, "x", self.k, cols_format=_E4M3)[1]
         if accumulate and out is None:
             raise ValueError("accumulate needs an out to add to")

@@ -226,6 +226,11 @@ def test_refusals():
            lambda: layer.weight_grad(x, dy[:4]), lambda: layer.weight_grad(x, dy, accumulate=True), lambda: layer.quantize(x[0]),
            lambda: layer.weight_grad(x, dy, out=torch.zeros(32, 64, device="cuda", dtype=BF), accumulate=True), lambda: op(64, 32, grad_format=BF),
            lambda: op(64, 32, dtype=torch.float64)]
+    from paper_2104_06069_amd.linear8 import Weight8
+    other = op(32, 64).quantize_weight(w.t().contiguous())
+    bad += [lambda: layer.weight_grad(x8, dy), lambda: layer.weight_grad(x, layer.quantize(dy)), lambda: layer.quantize(x8), lambda: layer.backward(x8, dy, w8),
+            lambda: layer.forward(x, Weight8(w8.w, w8.w)), lambda: layer.input_grad(dy, Weight8(w8.w, layer.quantize(w.t().contiguous()))),
+            lambda: layer.forward(x, Weight8(layer.quantize(w), w8.transposed)), lambda: layer.forward(x, other)]
     for k, call in enumerate(bad):
         with pytest.raises(ValueError):
             call()

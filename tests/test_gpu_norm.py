@@ -252,6 +252,26 @@ def test_offsets_beyond_32_bits():
     assert torch.equal(dh, ref)
 
 
+def test_more_rows_than_a_grid_has_threads_for():
+    """2^21 rows of 1024 threads are as many as a launch counts."""
+    n, rows = 4100, (1 << 21) + 5
+    x = torch.zeros(rows, n, device="cuda", dtype=BF)
+    x[:3], x[-9:] = normal(3, n, seed=1, dtype=BF), normal(9, n, seed=2, dtype=BF)
+    norm = op(n, dtype=BF)
+    y, _, rstd = norm.forward(x)
+    for part in (slice(0, 3), slice(rows - 9, rows)):
+        want, want_rstd = want_forward(x[part], None, 1e-6)
+        within(y[part], want, (2.0 ** -19 + HALF[BF]) * want.abs(), "y")
+        within(rstd[part], want_rstd[:, 0], 2.0 ** -20 * want_rstd[:, 0], "rstd")
+    assert (y[3:1000] == 0).all() and (y[rows - 1000:rows - 9] == 0).all()
+    del y
+    y8, _, _ = norm.forward8(x)
+    at = torch.arange(rows - 9, rows, device="cuda")
+    numbers = y8.buffer[(rows - 9) * y8.ld:rows * y8.ld].view(9, y8.ld)[:, :n].view(E4M3).cpu().double()
+    scales = y8.scales[at].cpu().double()
+    within(numbers * spread(scales, (9, n)), want, (2.0 ** -19 + 2.0 ** -4) * want.abs() + spread(scales, (9, n)) * 2.0 ** -10, "y in 8 bits")
+
+
 def test_refusals():
     norm = op(64, dtype=BF)
     x, w = torch.zeros(3, 64, device="cuda", dtype=BF), torch.ones(64, device="cuda")

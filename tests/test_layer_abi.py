@@ -62,7 +62,7 @@ def test_create_refuses(ob):
     for k, n, rows in ((0, 1, 1), (1, 0, 1), (1 << 21, 1, 1), (1, 1 << 21, 1), (1, 1, -1), (1, 1, (1 << 22) + 1)):
         assert L.ob_linear8_create(C.byref(ob.ObLinear8Config(k, n, rows)), C.byref(out)) == -2 and not out.value
     for offs, eps, scale in (([0, 5, 3], 0, 1), ([1, 5], 0, 1), ([0, 5], -1, 1), ([0, 5], nan, 1), ([0, 5], 0, 0), ([0, 5], 0, nan), ([0, 5], 0, inf),
-                             ([0, (1 << 40) + 1], 0, 1)):
+                             ([0, (1 << 35) + 1], 0, 1)):
         cfg = ob.ObClipConfig(len(offs) - 1, (C.c_int64 * len(offs))(*offs), eps, scale)
         assert L.ob_clip_create(C.byref(cfg), C.byref(out)) == -2 and not out.value, (offs, eps, scale)
     assert L.ob_clip_create(C.byref(ob.ObClipConfig(0, (C.c_int64 * 1)(0), 0, 1)), C.byref(out)) == -2
