@@ -66,8 +66,8 @@ ob_status with_backward_size(int64_t n, F f) {
 // rows that a workgroup of k_norm_backward has at a time
 int sets_of(int64_t n) { return n <= 1024 ? 8 : n <= 2048 ? 2 : 1; }
 // and workgroups of it, as many as the card runs at once (16384 x 2048 with 256 / 512 / 768 / 1024 of them: 81.4 / 62.3 / 57.9 / 68.9 us; 32768 x 1024,
-// where two wavefronts' registers less fit: 512 / 768: 61.8 / 74.4)
-int parts_of(int64_t n) { return n <= 512 || (n > 1024 && n <= 4096) ? 768 : 512; }
+// where two wavefronts' registers less fit: 512 / 768: 61.8 / 74.4; binary32 16384 x 2048: 113 / 136)
+int parts_of(int64_t n, bool f32) { return !f32 && (n <= 512 || (n > 1024 && n <= 4096)) ? 768 : 512; }
 
 bool rows_wrong(int64_t ld, int64_t n) { return ld < n || ld >= MOST_LD; }
 
@@ -85,7 +85,7 @@ ob_status ob_norm_create(const ob_norm_config* cfg, ob_norm_ctx** out) {
   if (!ctx) return OB_ERR_ARG;
   ctx->cfg = *cfg;
   hipError_t e = hipGetDevice(&ctx->device);
-  ctx->most_parts = parts_of(cfg->n);
+  ctx->most_parts = parts_of(cfg->n, cfg->dtype == OB_F32);
   ctx->bytes = (size_t)ctx->most_parts * cfg->n * sizeof(float);
   if (e == hipSuccess) e = hipMalloc(&ctx->d_partial, ctx->bytes);
   if (e != hipSuccess) {

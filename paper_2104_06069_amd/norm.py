@@ -27,7 +27,7 @@ class RMSNorm:
         self.ctx = None
         if dtype not in _OB_DTYPE or self.residual_dtype not in (dtype, torch.float32) or weight_dtype not in _OB_DTYPE:
             raise ValueError("types are torch.float32, torch.float16 and torch.bfloat16; the residual's is dtype or torch.float32")
-        self._index, self._call = torch.cuda.current_device(), ob.lib().ob_norm_forward
+        self._index, self._call, self._backward = torch.cuda.current_device(), ob.lib().ob_norm_forward, ob.lib().ob_norm_backward
         self.ctx = ob.ob_norm_create(self.n, _OB_DTYPE[dtype], _OB_DTYPE[self.residual_dtype], _OB_DTYPE[weight_dtype], eps)
 
     def close(self):
@@ -52,7 +52,7 @@ class RMSNorm:
         return t, ld
 
     def _weight(self, t):
-        if t is not None and (t.dtype != self.weight_dtype or tuple(t.shape) != (self.n,) or not t.is_contiguous() or t.device != self.device):
+        if t is not None and (t.dtype is not self.weight_dtype or t.shape != (self.n,) or not t.is_contiguous() or t.get_device() != self._index):
             raise ValueError(f"weight: {self.n} adjacent {self.weight_dtype} on {self.device}")
 
     def _forward(self, x, weight, residual, h, y, want_y, format):
@@ -61,8 +61,7 @@ class RMSNorm:
         dense, ldr, ldh, ldy = (rows, n), n, n, n
         whole = x.dtype is self.dtype and x.shape == dense and x.is_contiguous() and x.get_device() == self._index
         ldx = n if whole else rows_of(x, n, (self.dtype,), self.device, "x")
-        if weight is not None and not (weight.dtype is self.weight_dtype and weight.shape == (n,) and weight.is_contiguous() and weight.get_device() == self._index):
-            self._weight(weight)
+        self._weight(weight)
         if residual is None:
             if h is not None:
                 raise ValueError("h is x where there is no residual")
@@ -106,22 +105,33 @@ class RMSNorm:
     def backward(self, dy, h, rstd, weight=None, dres=None, dweight=None, accumulate=False, out=None):
         """-> (dh, dweight): the gradient of h, so of x and of the residual alike, and of the weight in float32 (into `dweight` if
         given; with accumulate, added to what it holds).  dres: the gradient that h has from elsewhere."""
-        lddy, rows = rows_of(dy, self.n, (self.dtype,), self.device, "dy"), dy.shape[0]
-        h, ldh = self._like(h, rows, self.residual_dtype, "h")
+        n, rows, index = self.n, dy.shape[0], self._index
+        dense, lddy, ldh, lddres, lddh = (rows, n), n, n, n, n
+        if not (dy.dtype is self.dtype and dy.shape == dense and dy.is_contiguous() and dy.get_device() == index):
+            lddy = rows_of(dy, n, (self.dtype,), self.device, "dy")
+        whole = h.dtype is self.residual_dtype and h.shape == dense and h.is_contiguous() and h.get_device() == index
+        if not whole:
+            h, ldh = self._like(h, rows, self.residual_dtype, "h")
         self._weight(weight)
-        if rstd.dtype != torch.float32 or tuple(rstd.shape) != (rows,) or not rstd.is_contiguous() or rstd.device != self.device:
+        if rstd.dtype is not torch.float32 or rstd.shape != (rows,) or not rstd.is_contiguous() or rstd.get_device() != index:
             raise ValueError(f"rstd: {rows} adjacent torch.float32 on {self.device}")
-        lddres = self.n
-        if dres is not None:
+        if dres is not None and not (dres.dtype is self.residual_dtype and dres.shape == dense and dres.is_contiguous() and dres.get_device() == index):
             dres, lddres = self._like(dres, rows, self.residual_dtype, "dres")
-        dh, lddh = self._like(out, rows, self.residual_dtype, "out")
+        if out is None and whole:
+            dh = torch.empty_like(h)
+        else:
+            dh, lddh = self._like(out, rows, self.residual_dtype, "out")
         if dweight is None:
             if accumulate:
                 raise ValueError("accumulate needs a dweight to add to")
-            dweight = torch.empty(self.n, device=self.device, dtype=torch.float32)
-        elif dweight.dtype != torch.float32 or tuple(dweight.shape) != (self.n,) or not dweight.is_contiguous() or dweight.device != self.device:
-            raise ValueError(f"dweight: {self.n} adjacent torch.float32 on {self.device}")
-        ob.ob_norm_backward(self.ctx, dy, lddy, h, ldh, rstd, weight, dres, lddres, rows, dh, lddh, dweight, accumulate, _current_stream(self.device))
+            dweight = torch.empty(n, device=self.device, dtype=torch.float32)
+        elif dweight.dtype is not torch.float32 or dweight.shape != (n,) or not dweight.is_contiguous() or dweight.get_device() != index:
+            raise ValueError(f"dweight: {n} adjacent torch.float32 on {self.device}")
+        status = self._backward(self.ctx, dy.data_ptr(), lddy, h.data_ptr(), ldh, rstd.data_ptr(), None if weight is None else weight.data_ptr(),
+                                None if dres is None else dres.data_ptr(), lddres, rows, dh.data_ptr(), lddh, dweight.data_ptr(), bool(accumulate),
+                                _current_stream(self.device))
+        if status:
+            raise ob.ObLambError(status, "ob_norm_backward", ob.lib().ob_norm_last_hip_error(self.ctx).decode())
         return dh, dweight
 
     def __call__(self, x, weight=None, residual=None):
