@@ -63,11 +63,12 @@ auto with_product(int kind, int format, bool wide, F f) {
   return format == OB_E4M3 ? with_format(std::integral_constant<int, E4M3>{}) : with_format(std::integral_constant<int, E5M2>{});
 }
 
-// f(format, type of the results)
+// f(format, type of the results, ADD_F32 among them)
 template <class F>
 auto with_flow(int format, int out, F f) {
   const auto with_out = [&](auto format) {
     if (out == OB_F32) return f(format, std::integral_constant<int, F32>{});
+    if (out == ADD_F32) return f(format, std::integral_constant<int, ADD_F32>{});
     if (out == OB_F16) return f(format, std::integral_constant<int, F16>{});
     return f(format, std::integral_constant<int, BF16>{});
   };
@@ -82,7 +83,7 @@ hipError_t allow_products() {
         if (e == hipSuccess)
           e = with_product(kind, format, wide, [](auto k, auto f, auto w) { return allow_lds(k_product8<Tile8<k>, f, w>, Product8<Tile8<k>, f, w>::LDS_BYTES); });
   for (const int format : {E4M3, E5M2})
-    for (const int out : {F32, F16, BF16})
+    for (const int out : {(int)F32, (int)F16, (int)BF16, ADD_F32})
       if (e == hipSuccess) e = with_flow(format, out, [](auto f, auto o) { return allow_lds(k_product8_flow<f, o>, Flow8<f, o>::LDS_BYTES); });
   return e;
 }
@@ -141,9 +142,9 @@ ob_status product(ob_linear8_ctx* ctx, const Given& a, int format, const Given& 
     return hip_ok(ctx, hipGetLastError(), "k_product8_few") ? OB_OK : OB_ERR_HIP;
   }
   const bool wide = out_dtype == OB_F32, eights = cols % 8 == 0 && ldo % 8 == 0 && !off(out, 16) && ldo <= ((int64_t)1 << 20);
-  const Plan8 plan = plan8(rows, cols, p.slabs, wide, eights && !accumulate && p.slabs >= 2);
+  const Plan8 plan = plan8(rows, cols, p.slabs, wide, eights && p.slabs >= 2);
   p.parts = plan.parts;
-  if (plan.kind == FLOW256) return with_flow(format, out_dtype, [&](auto f, auto o) { return launch_flow<f, o>(ctx, p, s); });
+  if (plan.kind == FLOW256) return with_flow(format, accumulate ? ADD_F32 : out_dtype, [&](auto f, auto o) { return launch_flow<f, o>(ctx, p, s); });
   return with_product(plan.kind, format, wide, [&](auto k, auto f, auto w) { return launch_product<Tile8<k>, f, w>(ctx, p, s); });
 }
 

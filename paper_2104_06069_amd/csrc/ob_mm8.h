@@ -244,9 +244,10 @@ struct Product8 {
 //   16-bit results   8192^3 in 417 us, 2.63 PFLOP/s (the library's product with one scale for each matrix: 2.62 to 2.71); 16384 x 8192 by 2048 226 us
 //   binary32         a row's operand is made bfloat16 once a slab, a column's once a column: 8192 x 2048 by 32768 in 675 us, 1.63 PFLOP/s (the
 //                    library's bfloat16 product at 8192^3: 1.31); with two rows' products in turn, which need more registers, 730
+constexpr int ADD_F32 = 3;      // of types of results: binary32, added to what is there
 template <int FORMAT, int OUT>
 struct Flow8 {
-  static constexpr bool WIDE = OUT == F32;
+  static constexpr bool WIDE = OUT == F32 || OUT == ADD_F32;
   static constexpr int BM = 256, BN = 256, NT = 256, FM = 8, FN = 8;
   using A = Rows8<BM, NT>;
   using B = Rows8<BN, NT>;
@@ -395,16 +396,25 @@ struct Flow8 {
     const int high = min(rows - r0, BM), wide = min(cols - c0, BN);
     if constexpr (WIDE) {
       const Buffer to = buffer_of(static_cast<uint8_t*>(out) + (r0 * ldo + c0) * 4, ((high - 1) * ldo + wide) * 4);
+      typedef unsigned v4u __attribute__((ext_vector_type(4)));
 #pragma unroll
-      for (int i = 0; i < FM; ++i)
+      for (int i = 0; i < FM; ++i) {
+        v4f old[FN];
+        int at[FN];
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+          const int r = wm * 128 + i * 16 + (lane & 15), c = wn * 128 + j * 16 + (lane >> 4) * 4;
+          at[j] = r < high && c < wide ? (r * (int)ldo + c) * 4 : 0x7ffffff0;
+          if constexpr (OUT == ADD_F32) old[j] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(to, at[j], 0, 0));
+        }
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
           v4f v = acc[i][j];
           asm volatile("" : "+a"(v)::"memory");
-          const int r = wm * 128 + i * 16 + (lane & 15), c = wn * 128 + j * 16 + (lane >> 4) * 4;
-          const int at = r < high && c < wide ? (r * (int)ldo + c) * 4 : 0x7ffffff0;
-          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(unsigned __attribute__((ext_vector_type(4))), v), to, at, 0, 0);
+          if constexpr (OUT == ADD_F32) v += old[j];
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, v), to, at[j], 0, 0);
         }
+      }
       return;
     }
     const Buffer to = buffer_of(static_cast<uint8_t*>(out) + (r0 * ldo + c0) * 2, ((high - 1) * ldo + wide) * 2);

@@ -280,3 +280,16 @@ def test_many_tiles(rows, k, n, dtype):
     assert (((got - want).abs() <= bound) | beyond).all()
     assert (got[~beyond] - want[~beyond]).norm() / want[~beyond].norm() <= HALF[dtype] + (2e-6 if dtype == F32 else 1e-4)
     assert torch.equal(layer.forward(x8, w8), y)
+
+
+@pytest.mark.parametrize("rows,k,n", [(2100, 4096, 4096), (2100, 4096, 8190), (2100, 4090, 4096), (1000, 200, 4096)])
+def test_accumulating_into_many_tiles(rows, k, n):
+    layer = op(k, n)
+    x, dy = numbers(rows, k, BF, 1), numbers(rows, n, BF, 2)
+    once = layer.weight_grad(x, dy)
+    flat = torch.randn(n * k + 16, device="cuda")
+    view, start = flat[8:8 + n * k].view(n, k), flat.clone()
+    layer.weight_grad(x, dy, out=view, accumulate=True)
+    assert torch.equal(view, start[8:8 + n * k].view(n, k) + once) and torch.equal(flat[:8], start[:8]) and torch.equal(flat[-8:], start[-8:])
+    layer.weight_grad(x, dy, out=view)
+    assert torch.equal(view, once)

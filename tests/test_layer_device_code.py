@@ -34,7 +34,7 @@ def function(text, part):
     return text[start.end():text.index(".Lfunc_end", start.end())]
 
 
-@pytest.mark.parametrize("variant,stores,products", [("ILi0ELi2", 32, 64), ("ILi1ELi1", 32, 64), ("ILi0ELi0", 64, 256), ("ILi1ELi0", 64, 256)])
+@pytest.mark.parametrize("variant,stores,products", [("ILi0ELi2", 32, 64), ("ILi1ELi1", 32, 64), ("ILi0ELi0", 64, 256), ("ILi1ELi0", 64, 256), ("ILi0ELi3", 64, 256)])
 def test_stores_are_counted_with_the_loads(text, variant, stores, products):
     """k_product8_flow waits for loads by how many loads and stores are behind them: a tile's stores are as many whatever part of the tile exists, in
     one piece without branches, its loop has 18 loads a slab, and nothing else goes to memory."""
@@ -45,7 +45,9 @@ def test_stores_are_counted_with_the_loads(text, variant, stores, products):
     code = [line for line in code if line]
     at = [i for i, line in enumerate(code) if line.startswith("buffer_store")]
     assert len(at) == stores
-    assert not [line for line in code[at[0]:at[-1]] if line.startswith((".LBB", "s_cbranch", "s_branch", "buffer_load"))]
+    assert not [line for line in code[at[0]:at[-1]] if line.startswith((".LBB", "s_cbranch", "s_branch"))]
+    old = [line for line in code if line.startswith("buffer_load") and "lds" not in line]      # (what results are added to: waited for, and with it all before)
+    assert len(old) == (64 if variant.endswith("Li3") else 0)
     assert len([line for line in code if line.startswith("v_mfma")]) == 2 * products
     assert len([line for line in code if line.startswith("buffer_load") and "lds" in line]) == 36 + 2 * 18
     assert not [line for line in code if line.startswith(("scratch", "global_", "flat_"))]
