@@ -150,6 +150,14 @@ ob_status product(ob_linear8_ctx* ctx, const Given& a, int format, const Given& 
 
 template <int DTYPE>
 void launch_quantize(const QuantizeArgs& p, bool square, hipStream_t s) {
+  const int64_t blocks = (int64_t)p.rows * ((p.cols + BLOCK8 - 1) / BLOCK8);
+  if (!square && !p.data_t && blocks <= (int64_t)1 << 28) {      // (a grid counts its threads in 32 bits)
+    // One block a lane group / four, us: 4096 x 512 (16384 blocks) 3.4 / 4.2, 4096 x 2048 (65536) 7.4 / 6.8: where every CU has workgroups either way, the
+    // loads of four in flight count for more.
+    if (blocks <= 32 * 1024) hipLaunchKernelGGL((k_quantize8_rows<DTYPE, 1>), dim3((unsigned)((blocks + 15) / 16)), dim3(256), 0, s, p);
+    else hipLaunchKernelGGL((k_quantize8_rows<DTYPE, 4>), dim3((unsigned)((blocks + 63) / 64)), dim3(256), 0, s, p);
+    return;
+  }
   const dim3 grid((unsigned)((p.cols + BLOCK8 - 1) / BLOCK8), (unsigned)((p.rows + BLOCK8 - 1) / BLOCK8));
   if (square) hipLaunchKernelGGL((k_quantize8<DTYPE, true>), grid, dim3(256), 0, s, p);
   else hipLaunchKernelGGL((k_quantize8<DTYPE, false>), grid, dim3(256), 0, s, p);

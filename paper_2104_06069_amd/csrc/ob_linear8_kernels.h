@@ -114,6 +114,40 @@ __global__ __launch_bounds__(256) void k_quantize8(QuantizeArgs p) {
   }
 }
 
+// Rows alone: a block of 128 to sixteen lanes, EACH blocks of them, wherever they lie: more workgroups than tiles, and no exchange between wavefronts.  With
+// tiles / so: 1777 x 1000 5.6 / 3.6 us, 32768 x 2048 36.5 / 32.5, 32768 x 8192 152 / 144.
+template <int DTYPE, int EACH>
+__global__ __launch_bounds__(256) void k_quantize8_rows(QuantizeArgs p) {
+  constexpr int GROUP = 16 * EACH;      // blocks of a workgroup
+  const int blocks = (p.cols + BLOCK8 - 1) / BLOCK8, l = threadIdx.x & 15;
+  const int64_t first = (int64_t)blockIdx.x * GROUP, row0 = first / blocks;
+  const int rest = (int)(first - row0 * blocks);
+  int64_t row[EACH];
+  int block[EACH];
+  float v[EACH][8];
+#pragma unroll
+  for (int u = 0; u < EACH; ++u) {
+    const int at = rest + u * 16 + (threadIdx.x >> 4), down = at / blocks;
+    row[u] = row0 + down;
+    block[u] = at - down * blocks;
+    load8<DTYPE>(p.src, row[u] * p.lds + block[u] * BLOCK8 + l * 8, row[u] < p.rows ? p.cols - block[u] * BLOCK8 - l * 8 : 0, v[u]);
+  }
+#pragma unroll
+  for (int u = 0; u < EACH; ++u) {
+    unsigned most = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) most = max(most, magnitude(v[u][e]));
+#pragma unroll
+    for (int d = 8; d >= 1; d >>= 1) most = max(most, (unsigned)__shfl_xor((int)most, d));
+    const int byte = scale_byte(most, p.format);
+    if (row[u] < p.rows) {
+      *reinterpret_cast<v2i*>(p.data + row[u] * p.ld + block[u] * BLOCK8 + l * 8) =
+          bytes_before(bytes8(v[u], inverse_scale(byte), p.format), p.cols - block[u] * BLOCK8 - l * 8);
+      if (l == 0) p.scales[row[u] * p.ld_scales + block[u]] = (uint8_t)byte;
+    }
+  }
+}
+
 // ---- products --------------------------------------------------------------------------------------------------------
 struct Product8Args {
   Operand8 a, b;
