@@ -30,7 +30,7 @@ constexpr int64_t MOST = (int64_t)1 << 22;      // rows, columns and distances b
 
 // Tiles by their side (ob_linear8_plan.h)
 template <int KIND>
-using Tile8 = std::conditional_t<KIND == W256, Shape<256, 256, 64, 2, 4>, std::conditional_t<KIND == W128, Shape<128, 128, 64, 2, 2>, Shape<64, 64, 64, 2, 2, 3>>>;
+using Tile8 = std::conditional_t<KIND == W256, Shape<256, 256, 64, 2, 4>, std::conditional_t<KIND == W128, Shape<128, 128, 64, 2, 2>, Shape<64, 64, 64, 2, 2, KIND == TEAMS64 ? 4 : 3, KIND == TEAMS64 ? 2 : 1>>>;
 
 template <int FORMAT, int OUT>
 ob_status launch_flow(ob_linear8_ctx* ctx, const Product8Args& p, hipStream_t s) {
@@ -57,6 +57,7 @@ auto with_product(int kind, int format, bool wide, F f) {
   const auto with_kind = [&](auto format, auto wide) {
     if (kind == W256) return f(std::integral_constant<int, W256>{}, format, wide);
     if (kind == W128) return f(std::integral_constant<int, W128>{}, format, wide);
+    if (kind == TEAMS64) return f(std::integral_constant<int, TEAMS64>{}, format, wide);
     return f(std::integral_constant<int, W64>{}, format, wide);
   };
   const auto with_format = [&](auto format) { return wide ? with_kind(format, std::true_type{}) : with_kind(format, std::false_type{}); };

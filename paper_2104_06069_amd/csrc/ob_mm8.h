@@ -86,18 +86,24 @@ __device__ __forceinline__ float scale_value(int byte) { return __uint_as_float(
 template <class S, int FORMAT, bool WIDE>
 struct Product8 {
   static constexpr int BM = S::BM, BN = S::BN, FM = S::FM, FN = S::FN;
-  static_assert(S::BK * 2 == BLOCK8 && S::TEAMS == 1, "slabs of a block");      // (BK of pairs of bytes)
-  using A = Rows8<BM, S::NT>;
-  using B = Rows8<BN, S::NT>;
+  static_assert(S::BK * 2 == BLOCK8, "slabs of a block");      // (BK of pairs of bytes)
+  static constexpr int THREADS = S::WAVES * 64;                // of a team
+  using A = Rows8<BM, THREADS>;
+  using B = Rows8<BN, THREADS>;
   static constexpr int SCALE_WAVES = (BM + BN) / 64, SCALES = (BM + BN) * BLOCK8;      // (64 rows' scales a load); where a slab's scales begin
   static_assert(SCALE_WAVES <= S::WAVES, "a row's scales for each lane");
   static constexpr int STAGE = (BM + BN) * (BLOCK8 + 4);
-  static constexpr int LDS_BYTES = S::STAGES * STAGE > Results<S>::LDS_BYTES ? S::STAGES * STAGE : Results<S>::LDS_BYTES;
+  static constexpr int SUMS = Results<S>::LDS_BYTES, ENDS = SUMS + (S::TEAMS - 1) * S::WAVES * FM * FN * 1024;      // (the second team's, behind the results)
+  static constexpr int LDS_BYTES = S::TEAMS * S::STAGES * STAGE > ENDS ? S::TEAMS * S::STAGES * STAGE : ENDS;
   typedef v4f Acc[FM][FN];
 
-  // Slabs t0 .. t0 + n - 1 of K.  The layout of acc is Product's.
+  // Slabs t0 .. t0 + n - 1 of K.  The layout of acc is Product's.  With two teams each has slabs of its own, every second one, and
+  // the first one has the sums of both at the end.
   __device__ static void run(const Operand8& a, const Operand8& b, int r0, int c0, int t0, int n, uint8_t* lds, Acc& acc) {
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tid = threadIdx.x % THREADS, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int team = __builtin_amdgcn_readfirstlane((int)threadIdx.x / THREADS);
+    uint8_t* const own = lds + team * S::STAGES * STAGE;
+    const auto slab_at = [&](int t) { return t0 + t * S::TEAMS + team; };
     const int wm = wave / S::WN, wn = wave % S::WN;
     A sa;
     B sb;
@@ -108,28 +114,44 @@ struct Product8 {
     scales.init(of_a ? a.scales : b.scales, of_a ? a.ld_scales : b.ld_scales, of_a ? a.rows : b.rows, of_a ? a.shift : b.shift,
                 of_a ? r0 + wave * 64 : c0 + wave * 64 - BM, lane);
     const auto load = [&](int t) {
-      uint8_t* const s = lds + t % S::STAGES * STAGE;
+      uint8_t* const s = own + t % S::STAGES * STAGE;
 #pragma unroll
-      for (int j = 0; j < A::PER; ++j) sa.load(t0 + t, s, wave, j);
+      for (int j = 0; j < A::PER; ++j) sa.load(slab_at(t), s, wave, j);
 #pragma unroll
-      for (int j = 0; j < B::PER; ++j) sb.load(t0 + t, s + BM * BLOCK8, wave, j);
-      if (wave < SCALE_WAVES) scales.load(t0 + t, s + SCALES + wave * 256);
+      for (int j = 0; j < B::PER; ++j) sb.load(slab_at(t), s + BM * BLOCK8, wave, j);
+      if (wave < SCALE_WAVES) scales.load(slab_at(t), s + SCALES + wave * 256);
     };
     // Where a lane's pieces q and q + 4 of its row, and that row's scales, lie in a slab; fragments are 16 rows apart
     const int i = lane & 15, row_a = wm * (BM / S::WM) + i, row_b = BM + wn * (BN / S::WN) + i, piece = ((lane >> 4) ^ (i & 7)) * 16;
     const int a_lo = row_a * BLOCK8 + piece, a_hi = row_a * BLOCK8 + (piece ^ 64), b_lo = row_b * BLOCK8 + piece, b_hi = row_b * BLOCK8 + (piece ^ 64);
-    const auto base = in_lds<uint8_t>(lds);
+    const auto base = in_lds<uint8_t>(own);
     const auto read = [&](int lo, int hi, int row, int slab, int f, int t, v8i& to, int& e) {
       const int s = slab * STAGE;
       const v4i x = *(__attribute__((address_space(3))) const v4i*)(base + (s + lo) + f * 16 * BLOCK8);
       const v4i y = *(__attribute__((address_space(3))) const v4i*)(base + (s + hi) + f * 16 * BLOCK8);
       to = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
-      e = *(base + (s + SCALES + row * 4 + ((t0 + t) & 3)) + f * 64);
+      e = *(base + (s + SCALES + row * 4 + (slab_at(t) & 3)) + f * 64);
     };
     const auto read_a = [&](int slab, int f, int t, v8i& to, int& e) { read(a_lo, a_hi, row_a, slab, f, t, to, e); };
     const auto read_b = [&](int slab, int f, int t, v8i& to, int& e) { read(b_lo, b_hi, row_b, slab, f, t, to, e); };
     if constexpr (S::TURNS) turns(n, load, read_a, read_b, acc);
-    else straight(n, wave, load, read_a, read_b, acc);
+    else straight((n + S::TEAMS - 1) / S::TEAMS, (n + S::TEAMS - 1 - team) / S::TEAMS, wave, load, read_a, read_b, acc);
+    if constexpr (S::TEAMS > 1) {
+      static_assert(S::TEAMS == 2, "one other team's sums");
+      float* const at = reinterpret_cast<float*>(lds + SUMS) + (wave * FM * FN * 64 + lane) * 4;
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+          if (team) *in_lds<v4f>(at + (i * FN + j) * 256) = acc[i][j];
+      lds_done();
+      group_barrier();
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+          if (!team) acc[i][j] += *in_lds<const v4f>(at + (i * FN + j) * 256);
+    }
   }
 
  private:
@@ -157,17 +179,19 @@ struct Product8 {
     }
   }
 
+  // n slabs, of `rounds` that every team waits through
   template <class L, class RA, class RB>
-  __device__ static __forceinline__ void straight(int n, int wave, L load, RA read_a, RB read_b, Acc& acc) {
+  __device__ static __forceinline__ void straight(int rounds, int n, int wave, L load, RA read_a, RB read_b, Acc& acc) {
     constexpr int AHEAD = S::STAGES - 1, LOADS = A::PER + B::PER;      // loads of a slab, one more for scales
 #pragma unroll
     for (int t = 0; t < AHEAD; ++t)
       if (t < n) load(t);
-    for (int t = 0; t < n; ++t) {
+    for (int t = 0; t < rounds; ++t) {
       if (AHEAD == 1 || t + AHEAD > n) loads_done();
       else if (wave < SCALE_WAVES) loads_left<(LOADS + 1) * (AHEAD - 1)>();
       else loads_left<LOADS * (AHEAD - 1)>();
       group_barrier();      // slab t is there, and nobody reads slab t - 1 any more
+      if (S::TEAMS > 1 && t >= n) break;      // (the last round: the barrier below is next for everybody)
       if (t + AHEAD < n) load(t + AHEAD);
       const int s = t % S::STAGES;
       v8i fa[FM], fb[FN];

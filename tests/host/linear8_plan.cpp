@@ -11,7 +11,7 @@ using namespace obl;
 int main() {
   long long rows, cols, slabs;
   int wide, eights;
-  const char* const names[] = {"W256", "W128", "W64", "FLOW256"};
+  const char* const names[] = {"W256", "W128", "W64", "TEAMS64", "FLOW256"};
   while (std::cin >> rows >> cols >> slabs >> wide >> eights) {
     if (few8(rows, slabs)) {
       const FewPlan8 p = few_plan8(cols, slabs);

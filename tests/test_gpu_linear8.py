@@ -263,7 +263,7 @@ def test_few_rows(rows, k, n, dtype):
         product_near(few.weight_grad(xs, g), values(few._quantize(g, "dy", rows, None, E4M3)[1]), values(few._quantize(xs, "x", k, None, E4M3)[1]), 300, "dw")
 
 
-@pytest.mark.parametrize("rows,k,n", [(4096, 512, 2048), (5000, 300, 4200), (4070, 1000, 4090), (4090, 2100, 4096), (8190, 2100, 4096), (20000, 400, 1032), (4097, 300, 4097), (2100, 1000, 3000), (600, 4100, 2056), (3000, 130, 3000), (70, 5000, 70)])
+@pytest.mark.parametrize("rows,k,n", [(4096, 512, 2048), (5000, 300, 4200), (4070, 1000, 4090), (4090, 2100, 4096), (8190, 2100, 4096), (20000, 400, 1032), (4097, 300, 4097), (2100, 1000, 3000), (600, 4100, 2056), (3000, 130, 3000), (70, 5000, 70), (70, 30000, 100), (100, 2000, 130), (1000, 1100, 990)])
 @pytest.mark.parametrize("dtype", (BF, F16, F32))
 def test_many_tiles(rows, k, n, dtype):
     """Sizes that take every kind of tile, several for a workgroup, and sums in parts; sums in 64 bits on the device."""

@@ -41,8 +41,8 @@ def test_the_sizes_of_the_tests_reach_every_kind(ask):
             for (rows, k, n), plan in zip(cases, ask([(rows, n, (k + 127) // 128, wide, n % 8 == 0) for rows, k, n in cases])):
                 found.add((wide,) + (plan if plan[0] == "few" else (plan[0], plan[1] != "1")))
     for wide in (False, True):
-        assert {(wide, kind, False) for kind in ("W256", "W128", "W64")} <= found, found
-        assert (wide, "W64", True) in found
+        assert {(wide, kind, False) for kind in ("W256", "W128", "W64", "TEAMS64")} <= found, found
+        assert (wide, "W64", True) in found and (wide, "TEAMS64", True) in found
         assert {(wide, "few", "32", "8"), (wide, "few", "16", "8"), (wide, "few", "16", "16")} <= found, found
         assert (wide, "FLOW256", False) in found
 
