@@ -45,9 +45,10 @@ struct Plan8 {
 };
 
 // Few rows: k_product8_few, whose workgroups have all of the rows and 16 or 32 columns, and read all of the rows each.  Microseconds
-// with it / with tiles, the host's call of 6.3 included: 1 row of 8192 x 2048 6.2 / 7.8, 32 rows 6.6 / 7.9, 33 rows 10.2 / 7.9; 1 row of
-// 2048 x 8192 7.0 / 11.0, 16 rows 11.2 / 12.8, 32 rows 16.6 / 13.0; 1 row of 8192 x 8192 12.9 / 14.8, 16 rows 20.1 / 15.1.
-constexpr bool few8(int64_t rows, int64_t slabs) { return rows <= 32 && rows * slabs <= 512; }
+// with it / with tiles, 16-bit results, the host's call of 6.2 included: 1 row of 8192 x 2048 6.2 / 6.8, 32 rows 6.6 / 6.9, 33 rows 10.2 / 7.9; 1 row
+// of 2048 x 8192 7.0 / 9.2, 8 rows 9.2 / 9.9, 16 rows 11.2 / 10.3, 32 rows 16.6 / 11.0; 4 rows of 8192 x 8192 14.1 / 14.8, 8 rows 16.2 / 14.9 (binary32: 16.9 /
+// 18.1).  A long K alone, shared by 16 wavefronts at most: 1 row of 512 x 16384 11.4 / 10.6, of 1024 x 65536 40 / 19.
+constexpr bool few8(int64_t rows, int64_t slabs) { return rows <= 32 && rows * slabs <= 512 && slabs < 128; }
 struct FewPlan8 {
   int columns, waves;      // 16 or 32; 8 or 16
 };

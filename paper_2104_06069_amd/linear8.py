@@ -44,8 +44,9 @@ class Linear8:
         self._calls = L.ob_linear8_quantize, L.ob_linear8_forward, L.ob_linear8_input_grad, L.ob_linear8_weight_grad, L.ob_linear8_forward_few
         self._index = torch.cuda.current_device()
         self.ctx = ob.ob_linear8_create(self.k, self.n, max_rows)
-        # rows whose numbers the product itself makes 8 bits (one launch): few, or short ones, up to 512 blocks of 128 in all
-        self._few_rows = min(ob.OB_LINEAR8_FEW_ROWS, 512 // ((self.k + 127) // 128))
+        # rows whose numbers the product itself makes 8 bits (one launch): few, or short ones, up to 512 blocks of 128 in all, 127 in a row
+        blocks = (self.k + 127) // 128
+        self._few_rows = min(ob.OB_LINEAR8_FEW_ROWS, 512 // blocks) if blocks < 128 else 0
 
     def close(self):
         if self.ctx is not None:

@@ -243,7 +243,7 @@ def test_refusals():
 
 
 @pytest.mark.parametrize("rows,k,n", [(1, 1024, 4096), (1, 100, 72), (3, 9000, 40), (16, 2048, 9000), (7, 130, 8200), (16, 500, 300), (15, 3000, 16), (31, 2100, 8192),
-                                      (32, 130, 20), (50, 2500, 33), (64, 700, 8200)])
+                                      (32, 130, 20), (50, 2500, 33), (64, 700, 8200), (1, 17000, 200)])
 @pytest.mark.parametrize("dtype", (BF, F16, F32))
 def test_few_rows(rows, k, n, dtype):
     """One token and a few: from x itself and from its 8 bits, the same."""
