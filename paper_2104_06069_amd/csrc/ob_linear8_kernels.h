@@ -14,13 +14,21 @@ struct QuantizeArgs {
   int64_t ld, ld_scales, ld_t, ld_scales_t;
 };
 
-// Bytes of numbers from `left` on are zeros
-__device__ __forceinline__ v2i bytes_before(v2i q, int left) {
-  if (left >= 8) return q;
-  const unsigned long long keep = left <= 0 ? 0 : ~0ull >> (64 - 8 * left);
-  q.x &= (int)(unsigned)keep;
-  q.y &= (int)(unsigned)(keep >> 32);
-  return q;
+// Column e of eight rows' eight numbers
+template <int DTYPE>
+__device__ __forceinline__ Raw8<DTYPE> column(const Raw8<DTYPE> (&v)[8], int e) {
+  Raw8<DTYPE> r;
+  if constexpr (DTYPE == F32) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      r.lo[i] = e < 4 ? v[i].lo[e & 3] : v[i].hi[e & 3];
+      r.hi[i] = e < 4 ? v[i + 4].lo[e & 3] : v[i + 4].hi[e & 3];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r.h[i] = v[i].h[e];
+  }
+  return r;
 }
 
 // A workgroup takes 128 x 128 numbers, a thread eight adjacent rows by eight adjacent columns of them: a row's block is that of
@@ -29,60 +37,56 @@ __device__ __forceinline__ v2i bytes_before(v2i q, int left) {
 // column's number, or the lanes of a row would meet in one bank.
 template <int DTYPE, bool SQUARE>
 __global__ __launch_bounds__(256) void k_quantize8(QuantizeArgs p) {
+  using Magnitudes = typename Raw8<DTYPE>::Magnitudes;
   __shared__ __align__(16) uint8_t turned[BLOCK8 * BLOCK8];
-  __shared__ unsigned most_of[4][BLOCK8];
+  __shared__ __align__(16) Magnitudes most_of[4][16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, rg = tid >> 4, cg = tid & 15;
   const int r0 = blockIdx.y * BLOCK8, c0 = blockIdx.x * BLOCK8, left = p.cols - c0 - cg * 8, below = p.rows - r0 - rg * 8;
-  float v[8][8];
+  Raw8<DTYPE> v[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) load8<DTYPE>(p.src, (int64_t)(r0 + rg * 8 + i) * p.lds + c0 + cg * 8, i < below ? left : 0, v[i]);
-  unsigned row_most[8], col_most[8] = {};
+  for (int i = 0; i < 8; ++i) v[i].load(p.src, (int64_t)(r0 + rg * 8 + i) * p.lds + c0 + cg * 8, i < below ? left : 0);
+  Magnitudes rows, cols = v[0].magnitudes();      // of this thread's eight rows, and columns
+  rows[0] = highest(cols);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    row_most[i] = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const unsigned m = magnitude(v[i][e]);
-      row_most[i] = max(row_most[i], m);
-      col_most[e] = max(col_most[e], m);
-    }
+  for (int i = 1; i < 8; ++i) {
+    const Magnitudes m = v[i].magnitudes();
+    rows[i] = highest(m);
+    cols = __builtin_elementwise_max(cols, m);
   }
+  const auto of_wave = [&](Magnitudes m) {      // lanes of the same columns
+#pragma unroll
+    for (int d = 32; d >= 16; d >>= 1) {
+      Magnitudes o;
+      int w[sizeof(m) / 4];
+      __builtin_memcpy(w, &m, sizeof(m));
+#pragma unroll
+      for (int& k : w) k = __shfl_xor(k, d);
+      __builtin_memcpy(&o, w, sizeof(m));
+      m = __builtin_elementwise_max(m, o);
+    }
+    return m;
+  };
   if constexpr (SQUARE) {
-    unsigned m = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) m = max(m, col_most[e]);
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) m = max(m, (unsigned)__shfl_xor((int)m, d));
-    if (lane == 0) most_of[wave][0] = m;
+    cols = of_wave(highest_of_16(cols));
+    if (lane == 0) most_of[wave][0] = cols;
     __syncthreads();
-    m = max(max(most_of[0][0], most_of[1][0]), max(most_of[2][0], most_of[3][0]));
+    const auto m = highest(__builtin_elementwise_max(__builtin_elementwise_max(most_of[0][0], most_of[1][0]), __builtin_elementwise_max(most_of[2][0], most_of[3][0])));
 #pragma unroll
-    for (int e = 0; e < 8; ++e) row_most[e] = col_most[e] = m;
+    for (int e = 0; e < 8; ++e) rows[e] = cols[e] = m;
   } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-#pragma unroll
-      for (int d = 8; d >= 1; d >>= 1) row_most[i] = max(row_most[i], (unsigned)__shfl_xor((int)row_most[i], d));
+    rows = highest_of_16(rows);
     if (p.data_t) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-#pragma unroll
-        for (int d = 32; d >= 16; d >>= 1) col_most[e] = max(col_most[e], (unsigned)__shfl_xor((int)col_most[e], d));
-        if (lane < 16) most_of[wave][cg * 8 + e] = col_most[e];
-      }
+      cols = of_wave(cols);
+      if (lane < 16) most_of[wave][cg] = cols;
       __syncthreads();
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int c = cg * 8 + e;
-        col_most[e] = max(max(most_of[0][c], most_of[1][c]), max(most_of[2][c], most_of[3][c]));
-      }
+      cols = __builtin_elementwise_max(__builtin_elementwise_max(most_of[0][cg], most_of[1][cg]), __builtin_elementwise_max(most_of[2][cg], most_of[3][cg]));
     }
   }
   if (p.data) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int byte = scale_byte(row_most[i], p.format);
-      const v2i q = bytes_before(bytes8(v[i], inverse_scale(byte), p.format), left);
+      const int byte = scale_byte(Raw8<DTYPE>::of_binary32(rows[i]), p.format);
+      const v2i q = bytes8(v[i], byte, p.format, left);
       if (i < below) {
         const int64_t row = r0 + rg * 8 + i;
         *reinterpret_cast<v2i*>(p.data + row * p.ld + c0 + cg * 8) = q;
@@ -93,11 +97,8 @@ __global__ __launch_bounds__(256) void k_quantize8(QuantizeArgs p) {
   if (p.data_t) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const int byte = scale_byte(col_most[e], p.format_t);
-      float w[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) w[i] = v[i][e];
-      *reinterpret_cast<v2i*>(turned + (cg * 8 + e) * BLOCK8 + (rg / 2 ^ (cg & 7)) * 16 + rg % 2 * 8) = bytes_before(bytes8(w, inverse_scale(byte), p.format_t), below);
+      const int byte = scale_byte(Raw8<DTYPE>::of_binary32(cols[e]), p.format_t);
+      *reinterpret_cast<v2i*>(turned + (cg * 8 + e) * BLOCK8 + (rg / 2 ^ (cg & 7)) * 16 + rg % 2 * 8) = bytes8(column(v, e), byte, p.format_t, below);
       if (rg == 0 && e < left) {
         const int64_t col = c0 + cg * 8 + e;
         if (!SQUARE) p.scales_t[col * p.ld_scales_t + blockIdx.y] = (uint8_t)byte;
@@ -124,25 +125,20 @@ __global__ __launch_bounds__(256) void k_quantize8_rows(QuantizeArgs p) {
   const int rest = (int)(first - row0 * blocks);
   int64_t row[EACH];
   int block[EACH];
-  float v[EACH][8];
+  Raw8<DTYPE> v[EACH];
 #pragma unroll
   for (int u = 0; u < EACH; ++u) {
     const int at = rest + u * 16 + (threadIdx.x >> 4), down = at / blocks;
     row[u] = row0 + down;
     block[u] = at - down * blocks;
-    load8<DTYPE>(p.src, row[u] * p.lds + block[u] * BLOCK8 + l * 8, row[u] < p.rows ? p.cols - block[u] * BLOCK8 - l * 8 : 0, v[u]);
+    v[u].load(p.src, row[u] * p.lds + block[u] * BLOCK8 + l * 8, row[u] < p.rows ? p.cols - block[u] * BLOCK8 - l * 8 : 0);
   }
 #pragma unroll
   for (int u = 0; u < EACH; ++u) {
-    unsigned most = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) most = max(most, magnitude(v[u][e]));
-#pragma unroll
-    for (int d = 8; d >= 1; d >>= 1) most = max(most, (unsigned)__shfl_xor((int)most, d));
-    const int byte = scale_byte(most, p.format);
+    const int byte = scale_byte(Raw8<DTYPE>::of_binary32(highest_of_16(highest(v[u].magnitudes()))), p.format);
     if (row[u] < p.rows) {
       *reinterpret_cast<v2i*>(p.data + row[u] * p.ld + block[u] * BLOCK8 + l * 8) =
-          bytes_before(bytes8(v[u], inverse_scale(byte), p.format), p.cols - block[u] * BLOCK8 - l * 8);
+          bytes8(v[u], byte, p.format, p.cols - block[u] * BLOCK8 - l * 8);
       if (l == 0) p.scales[row[u] * p.ld_scales + block[u]] = (uint8_t)byte;
     }
   }
@@ -236,22 +232,21 @@ struct FewArgs {
 // A lane's pieces q and q + 4 of a row's block, in 8 bits, and the block's scale
 template <int DTYPE>
 __device__ __forceinline__ void quantized_fragment(const FewArgs& f, int row, int slab, int lane, v8i& to, int& scale) {
-  float v[4][8];
+  Raw8<DTYPE> v[4];
   unsigned most = 0;
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
     const int at = slab * BLOCK8 + (lane >> 4) * 16 + (u & 1) * 8 + (u >> 1) * 64;
-    load8<DTYPE>(f.x, row * f.ldx + at, f.k - at, v[u]);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) most = max(most, magnitude(v[u][e]));
+    v[u].load(f.x, row * f.ldx + at, f.k - at);
+    most = max(most, highest(v[u].magnitudes()));
   }
 #pragma unroll
   for (int d = 32; d >= 16; d >>= 1) most = max(most, (unsigned)__shfl_xor((int)most, d));
-  scale = scale_byte(most, f.format);
+  scale = scale_byte(Raw8<DTYPE>::of_binary32(most), f.format);
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
     const int at = slab * BLOCK8 + (lane >> 4) * 16 + (u & 1) * 8 + (u >> 1) * 64;
-    const v2i q = bytes_before(bytes8(v[u], inverse_scale(scale), f.format), f.k - at);
+    const v2i q = bytes8(v[u], scale, f.format, f.k - at);
     to[u * 2] = q.x;
     to[u * 2 + 1] = q.y;
   }

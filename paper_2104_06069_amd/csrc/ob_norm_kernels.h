@@ -97,21 +97,12 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void k_norm_forward(NormArgs p) 
     }
     if (p.y && left > 0) store8<X>(p.y, row * p.ldy + at, left, y);
     if (p.data) {
-      unsigned most = 0;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
+      for (int e = 0; e < 8; ++e)
         if (e >= left) y[e] = 0;      // (0 times an rstd that is not finite)
-        most = max(most, magnitude(y[e]));
-      }
-#pragma unroll
-      for (int d = 8; d >= 1; d >>= 1) most = max(most, (unsigned)__shfl_xor((int)most, d));
-      const int byte = scale_byte(most, p.format), padded = (p.n + BLOCK8 - 1) / BLOCK8 * BLOCK8;
-      v2i q = bytes8(y, inverse_scale(byte), p.format);
-      if (left < 8) {      // behind the row's end: zeros in a block of NaNs too
-        unsigned long long keep = left <= 0 ? 0 : ~0ull >> (64 - 8 * left);
-        q.x &= (int)(unsigned)keep;
-        q.y &= (int)(unsigned)(keep >> 32);
-      }
+      const Raw8<F32> raw{v4f{y[0], y[1], y[2], y[3]}, v4f{y[4], y[5], y[6], y[7]}};
+      const int byte = scale_byte(highest_of_16(highest(raw.magnitudes())), p.format), padded = (p.n + BLOCK8 - 1) / BLOCK8 * BLOCK8;
+      const v2i q = bytes8(raw, byte, p.format, left);      // (behind the row's end zeros, in a block of NaNs too)
       if (at < padded) *reinterpret_cast<v2i*>(p.data + row * p.ld + at) = q;
       if (at % BLOCK8 == 0 && left > 0) p.scales[row * p.ld_scales + at / BLOCK8] = (uint8_t)byte;
     }
