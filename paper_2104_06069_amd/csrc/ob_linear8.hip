@@ -152,16 +152,22 @@ ob_status product(ob_linear8_ctx* ctx, const Given& a, int format, const Given& 
 template <int DTYPE>
 void launch_quantize(const QuantizeArgs& p, bool square, hipStream_t s) {
   const int64_t blocks = (int64_t)p.rows * ((p.cols + BLOCK8 - 1) / BLOCK8);
+  // Past the caches where the numbers fill most of the 256 MB behind them.  Through / past them, us, to rows and transpose of bfloat16: 32768 x 8192
+  // (512 MB) 238 / 182, 16384 x 8192 113 / 94, 24576 x 4096 (192 MB) 82 / 72, 32768 x 2048 (128 MB) 49.7 / 51.5; rows alone 139 / 129, 71 / 63, 51 / 48,
+  // 31.5 / 32.3.
+  const bool past = (int64_t)p.rows * p.cols * (DTYPE == F32 ? 4 : 2) > (int64_t)128 << 20;
   if (!square && !p.data_t && blocks <= (int64_t)1 << 28) {      // (a grid counts its threads in 32 bits)
     // One block a lane group / four, us: 4096 x 512 (16384 blocks) 3.4 / 4.2, 4096 x 2048 (65536) 7.4 / 6.8: where every CU has workgroups either way, the
     // loads of four in flight count for more.
-    if (blocks <= 32 * 1024) hipLaunchKernelGGL((k_quantize8_rows<DTYPE, 1>), dim3((unsigned)((blocks + 15) / 16)), dim3(256), 0, s, p);
-    else hipLaunchKernelGGL((k_quantize8_rows<DTYPE, 4>), dim3((unsigned)((blocks + 63) / 64)), dim3(256), 0, s, p);
+    if (blocks <= 32 * 1024) hipLaunchKernelGGL((k_quantize8_rows<DTYPE, 1, false>), dim3((unsigned)((blocks + 15) / 16)), dim3(256), 0, s, p);
+    else if (past) hipLaunchKernelGGL((k_quantize8_rows<DTYPE, 4, true>), dim3((unsigned)((blocks + 63) / 64)), dim3(256), 0, s, p);
+    else hipLaunchKernelGGL((k_quantize8_rows<DTYPE, 4, false>), dim3((unsigned)((blocks + 63) / 64)), dim3(256), 0, s, p);
     return;
   }
   const dim3 grid((unsigned)((p.cols + BLOCK8 - 1) / BLOCK8), (unsigned)((p.rows + BLOCK8 - 1) / BLOCK8));
-  if (square) hipLaunchKernelGGL((k_quantize8<DTYPE, true>), grid, dim3(256), 0, s, p);
-  else hipLaunchKernelGGL((k_quantize8<DTYPE, false>), grid, dim3(256), 0, s, p);
+  if (square) hipLaunchKernelGGL((k_quantize8<DTYPE, true, false>), grid, dim3(256), 0, s, p);
+  else if (past) hipLaunchKernelGGL((k_quantize8<DTYPE, false, true>), grid, dim3(256), 0, s, p);
+  else hipLaunchKernelGGL((k_quantize8<DTYPE, false, false>), grid, dim3(256), 0, s, p);
 }
 
 }  // namespace

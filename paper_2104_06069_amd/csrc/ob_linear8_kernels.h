@@ -14,6 +14,12 @@ struct QuantizeArgs {
   int64_t ld, ld_scales, ld_t, ld_scales_t;
 };
 
+template <bool PAST>
+__device__ __forceinline__ void write8(uint8_t* p, v2i q) {
+  if constexpr (PAST) __builtin_nontemporal_store(q, reinterpret_cast<v2i*>(p));
+  else *reinterpret_cast<v2i*>(p) = q;
+}
+
 // Column e of eight rows' eight numbers
 template <int DTYPE>
 __device__ __forceinline__ Raw8<DTYPE> column(const Raw8<DTYPE> (&v)[8], int e) {
@@ -34,8 +40,9 @@ __device__ __forceinline__ Raw8<DTYPE> column(const Raw8<DTYPE> (&v)[8], int e) 
 // A workgroup takes 128 x 128 numbers, a thread eight adjacent rows by eight adjacent columns of them: a row's block is that of
 // sixteen adjacent lanes, a column's that of sixteen lanes one from each group of those, four in a wavefront.  The transposed
 // bytes are turned in LDS, so that both results go out 128 bytes of a row at a time; there the 16-byte pieces of a column are permuted by the
-// column's number, or the lanes of a row would meet in one bank.
-template <int DTYPE, bool SQUARE>
+// column's number, or the lanes of a row would meet in one bank.  PAST (the rule is launch_quantize's): numbers are read and rows written past the
+// caches; the transposed bytes are not, which are 128 of a row at a time.
+template <int DTYPE, bool SQUARE, bool PAST>
 __global__ __launch_bounds__(256) void k_quantize8(QuantizeArgs p) {
   using Magnitudes = typename Raw8<DTYPE>::Magnitudes;
   __shared__ __align__(16) uint8_t turned[BLOCK8 * BLOCK8];
@@ -44,7 +51,7 @@ __global__ __launch_bounds__(256) void k_quantize8(QuantizeArgs p) {
   const int r0 = blockIdx.y * BLOCK8, c0 = blockIdx.x * BLOCK8, left = p.cols - c0 - cg * 8, below = p.rows - r0 - rg * 8;
   Raw8<DTYPE> v[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i].load(p.src, (int64_t)(r0 + rg * 8 + i) * p.lds + c0 + cg * 8, i < below ? left : 0);
+  for (int i = 0; i < 8; ++i) v[i].template load<PAST>(p.src, (int64_t)(r0 + rg * 8 + i) * p.lds + c0 + cg * 8, i < below ? left : 0);
   Magnitudes rows, cols = v[0].magnitudes();      // of this thread's eight rows, and columns
   rows[0] = highest(cols);
 #pragma unroll
@@ -89,7 +96,7 @@ __global__ __launch_bounds__(256) void k_quantize8(QuantizeArgs p) {
       const v2i q = bytes8(v[i], byte, p.format, left);
       if (i < below) {
         const int64_t row = r0 + rg * 8 + i;
-        *reinterpret_cast<v2i*>(p.data + row * p.ld + c0 + cg * 8) = q;
+        write8<PAST>(p.data + row * p.ld + c0 + cg * 8, q);
         if (cg == 0 && (!SQUARE || (rg == 0 && i == 0))) p.scales[(SQUARE ? row / BLOCK8 : row) * p.ld_scales + blockIdx.x] = (uint8_t)byte;
       }
     }
@@ -116,8 +123,8 @@ __global__ __launch_bounds__(256) void k_quantize8(QuantizeArgs p) {
 }
 
 // Rows alone: a block of 128 to sixteen lanes, EACH blocks of them, wherever they lie: more workgroups than tiles, and no exchange between wavefronts.  With
-// tiles / so: 1777 x 1000 5.6 / 3.6 us, 32768 x 2048 36.5 / 32.5, 32768 x 8192 152 / 144.
-template <int DTYPE, int EACH>
+// tiles / so: 1777 x 1000 5.6 / 3.6 us, 32768 x 2048 36.5 / 31.4, 32768 x 8192 152 / 129.
+template <int DTYPE, int EACH, bool PAST>
 __global__ __launch_bounds__(256) void k_quantize8_rows(QuantizeArgs p) {
   constexpr int GROUP = 16 * EACH;      // blocks of a workgroup
   const int blocks = (p.cols + BLOCK8 - 1) / BLOCK8, l = threadIdx.x & 15;
@@ -131,14 +138,13 @@ __global__ __launch_bounds__(256) void k_quantize8_rows(QuantizeArgs p) {
     const int at = rest + u * 16 + (threadIdx.x >> 4), down = at / blocks;
     row[u] = row0 + down;
     block[u] = at - down * blocks;
-    v[u].load(p.src, row[u] * p.lds + block[u] * BLOCK8 + l * 8, row[u] < p.rows ? p.cols - block[u] * BLOCK8 - l * 8 : 0);
+    v[u].template load<PAST>(p.src, row[u] * p.lds + block[u] * BLOCK8 + l * 8, row[u] < p.rows ? p.cols - block[u] * BLOCK8 - l * 8 : 0);
   }
 #pragma unroll
   for (int u = 0; u < EACH; ++u) {
     const int byte = scale_byte(Raw8<DTYPE>::of_binary32(highest_of_16(highest(v[u].magnitudes()))), p.format);
     if (row[u] < p.rows) {
-      *reinterpret_cast<v2i*>(p.data + row[u] * p.ld + block[u] * BLOCK8 + l * 8) =
-          bytes8(v[u], byte, p.format, p.cols - block[u] * BLOCK8 - l * 8);
+      write8<PAST>(p.data + row[u] * p.ld + block[u] * BLOCK8 + l * 8, bytes8(v[u], byte, p.format, p.cols - block[u] * BLOCK8 - l * 8));
       if (l == 0) p.scales[row[u] * p.ld_scales + block[u]] = (uint8_t)byte;
     }
   }

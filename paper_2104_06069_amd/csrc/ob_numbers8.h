@@ -36,15 +36,18 @@ __device__ __forceinline__ v2i bytes_of_nans(int left) {
   return v2i{(int)(0x7f7f7f7fu & (unsigned)keep), (int)(0x7f7f7f7fu & (unsigned)(keep >> 32))};
 }
 
-// Eight adjacent elements of one type as memory has them.  Those from `left` on do not exist and read as zeros.
+// Eight adjacent elements of one type as memory has them.  Those from `left` on do not exist and read as zeros.  PAST the caches: nothing
+// of what is read stays there.
 template <int DTYPE>
 struct Raw8 {
   v8s h;
+  template <bool PAST = false>
   __device__ __forceinline__ void load(const void* p, int64_t at, int left) {
     const uint16_t* const s = static_cast<const uint16_t*>(p) + at;
     h = v8s{};
     if (left >= 8) {
-      h = *reinterpret_cast<const v8s_any*>(s);
+      if constexpr (PAST) h = __builtin_nontemporal_load(reinterpret_cast<const v8s_any*>(s));
+      else h = *reinterpret_cast<const v8s_any*>(s);
     } else {
 #pragma unroll
       for (int e = 0; e < 7; ++e)
@@ -77,7 +80,13 @@ struct Raw8 {
 template <>
 struct Raw8<F32> {
   v4f lo, hi;
+  template <bool PAST = false>
   __device__ __forceinline__ void load(const void* p, int64_t at, int left) {
+    if (PAST && left >= 8) {
+      lo = __builtin_nontemporal_load(reinterpret_cast<const v4f_any*>(static_cast<const float*>(p) + at));
+      hi = __builtin_nontemporal_load(reinterpret_cast<const v4f_any*>(static_cast<const float*>(p) + at + 4));
+      return;
+    }
     lo = load4(p, F32, at, left);
     hi = load4(p, F32, at + 4, left - 4);
   }

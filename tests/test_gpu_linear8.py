@@ -56,6 +56,27 @@ def test_quantize(rows, width, pitch, dtype, fmt):
     same8(w8.transposed, (q.t(), scales.t()), "squares, transposed")
 
 
+@pytest.mark.parametrize("rows,width,dtype", [(40001, 1701, BF), (70000, 960, F16), (19000, 1900, F32)])
+def test_quantize_past_the_caches(rows, width, dtype):
+    """More numbers than the rule for that asks for (128 MB): the same as a few thousand rows at a time."""
+    gen = torch.Generator("cuda").manual_seed(1)
+    t = (torch.randn(rows, width, generator=gen, device="cuda") * torch.exp(torch.randn(rows, 1, generator=gen, device="cuda"))).to(dtype)
+    assert t.numel() * t.element_size() > 128 << 20
+    t[77, 5], t[rows - 1, width - 1] = float("inf"), float("nan")
+    layer = op(width, 64)
+    alone, (m, mt), turned = layer.quantize(t, E5M2), layer._quantize(t, "t", width, E4M3, E5M2), layer._quantize(t, "t", width, None, E4M3)[1]
+    for i in range(0, rows, 4096):
+        part = t[i:i + 4096]
+        k, j = part.shape[0], i // 128
+        want, (w, wt), wturned = layer.quantize(part, E5M2), layer._quantize(part, "t", width, E4M3, E5M2), layer._quantize(part, "t", width, None, E4M3)[1]
+        for got, of in ((alone, want), (m, w)):
+            assert torch.equal(got.buffer[:rows * got.ld].view(rows, -1)[i:i + k], of.buffer[:k * of.ld].view(k, -1))
+            assert torch.equal(got.scales.view(torch.uint8)[i:i + k], of.scales.view(torch.uint8))
+        for got, of in ((mt, wt), (turned, wturned)):
+            assert torch.equal(got.buffer[:width * got.ld].view(width, -1)[:, i:i + of.ld], of.buffer[:width * of.ld].view(width, -1))
+            assert torch.equal(got.scales.view(torch.uint8)[:, j:j + (k + 127) // 128], of.scales.view(torch.uint8))
+
+
 @pytest.mark.parametrize("fmt,largest", [(E4M3, 448.0), (E5M2, 57344.0)])
 def test_quantize_at_the_borders(fmt, largest):
     """Largest magnitudes at the border between two scales and a bit beside it, ties, numbers below the format's and binary32's smallest, and what
