@@ -157,7 +157,7 @@ void launch_quantize(const QuantizeArgs& p, bool square, hipStream_t s) {
   // 31.5 / 32.3.
   const bool past = (int64_t)p.rows * p.cols * (DTYPE == F32 ? 4 : 2) > (int64_t)128 << 20;
   if (!square && !p.data_t && blocks <= (int64_t)1 << 28) {      // (a grid counts its threads in 32 bits)
-    // One block a lane group / four, us: 4096 x 512 (16384 blocks) 3.4 / 4.2, 4096 x 2048 (65536) 7.4 / 6.8: where every CU has workgroups either way, the
+    // One block a lane group / four, us: 4096 x 512 (16384 blocks) 3.3 / 3.7, 4096 x 1024 4.4 / 4.3, 4096 x 2048 6.9 / 6.1: where every CU has workgroups either way, the
     // loads of four in flight count for more.
     if (blocks <= 32 * 1024) hipLaunchKernelGGL((k_quantize8_rows<DTYPE, 1, false>), dim3((unsigned)((blocks + 15) / 16)), dim3(256), 0, s, p);
     else if (past) hipLaunchKernelGGL((k_quantize8_rows<DTYPE, 4, true>), dim3((unsigned)((blocks + 63) / 64)), dim3(256), 0, s, p);

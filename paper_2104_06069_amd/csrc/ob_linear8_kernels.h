@@ -123,7 +123,7 @@ __global__ __launch_bounds__(256) void k_quantize8(QuantizeArgs p) {
 }
 
 // Rows alone: a block of 128 to sixteen lanes, EACH blocks of them, wherever they lie: more workgroups than tiles, and no exchange between wavefronts.  With
-// tiles / so: 1777 x 1000 5.6 / 3.6 us, 32768 x 2048 36.5 / 31.4, 32768 x 8192 152 / 129.
+// tiles / so: 1777 x 1000 5.0 / 3.4 us, 32768 x 2048 35.3 / 31.5, 32768 x 8192 140 / 126.
 template <int DTYPE, int EACH, bool PAST>
 __global__ __launch_bounds__(256) void k_quantize8_rows(QuantizeArgs p) {
   constexpr int GROUP = 16 * EACH;      // blocks of a workgroup
