@@ -98,6 +98,7 @@ __global__ __launch_bounds__(256) void k_clip_norm(ClipArgs p) {
     if ((threadIdx.x & 63) == 0) {
       __hip_atomic_store(&p.layer_sums[l], v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       if (p.layer_norms) p.layer_norms[l] = norm_of(v, p.grad_scale);
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // (there before the arrival: thread 0's fence waits for its own wavefront's stores alone)
     }
   }
   __syncthreads();

@@ -51,3 +51,21 @@ def test_stores_are_counted_with_the_loads(text, variant, stores, products):
     assert len([line for line in code if line.startswith("v_mfma")]) == 2 * products
     assert len([line for line in code if line.startswith("buffer_load") and "lds" in line]) == 36 + 2 * 18
     assert not [line for line in code if line.startswith(("scratch", "global_", "flat_"))]
+
+
+def test_a_tensors_sum_is_there_before_the_arrival(text):
+    """k_clip_norm counts workgroups that are done, from a single thread: each of the four wavefronts that store a tensor's sum waits for
+    that store before the barrier that thread is behind, and the count follows the barrier."""
+    name, text = text
+    if name != "ob_clip":
+        pytest.skip("of the clipping")
+    code = [line.split(";")[0].strip() for line in function(text, "k_clip_norm").split("\n")]
+    arrival = next(i for i, line in enumerate(code) if line.startswith("global_atomic_add"))
+    barrier = max(i for i, line in enumerate(code[:arrival]) if line.startswith("s_barrier"))
+    stores = [i for i, line in enumerate(code[:barrier]) if line.startswith("global_store")]
+    assert stores
+    assert [line for line in code[stores[-1]:barrier] if re.match(r"s_waitcnt vmcnt\(0\)", line)]
+    after = [line for line in code[stores[0]:stores[-1]] if line.startswith("s_cbranch")]      # (around the norm's store, where there is none to write)
+    for line in after:
+        label = line.split()[-1] + ":"
+        assert code[:barrier].index(label) <= next(i for i in range(stores[-1], barrier) if re.match(r"s_waitcnt vmcnt\(0\)", code[i])), line
