@@ -45,8 +45,10 @@ enum { OB_BLOCK_ROWS = 0, OB_BLOCK_SQUARE = 1 };
  *   backward   g = dy weight, xhat = h rstd
  *              dh = dres + rstd (g - xhat mean(g xhat))          (dres NULL: 0), rounded to h's type
  *              dweight = sum over rows of dy xhat                 (+= with accumulate)
- * on rows of n numbers, in binary32, with y and xhat those of the rounded h.  dh is the gradient of x and of the residual.  A row of zeros with
- * eps = 0 gives NaNs; a row with an infinity has rstd 0, zeros, and a NaN where the infinity was; one with a NaN gives NaNs.
+ * on rows of n numbers, in binary32, with y and xhat those of the rounded h.  Squares are summed in binary64 where their sum leaves binary32's
+ * range, so that rows of any finite numbers have their norm.  dh is the gradient of x and of the residual.  A row of zeros with eps = 0 gives
+ * NaNs, and one with a root mean square below 2^-128 an rstd, and numbers, of infinity; a row with an infinity has rstd 0, zeros, and a NaN where
+ * the infinity was; one with a NaN gives NaNs.
  */
 typedef struct ob_norm_ctx ob_norm_ctx; /* opaque */
 

@@ -19,14 +19,15 @@ struct NormArgs {
   float eps;
 };
 
-__device__ __forceinline__ float wave_sum(float v) {
+template <class V>
+__device__ __forceinline__ V wave_sum(V v) {
 #pragma unroll
   for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d);
   return v;
 }
 // The sum over the T threads of a row; `part` holds a place for each wavefront of the workgroup, not in use by another sum.
-template <int T>
-__device__ __forceinline__ float row_sum(float v, float* part) {
+template <int T, class V>
+__device__ __forceinline__ V row_sum(V v, V* part) {
   v = wave_sum(v);
   if constexpr (T > 64) {
     const int wave = threadIdx.x / 64, first = threadIdx.x / T * (T / 64);
@@ -39,10 +40,15 @@ __device__ __forceinline__ float row_sum(float v, float* part) {
   return v;
 }
 
+// Whether a row's mean of squares, with eps, lies where binary32 has lost nothing of it: no square above its largest number, and none
+// that counts below its smallest
+__device__ __forceinline__ bool in_range(float mean) { return mean >= 0x1p-100f && mean <= 0x1.fffffep127f; }
+
 template <int X, int H, int T, int C>
 __global__ __launch_bounds__(T < 256 ? 256 : T) void k_norm_forward(NormArgs p) {
   constexpr int NT = T < 256 ? 256 : T;
   __shared__ float part[NT / 64];
+  __shared__ double part64[NT / 64];
   const int t = threadIdx.x % T;
   const int64_t row = (int64_t)blockIdx.x * (NT / T) + threadIdx.x / T;
   const bool there = row < p.rows;
@@ -79,8 +85,28 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void k_norm_forward(NormArgs p) 
     for (int e = 0; e < 8; ++e) sum += h[c][e] * h[c][e];
   }
   sum = row_sum<T>(sum, part);
+  const float mean = sum / (float)p.n + p.eps;
+  float rstd = 1.0f / sqrtf(mean);
+  bool again = !in_range(mean);
+  if constexpr (T > 64 && NT > T) {      // rows of a workgroup go to the same barriers
+#pragma unroll
+    for (int r = 0; r < NT / T; ++r) {
+      float s = 0;
+#pragma unroll
+      for (int w = 0; w < T / 64; ++w) s += part[r * (T / 64) + w];
+      again |= !in_range(s / (float)p.n + p.eps);
+    }
+  }
+  if (again) {      // squares of binary32 numbers are exact in binary64, and their sums are in its range
+    double s = 0;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s = fma((double)h[c][e], (double)h[c][e], s);
+    s = row_sum<T>(s, part64);
+    if (!in_range(mean)) rstd = (float)(1.0 / sqrt(s / (double)p.n + (double)p.eps));
+  }
   if (!there) return;
-  const float rstd = 1.0f / sqrtf(sum / (float)p.n + p.eps);
   if (t == 0 && p.rstd) p.rstd[row] = rstd;
 #pragma unroll
   for (int c = 0; c < C; ++c) {

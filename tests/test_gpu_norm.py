@@ -170,6 +170,34 @@ def test_zeros_without_eps_and_large_numbers():
     within(y[1], torch.ones(64, dtype=torch.float64), torch.tensor(2.0 ** -19), "y")
 
 
+@pytest.mark.parametrize("types", [(F32, F32), (BF, BF), (F16, F32)])
+@pytest.mark.parametrize("n", (1, 300, 700, 1500, 3000, 5000, 16384))
+def test_rows_beyond_the_squares_of_binary32(n, types):
+    """Rows whose squares over- or underflow in binary32, each next to an ordinary one, whose result is the one it has alone.  rstd is off by a
+    rounding where it is below the normal numbers, 2^-150; what test_forward allows holds y."""
+    x_type, h_type = types
+    gen = torch.Generator().manual_seed(n)
+    sizes = torch.tensor([1e18, 1.0, 1e20, 1.0, 1e30, 3e38, 1.0, 1e-22, 1.0, 1e-30, 1e-37])[:, None]
+    r = ((0.1 + 0.9 * torch.rand(11, n, generator=gen)) * torch.randint(0, 2, (11, n), generator=gen).mul(2).sub(1) * sizes).to(h_type).cuda()
+    x, w = torch.zeros(11, n, device="cuda", dtype=x_type), (1.0 + normal(1, n, seed=3, sigma=0.2)[0])
+    for eps in (0.0, 1e-38, 1e-6):
+        norm = op(n, dtype=x_type, residual_dtype=h_type, eps=eps)
+        eps = torch.tensor(eps).double().item()      # (what the call is handed)
+        y, h, rstd = norm.forward(x, w, r)
+        assert torch.equal(h, r)
+        want, want_rstd = want_forward(h, w, eps)
+        within(rstd, want_rstd[:, 0], 2.0 ** -20 * want_rstd[:, 0] + 2.0 ** -150, "rstd")
+        # (below bfloat16's normal numbers, where eps is far above a row's squares, its step is 2^-133)
+        within(y, want, (2.0 ** -19 + HALF[x_type]) * want.abs() + max(LOWEST[x_type], 2.0 ** -133), "y")
+        y8, _, rstd8 = norm.forward8(x, w, r)
+        assert torch.equal(rstd8, rstd)
+        within(values(y8), want, (2.0 ** -19 + 2.0 ** -4) * want.abs() + spread(y8.scales.cpu().double(), want.shape) * 2.0 ** -10, "y in 8 bits")
+        rest = [1, 3, 6, 8]
+        alone, _, rstd1 = norm.forward(x[rest].contiguous(), w, r[rest].contiguous())
+        assert torch.equal(alone, y[rest]) and torch.equal(rstd1, rstd[rest])
+        norm.close()
+
+
 def test_gradients_against_differences():
     """Autograd's backward against central differences of the definition in 64 bits: the third derivative's share of them at 1e-4 is
     below 1e-6 of the numbers met here, and binary32 results are off by 2^-18 of the magnitudes."""
