@@ -69,3 +69,9 @@ def test_a_tensors_sum_is_there_before_the_arrival(text):
     for line in after:
         label = line.split()[-1] + ":"
         assert code[:barrier].index(label) <= next(i for i in range(stores[-1], barrier) if re.match(r"s_waitcnt vmcnt\(0\)", code[i])), line
+
+
+@pytest.mark.parametrize("variant,stores,products", [("ILi0ELi1", 32, 64), ("ILi1ELi2", 32, 64), ("ILi1ELi3", 64, 256)])
+def test_the_other_variants_count_the_same(text, variant, stores, products):
+    """The results' types and formats that the list above leaves out."""
+    test_stores_are_counted_with_the_loads(text, variant, stores, products)

@@ -55,3 +55,20 @@ def test_any_size(ask):
     assert len(ask(questions)) == len(questions)
     small = [(size(10), size(10), size(15), rng.random() < 0.5, 1) for _ in range(20000)]
     assert any(int(a[1]) > 1 for a in ask(small) if a[0] != "few")
+
+
+def test_the_products_of_both_formats_reach_every_kind(ask):
+    """Each size of tests/test_gpu_linear8_tiles.py goes through forward and both gradients, in both formats, into 16 and 32 bits."""
+    pytest.importorskip("torch")
+    from tests.test_gpu_linear8_tiles import TILES
+    found = set()
+    for wide in (False, True):
+        for (rows, depth, cols), plan in zip(TILES, ask([(rows, cols, (depth + 127) // 128, wide, cols % 8 == 0) for rows, depth, cols in TILES])):
+            found.add((wide, plan[0], plan[1] != "1"))
+            if plan[0] == "FLOW256":      # (several tiles for a workgroup, of two slabs and of more)
+                found.add((wide, plan[0], "two" if depth <= 256 else "more") if -(-rows // 256) * -(-cols // 256) > 2 * 256 else None)
+    for wide in (False, True):
+        assert {(wide, kind, False) for kind in ("W256", "W128", "FLOW256")} <= found, found
+        assert {(wide, "FLOW256", "two"), (wide, "FLOW256", "more")} <= found, found
+        assert any((wide, kind, True) in found for kind in ("W64", "TEAMS64"))
+    assert {kind for _, kind, _ in found - {None}} == {"W256", "W128", "W64", "TEAMS64", "FLOW256"}, found
