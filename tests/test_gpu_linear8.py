@@ -314,3 +314,26 @@ def test_accumulating_into_many_tiles(rows, k, n):
     assert torch.equal(view, start[8:8 + n * k].view(n, k) + once) and torch.equal(flat[:8], start[:8]) and torch.equal(flat[-8:], start[-8:])
     layer.weight_grad(x, dy, out=view)
     assert torch.equal(view, once)
+
+
+@pytest.mark.parametrize("rows,k,n", [(1, 1024, 4096), (5, 100, 72), (16, 2048, 9000), (7, 130, 8200), (16, 9000, 40), (3, 17000, 64)])
+@pytest.mark.parametrize("dtype", (BF, F16, F32))
+def test_few_rows_made_e5m2_on_the_way(rows, k, n, dtype):
+    """ob_linear8_forward_few with the other format, from rows some elements apart into rows some apart."""
+    from paper_2104_06069_amd import binding as ob
+    codes = {F32: ob.OB_F32, F16: ob.OB_F16, BF: ob.OB_BF16}
+    layer = op(k, n)
+    x, w8 = numbers(rows, k, dtype, 1, pitch=3), layer.quantize_weight(numbers(n, k, BF, 2))
+    x8 = layer.quantize(x, E5M2)
+    for out_dtype in (BF, F16, F32):
+        wide = torch.full((rows, n + 5), 5.0, device="cuda", dtype=out_dtype)
+        y = wide[:, 2:n + 2]
+        ob.ob_linear8_forward_few(layer.ctx, x, codes[dtype], k + 3, ob.OB_E5M2, *w8.w.address(), rows, y, n + 5, codes[out_dtype],
+                                  torch.cuda.current_stream().cuda_stream)
+        product_near(y, values(x8), values(w8.w), k, "y")
+        product_near(layer.forward(x8, w8, out_dtype=out_dtype), values(x8), values(w8.w), k, "y from 8 bits")
+        assert (wide[:, :2] == 5).all() and (wide[:, n + 2:] == 5).all()
+    with pytest.raises(RuntimeError):
+        ob.ob_linear8_forward_few(layer.ctx, x, codes[dtype], k + 3, 2, *w8.w.address(), rows, y, n + 5, ob.OB_F32)
+    with pytest.raises(RuntimeError):
+        ob.ob_linear8_forward_few(layer.ctx, x, codes[dtype], k + 3, ob.OB_E5M2, *w8.w.address(), ob.OB_LINEAR8_FEW_ROWS + 1, y, n + 5, ob.OB_F32)
