@@ -84,7 +84,9 @@ ob_status ob_norm_backward(ob_norm_ctx* ctx, const void* dy, int64_t lddy, const
  *   weight_grad  dW [n, k]    = dy^T x  (+=)    with the transposes of dy and x, [n, rows] and [k, rows]
  * Operands are matrices of 8 bits with scales as above: W in squares and e4m3, the transpose of x in e4m3, x and dy in either
  * format, with the scales of rows.  Products are summed in binary32 and each result is rounded once:
- *   OB_F32          exact products (an error of 7e-8 over a matrix of normal numbers, 8192 deep)
+ *   OB_F32          exact products (an error of 7e-8 over a matrix of normal numbers, 8192 deep) of numbers, scale applied, from 2^-133 to below 2^128:
+ *                   of all in a block whose scale is 2^-124 or more in e4m3, 2^-117 in e5m2.  Smaller numbers lose bits, or are zeros, and what is
+ *                   2^128 in 8 bits is an infinity
  *   OB_F16, OB_BF16 at twice the rate: of eight adjacent products each is cut off 13 bits below the largest power of two among
  *                   them before they are summed, 1.5e-5 over such a matrix, where the result's rounding makes 2e-4 or 1.7e-3
  * quantize makes any of the operands, a matrix and its transpose in one pass.

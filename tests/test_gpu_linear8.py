@@ -337,3 +337,20 @@ def test_few_rows_made_e5m2_on_the_way(rows, k, n, dtype):
         ob.ob_linear8_forward_few(layer.ctx, x, codes[dtype], k + 3, 2, *w8.w.address(), rows, y, n + 5, ob.OB_F32)
     with pytest.raises(RuntimeError):
         ob.ob_linear8_forward_few(layer.ctx, x, codes[dtype], k + 3, ob.OB_E5M2, *w8.w.address(), ob.OB_LINEAR8_FEW_ROWS + 1, y, n + 5, ob.OB_F32)
+
+
+@pytest.mark.parametrize("fmt,largest,lowest", [(E4M3, 448.0, -124), (E5M2, 57344.0, -117)])
+@pytest.mark.parametrize("rows", (5, 70, 8192))
+def test_binary32_results_are_exact_down_to_these_scales(rows, fmt, largest, lowest):
+    """Numbers down to 2^-133, bfloat16's smallest: multiples of it up to 200, times whole numbers up to 8 (times 2^90), 256 of them: sums below 2^19
+    such units, exact in binary32."""
+    k, n = 256, 2048
+    layer = op(k, n, dtype=F32)
+    gen = torch.Generator().manual_seed(rows)
+    x = torch.randint(-200, 201, (rows, k), generator=gen).double() * 2.0 ** -133
+    x[:, 0] = x[:, 128] = largest * 2.0 ** lowest
+    w = torch.randint(-8, 9, (n, k), generator=gen).float() * 2.0 ** 90
+    w[:, 0] = w[:, 128] = 0      # (beside numbers that set the scale)
+    x8, w8 = layer.quantize(x.float().cuda(), fmt), layer.quantize_weight(w.cuda())
+    assert (x8.scales.cpu().double() == 2.0 ** lowest).all()
+    assert torch.equal(layer.forward(x8, w8).double(), values(x8).cuda() @ values(w8.w).cuda().T.contiguous())
