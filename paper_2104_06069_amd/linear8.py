@@ -107,6 +107,8 @@ class Linear8:
 
     def _out(self, out, rows, width, dtype, dtypes, what="out"):
         if out is None:
+            if dtype not in dtypes:
+                raise ValueError(f"{what}: {' or '.join(map(str, dtypes))}, not {dtype}")
             return torch.empty((rows, width), device=self.device, dtype=dtype), width
         ld = rows_of(out, width, dtypes, self.device, what)
         if out.shape[0] != rows:

@@ -354,3 +354,13 @@ def test_binary32_results_are_exact_down_to_these_scales(rows, fmt, largest, low
     x8, w8 = layer.quantize(x.float().cuda(), fmt), layer.quantize_weight(w.cuda())
     assert (x8.scales.cpu().double() == 2.0 ** lowest).all()
     assert torch.equal(layer.forward(x8, w8).double(), values(x8).cuda() @ values(w8.w).cuda().T.contiguous())
+
+
+def test_types_of_results_are_refused_like_others():
+    layer = op(64, 32)
+    x, dy = torch.zeros(20, 64, device="cuda", dtype=BF), torch.zeros(20, 32, device="cuda", dtype=BF)
+    w8 = layer.quantize_weight(torch.zeros(32, 64, device="cuda"))
+    for call in (lambda: layer.forward(x, w8, out_dtype=torch.float64), lambda: layer.forward(x[:1], w8, out_dtype=E4M3), lambda: layer.input_grad(dy, w8, out_dtype=torch.int32),
+                 lambda: layer.weight_grad(x, dy, out_dtype=torch.float64), lambda: layer.backward(x, dy, w8, dw_dtype=E5M2)):
+        with pytest.raises(ValueError):
+            call()
