@@ -67,3 +67,26 @@ def test_weight_gradient(rows, depth, cols, fmt):
          depth)
     start = torch.randn(rows, cols, generator=torch.Generator("cuda").manual_seed(7), device="cuda")
     assert torch.equal(layer.weight_grad(x, dy, out=start.clone(), accumulate=True), start + once)
+
+
+@pytest.mark.parametrize("rows,depth,cols", [(5, 300, 80), (40, 3000, 72)] + TILES[1:6])
+def test_rows_that_are_not_finite_stay_alone(rows, depth, cols):
+    """An infinity or a NaN in a row of x, in its last block too, makes that row of the result NaNs and no other number different, in every type; and one in x of
+    a weight gradient its column."""
+    layer = op(depth, cols)
+    x, w8 = numbers(rows, depth, 1), layer.quantize_weight(numbers(cols, depth, 2))
+    bad = x.clone()
+    at = [1, rows // 2, rows - 1]
+    bad[at[0], 0], bad[at[1], depth - 1], bad[at[2], depth // 2] = float("inf"), float("nan"), -float("inf")
+    rest = torch.ones(rows, dtype=torch.bool, device="cuda")
+    rest[at] = False
+    for t in (BF, F16, F32):
+        y, z = layer.forward(x, w8, out_dtype=t), layer.forward(bad, w8, out_dtype=t)
+        assert z[~rest].isnan().all() and torch.equal(z[rest], y[rest]), t
+    grad = op(rows, cols)      # dw [cols, rows] from x [depth, rows]
+    x, dy = numbers(depth, rows, 3), numbers(depth, cols, 4)
+    bad = x.clone()
+    bad[0, at[0]], bad[depth - 1, at[1]], bad[depth // 2, at[2]] = float("nan"), float("inf"), float("nan")
+    for t in (BF, F32):
+        y, z = grad.weight_grad(x, dy, out_dtype=t), grad.weight_grad(bad, dy, out_dtype=t)
+        assert z[:, ~rest].isnan().all() and torch.equal(z[:, rest], y[:, rest]), t
