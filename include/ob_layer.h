@@ -133,7 +133,8 @@ ob_status ob_linear8_weight_grad(ob_linear8_ctx* ctx, const void* dy_t, int64_t 
  *   norm   layer_norms[l] = grad_scale ||g_l||_2, norm = grad_scale ||g||_2      squares summed in binary64, rounded once
  *   apply  out = g f, f = grad_scale min(1, max_norm / (norm + eps)) in binary32: norm is read on the device, formed by `norm` or
  *          elsewhere (for instance summed over ranks).  out == g with the same type: in place, and if f is 1 nothing is written.
- * A norm that is NaN makes every f NaN; an infinite one makes it 0 (finite gradients become 0, others NaN).
+ * A norm that is NaN makes every f NaN; an infinite one, which finite gradients have where theirs is beyond binary32, makes it 0 (finite
+ * gradients become 0, others NaN), unless max_norm is infinite too.
  */
 typedef struct ob_clip_ctx ob_clip_ctx; /* opaque */
 

@@ -32,7 +32,7 @@ class Linear8:
     def __init__(self, k, n, dtype=torch.bfloat16, grad_format=_E4M3, max_rows=1 << 22, device="cuda:0"):
         """dtype: of results, unless a call says otherwise; grad_format: of dy in 8 bits.  Products of few tiles share the object's
         workspace: calls on one object, those of autograd among them, must not overlap in time; on several streams, each has to wait for
-        the one before."""
+        the one before.  The object holds no weights, only 32 MB of workspace: layers of one shape may share it."""
         self.device = torch.device(device)
         torch.cuda.set_device(self.device)
         self.ctx = None

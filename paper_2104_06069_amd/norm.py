@@ -20,7 +20,7 @@ class RMSNorm:
     def __init__(self, n, dtype=torch.bfloat16, residual_dtype=None, weight_dtype=torch.float32, eps=1e-6, device="cuda:0"):
         """n: 1 to 16384.  dtype: of x, y and dy; residual_dtype: of residual, h and their gradients, dtype or torch.float32 (default: dtype).
         Weight gradients share the object's workspace: calls of backward on one object must not overlap in time; on several streams,
-        each has to wait for the one before."""
+        each has to wait for the one before.  The object holds no weights, only that workspace: layers of one width may share it."""
         self.device = torch.device(device)
         torch.cuda.set_device(self.device)
         self.n, self.dtype, self.residual_dtype, self.weight_dtype = int(n), dtype, residual_dtype or dtype, weight_dtype
