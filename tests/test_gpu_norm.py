@@ -198,6 +198,21 @@ def test_rows_beyond_the_squares_of_binary32(n, types):
         norm.close()
 
 
+@pytest.mark.parametrize("n", (300, 700, 3000, 16384))
+def test_gradients_of_rows_beyond_the_squares_of_binary32(n):
+    """Against autograd in 64 bits: 2^-18 of the magnitudes that a gradient is the difference of, which are at most about twice its own here; a
+    gradient of the largest rows and their rstd are below the normal numbers, 2^-21 off more."""
+    gen = torch.Generator().manual_seed(n)
+    sizes = torch.tensor([1e18, 1e20, 1.0, 1e30, 3e38, 1e-22, 1e-30])[:, None]
+    x = ((0.1 + 0.9 * torch.rand(7, n, generator=gen)) * torch.randint(0, 2, (7, n), generator=gen).mul(2).sub(1) * sizes).cuda().requires_grad_()
+    w, dy = (1.0 + normal(1, n, seed=3, sigma=0.2)[0]).requires_grad_(), normal(7, n, seed=4)
+    op(n, dtype=F32, eps=0.0)(x, w).backward(dy)
+    xd, wd = x.detach().double().requires_grad_(), w.detach().double().requires_grad_()
+    (xd / xd.square().mean(1, keepdim=True).sqrt() * wd).backward(dy.double())
+    assert ((x.grad.double() - xd.grad).norm(dim=1) <= 2.0 ** -16.5 * xd.grad.norm(dim=1)).all()
+    assert (w.grad.double() - wd.grad).norm() <= 2.0 ** -18 * wd.grad.norm()
+
+
 def test_gradients_against_differences():
     """Autograd's backward against central differences of the definition in 64 bits: the third derivative's share of them at 1e-4 is
     below 1e-6 of the numbers met here, and binary32 results are off by 2^-18 of the magnitudes."""
